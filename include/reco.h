@@ -69,8 +69,33 @@ typedef enum {
     RECO_OP_SELECT = 1,
     RECO_OP_DECODE = 2,
     RECO_OP_PPL = 3,
-    RECO_OP_SAMPLE = 4
+    RECO_OP_SAMPLE = 4,
+    RECO_OP_PAGED_DECODE = 5, /* the paged calls: sized by reco_paged_workspace_bytes */
+    RECO_OP_PAGED_WEIGHTS = 6,
+    RECO_OP_PAGED_EVICT = 7
 } reco_op;
+
+/* A paged cache: the rows of a sequence lie in pages of one pool that all sequences
+ * share, so that rows freed by compression or eviction serve other sequences.  K and V
+ * are separate contiguous arrays of shape [n_layers][n_pages][H_kv][page][d].  Row j of
+ * unit (layer, b, h) is row j % page of [layer][table[b][j / page]][h]: one table row
+ * per sequence serves all its layers and heads.  lens[n_layers][B][H_kv] (int32, device)
+ * holds each unit's length, at most max_pages * page.  Table entries that a call needs
+ * no row of are not looked at and may hold anything.                                */
+typedef struct {
+    void *k;              /* device, [n_layers][n_pages][H_kv][page][d], dtype */
+    void *v;              /* device, same shape and dtype as k */
+    const int32_t *table; /* device, [B][max_pages], pages of each sequence in order */
+    int n_layers;         /* >= 1 */
+    int B;                /* sequences, >= 1 */
+    int H_q;              /* query heads, a multiple of H_kv */
+    int H_kv;             /* KV heads, >= 1 */
+    int n_pages;          /* pages of the pool, >= 1 */
+    int max_pages;        /* table entries per sequence, >= 1 */
+    int page;             /* rows per page: 16, 32, 64, 128 or 256 */
+    int d;                /* head dimension: 64 or 128 */
+    reco_dtype dtype;     /* RECO_F32 or RECO_BF16 */
+} reco_paged_kv;
 
 /* ---------------------------------------------------------------- host helpers */
 
@@ -98,6 +123,12 @@ int reco_probe_trigger(float v_prev, float v_cur, float tau_h);
  * size per sequence (reco_penalty_sample needs B times it).  The size does not
  * depend on the device or on lens.  Alignment: 256 bytes.                      */
 reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *bytes_out);
+
+/* Workspace bytes a paged call needs for this cache: RECO_OP_PAGED_DECODE,
+ * RECO_OP_PAGED_WEIGHTS (it holds the logits of a token, 4 bytes per query head and row
+ * of max_pages * page) or RECO_OP_PAGED_EVICT.  Only the sizes in kv are read.  The size
+ * does not depend on the device or on lens.  Alignment: 256 bytes.                   */
+reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size_t *bytes_out);
 
 /* Thread-local message describing the last non-OK status ("" if none).        */
 const char *reco_last_error(void);
@@ -271,6 +302,78 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
                                   int32_t *lens, float scale, void *out, reco_dtype out_dtype, float *ring,
                                   int slots, int64_t *slot, void *q_ring, void *ws, size_t ws_bytes,
                                   cudaStream_t stream);
+
+/* Decode attention of one new token over a paged cache (the per-token attention of
+ * reco_decode_attn, Sec. 1; Sec. 2.2, with the rows in pages), with an optional sliding
+ * window.  If k_new and v_new are both non-NULL, each unit first appends its new row at
+ * index lens[unit], in the page that its table names; lens is advanced when the call
+ * finishes.  With n rows in the unit then, query head hq of the unit sees
+ *   all rows                                        (window == 0), or
+ *   the rows j < sinks and the rows j >= n - window (window > 0),
+ *   out[layer,b,hq,:] = softmax_j(scale * q[layer,b,hq,:] . K_j) V_j over the rows seen,
+ *   lse[layer,b,hq]   = natural log of the softmax sum.
+ * Rows not seen are not read (whole pages of them may have been given away); NaN or
+ * infinities in them or behind the last row change nothing.
+ *   q            : [n_layers][B][H_q][d], cache dtype (device)
+ *   k_new, v_new : [n_layers][B][H_kv][d], cache dtype (device) or both NULL
+ *   lens         : [n_layers][B][H_kv] int32 (device, advanced by an append)
+ *   window, sinks: window 0 sees every row (sinks must be 0 then)
+ *   out          : [n_layers][B][H_q][d] of out_dtype (RECO_F32 or RECO_BF16)
+ *   lse          : [n_layers][B][H_q] float32 or NULL
+ *   ws           : reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) bytes,
+ *                  zero-filled before its first use; every call leaves it reusable;
+ *                  calls (captured graphs too) that share one must not overlap on the GPU
+ * Sequences may share pages that are only read; a page that receives a new row belongs
+ * to one sequence.  A unit without rows gives zeros and lse = -inf.  A unit with a length
+ * outside [0, max_pages * page], with no room to append, or whose table names a page
+ * outside [0, n_pages) for a row it needs, writes zeros and lse = -inf, keeps its length
+ * and sets the device error word.  At most 16 query heads per KV head.                */
+reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
+                                   int32_t *lens, float scale, int window, int sinks, void *out,
+                                   reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes,
+                                   cudaStream_t stream);
+
+/* reco_paged_decode_attn, with the attention weight of every row it sees added to a
+ * running sum per cached row (what Eq. 2 sums over its window of queries, Sec. 3.2, here
+ * over every decoded token, as the tokens are decoded):
+ *   weights[unit, j] += (1/G) * sum_g softmax_j(scale * q[layer,b,h*G+g,:] . K_j)
+ * for the rows j seen; an appended row starts at its own weight (what its entry held
+ * before does not count).  The entries of other rows are left as they are, and so are all
+ * entries of a unit that is in error.
+ *   weights : [n_layers][B][H_kv][max_pages * page] float32 (device, in/out)
+ *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, otherwise as
+ *             reco_paged_decode_attn's
+ * Every other argument and result is that of reco_paged_decode_attn.  The same inputs
+ * give the same sums bit for bit.                                                    */
+reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *q, const void *k_new,
+                                           const void *v_new, int32_t *lens, float scale, int window, int sinks,
+                                           void *out, reco_dtype out_dtype, float *lse, float *weights, void *ws,
+                                           size_t ws_bytes, cudaStream_t stream);
+
+/* Eviction of a paged cache down to a budget by accumulated attention weight (the
+ * selection and compaction of Sec. 3.2 with running sums of reco_paged_decode_attn_weights
+ * in place of Eq. 2's scores, at any token instead of at a step boundary).
+ * For unit (layer, b, h) with L = lens[unit] > m = budget[b]:
+ *   kept = the rows j < sinks, the m-sinks-w rows sinks <= j < L-w with the largest
+ *          weights[unit, j] (float32 order, NaN above everything; equal weights keep the
+ *          lower index) and the latest rows L-w .. L-1, in ascending order;
+ *   K[unit, r] = K[unit, kept[r]], V and weights[unit, r] likewise, for r < m (in place);
+ *   lens[unit] = m.
+ * A unit with L <= budget[b] is left as it is: the call may follow every token.  Pages
+ * from row m on are free afterwards; the table is not changed.
+ *   weights  : [n_layers][B][H_kv][max_pages * page] float32 (device, in/out)
+ *   lens     : [n_layers][B][H_kv] int32 (device, in: L, out: m where cut)
+ *   budget   : [B] int32 (device), >= sinks + w for a sequence that is cut
+ *   w, sinks : >= 0, w + sinks <= max_pages * page
+ *   kept_idx : [n_layers][B][H_kv][max_pages * page] int32 (device) or NULL; if given,
+ *              the first m entries of each unit that is cut receive `kept`
+ *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes
+ * No two table entries for rows of live sequences may name the same page.  A unit with a
+ * length outside [0, max_pages * page], one to be cut below sinks + w, or one to be cut
+ * whose table names a page outside [0, n_pages) for one of its rows is left untouched
+ * (device error word set).                                                           */
+reco_status reco_paged_evict(const reco_paged_kv *kv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                             int sinks, int32_t *kept_idx, void *ws, size_t ws_bytes, cudaStream_t stream);
 
 /* Eq. 3 + Eq. 4 (Sec. 3.3, reward-banded reflection penalty), in place:
  *   beta_b = 0, beta/2 or beta by the band of rewards[b] (float32 compares);

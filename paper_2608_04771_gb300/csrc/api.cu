@@ -77,6 +77,32 @@ reco_status check_kv(const reco_kv *kv, bool need_kv_ptrs = true)
     return RECO_OK;
 }
 
+reco_status check_paged(const reco_paged_kv *kv, bool need_ptrs = true)
+{
+    if (!kv) return fail(RECO_EINVAL, "paged kv descriptor is NULL");
+    if (kv->n_layers < 1 || kv->B < 1 || kv->H_kv < 1 || kv->H_q < 1 || kv->n_pages < 1 || kv->max_pages < 1)
+        return fail(RECO_EINVAL, "paged kv dimensions must be >= 1 (layers %d, B %d, H_q %d, H_kv %d, pages %d, %d per sequence)",
+                    kv->n_layers, kv->B, kv->H_q, kv->H_kv, kv->n_pages, kv->max_pages);
+    if (kv->H_q % kv->H_kv != 0) return fail(RECO_EINVAL, "H_q (%d) is not a multiple of H_kv (%d)", kv->H_q, kv->H_kv);
+    if (kv->dtype != RECO_F32 && kv->dtype != RECO_BF16) return fail(RECO_EINVAL, "unknown dtype %d", (int)kv->dtype);
+    if (kv->d != 64 && kv->d != 128) return fail(RECO_EUNSUPPORTED, "head dim %d (supported: 64, 128)", kv->d);
+    if (kv->page < 16 || kv->page > 256 || (kv->page & (kv->page - 1)) != 0)
+        return fail(RECO_EUNSUPPORTED, "page of %d rows (supported: 16, 32, 64, 128, 256)", kv->page);
+    const long long units = (long long)kv->n_layers * kv->B;
+    if (units > 65535 || units * kv->H_kv > 65535) return fail(RECO_EUNSUPPORTED, "%lld units exceed 65535", units * kv->H_kv);
+    if ((long long)kv->max_pages * kv->page > (1LL << 30))
+        return fail(RECO_EUNSUPPORTED, "%lld rows per sequence exceed 2^30", (long long)kv->max_pages * kv->page);
+    // rows of a pool are addressed by tensor-map coordinates, 32-bit integers
+    const double rows = (double)kv->n_layers * kv->n_pages * kv->H_kv * kv->page;
+    if (rows >= 2147483648.0) return fail(RECO_EUNSUPPORTED, "a pool of %.0f rows (at most 2^31 - 1)", rows);
+    if (need_ptrs) {
+        if (!kv->k || !kv->v || !kv->table) return fail(RECO_EINVAL, "K, V or table pointer is NULL");
+        if (!al16(kv->k) || !al16(kv->v)) return fail(RECO_EINVAL, "K and V must be 16-byte aligned");
+        if ((uintptr_t)kv->table & 3u) return fail(RECO_EINVAL, "table must be 4-byte aligned");
+    }
+    return RECO_OK;
+}
+
 reco_status check_ws(void *ws, size_t have, size_t need)
 {
     if (need == 0) return RECO_OK;
@@ -226,8 +252,26 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
         if (w < 0) return fail(RECO_EINVAL, "answer rows B*n must be >= 0");
         *bytes_out = reco::align256((size_t)w * 4);
         return RECO_OK;
+    case RECO_OP_PAGED_DECODE:
+    case RECO_OP_PAGED_WEIGHTS:
+    case RECO_OP_PAGED_EVICT:
+        return fail(RECO_EINVAL, "op %d is sized by reco_paged_workspace_bytes", (int)op);
     }
     return fail(RECO_EINVAL, "unknown op %d", (int)op);
+}
+
+reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size_t *bytes_out)
+{
+    if (!bytes_out) return fail(RECO_EINVAL, "NULL pointer");
+    reco_status st = check_paged(kv, false);
+    if (st != RECO_OK) return st;
+    if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS)
+        *bytes_out = reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
+    else if (op == RECO_OP_PAGED_EVICT)
+        *bytes_out = reco::paged_evict_ws_layout(*kv, nullptr).bytes;
+    else
+        return fail(RECO_EINVAL, "op %d is not a paged call", (int)op);
+    return RECO_OK;
 }
 
 reco_status reco_check(cudaStream_t stream)
@@ -244,10 +288,11 @@ reco_status reco_check(cudaStream_t stream)
     if (h) {
         if ((e = cudaMemsetAsync(p, 0, sizeof h, stream)) != cudaSuccess) return cuda_fail(e, "clear error word");
         if ((e = cudaStreamSynchronize(stream)) != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
-        return fail(RECO_EDEVICE, "device error word 0x%x:%s%s%s%s%s%s%s", h, (h & reco::ERR_LEN) ? " length-out-of-range" : "",
+        return fail(RECO_EDEVICE, "device error word 0x%x:%s%s%s%s%s%s%s%s", h, (h & reco::ERR_LEN) ? " length-out-of-range" : "",
                     (h & reco::ERR_KEEP) ? " keep-out-of-range" : "", (h & reco::ERR_ID) ? " id-out-of-range" : "",
                     (h & reco::ERR_TOKEN) ? " token-out-of-range" : "", (h & reco::ERR_ROOM) ? " no-room-to-append" : "",
-                    (h & reco::ERR_INTERNAL) ? " internal-check" : "", (h & reco::ERR_NORM) ? " normaliser-not-finite" : "");
+                    (h & reco::ERR_INTERNAL) ? " internal-check" : "", (h & reco::ERR_NORM) ? " normaliser-not-finite" : "",
+                    (h & reco::ERR_PAGE) ? " page-out-of-range" : "");
     }
     return RECO_OK;
 }
@@ -408,7 +453,74 @@ reco_status decode_checked(const reco_kv *kv, const void *q, const void *k_new, 
 }
 }  // namespace
 
+namespace {
+reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
+                                 int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
+                                 float *lse, float *weights, void *ws, size_t ws_bytes, cudaStream_t stream,
+                                 const char *name)
+{
+    reco_status st = check_paged(kv);
+    if (st != RECO_OK) return st;
+    if (!q || !lens || !out) return fail(RECO_EINVAL, "NULL q, lens or out");
+    if ((k_new == nullptr) != (v_new == nullptr)) return fail(RECO_EINVAL, "k_new and v_new must both be given or both NULL");
+    if (!al16(q) || !al16(out) || (k_new && (!al16(k_new) || !al16(v_new))))
+        return fail(RECO_EINVAL, "q, out, k_new and v_new must be 16-byte aligned");
+    if (((uintptr_t)lens & 3u) || ((uintptr_t)lse & 3u) || ((uintptr_t)weights & 3u))
+        return fail(RECO_EINVAL, "lens, lse and weights must be 4-byte aligned");
+    if (out_dtype != RECO_F32 && out_dtype != RECO_BF16) return fail(RECO_EINVAL, "unknown out_dtype %d", (int)out_dtype);
+    if (window < 0 || sinks < 0) return fail(RECO_EINVAL, "window %d and sinks %d must be >= 0", window, sinks);
+    if (window == 0 && sinks > 0) return fail(RECO_EINVAL, "sinks without a window (window 0 sees every row)");
+    const int G = kv->H_q / kv->H_kv;
+    if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
+    if (!(scale == scale)) return fail(RECO_EINVAL, "scale is NaN");
+    reco::PagedDecodeWs lay = reco::paged_decode_ws_layout(*kv, weights != nullptr, ws);
+    if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK) return st;
+    unsigned *err;
+    if ((st = error_word(&err)) != RECO_OK) return st;
+    cudaError_t e = reco::launch_paged_decode(*kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse,
+                                              weights, lay, err, stream);
+    return e == cudaSuccess ? RECO_OK : cuda_fail(e, name);
+}
+}  // namespace
+
 extern "C" {
+
+reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
+                                   int32_t *lens, float scale, int window, int sinks, void *out,
+                                   reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes, cudaStream_t stream)
+{
+    return paged_decode_checked(kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse, nullptr, ws,
+                                ws_bytes, stream, "reco_paged_decode_attn launch");
+}
+
+reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *q, const void *k_new,
+                                           const void *v_new, int32_t *lens, float scale, int window, int sinks,
+                                           void *out, reco_dtype out_dtype, float *lse, float *weights, void *ws,
+                                           size_t ws_bytes, cudaStream_t stream)
+{
+    if (!weights) return fail(RECO_EINVAL, "weights is NULL");
+    return paged_decode_checked(kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse, weights, ws,
+                                ws_bytes, stream, "reco_paged_decode_attn_weights launch");
+}
+
+reco_status reco_paged_evict(const reco_paged_kv *kv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                             int sinks, int32_t *kept_idx, void *ws, size_t ws_bytes, cudaStream_t stream)
+{
+    reco_status st = check_paged(kv);
+    if (st != RECO_OK) return st;
+    if (!weights || !lens || !budget) return fail(RECO_EINVAL, "NULL weights, lens or budget");
+    if (((uintptr_t)weights & 3u) || ((uintptr_t)lens & 3u) || ((uintptr_t)budget & 3u) || ((uintptr_t)kept_idx & 3u))
+        return fail(RECO_EINVAL, "weights, lens, budget and kept_idx must be 4-byte aligned");
+    const int cap = reco::paged_cap(*kv);
+    if (w < 0 || sinks < 0 || w > cap || sinks > cap - w)
+        return fail(RECO_EINVAL, "w = %d and sinks = %d must be >= 0 and together at most the %d rows of a sequence", w, sinks, cap);
+    reco::SelectWs lay = reco::paged_evict_ws_layout(*kv, ws);
+    if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK) return st;
+    unsigned *err;
+    if ((st = error_word(&err)) != RECO_OK) return st;
+    cudaError_t e = reco::launch_paged_evict(*kv, weights, lens, budget, w, sinks, kept_idx, lay, err, stream);
+    return e == cudaSuccess ? RECO_OK : cuda_fail(e, "reco_paged_evict launch");
+}
 
 reco_status reco_decode_attn(const reco_kv *kv, const void *q, const void *k_new, const void *v_new, int32_t *lens,
                              float scale, void *out, reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes,

@@ -15,6 +15,7 @@ enum : unsigned {
     ERR_ROOM = 16u,  // no room to append a decoded row
     ERR_INTERNAL = 32u,  // an internal consistency check failed (the access was skipped)
     ERR_NORM = 64u,  // a window row's log-normaliser passed to scoring is not finite
+    ERR_PAGE = 128u,  // a table entry outside [0, n_pages) for a row that is needed
 };
 
 constexpr float kLog2e = 1.4426950408889634f;

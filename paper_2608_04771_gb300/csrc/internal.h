@@ -61,9 +61,23 @@ struct DecodeWs {
     size_t bytes;
 };
 
+// What the paged decode needs beside the decode's own regions: with weights, the token's
+// logits and normalisers.
+struct PagedDecodeWs {
+    DecodeWs dec;
+    float *lse2;    // [n_layers * B * H_q]         log2 of the softmax sums
+    float *logits;  // [n_layers * B * H_q][cap]    scale * log2(e) * q . k, rows a multiple of 16 floats
+    size_t bytes;
+};
+
 ScoreWs score_ws_layout(const reco_kv &kv, int w, void *base);
 SelectWs select_ws_layout(const reco_kv &kv, void *base);
 DecodeWs decode_ws_layout(const reco_kv &kv, void *base);
+PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base);
+SelectWs paged_evict_ws_layout(const reco_paged_kv &kv, void *base);
+
+// Rows a unit of the paged cache may hold.
+inline int paged_cap(const reco_paged_kv &kv) { return kv.max_pages * kv.page; }
 
 // Launchers return cudaSuccess or the launch error.  All arguments validated by the caller.
 cudaError_t launch_score(const reco_kv &kv, const void *q_win, const int32_t *lens, const int32_t *keep, int w,
@@ -88,6 +102,12 @@ cudaError_t launch_decode(const reco_kv &kv, const void *q, const void *k_new, c
                           int32_t *lens, float scale, void *out, reco_dtype out_dtype, float *lse,
                           const DecodeWs &ws, unsigned *err, cudaStream_t s, float *ring = nullptr,
                           int slots = 0, long long *slot = nullptr, void *qring = nullptr);
+// weights: nullptr, or the running sums that the rows' attention weights are added to.
+cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new,
+                                int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
+                                float *lse, float *weights, const PagedDecodeWs &ws, unsigned *err, cudaStream_t s);
+cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                               int sinks, int32_t *kept_idx, const SelectWs &ws, unsigned *err, cudaStream_t s);
 cudaError_t launch_penalty(float *logits, int B, int V, const int32_t *ids, int n_ids,
                            const float *rewards, float tau_l, float tau_h, float beta, float *beta_out,
                            unsigned *err, cudaStream_t s);

@@ -42,6 +42,14 @@ SelectWs select_ws_layout(const reco_kv &kv, void *base)
     return ws;
 }
 
+// The paged cache as the selection sees it: units of at most cap rows.
+static reco_kv paged_units(const reco_paged_kv &kv)
+{
+    return reco_kv{kv.k, kv.v, kv.n_layers, kv.B, kv.H_q, kv.H_kv, paged_cap(kv), kv.d, kv.dtype};
+}
+
+SelectWs paged_evict_ws_layout(const reco_paged_kv &kv, void *base) { return select_ws_layout(paged_units(kv), base); }
+
 // Most candidates a unit may have for the shared-memory selection (192 KB of keys).
 constexpr int kSelectSmemKeys = 48 * 1024;
 
@@ -64,6 +72,45 @@ __device__ __forceinline__ uint32_t order_key(float f)
     uint32_t u = __float_as_uint(f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+
+// What a selection does with a unit of L rows and a count m, and how a score is ordered.  Rows
+// before `first` and the last w are kept; the candidates lie between.
+
+// Down to exactly keep[b] rows: a count above the length is an error, one equal to it the identity.
+struct KeepRule {
+    static constexpr bool BUDGET = false;
+    int w;
+    static constexpr int first = 0;
+    __device__ __forceinline__ unsigned error(int L, int m, int L_cap) const
+    {
+        return (L < w || L > L_cap) ? ERR_LEN : ((m < w || m > L) ? ERR_KEEP : 0u);
+    }
+    __device__ __forceinline__ bool leave(int, int) const { return false; }
+    __device__ __forceinline__ bool bad_page(int, int) const { return false; }
+    __device__ __forceinline__ int entries(int) const { return 0; }
+    __device__ __forceinline__ uint32_t key(float f) const { return order_key(f); }
+};
+
+// Down to at most budget[b] rows of a paged cache: a unit within its budget is left alone, one whose
+// table names a page that the pool does not have is refused before anything moves.
+struct BudgetRule {
+    static constexpr bool BUDGET = true;
+    int w, first;
+    const int32_t *table;
+    int max_pages, n_pages, page;
+    __device__ __forceinline__ unsigned error(int L, int m, int L_cap) const
+    {
+        return (L < 0 || L > L_cap) ? ERR_LEN : ((L > m && m < first + w) ? ERR_KEEP : 0u);
+    }
+    __device__ __forceinline__ bool leave(int L, int m) const { return L <= m; }
+    __device__ __forceinline__ bool bad_page(int b, int i) const
+    {
+        return (unsigned)table[(long)b * max_pages + i] >= (unsigned)n_pages;
+    }
+    __device__ __forceinline__ int entries(int L) const { return (L + page - 1) / page; }
+    // -0 equals +0, and NaN lies above everything
+    __device__ __forceinline__ uint32_t key(float f) const { return f == f ? order_key(f + 0.f) : 0xffffffffu; }
+};
 
 // Exclusive block scan of a 0/1 flag.  `tot` must hold NT/32 + 1 ints.
 template <int NT>
@@ -92,9 +139,9 @@ __device__ __forceinline__ int block_scan_flag(bool flag, int *tot, int &total)
     return res;
 }
 
-template <int NT>
+template <int NT, class Rule>
 __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scores, const int32_t *lens,
-                                                  int32_t *lens_out, const int32_t *__restrict__ keep, int w, int B, int Hkv,
+                                                  int32_t *lens_out, const int32_t *__restrict__ keep, Rule rule, int B, int Hkv,
                                                   int L_cap, int32_t *__restrict__ idx_out,
                                                   int32_t *__restrict__ count, long units, unsigned *err)
 {
@@ -110,20 +157,38 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
     for (long u = blockIdx.x; u < units; u += gridDim.x, ++it) {  // a few CTAs per SM walk the units
         const int tid = threadIdx.x, lane = tid & 31;
         const int L = s_lm[it].x, m = s_lm[it].y;  // the grid gives no CTA more than kWalkAhead units
-        if (L < w || L > L_cap || m < w || m > L) {
+        const int w = rule.w, first = rule.first;
+        unsigned bad = rule.error(L, m, L_cap);
+        if constexpr (Rule::BUDGET) {
+            if (bad == 0u && rule.leave(L, m)) {
+                if (tid == 0) count[u] = 0;
+                continue;
+            }
+            if (bad == 0u) {
+                const int b = (int)((u / Hkv) % B), n = rule.entries(L);
+                bool any = false;
+                for (int i = tid; i < n; i += NT) any |= rule.bad_page(b, i);
+                if (__syncthreads_or(any)) bad = ERR_PAGE;
+            }
+        }
+        if (bad != 0u) {
             if (tid == 0) {
                 count[u] = 0;
-                raise_error(err, (L < w || L > L_cap) ? ERR_LEN : ERR_KEEP);
+                raise_error(err, bad);
             }
             continue;
         }
-        const int nc = L - w, kc = m - w;
-        const float *s = scores + u * L_cap;
+        const int nc = L - w - first, kc = m - w - first;
+        const float *s = scores + u * L_cap + first;
         int32_t *idx = idx_out + u * L_cap;
         if (kc == nc) {  // keep everything: identity, nothing moves (the compaction skips it)
             for (int j = tid; j < L; j += NT) idx[j] = j;
             if (tid == 0) count[u] = 0;
             continue;
+        }
+        if constexpr (Rule::BUDGET) {
+            for (int j = tid; j < first; j += NT) idx[j] = j;
+            idx += first;
         }
         uint32_t T = 0xffffffffu;
         int need = 0;
@@ -141,7 +206,7 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
                 for (int jb = 0; jb < nc; jb += NT) {
                     const int j = jb + tid;
                     const bool valid = j < nc;
-                    const uint32_t key = valid ? order_key(s[j]) : 0u;
+                    const uint32_t key = valid ? rule.key(s[j]) : 0u;
                     const bool match = valid && (key & mask) == prefix;
                     const uint32_t bin = (key >> shift) & 255u;
                     if (match) atomicAdd(&hist[bin], 1);
@@ -183,18 +248,18 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
         for (int jb = 0; jb < nc; jb += NT) {
             const int j = jb + tid;
             const bool valid = j < nc;
-            const uint32_t key = valid ? order_key(s[j]) : 0u;
+            const uint32_t key = valid ? rule.key(s[j]) : 0u;
             const bool gt = valid && key > T;
             const bool eq = valid && key == T;
             int eq_tot, f_tot;
             const int eq_rank = block_scan_flag<NT>(eq, tot, eq_tot) + base_eq;
             const bool flag = gt || (eq && eq_rank < need);
             const int pos = block_scan_flag<NT>(flag, tot, f_tot) + base_pos;
-            if (flag) idx[pos] = j;
+            if (flag) idx[pos] = first + j;
             base_eq += eq_tot;
             base_pos += f_tot;
         }
-        for (int t = tid; t < w; t += NT) idx[kc + t] = nc + t;
+        for (int t = tid; t < w; t += NT) idx[kc + t] = first + nc + t;
         if (tid == 0) {
             count[u] = m;
             if (lens_out) lens_out[u] = m;
@@ -220,9 +285,9 @@ constexpr int kWholeBin = 0x7fffffff;
 // Where there are more units than SMs, smaller CTAs share an SM and one counts
 // while another waits at a barrier (512 units of 15000 to 16384 candidates: 54 -> 45 us).
 constexpr int kFewKeys = 8;  // keys per thread
-template <int NT, bool FEW>
+template <int NT, bool FEW, class Rule>
 __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__ scores, const int32_t *lens,
-                                                       int32_t *lens_out, const int32_t *__restrict__ keep, int w, int B, int Hkv,
+                                                       int32_t *lens_out, const int32_t *__restrict__ keep, Rule rule, int B, int Hkv,
                                                        int L_cap, int32_t *__restrict__ idx_out,
                                                        int32_t *__restrict__ count, long units, unsigned *err)
 {
@@ -243,25 +308,43 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
     int it = 0;
     for (long u = blockIdx.x; u < units; u += gridDim.x, ++it) {  // a few CTAs per SM walk the units
         const int L = s_lm[it].x, m = s_lm[it].y;  // the grid gives no CTA more than kWalkAhead units
-        if (L < w || L > L_cap || m < w || m > L) {
+        const int w = rule.w, first = rule.first;
+        unsigned bad = rule.error(L, m, L_cap);
+        if constexpr (Rule::BUDGET) {
+            if (bad == 0u && rule.leave(L, m)) {
+                if (tid == 0) count[u] = 0;
+                continue;
+            }
+            if (bad == 0u) {
+                const int b = (int)((u / Hkv) % B), n = rule.entries(L);
+                bool any = false;
+                for (int i = tid; i < n; i += NT) any |= rule.bad_page(b, i);
+                if (__syncthreads_or(any)) bad = ERR_PAGE;
+            }
+        }
+        if (bad != 0u) {
             if (tid == 0) {
                 count[u] = 0;
-                raise_error(err, (L < w || L > L_cap) ? ERR_LEN : ERR_KEEP);
+                raise_error(err, bad);
             }
             continue;
         }
-        const int nc = L - w, kc = m - w;
-        const float *s = scores + u * L_cap;
+        const int nc = L - w - first, kc = m - w - first;
+        const float *s = scores + u * L_cap + first;
         int32_t *idx = idx_out + u * L_cap;
         if (kc == nc) {  // keep everything: identity, nothing moves (the compaction skips it)
             for (int j = tid; j < L; j += NT) idx[j] = j;
             if (tid == 0) count[u] = 0;
             continue;
         }
+        if constexpr (Rule::BUDGET) {
+            for (int j = tid; j < first; j += NT) idx[j] = j;
+            idx += first;
+        }
         uint32_t lo = 0xffffffffu, hi = 0;
 #pragma unroll 8
         for (int j = tid; j < nc; j += NT) {
-            const uint32_t key = order_key(__ldcg(s + j));
+            const uint32_t key = rule.key(__ldcg(s + j));
             keys[j] = key;
             lo = min(lo, key);
             hi = max(hi, key);
@@ -397,11 +480,11 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
             const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
             const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
             const unsigned fb = __ballot_sync(0xffffffffu, flag);
-            if (flag) idx[pos + __popc(fb & below)] = j;
+            if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
             e_run += __popc(eb);
             pos += __popc(fb);
         }
-        for (int t = tid; t < w; t += NT) idx[kc + t] = nc + t;
+        for (int t = tid; t < w; t += NT) idx[kc + t] = first + nc + t;
         if (tid == 0) {
             count[u] = m;
             if (lens_out) lens_out[u] = m;
@@ -418,16 +501,16 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
 constexpr int kWarpThreads = 256;
 
 // The kept candidates of a unit, kc of its nc <= 32 * K, into idx.
-template <int K>
-__device__ __forceinline__ void select_in_warp(const float *__restrict__ s, int nc, int kc, int32_t *__restrict__ idx,
-                                               int lane)
+template <int K, class Rule>
+__device__ __forceinline__ void select_in_warp(const Rule &rule, const float *__restrict__ s, int nc, int kc,
+                                               int32_t *__restrict__ idx, int lane)
 {
     uint32_t key[K], lo = 0xffffffffu, hi = 0;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         const int j = 32 * i + lane;
         const float x = j < nc ? __ldcg(s + j) : 0.f;
-        key[i] = j < nc ? order_key(x) : 0u;  // order_key is 0 for no score but the NaN of all ones
+        key[i] = j < nc ? rule.key(x) : 0u;  // order_key is 0 for no score but the NaN of all ones
         if (j < nc) {
             lo = min(lo, key[i]);
             hi = max(hi, key[i]);
@@ -468,16 +551,16 @@ __device__ __forceinline__ void select_in_warp(const float *__restrict__ s, int 
         const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
         const bool flag = (j < nc && key[i] > T) || (is_eq && e_run + __popc(eb & below) < need);
         const unsigned fb = __ballot_sync(0xffffffffu, flag);
-        if (flag) idx[pos + __popc(fb & below)] = j;
+        if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
         e_run += __popc(eb);
         pos += __popc(fb);
     }
 }
 
-template <int K>
+template <int K, class Rule>
 __global__ void __launch_bounds__(kWarpThreads) select_topm_warp(const float *__restrict__ scores, const int32_t *lens,
                                                                  int32_t *lens_out, const int32_t *__restrict__ keep,
-                                                                 int w, int B, int Hkv, int L_cap,
+                                                                 Rule rule, int B, int Hkv, int L_cap,
                                                                  int32_t *__restrict__ idx_out,
                                                                  int32_t *__restrict__ count, int units, unsigned *err)
 {
@@ -486,30 +569,48 @@ __global__ void __launch_bounds__(kWarpThreads) select_topm_warp(const float *__
     const int u = blockIdx.x * (kWarpThreads / 32) + (threadIdx.x >> 5);
     if (u >= units) return;
     const int L = lens[u], m = keep[(u / Hkv) % B];
-    if (L < w || L > L_cap || m < w || m > L) {
+    const int w = rule.w, first = rule.first;
+    unsigned bad = rule.error(L, m, L_cap);
+    if constexpr (Rule::BUDGET) {
+        if (bad == 0u && rule.leave(L, m)) {
+            if (lane == 0) count[u] = 0;
+            return;
+        }
+        if (bad == 0u) {
+            const int b = (u / Hkv) % B, n = rule.entries(L);
+            bool any = false;
+            for (int i = lane; i < n; i += 32) any |= rule.bad_page(b, i);
+            if (__any_sync(0xffffffffu, any)) bad = ERR_PAGE;
+        }
+    }
+    if (bad != 0u) {
         if (lane == 0) {
             count[u] = 0;
-            raise_error(err, (L < w || L > L_cap) ? ERR_LEN : ERR_KEEP);
+            raise_error(err, bad);
         }
         return;
     }
-    const int nc = L - w, kc = m - w;
-    const float *s = scores + (long)u * L_cap;
+    const int nc = L - w - first, kc = m - w - first;
+    const float *s = scores + (long)u * L_cap + first;
     int32_t *idx = idx_out + (long)u * L_cap;
     if (kc == nc) {  // keep everything: identity, nothing moves (the compaction skips it)
         for (int j = lane; j < L; j += 32) idx[j] = j;
         if (lane == 0) count[u] = 0;
         return;
     }
+    if constexpr (Rule::BUDGET) {
+        for (int j = lane; j < first; j += 32) idx[j] = j;
+        idx += first;
+    }
     // a cache's units are often far shorter than its rows (the trace's boundaries, units of 70 to 240
     // rows in a cache of up to 1024: 9.4 -> 5.8 us each)
     if (K > 8 && nc <= 32 * 8)
-        select_in_warp<8>(s, nc, kc, idx, lane);
+        select_in_warp<8>(rule, s, nc, kc, idx, lane);
     else if (K > 16 && nc <= 32 * 16)
-        select_in_warp<16>(s, nc, kc, idx, lane);
+        select_in_warp<16>(rule, s, nc, kc, idx, lane);
     else
-        select_in_warp<K>(s, nc, kc, idx, lane);
-    for (int t = lane; t < w; t += 32) idx[kc + t] = nc + t;
+        select_in_warp<K>(rule, s, nc, kc, idx, lane);
+    for (int t = lane; t < w; t += 32) idx[kc + t] = first + nc + t;
     if (lane == 0) {
         count[u] = m;
         if (lens_out) lens_out[u] = m;
@@ -545,8 +646,45 @@ struct CountFromKeep {
     }
 };
 
-template <class Count>
-__global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const int32_t *__restrict__ idx_all,
+// Where the rows of a unit lie: one after another, or in the pages that its sequence's table names
+// (of which the selection has checked all that hold rows).
+struct ContiguousRows {
+    char *K, *V;
+    struct Unit {
+        char *base;
+        int row_bytes;
+        __device__ __forceinline__ char *row(int r) const { return base + (long)r * row_bytes; }
+    };
+    __device__ __forceinline__ Unit unit(bool v, long u, int L_cap, int row_bytes) const
+    {
+        return Unit{(v ? V : K) + u * (long)L_cap * row_bytes, row_bytes};
+    }
+};
+struct PagedRows {
+    char *K, *V;
+    const int32_t *table;
+    int B, Hkv, n_pages, max_pages, shift;
+    struct Unit {
+        char *base;  // row 0 of page 0 of the unit's layer and head
+        const int32_t *table;
+        long page_bytes;  // from one page of the layer to the next
+        int row_bytes, shift;
+        __device__ __forceinline__ char *row(int r) const
+        {
+            return base + (long)__ldg(table + (r >> shift)) * page_bytes + (long)(r & ((1 << shift) - 1)) * row_bytes;
+        }
+    };
+    __device__ __forceinline__ Unit unit(bool v, long u, int, int row_bytes) const
+    {
+        const long lb = u / Hkv, layer = lb / B;
+        const long head_bytes = (long)row_bytes << shift;
+        return Unit{(v ? V : K) + (layer * n_pages * Hkv + u % Hkv) * head_bytes, table + (lb % B) * max_pages,
+                    Hkv * head_bytes, row_bytes, shift};
+    }
+};
+
+template <class Count, class Rows>
+__global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t *__restrict__ idx_all,
                                                     Count cnt, int L_cap, int row_bytes, long units, unsigned *err)
 {
     constexpr int P = 8;  // 16-byte pieces per 128-byte slice
@@ -566,7 +704,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const i
     for (long u = blockIdx.x; u < units; u += gridDim.x, ++it) {  // a few CTAs per SM walk the units
         const int m = s_ml[it].x, lim = s_ml[it].y;  // the grid gives no CTA more than kWalkAhead units
         if (m == 0) continue;
-        char *base = (blockIdx.y == 0 ? K : V) + u * (long)L_cap * row_bytes;
+        const auto unit = rows.unit(blockIdx.y != 0, u, L_cap, row_bytes);
         const int32_t *idx = idx_all + u * L_cap;
         const int rows_per_pass = blockDim.x / P;
         const int my_row = threadIdx.x / P;
@@ -582,7 +720,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const i
                     if (src < r || src >= lim) {  // never trust an index outside [r, lim)
                         raise_error(err, ERR_INTERNAL);
                     } else if (src != r) {
-                        v[i] = *reinterpret_cast<const uint4 *>(base + (long)src * row_bytes + off);
+                        v[i] = *reinterpret_cast<const uint4 *>(unit.row(src) + off);
                         dst[i] = r;
                     }
                 }
@@ -591,7 +729,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const i
         auto store = [&](const uint4 (&v)[U], const int (&dst)[U]) {
     #pragma unroll
             for (int i = 0; i < U; ++i)
-                if (dst[i] >= 0) *reinterpret_cast<uint4 *>(base + (long)dst[i] * row_bytes + off) = v[i];
+                if (dst[i] >= 0) *reinterpret_cast<uint4 *>(unit.row(dst[i]) + off) = v[i];
         };
         // Two chunks in registers: the next chunk's reads are issued before this chunk's
         // writes (its sources lie at or above its first destination, above every row this
@@ -607,6 +745,35 @@ __global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const i
             load(r0 + 2 * step, va, da);
             __syncthreads();
             store(vb, db);
+        }
+    }
+}
+
+// weights[u, r] = weights[u, idx[r]] for the units that the selection cut, in place: a chunk's reads, a
+// barrier, then its writes, as in compact_rows.
+__global__ void __launch_bounds__(256) compact_weights(float *weights, const int32_t *__restrict__ idx_all,
+                                                       const int32_t *__restrict__ count, int L_cap, long units)
+{
+    constexpr int U = 4;
+    wait_prior_grid();
+    for (long u = blockIdx.x; u < units; u += gridDim.x) {
+        const int m = count[u];
+        float *wt = weights + u * L_cap;
+        const int32_t *idx = idx_all + u * L_cap;
+        for (int r0 = 0; r0 < m; r0 += U * (int)blockDim.x) {
+            float x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int r = r0 + i * (int)blockDim.x + (int)threadIdx.x;
+                if (r < m) x[i] = wt[idx[r]];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int r = r0 + i * (int)blockDim.x + (int)threadIdx.x;
+                if (r < m) wt[r] = x[i];
+            }
+            __syncthreads();
         }
     }
 }
@@ -639,24 +806,25 @@ static unsigned walk_grid(F fn, int threads, size_t smem, long units, int per_un
     return (unsigned)std::min(units, ctas);
 }
 
-template <int NT>
+template <int NT, class Rule>
 static cudaError_t launch_select_smem(const reco_kv &kv, size_t key_bytes, long units, const float *scores,
-                                      const int32_t *lens, int32_t *lens_out, const int32_t *keep, int w, int32_t *idx,
+                                      const int32_t *lens, int32_t *lens_out, const int32_t *keep, Rule rule, int32_t *idx,
                                       int32_t *count, unsigned *err, cudaStream_t s)
 {
-    auto fn = kv.L_cap - w <= kFewKeys * NT ? select_topm_smem<NT, true> : select_topm_smem<NT, false>;
+    auto fn = kv.L_cap - rule.w - rule.first <= kFewKeys * NT ? select_topm_smem<NT, true, Rule> : select_topm_smem<NT, false, Rule>;
     const cudaError_t e = allow_smem((const void *)fn, (int)kSelectSmemKeys * (int)sizeof(uint32_t));
     if (e != cudaSuccess) return e;
     return launch_pdl(fn, dim3(walk_grid(fn, NT, key_bytes, units, 1)), dim3(NT), key_bytes, s, scores, lens, lens_out,
-                      keep, w, kv.B, kv.H_kv, kv.L_cap, idx, count, units, err);
+                      keep, rule, kv.B, kv.H_kv, kv.L_cap, idx, count, units, err);
 }
 
+template <class Rule>
 static cudaError_t launch_select(const reco_kv &kv, const float *scores, const int32_t *lens, int32_t *lens_out,
-                                 const int32_t *keep, int w, int32_t *idx, int32_t *count, unsigned *err,
+                                 const int32_t *keep, Rule rule, int32_t *idx, int32_t *count, unsigned *err,
                                  cudaStream_t s)
 {
     const long units = (long)kv.n_layers * kv.B * kv.H_kv;
-    const int most = kv.L_cap - w;  // candidates of a unit
+    const int most = kv.L_cap - rule.w - rule.first;  // candidates of a unit
     const int sms = device_sm_count();
     cudaError_t e;
     // A warp per unit costs 3.5 to 4 us up to 256 candidates, 6 up to 512 and 9.5 up to 1024, whatever the
@@ -664,10 +832,10 @@ static cudaError_t launch_select(const reco_kv &kv, const float *scores, const i
     // per unit, which grows with the units: 520 rows, 304 units 5.9 by warps and 5.1 by CTAs, 608 units
     // 6.0 and 6.0, 1216 units 6.1 and 9.5; 1030 rows, 608 units 9.5 and 7.5, 1216 units 9.5 and 11.6.
     if (most <= 32 * 8 || (most <= 32 * 32 && units > (most <= 32 * 16 ? 4L : 6L) * sms)) {
-        auto fn = most <= 32 * 8 ? select_topm_warp<8> : (most <= 32 * 16 ? select_topm_warp<16> : select_topm_warp<32>);
+        auto fn = most <= 32 * 8 ? select_topm_warp<8, Rule> : (most <= 32 * 16 ? select_topm_warp<16, Rule> : select_topm_warp<32, Rule>);
         constexpr int per = kWarpThreads / 32;
         e = launch_pdl(fn, dim3((unsigned)((units + per - 1) / per)), dim3(kWarpThreads), 0, s, scores, lens, lens_out,
-                       keep, w, kv.B, kv.H_kv, kv.L_cap, idx, count, (int)units, err);
+                       keep, rule, kv.B, kv.H_kv, kv.L_cap, idx, count, (int)units, err);
         if (e != cudaSuccess) return e;
         return cudaGetLastError();
     }
@@ -682,28 +850,28 @@ static cudaError_t launch_select(const reco_kv &kv, const float *scores, const i
         // 13.7 / 15.4 / 19.5; 8 of 4104 rows 24.6 / 29 / 37.
         const long held = (long)((227 * 1024) / (key_bytes + 4096)), per_sm = std::min((units + sms - 1) / sms, held);
         if ((per_sm <= 1 && most > 2048) || (per_sm == 2 && most > 16 * 1024))
-            e = launch_select_smem<1024>(kv, key_bytes, units, scores, lens, lens_out, keep, w, idx, count, err, s);
+            e = launch_select_smem<1024>(kv, key_bytes, units, scores, lens, lens_out, keep, rule, idx, count, err, s);
         else if (per_sm <= 3)
-            e = launch_select_smem<512>(kv, key_bytes, units, scores, lens, lens_out, keep, w, idx, count, err, s);
+            e = launch_select_smem<512>(kv, key_bytes, units, scores, lens, lens_out, keep, rule, idx, count, err, s);
         else
-            e = launch_select_smem<256>(kv, key_bytes, units, scores, lens, lens_out, keep, w, idx, count, err, s);
+            e = launch_select_smem<256>(kv, key_bytes, units, scores, lens, lens_out, keep, rule, idx, count, err, s);
         if (e != cudaSuccess) return e;
     } else {
-        const unsigned grid = walk_grid(select_topm<1024>, 1024, 0, units, 1);
-        e = launch_pdl(select_topm<1024>, dim3(grid), dim3(1024), 0, s, scores, lens, lens_out, keep, w,
+        const unsigned grid = walk_grid(select_topm<1024, Rule>, 1024, 0, units, 1);
+        e = launch_pdl(select_topm<1024, Rule>, dim3(grid), dim3(1024), 0, s, scores, lens, lens_out, keep, rule,
                                    kv.B, kv.H_kv, kv.L_cap, idx, count, units, err);
         if (e != cudaSuccess) return e;
     }
     return cudaGetLastError();
 }
 
-template <class Count>
+template <class Count, class Rows>
 static dim3 compact_grid(const reco_kv &kv, int &row_bytes, long &units)
 {
     row_bytes = kv.d * (kv.dtype == RECO_F32 ? 4 : 2);
     units = (long)kv.n_layers * kv.B * kv.H_kv;
     const int per_unit = 2 * (row_bytes / 128);  // K and V, 128-byte column slices
-    return dim3(walk_grid(compact_rows<Count>, 256, 0, units, per_unit), 2, row_bytes / 128);
+    return dim3(walk_grid(compact_rows<Count, Rows>, 256, 0, units, per_unit), 2, row_bytes / 128);
 }
 
 cudaError_t launch_select_compact(const reco_kv &kv, const float *scores, int32_t *lens,
@@ -711,12 +879,13 @@ cudaError_t launch_select_compact(const reco_kv &kv, const float *scores, int32_
                                   unsigned *err, cudaStream_t s)
 {
     int32_t *idx = kept_idx ? kept_idx : ws.idx;
-    cudaError_t e = launch_select(kv, scores, lens, lens, keep, w, idx, ws.count, err, s);
+    cudaError_t e = launch_select(kv, scores, lens, lens, keep, KeepRule{w}, idx, ws.count, err, s);
     if (e != cudaSuccess) return e;
     int row_bytes;
     long units;
-    const dim3 grid = compact_grid<CountFromSelect>(kv, row_bytes, units);
-    e = launch_pdl(compact_rows<CountFromSelect>, grid, dim3(256), 0, s, (char *)kv.k, (char *)kv.v, (const int32_t *)idx,
+    const dim3 grid = compact_grid<CountFromSelect, ContiguousRows>(kv, row_bytes, units);
+    e = launch_pdl(compact_rows<CountFromSelect, ContiguousRows>, grid, dim3(256), 0, s,
+                   ContiguousRows{(char *)kv.k, (char *)kv.v}, (const int32_t *)idx,
                    CountFromSelect{ws.count, kv.L_cap}, kv.L_cap, row_bytes, units, err);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -724,7 +893,7 @@ cudaError_t launch_select_compact(const reco_kv &kv, const float *scores, int32_
 cudaError_t launch_select_only(const reco_kv &kv, const float *scores, const int32_t *lens, const int32_t *keep,
                                int w, int32_t *kept_idx, const SelectWs &ws, unsigned *err, cudaStream_t s)
 {
-    return launch_select(kv, scores, lens, nullptr, keep, w, kept_idx, ws.count, err, s);
+    return launch_select(kv, scores, lens, nullptr, keep, KeepRule{w}, kept_idx, ws.count, err, s);
 }
 
 cudaError_t launch_compact(const reco_kv &kv, const int32_t *kept_idx, int32_t *lens, const int32_t *keep, int w,
@@ -732,13 +901,34 @@ cudaError_t launch_compact(const reco_kv &kv, const int32_t *kept_idx, int32_t *
 {
     int row_bytes;
     long units;
-    const dim3 grid = compact_grid<CountFromKeep>(kv, row_bytes, units);
-    cudaError_t e = launch_pdl(compact_rows<CountFromKeep>, grid, dim3(256), 0, s, (char *)kv.k, (char *)kv.v,
-                               kept_idx, CountFromKeep{lens, keep, w, kv.B, kv.H_kv, kv.L_cap}, kv.L_cap, row_bytes,
+    const dim3 grid = compact_grid<CountFromKeep, ContiguousRows>(kv, row_bytes, units);
+    cudaError_t e = launch_pdl(compact_rows<CountFromKeep, ContiguousRows>, grid, dim3(256), 0, s,
+                               ContiguousRows{(char *)kv.k, (char *)kv.v}, kept_idx, CountFromKeep{lens, keep, w, kv.B, kv.H_kv, kv.L_cap}, kv.L_cap, row_bytes,
                                units, err);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
     e = launch_pdl(compact_set_lens, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, lens, keep, units, w, kv.B,
                    kv.H_kv, kv.L_cap);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_paged_evict(const reco_paged_kv &pkv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                               int sinks, int32_t *kept_idx, const SelectWs &ws, unsigned *err, cudaStream_t s)
+{
+    const reco_kv kv = paged_units(pkv);
+    int32_t *idx = kept_idx ? kept_idx : ws.idx;
+    const BudgetRule rule{w, sinks, pkv.table, pkv.max_pages, pkv.n_pages, pkv.page};
+    cudaError_t e = launch_select(kv, weights, lens, lens, budget, rule, idx, ws.count, err, s);
+    if (e != cudaSuccess) return e;
+    const int shift = __builtin_ctz((unsigned)pkv.page);
+    const PagedRows rows{(char *)pkv.k, (char *)pkv.v, pkv.table, pkv.B, pkv.H_kv, pkv.n_pages, pkv.max_pages, shift};
+    int row_bytes;
+    long units;
+    const dim3 grid = compact_grid<CountFromSelect, PagedRows>(kv, row_bytes, units);
+    e = launch_pdl(compact_rows<CountFromSelect, PagedRows>, grid, dim3(256), 0, s, rows, (const int32_t *)idx,
+                   CountFromSelect{ws.count, kv.L_cap}, kv.L_cap, row_bytes, units, err);
+    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_pdl(compact_weights, dim3(walk_grid(compact_weights, 256, 0, units, 1)), dim3(256), 0, s, weights,
+                   (const int32_t *)idx, (const int32_t *)ws.count, kv.L_cap, units);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -17,12 +17,14 @@ _lib = None
 RECO_OK, RECO_EINVAL, RECO_EUNSUPPORTED, RECO_ECUDA, RECO_EDEVICE = range(5)
 RECO_F32, RECO_BF16 = 0, 1
 RECO_OP_SCORE, RECO_OP_SELECT, RECO_OP_DECODE, RECO_OP_PPL, RECO_OP_SAMPLE = range(5)
+RECO_OP_PAGED_DECODE, RECO_OP_PAGED_WEIGHTS, RECO_OP_PAGED_EVICT = range(5, 8)
 
 EXPORTS = ("reco_retention_ratio", "reco_keep_count", "reco_penalty_band", "reco_probe_trigger",
            "reco_workspace_bytes", "reco_last_error", "reco_check", "reco_score_cache",
            "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact", "reco_select_topm", "reco_compact",
            "reco_decode_attn", "reco_decode_attn_ring", "reco_reflect_penalty", "reco_penalty_sample", "reco_answer_ppl",
-           "reco_answer_ppl_static")
+           "reco_answer_ppl_static", "reco_paged_workspace_bytes", "reco_paged_decode_attn",
+           "reco_paged_decode_attn_weights", "reco_paged_evict")
 RECO_PPL_STATIC_MAX_ROWS = 65536
 
 
@@ -36,6 +38,13 @@ class reco_kv(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_layers", ctypes.c_int),
                 ("B", ctypes.c_int), ("H_q", ctypes.c_int), ("H_kv", ctypes.c_int),
                 ("L_cap", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class reco_paged_kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("n_layers", ctypes.c_int), ("B", ctypes.c_int), ("H_q", ctypes.c_int), ("H_kv", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("max_pages", ctypes.c_int), ("page", ctypes.c_int), ("d", ctypes.c_int),
+                ("dtype", ctypes.c_int)]
 
 
 def library_path() -> Path:
@@ -76,7 +85,13 @@ def lib():
     L.reco_penalty_sample.argtypes = [vp, i32, i32, vp, i32, vp, f32, f32, f32, vp, vp, vp, vp, sz, vp]
     L.reco_answer_ppl.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, sz, vp]
     L.reco_answer_ppl_static.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, vp, vp]
-    for name in ("reco_retention_ratio", "reco_keep_count", "reco_workspace_bytes", "reco_check",
+    pkvp = ctypes.POINTER(reco_paged_kv)
+    L.reco_paged_workspace_bytes.argtypes = [i32, pkvp, ctypes.POINTER(sz)]
+    L.reco_paged_decode_attn.argtypes = [pkvp, vp, vp, vp, vp, f32, i32, i32, vp, i32, vp, vp, sz, vp]
+    L.reco_paged_decode_attn_weights.argtypes = [pkvp, vp, vp, vp, vp, f32, i32, i32, vp, i32, vp, vp, vp, sz, vp]
+    L.reco_paged_evict.argtypes = [pkvp, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+    for name in ("reco_paged_workspace_bytes", "reco_paged_decode_attn", "reco_paged_decode_attn_weights",
+                 "reco_paged_evict", "reco_retention_ratio", "reco_keep_count", "reco_workspace_bytes", "reco_check",
                  "reco_score_cache", "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact",
                  "reco_select_topm", "reco_compact",
                  "reco_decode_attn", "reco_decode_attn_ring", "reco_reflect_penalty", "reco_penalty_sample",
@@ -241,6 +256,98 @@ def reco_decode_attn_ring(kv: reco_kv, q, k_new, v_new, lens, scale: float, out,
     _ok(lib().reco_decode_attn_ring(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(lens), float(scale),
                                     _ptr(out), _dtype_code(out.dtype), _ptr(ring), S, _ptr(slot), _ptr(q_ring),
                                     _ptr(ws), ws.numel(), _stream(stream)))
+
+
+# ---------------------------------------------------------------- the paged cache
+def make_paged_kv(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, H_q: int) -> reco_paged_kv:
+    """Describe contiguous [layers, n_pages, H_kv, page, d] pools K and V and an int32 [B, max_pages]
+    table of each sequence's pages.  The description keeps the three tensors alive."""
+    if K.shape != V.shape or K.dtype != V.dtype or K.dim() != 5:
+        raise ValueError("K and V must be [layers, n_pages, H_kv, page, d] with equal shape and dtype")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("table must be an int32 [B, max_pages] tensor")
+    if not (K.is_contiguous() and V.is_contiguous() and table.is_contiguous()):
+        raise ValueError("K, V and table must be contiguous")
+    if K.device != V.device or K.device != table.device:
+        raise ValueError("K, V and table must be on one device")
+    Ly, n_pages, Hkv, page, d = K.shape
+    B, max_pages = table.shape
+    kv = reco_paged_kv(K.data_ptr(), V.data_ptr(), table.data_ptr(), Ly, B, H_q, Hkv, n_pages, max_pages, page, d,
+                       _dtype_code(K.dtype))
+    kv.tensors = (K, V, table)
+    return kv
+
+
+def _paged_args(kv: reco_paged_kv, ws, args):
+    """args: (name, tensor or None, shape, dtype or None).  The library takes bare pointers: a tensor
+    of another shape, type or device, or with gaps, would be read out of place."""
+    dev = kv.tensors[0].get_device()
+    for name, t, shape, dtype in args:
+        if t is None:
+            continue
+        if t.shape != shape or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"{name} must be {list(shape)}" + (f" of {dtype}" if dtype else "") +
+                             f", not {list(t.shape)} of {t.dtype}")
+        if not t.is_contiguous() or t.get_device() != dev:
+            raise ValueError(f"{name} must be contiguous and on the cache's device")
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != dev:
+        raise ValueError("ws must be a contiguous uint8 tensor on the cache's device")
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("the cache must be on the current CUDA device")
+
+
+def reco_paged_workspace_bytes(op: int, kv: reco_paged_kv) -> int:
+    out = ctypes.c_size_t()
+    _ok(lib().reco_paged_workspace_bytes(op, ctypes.byref(kv), ctypes.byref(out)))
+    return out.value
+
+
+def paged_workspace(op: int, kv: reco_paged_kv, device="cuda") -> torch.Tensor:
+    """A workspace for a paged call, with its counters zero as the decode needs them before its first use
+    (the logits of a call with weights lie behind what a call without needs, and need no fill)."""
+    ws = torch.empty(max(reco_paged_workspace_bytes(op, kv), 256), dtype=torch.uint8, device=device)
+    if op != RECO_OP_PAGED_EVICT:
+        ws[:reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv)].zero_()
+    return ws
+
+
+def _paged_decode_args(kv, q, k_new, v_new, lens, out, lse):
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new must both be given or both be None")
+    qs, new, dt = (kv.n_layers, kv.B, kv.H_q, kv.d), (kv.n_layers, kv.B, kv.H_kv, kv.d), kv.tensors[0].dtype
+    return [("q", q, qs, dt), ("k_new", k_new, new, dt), ("v_new", v_new, new, dt), ("lens", lens, new[:3], torch.int32),
+            ("out", out, qs, None), ("lse", lse, qs[:3], torch.float32)]
+
+
+def reco_paged_decode_attn(kv: reco_paged_kv, q, k_new, v_new, lens, scale: float, out, lse, ws, window: int = 0,
+                           sinks: int = 0, stream=None):
+    """window > 0: a query sees the first `sinks` rows and the latest `window` rows (the new one included)."""
+    _paged_args(kv, ws, _paged_decode_args(kv, q, k_new, v_new, lens, out, lse))
+    _ok(lib().reco_paged_decode_attn(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(lens), float(scale),
+                                     int(window), int(sinks), _ptr(out), _dtype_code(out.dtype), _ptr(lse), _ptr(ws),
+                                     ws.numel(), _stream(stream)))
+
+
+def reco_paged_decode_attn_weights(kv: reco_paged_kv, q, k_new, v_new, lens, scale: float, out, lse, weights, ws,
+                                   window: int = 0, sinks: int = 0, stream=None):
+    """reco_paged_decode_attn that also adds each row's attention weight (the mean over the query heads of
+    its KV head) to weights [layers, B, H_kv, max_pages * page] float32."""
+    _paged_args(kv, ws, _paged_decode_args(kv, q, k_new, v_new, lens, out, lse) +
+                [("weights", weights, (kv.n_layers, kv.B, kv.H_kv, kv.max_pages * kv.page), torch.float32)])
+    _ok(lib().reco_paged_decode_attn_weights(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(lens),
+                                             float(scale), int(window), int(sinks), _ptr(out), _dtype_code(out.dtype),
+                                             _ptr(lse), _ptr(weights), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def reco_paged_evict(kv: reco_paged_kv, weights, lens, budget, w: int, sinks: int, kept_idx, ws, stream=None):
+    """Cuts every unit longer than budget[b] down to it: the first `sinks` rows, the latest `w` rows and the
+    rows of the largest weights between them stay, in order."""
+    unit = (kv.n_layers, kv.B, kv.H_kv)
+    rows = unit + (kv.max_pages * kv.page,)
+    _paged_args(kv, ws, [("weights", weights, rows, torch.float32), ("lens", lens, unit, torch.int32),
+                     ("budget", budget, (kv.B,), torch.int32), ("kept_idx", kept_idx, rows, torch.int32)])
+    _ok(lib().reco_paged_evict(ctypes.byref(kv), _ptr(weights), _ptr(lens), _ptr(budget), int(w), int(sinks),
+                               _ptr(kept_idx), _ptr(ws), ws.numel(), _stream(stream)))
 
 
 def reco_reflect_penalty(logits, ids, rewards, tau_l=0.4, tau_h=0.8, beta=4.0, beta_out=None,
