@@ -338,11 +338,13 @@ reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const
  * over every decoded token, as the tokens are decoded):
  *   weights[unit, j] += (1/G) * sum_g softmax_j(scale * q[layer,b,h*G+g,:] . K_j)
  * for the rows j seen; an appended row starts at its own weight (what its entry held
- * before does not count).  The entries of other rows are left as they are, and so are all
- * entries of a unit that is in error.
- *   weights : [n_layers][B][H_kv][max_pages * page] float32 (device, in/out)
- *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, otherwise as
- *             reco_paged_decode_attn's
+ * before does not count).  The entries of other rows are left as they are, and so are
+ * those of all rows of a unit that is in error.
+ *   weights : [n_layers][B][H_kv][max_pages * page] float32, 16-byte aligned (device,
+ *             in/out)
+ *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, of which the
+ *             first reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) are zero-filled
+ *             before its first use; otherwise as reco_paged_decode_attn's
  * Every other argument and result is that of reco_paged_decode_attn.  The same inputs
  * give the same sums bit for bit.                                                    */
 reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *q, const void *k_new,

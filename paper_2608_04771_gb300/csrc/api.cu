@@ -465,8 +465,8 @@ reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const v
     if ((k_new == nullptr) != (v_new == nullptr)) return fail(RECO_EINVAL, "k_new and v_new must both be given or both NULL");
     if (!al16(q) || !al16(out) || (k_new && (!al16(k_new) || !al16(v_new))))
         return fail(RECO_EINVAL, "q, out, k_new and v_new must be 16-byte aligned");
-    if (((uintptr_t)lens & 3u) || ((uintptr_t)lse & 3u) || ((uintptr_t)weights & 3u))
-        return fail(RECO_EINVAL, "lens, lse and weights must be 4-byte aligned");
+    if (((uintptr_t)lens & 3u) || ((uintptr_t)lse & 3u) || !al16(weights))
+        return fail(RECO_EINVAL, "lens and lse must be 4-byte aligned, weights 16-byte aligned");
     if (out_dtype != RECO_F32 && out_dtype != RECO_BF16) return fail(RECO_EINVAL, "unknown out_dtype %d", (int)out_dtype);
     if (window < 0 || sinks < 0) return fail(RECO_EINVAL, "window %d and sinks %d must be >= 0", window, sinks);
     if (window == 0 && sinks > 0) return fail(RECO_EINVAL, "sinks without a window (window 0 sees every row)");

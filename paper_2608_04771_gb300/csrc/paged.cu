@@ -1,11 +1,11 @@
 // paged.cu -- decode attention of one new token over a paged cache, and the accumulation of the
-// rows' attention weights.
+// rows' attention weights (Eq. 2's sums, taken token by token as the tokens are decoded).
 //
-// paged_decode: one CTA per unit; its warps take the visible rows in turn, each with an online
-// softmax over all query heads, and join at the end.  paged_weights: the second pass of a call
-// with weights, one warp per row, from the log-sum-exps of the first.
-#include "common.cuh"
-#include "internal.h"
+// The attention is the streamed kernel of decode_stream.cuh over pages.  A call with weights has it
+// leave its logits (4 G bytes a row, against 4 d bytes of K and V in bf16) in the workspace; they
+// become weights once a unit's log-sum-exps are known, in paged_weights, mostly from L2, where a
+// second product with K would read half of the cache again.
+#include "decode_stream.cuh"
 
 namespace reco {
 
@@ -27,190 +27,120 @@ PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void
     return ws;
 }
 
-struct PagedArgs {
-    void *K, *V;
-    const int32_t *table;
-    const void *q, *k_new, *v_new;
-    int32_t *lens;
-    void *out;
-    float *lse, *lse2, *weights;
-    int B, Hq, Hkv, G, cap, n_pages, max_pages, shift, append, out_bf16, window, sinks;
-    float c2;  // scale * log2(e)
-    unsigned *err;
-};
+// weights[u, j] += (1/G) sum_g 2^(logit - lse2) for the rows in sight.  Threads take four rows at a time
+// (a block of the decode holds all four or none).
+constexpr int kWeightThreads = 256, kWeightRows = 4 * kWeightThreads;
 
-// Row j of the unit, or -1 where the table names no page of the pool.
-__device__ __forceinline__ long paged_row(const PagedArgs &a, long u, int j)
+__global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__restrict__ logits,
+                                                                const float *__restrict__ lse2,
+                                                                const int32_t *__restrict__ lens, int G, int cap,
+                                                                int window, int sinks, float *weights)
 {
-    const long lb = u / a.Hkv;
-    const int e = a.table[(lb % a.B) * a.max_pages + (j >> a.shift)];
-    if ((unsigned)e >= (unsigned)a.n_pages) return -1;
-    return ((((lb / a.B) * a.n_pages + e) * a.Hkv + u % a.Hkv) << a.shift) + (j & ((1 << a.shift) - 1));
-}
-
-template <typename T, int D>
-__global__ void __launch_bounds__(128) paged_decode(PagedArgs a)
-{
-    constexpr int NW = 4, PER = D / 32, GM = 16;
-    __shared__ float sm_m[NW][GM], sm_l[NW][GM];
-    __shared__ float sm_o[NW][GM][D];
-    const long u = blockIdx.x;
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int L = a.lens[u];
-    bool ok = L >= 0 && L <= a.cap && (!a.append || L < a.cap);
-    if (!ok && threadIdx.x == 0) raise_error(a.err, (a.append && L == a.cap) ? ERR_ROOM : ERR_LEN);
-    const int n = ok ? L + a.append : 0;
-    const int start = a.window > 0 && n > a.window ? n - a.window : 0;  // rows from here on are seen
-    const int head = min(a.sinks, start);                               // and the rows before this
-    // all needed table entries first
-    bool bad = false;
-    for (int p = threadIdx.x; p << a.shift < n; p += blockDim.x)
-        if (((p + 1) << a.shift) > start || p << a.shift < head) bad |= paged_row(a, u, p << a.shift) < 0;
-    if (__syncthreads_or(bad)) {
-        if (threadIdx.x == 0) raise_error(a.err, ERR_PAGE);
-        ok = false;
-    }
-    const int Le = ok ? n : 0;
-    const long lb = u / a.Hkv;
-    const int h = (int)(u % a.Hkv), G = a.G;
-    T *K = reinterpret_cast<T *>(a.K), *V = reinterpret_cast<T *>(a.V);
-    const T *kn = reinterpret_cast<const T *>(a.k_new) + u * D, *vn = reinterpret_cast<const T *>(a.v_new) + u * D;
-    const T *qp = reinterpret_cast<const T *>(a.q) + (lb * a.Hq + (long)h * G) * D;
-    float q[GM][PER], o[GM][PER], m[GM], l[GM];
-#pragma unroll
-    for (int g = 0; g < GM; ++g) {
-        m[g] = -INFINITY;
-        l[g] = 0.f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            q[g][i] = g < G ? to_float(qp[(long)g * D + lane * PER + i]) : 0.f;
-            o[g][i] = 0.f;
-        }
-    }
-    for (int v = wid; v < head + Le - start; v += NW) {
-        const int j = v < head ? v : v - head + start;
-        const bool app = a.append && j == L;
-        const long r = paged_row(a, u, j);
-        const T *kr = app ? kn : K + r * D, *vr = app ? vn : V + r * D;
-        float kk[PER], vv[PER];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            kk[i] = to_float(kr[lane * PER + i]);
-            vv[i] = to_float(vr[lane * PER + i]);
-        }
-#pragma unroll
-        for (int g = 0; g < GM; ++g) {
-            if (g < G) {
-                float s = 0.f;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) s = fmaf(q[g][i], kk[i], s);
-                s = warp_sum(s) * a.c2;
-                const float mn = fmaxf(m[g], s);
-                const float base = mn == -INFINITY ? 0.f : mn;
-                const float al = fast_exp2(m[g] - base), p = fast_exp2(s - base);
-                l[g] = l[g] * al + p;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) o[g][i] = fmaf(o[g][i], al, p * vv[i]);
-                m[g] = mn;
-            }
-        }
-    }
-#pragma unroll
-    for (int g = 0; g < GM; ++g) {
-        if (g < G) {
-            if (lane == 0) {
-                sm_m[wid][g] = m[g];
-                sm_l[wid][g] = l[g];
-            }
-#pragma unroll
-            for (int i = 0; i < PER; ++i) sm_o[wid][g][lane * PER + i] = o[g][i];
-        }
-    }
+    wait_prior_grid();
+    const long u = blockIdx.y;
+    const int n = lens[u];
+    if (n < 0 || n > cap) return;  // reported by the decode
+    __shared__ float sm_lse[16];
+    if (threadIdx.x < G) sm_lse[threadIdx.x] = lse2[u * G + threadIdx.x];
     __syncthreads();
-    for (int e = threadIdx.x; e < G * D; e += blockDim.x) {
-        const int g = e / D, dd = e % D;
-        float M = -INFINITY;
-        for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w][g]);
-        float Ls = 0.f, O = 0.f;
-        if (M != -INFINITY) {
-            for (int w = 0; w < NW; ++w) {
-                const float wt = fast_exp2(sm_m[w][g] - M);
-                Ls += sm_l[w][g] * wt;
-                O += sm_o[w][g][dd] * wt;
-            }
-        }
-        const size_t row = (size_t)(lb * a.Hq + (long)h * G + g);
-        const float res = Ls > 0.f ? O / Ls : 0.f;
-        if (a.out_bf16)
-            reinterpret_cast<__nv_bfloat16 *>(a.out)[row * D + dd] = __float2bfloat16_rn(res);
-        else
-            reinterpret_cast<float *>(a.out)[row * D + dd] = res;
-        if (dd == 0) {
-            const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
-            if (a.lse) a.lse[row] = l2 * kLn2;
-            if (a.lse2) a.lse2[row] = l2;
-        }
-    }
-    if (ok && a.append) {
-        const long r = paged_row(a, u, L);
-        for (int e = threadIdx.x; e < D; e += blockDim.x) {
-            K[r * D + e] = kn[e];
-            V[r * D + e] = vn[e];
-        }
-        if (threadIdx.x == 0) {
-            a.lens[u] = L + 1;
-            if (a.weights) a.weights[u * a.cap + L] = 0.f;
-        }
-    }
-}
-
-template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_weights(PagedArgs a)
-{
-    constexpr int PER = D / 32;
-    const long u = blockIdx.x;
-    const int lane = threadIdx.x & 31;
-    const int n = a.lens[u];
-    if (n < 0 || n > a.cap) return;
-    const long lb = u / a.Hkv;
-    const size_t q0 = lb * a.Hq + (u % a.Hkv) * a.G;
     bool any = false;
-    for (int g = 0; g < a.G; ++g) any |= a.lse2[q0 + g] != -INFINITY;
-    if (!any) return;
-    const int start = a.window > 0 && n > a.window ? n - a.window : 0, head = min(a.sinks, start);
-    for (int v = blockIdx.y * 8 + (threadIdx.x >> 5); v < head + n - start; v += gridDim.y * 8) {
-        const int j = v < head ? v : v - head + start;
-        const T *kr = reinterpret_cast<const T *>(a.K) + paged_row(a, u, j) * D;
-        float w = 0.f;
-        for (int g = 0; g < a.G; ++g) {
-            const T *qp = reinterpret_cast<const T *>(a.q) + (q0 + g) * D;
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) s = fmaf(to_float(qp[lane * PER + i]), to_float(kr[lane * PER + i]), s);
-            s = warp_sum(s) * a.c2;
-            if (a.lse2[q0 + g] != -INFINITY) w += fast_exp2(s - a.lse2[q0 + g]);
+    for (int g = 0; g < G; ++g) any |= sm_lse[g] != -INFINITY;
+    if (!any) return;  // no rows, or in error
+    const int start = window > 0 && n > window ? n - window : 0, head = min(sinks, start);
+    const float inv = 1.f / (float)G;
+    for (int j0 = (blockIdx.x * kWeightThreads + threadIdx.x) * 4; j0 < n; j0 += gridDim.x * kWeightRows) {
+        if (j0 >= head && j0 + 4 <= start) continue;
+        float4 *dst = reinterpret_cast<float4 *>(weights + u * cap + j0);
+        const float *src = logits + u * G * cap + j0;
+        const float4 old = *dst;
+        float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int g = 0; g < G; ++g) {
+            const float4 x = __ldcs(reinterpret_cast<const float4 *>(src + (long)g * cap));
+            const float z = sm_lse[g];
+            if (z == -INFINITY) continue;
+            p.x += fast_exp2(x.x - z);
+            p.y += fast_exp2(x.y - z);
+            p.z += fast_exp2(x.z - z);
+            p.w += fast_exp2(x.w - z);
         }
-        if (lane == 0) a.weights[u * a.cap + j] += w / (float)a.G;
+        const float4 sum = make_float4(fmaf(p.x, inv, old.x), fmaf(p.y, inv, old.y), fmaf(p.z, inv, old.z),
+                                       fmaf(p.w, inv, old.w));
+        if (j0 + 4 <= n && (j0 + 4 <= head || j0 >= start)) {
+            *dst = sum;
+        } else {
+            auto seen = [&](int j) { return j < n && (j < head || j >= start); };
+            if (seen(j0)) dst->x = sum.x;
+            if (seen(j0 + 1)) dst->y = sum.y;
+            if (seen(j0 + 2)) dst->z = sum.z;
+            if (seen(j0 + 3)) dst->w = sum.w;
+        }
     }
-}
-
-template <typename T, int D> static cudaError_t launch(const PagedArgs &a, unsigned units, cudaStream_t s)
-{
-    paged_decode<T, D><<<units, 128, 0, s>>>(a);
-    if (a.weights) paged_weights<T, D><<<dim3(units, 8), 256, 0, s>>>(a);
-    return cudaGetLastError();
 }
 
 cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new,
                                 int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
                                 float *lse, float *weights, const PagedDecodeWs &ws, unsigned *err, cudaStream_t s)
 {
-    const PagedArgs a{kv.k, kv.v, kv.table, q, k_new, v_new, lens, out, lse, ws.lse2, weights, kv.B, kv.H_q, kv.H_kv,
-                      kv.H_q / kv.H_kv, paged_cap(kv), kv.n_pages, kv.max_pages, __builtin_ctz((unsigned)kv.page),
-                      k_new ? 1 : 0, out_dtype == RECO_BF16 ? 1 : 0, window, sinks, scale * kLog2e, err};
-    const unsigned units = (unsigned)(kv.n_layers * kv.B * kv.H_kv);
-    if (kv.dtype == RECO_F32) return kv.d == 64 ? launch<float, 64>(a, units, s) : launch<float, 128>(a, units, s);
-    return kv.d == 64 ? launch<__nv_bfloat16, 64>(a, units, s) : launch<__nv_bfloat16, 128>(a, units, s);
+    const bool f32 = kv.dtype == RECO_F32;
+    const int cap = paged_cap(kv);
+    DecodeArgs a = {};
+    a.K = kv.k;
+    a.V = kv.v;
+    a.counters = ws.dec.counters;
+    a.part_ml = ws.dec.part_ml;
+    a.part_o = ws.dec.part_o;
+    a.Hq = kv.H_q;
+    a.Hkv = kv.H_kv;
+    a.G = kv.H_q / kv.H_kv;
+    a.L_cap = cap;
+    a.append = k_new ? 1 : 0;
+    a.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;
+    a.c2 = scale * kLog2e;
+    a.err = err;
+    a.table = kv.table;
+    a.B = kv.B;
+    a.n_pages = kv.n_pages;
+    a.max_pages = kv.max_pages;
+    a.page_shift = __builtin_ctz((unsigned)kv.page);
+    a.window = window;
+    a.sinks = sinks;
+    const int units = kv.n_layers * kv.B * kv.H_kv;
+    const StreamKernel k = stream_kernel<true>(kv.d, f32, units, a.G, cap);
+    a.hs_min = k.hs;
+    CUtensorMap mk = {}, mv = {};
+    const unsigned long long rows = (unsigned long long)kv.n_layers * kv.n_pages * kv.H_kv * kv.page;
+    if (!f32 && (!encode_cache_map(&mk, kv.k, rows, kv.d) || !encode_cache_map(&mv, kv.v, rows, kv.d)))
+        return cudaErrorInvalidValue;
+    const size_t row_b = (size_t)kv.d * (f32 ? 4 : 2), out_b = (size_t)kv.d * (a.out_bf16 ? 2 : 4);
+    for (long long u0 = 0; u0 < units; u0 += k.part_units) {  // as many units as one plan holds
+        const int cu = (int)std::min(k.part_units, units - u0);
+        const size_t q0 = (size_t)u0 * a.G;
+        DecodeArgs at = a;
+        at.u0 = (int)u0;
+        at.units = cu;
+        at.hs_max = k.most_halves(cu, a.G);
+        at.q = static_cast<const char *>(q) + q0 * row_b;
+        at.k_new = k_new ? static_cast<const char *>(k_new) + (size_t)u0 * row_b : nullptr;
+        at.v_new = v_new ? static_cast<const char *>(v_new) + (size_t)u0 * row_b : nullptr;
+        at.lens = lens + u0;
+        at.out = static_cast<char *>(out) + q0 * out_b;
+        at.lse = lse ? lse + q0 : nullptr;
+        if (weights) {
+            at.lse2 = ws.lse2 + q0;
+            at.logits = ws.logits + q0 * cap;
+            at.weights = weights + (size_t)u0 * cap;
+        }
+        const cudaError_t e = launch_stream(k.fn, kv.d, mk, mv, at, ws.dec.part_slots, s);
+        if (e != cudaSuccess) return e;
+    }
+    if (!weights) return cudaSuccess;
+    // CTAs over a unit's rows: enough that all units together fill the GPU four times over, never more than
+    // the rows of a unit need (lengths are not known here, and CTAs without rows cost time too)
+    const int need = (cap + kWeightRows - 1) / kWeightRows, fill = 4 * 8 * device_sm_count() / units;
+    const cudaError_t e = launch_pdl(paged_weights, dim3(std::max(1, std::min(need, fill)), units), dim3(kWeightThreads),
+                                     0, s, (const float *)ws.logits, (const float *)ws.lse2, (const int32_t *)lens, a.G,
+                                     cap, window, sinks, weights);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace reco

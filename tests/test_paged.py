@@ -149,7 +149,7 @@ def test_descriptors_that_are_refused(L, bad, status):
     (dict(v_new=16), b"k_new", reco.RECO_EINVAL), (dict(q=24), b"aligned", reco.RECO_EINVAL),
     (dict(out=20), b"aligned", reco.RECO_EINVAL), (dict(k_new=16, v_new=24), b"aligned", reco.RECO_EINVAL),
     (dict(lens=18), b"aligned", reco.RECO_EINVAL), (dict(lse=17), b"aligned", reco.RECO_EINVAL),
-    (dict(weights=18), b"aligned", reco.RECO_EINVAL), (dict(out_dtype=7), b"out_dtype", reco.RECO_EINVAL),
+    (dict(weights=24), b"aligned", reco.RECO_EINVAL), (dict(out_dtype=7), b"out_dtype", reco.RECO_EINVAL),
     (dict(window=-1), b"window", reco.RECO_EINVAL), (dict(window=5, sinks=-1), b"sinks", reco.RECO_EINVAL),
     (dict(sinks=4), b"window", reco.RECO_EINVAL), (dict(scale=float("nan")), b"scale", reco.RECO_EINVAL),
     (dict(ws=None), b"workspace", reco.RECO_EINVAL), (dict(ws=128), b"aligned", reco.RECO_EINVAL),
