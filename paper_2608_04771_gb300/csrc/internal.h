@@ -61,10 +61,12 @@ struct DecodeWs {
     size_t bytes;
 };
 
-// What the paged decode needs beside the decode's own regions: with weights, the token's
-// logits and normalisers.
+// Regions of the paged decode's workspace; the last two for calls with weights: the token's
+// normalisers and logits.
 struct PagedDecodeWs {
-    DecodeWs dec;
+    int32_t *counters;  // [2 + units]: [0] stops and errors, [1] CTAs done, [2 + u] tickets
+    float *part_ml;     // [2 * CTAs][G][2]   (m log2, l)
+    float *part_o;      // [2 * CTAs][G][d]   unnormalised output
     float *lse2;    // [n_layers * B * H_q]         log2 of the softmax sums
     float *logits;  // [n_layers * B * H_q][cap]    scale * log2(e) * q . k, rows a multiple of 16 floats
     size_t bytes;

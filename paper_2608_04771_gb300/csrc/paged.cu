@@ -1,30 +1,583 @@
-// paged.cu -- decode attention of one new token over a paged cache, and the accumulation of the
-// rows' attention weights (Eq. 2's sums, taken token by token as the tokens are decoded).
+// paged.cu -- decode attention of one new token over a paged cache (the per-token attention of
+// Sec. 1, 2.2 and 4.2, rows in pages), and the accumulation of the rows' attention weights (Eq. 2's
+// sums, taken token by token as the tokens are decoded).
 //
-// The attention is the streamed kernel of decode_stream.cuh over pages.  A call with weights has it
-// leave its logits (4 G bytes a row, against 4 d bytes of K and V in bf16) in the workspace; they
-// become weights once a unit's log-sum-exps are known, in paged_weights, mostly from L2, where a
-// second product with K would read half of the cache again.
-#include "decode_stream.cuh"
+// paged_decode: persistent, one CTA per SM of eight warps that compute and one that copies.  The
+// blocks of rows of all units (8 KB of K and V at d = 128) are laid end to end and every CTA takes
+// an equal range of them; inside it the blocks go to the warps in turn, each into its own ring of
+// three stages, filled by TMA copies (bf16) or bulk copies (float32).  Lane w of the copying warp
+// feeds warp w: it walks the same units, looks the pages up (a block never straddles two), and waits
+// for free stages, so that the computing warps spend nothing on either.  What a warp does with a
+// block is decode_block.cuh's.  At the end of a unit's piece the warps join their (max, sum, output)
+// through shared memory; a unit cut between CTAs leaves one partial per CTA, which the last CTA to
+// finish (atomic ticket, no waiting) joins.  Units of many query heads (bf16 9 to 16, float32 5 to 16)
+// run on fewer streams of two or four warps each, a part of the heads per warp, all reading the stage
+// that was copied once.
+//
+// Many short units would spend their time joining: there every unit goes whole to one warp.
+//
+// A window leaves the blocks that hold rows in sight: the first `head` ones and those `gap` further on
+// are the unit's list, in which everything above counts; a block that a border crosses masks its rows.
+//
+// A call with weights has the kernel leave its logits (4 G bytes a row, against 4 d bytes of K and V in
+// bf16) in the workspace; paged_weights turns them into weights once the units' log-sum-exps are known.
+#include <algorithm>
+
+#include "decode_block.cuh"
+#include "internal.h"
 
 namespace reco {
 
+constexpr int kPagedWarps = 8;               // computing warps per CTA
+constexpr int kPagedThreads = 32 * kPagedWarps;  // and their threads; 32 more copy
+constexpr int kPagedStages = 24;             // ring stages per CTA
+constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
+constexpr int kStageBytes = 8192;            // a block of K and V rows at d = 128 (half of it at d = 64)
+constexpr int kMinBlocks = 16;               // blocks per working CTA at least (fewer CTAs rather than less)
+constexpr int kSnapDiv = 8;                  // a cut within this part of a CTA's range of a unit's end moves there
+constexpr int kWholeBlocks = 16;             // units of at most this many blocks go whole to a warp ...
+constexpr int kWholeUnits = 4;               // ... where every CTA has this many of them
+
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base)
 {
-    const reco_kv units{kv.k, kv.v, kv.n_layers, kv.B, kv.H_q, kv.H_kv, paged_cap(kv), kv.d, kv.dtype};
-    PagedDecodeWs ws;
-    ws.dec = decode_ws_layout(units, base);
-    size_t off = ws.dec.bytes;
+    size_t off = 0;
     auto take = [&](size_t bytes) {
         char *r = base ? (char *)base + off : nullptr;
         off += align256(bytes);
         return r;
     };
-    const size_t heads = (size_t)kv.n_layers * kv.B * kv.H_q;
+    const size_t units = (size_t)kv.n_layers * kv.B * kv.H_kv, heads = (size_t)kv.n_layers * kv.B * kv.H_q;
+    const size_t G = kv.H_q / kv.H_kv;
+    PagedDecodeWs ws;
+    ws.counters = (int32_t *)take((2 + units) * 4);
+    ws.part_ml = (float *)take(2 * kPagedMaxGrid * G * 2 * 4);
+    ws.part_o = (float *)take(2 * kPagedMaxGrid * G * kv.d * 4);
     ws.lse2 = weights ? (float *)take(heads * 4) : nullptr;
     ws.logits = weights ? (float *)take(heads * paged_cap(kv) * 4) : nullptr;
     ws.bytes = off;
     return ws;
+}
+
+struct PagedArgs {
+    void *K, *V;
+    const int32_t *table;
+    const void *q, *k_new, *v_new;
+    int32_t *lens;
+    void *out;
+    float *lse;      // or nullptr
+    float *lse2;     // or nullptr: log2 of the softmax sums
+    float *logits;   // or nullptr: [query head][cap] base-2 logits of the rows seen
+    float *weights;  // with logits: the running sums; an appended row's starts at zero
+    int32_t *counters;  // [0] warps that stopped and units in error, [1] CTAs done, [2 + u] tickets
+    float *part_ml, *part_o;
+    int units, B, Hq, Hkv, G, cap, n_pages, max_pages, shift, append, out_bf16, window, sinks;
+    float c2;  // scale * log2(e)
+    unsigned *err;
+};
+
+// Rows [h0, h1) of a unit are out of sight.  Its list of blocks: the first `head` ones, then those `gap`
+// further on.
+struct Sight {
+    int head, gap, h0, h1;
+};
+template <int KB> __device__ __forceinline__ Sight sight_of(const PagedArgs &a, int le)
+{
+    if (a.window == 0 || le <= a.window) return Sight{0, 0, 0, 0};
+    const int h1 = le - a.window, h0 = min(a.sinks, h1);
+    const int head = (h0 + KB - 1) / KB;
+    return Sight{head, max(0, h1 / KB - head), h0, h1};
+}
+
+// Rows of a unit with the appended one, 0 for a unit in error.
+__device__ __forceinline__ int rows_of(const PagedArgs &a, int L) { return unit_ok(L, a.cap, a.append) ? L + a.append : 0; }
+template <int KB> __device__ __forceinline__ int blocks_of(const PagedArgs &a, int le)
+{
+    return (le + KB - 1) / KB - sight_of<KB>(a, le).gap;
+}
+
+// A unit's table, and its row in page 0 of its layer.
+struct Pages {
+    const int32_t *table;
+    int base;
+};
+__device__ __forceinline__ Pages pages_of(const PagedArgs &a, int u)
+{
+    const int lb = u / a.Hkv, layer = lb / a.B;
+    return Pages{a.table + (long)(lb - layer * a.B) * a.max_pages, (layer * a.n_pages * a.Hkv + (u - lb * a.Hkv)) << a.shift};
+}
+__device__ __forceinline__ int page_entry(const PagedArgs &a, const Pages &p, int k) { return __ldg(p.table + (k >> a.shift)); }
+// Pool row of row k, -1 where its table entry e names no page of the pool.
+__device__ __forceinline__ int paged_row(const PagedArgs &a, const Pages &p, int k, int e)
+{
+    if ((unsigned)e >= (unsigned)a.n_pages) return -1;
+    return p.base + ((e * a.Hkv) << a.shift) + (k & ((1 << a.shift) - 1));
+}
+
+// The walk of a CTA over its range of blocks, a piece (its part of one unit) at a time.
+struct Piece {
+    int u, le, nb, lo, hi;  // unit, its rows, its blocks, and those of this piece: [lo, hi)
+    int at;                 // lo counted from the start of the CTA's range
+    Sight sg;
+};
+struct Walk {
+    int u, b, ub, nb, le, begin, end;
+};
+template <int KB> __device__ __forceinline__ bool next_piece(const PagedArgs &a, Walk &w, Piece &p)
+{
+    while (w.b < w.end) {
+        if (w.b >= w.ub + w.nb) {
+            w.ub += w.nb;
+            ++w.u;
+            w.le = rows_of(a, a.lens[w.u]);
+            w.nb = blocks_of<KB>(a, w.le);
+            continue;
+        }
+        p.u = w.u;
+        p.le = w.le;
+        p.nb = w.nb;
+        p.lo = w.b - w.ub;
+        p.hi = min(w.end - w.ub, w.nb);
+        p.at = w.b - w.begin;
+        p.sg = sight_of<KB>(a, w.le);
+        w.b = w.ub + p.hi;
+        return true;
+    }
+    return false;
+}
+
+__device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;" ::"n"(kPagedThreads) : "memory"); }
+
+__device__ __forceinline__ void put_lse(const PagedArgs &a, size_t row, float l2)
+{
+    if (a.lse) a.lse[row] = l2 * kLn2;
+    if (a.lse2) a.lse2[row] = l2;
+}
+
+__device__ __forceinline__ void store_out4(const PagedArgs &a, size_t i, float4 v)
+{
+    if (a.out_bf16) {
+        uint2 w;
+        w.x = pack_bf16(v.x, v.y);
+        w.y = pack_bf16(v.z, v.w);
+        *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + i) = w;
+    } else {
+        *reinterpret_cast<float4 *>(reinterpret_cast<float *>(a.out) + i) = v;
+    }
+}
+
+// Ring, then [warp][head][D] floats: the warps' outputs as they join (and, until then, each warp's scratch).
+template <class Block> constexpr int paged_smem()
+{
+    return 1024 + kPagedStages * (kStageBytes * Block::D / 128) + kPagedWarps * Block::GM * Block::D * 4;
+}
+
+template <class Block, int HS>
+__global__ void __launch_bounds__(kPagedThreads + 32, 1)
+    paged_decode(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, PagedArgs a)
+{
+    constexpr int D = Block::D, KB = Block::KB, GM = Block::GM;
+    constexpr int NW = kPagedWarps, NS = NW / HS, S = kPagedStages / NS, STAGE = kStageBytes * D / 128;
+    constexpr int NT = kPagedThreads + 32, CPR = Block::ROW / 16;
+    static_assert(Block::SCRATCH <= GM * D, "a warp's scratch lies in its part of the join buffer");
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t full[kPagedStages], empty[kPagedStages];
+    __shared__ int sm_row[kPagedStages];  // pool row of a stage's block, -1: none
+    __shared__ float2 sm_ml[2][NW][GM];   // joins: the warps' (max, sum), a sum of -1 for a piece in error
+    __shared__ int sm_scan[3][NT / 32];
+    __shared__ int sm_cut[2][3];  // unit, its first block and its number, at the start and the end of the range
+    __shared__ int sm_flags, sm_old;
+    const uint32_t raw0 = smem_addr(smem_raw), ring0 = (raw0 + 1023u) & ~1023u;
+    float *join = reinterpret_cast<float *>(smem_raw + (ring0 - raw0) + kPagedStages * STAGE);
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int P = a.units, G = a.G, GS = (G + HS - 1) / HS;
+    if (Block::TENSOR_MAPS && tid == 0) {
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+    }
+    if (tid < kPagedStages) {
+        mbar_init(smem_addr(&full[tid]), 1);
+        mbar_init(smem_addr(&empty[tid]), HS);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (tid == 0) sm_flags = 0;
+    wait_prior_grid();  // lens, the table, q and the new rows may come from the previous kernels
+
+    // ---- plan, the same in every CTA: blocks of all units, this CTA's range of them
+    const int seg = (P + NT - 1) / NT, u_lo = min(P, tid * seg), u_hi = min(P, u_lo + seg);
+    int my_b = 0, my_max = 0, my_ne = 0;
+#pragma unroll 4
+    for (int u = u_lo; u < u_hi; ++u) {
+        const int L = __ldcg(a.lens + u);
+        if (blockIdx.x == 0 && !unit_ok(L, a.cap, a.append))
+            raise_error(a.err, (a.append && L == a.cap) ? ERR_ROOM : ERR_LEN);
+        const int nb = blocks_of<KB>(a, rows_of(a, L));
+        my_b += nb;
+        my_max = max(my_max, nb);
+        my_ne += nb > 0;
+    }
+    int incl = my_b;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
+    my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
+    if (lane == 31) sm_scan[0][wid] = incl;
+    if (lane == 0) {
+        sm_scan[1][wid] = my_max;
+        sm_scan[2][wid] = my_ne;
+    }
+    __syncthreads();
+    int NB = 0, before = incl - my_b, max_nb = 0, n_ne = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+        before += w < wid ? sm_scan[0][w] : 0;
+        NB += sm_scan[0][w];
+        max_nb = max(max_nb, sm_scan[1][w]);
+        n_ne += sm_scan[2][w];
+    }
+    const int W = max(1, min((int)gridDim.x, NB / kMinBlocks));  // CTAs with work
+    const bool whole = max_nb <= kWholeBlocks && n_ne >= kWholeUnits * W;
+    const int T = whole ? 1 << 30 : max(1, NB / W / kSnapDiv);  // a cut nearer to a unit's end moves there
+    const int c = blockIdx.x;
+    auto ideal = [&](int k) { return (int)((long long)k * NB / W); };
+    if (c < W && NB > 0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int t = ideal(c + k);
+            if (t >= before && t < before + my_b) {  // in one of this thread's units
+                int ub = before, u = u_lo, nb = 0;
+                for (; u < u_hi; ++u) {
+                    nb = blocks_of<KB>(a, rows_of(a, __ldcg(a.lens + u)));
+                    if (t < ub + nb) break;
+                    ub += nb;
+                }
+                sm_cut[k][0] = u;
+                sm_cut[k][1] = ub;
+                sm_cut[k][2] = nb;
+            }
+        }
+    }
+    __syncthreads();
+    Walk start;
+    start.begin = start.end = 0;
+    if (c < W && NB > 0) {
+        auto cut = [&](int k) {
+            const int t = ideal(c + k), ub = sm_cut[k][1], ue = ub + sm_cut[k][2];
+            if (t >= NB) return NB;
+            if (min(t - ub, ue - t) >= T) return t;
+            return t - ub <= ue - t ? ub : ue;
+        };
+        start.begin = cut(0);
+        start.end = cut(1);
+        start.u = sm_cut[0][0];
+        start.ub = sm_cut[0][1];
+        start.nb = sm_cut[0][2];
+        start.le = rows_of(a, __ldcg(a.lens + start.u));
+    }
+    start.b = start.begin;
+
+    if (wid == NW) {
+        // ---- copies: lane s feeds stream s
+        if (lane < NS) {
+            constexpr unsigned MASK = (1u << NS) - 1u;
+            const uint64_t policy = l2_evict_first_policy();  // K and V rows are read once
+            Walk w = start;
+            Piece p = {};
+            Pages pg = {};
+            int i = 0, e = 0, n = 0;  // next block of the piece, its table entry, pieces seen
+            auto first_row = [&]() { return KB * (i + (i >= p.sg.head ? p.sg.gap : 0)); };
+            auto begin_piece = [&]() {
+                while (next_piece<KB>(a, w, p)) {
+                    const int k = n++;
+                    i = whole ? p.lo : p.lo + ((lane - p.at) & (NS - 1));
+                    if (whole ? (k & (NS - 1)) != lane : i >= p.hi) continue;
+                    pg = pages_of(a, p.u);
+                    e = page_entry(a, pg, first_row());
+                    return true;
+                }
+                return false;
+            };
+            bool have = begin_piece();
+            uint32_t issued = 0, slot = 0, par = 1;
+            long long idle = 0;
+            while (__any_sync(MASK, have)) {
+                const int st = lane * S + (int)slot;
+                const bool go = have && mbar_test(smem_addr(&empty[st]), par);
+                if (go) {
+                    const int k = first_row(), row = paged_row(a, pg, k, e);
+                    const uint32_t bar = smem_addr(&full[st]), dst = ring0 + (uint32_t)st * STAGE;
+                    sm_row[st] = row;
+                    fence_async_shared();
+                    if (row >= 0)
+                        Block::load(dst, bar, &tmK, &tmV, a.K, a.V, (typename Block::RowIndex)row,
+                                    min(KB, p.le - a.append - k), policy);
+                    else
+                        mbar_expect_tx(bar, 0);  // what the stage holds counts for nothing
+                    ++issued;
+                    if (++slot == (uint32_t)S) {
+                        slot = 0;
+                        par ^= 1u;
+                    }
+                    i += whole ? 1 : NS;
+                    if (i >= p.hi)
+                        have = begin_piece();
+                    else
+                        e = page_entry(a, pg, first_row());
+                }
+                if (__any_sync(MASK, go)) {
+                    idle = 0;
+                } else {
+                    if (++idle > kSpinLimit / 4) {  // a warp stopped taking its blocks
+                        raise_error(a.err, ERR_INTERNAL);
+                        break;
+                    }
+                    __nanosleep(20);
+                }
+            }
+            // no copy is left in flight when the CTA ends
+            for (uint32_t j = issued > (uint32_t)S ? issued - S : 0; j < issued; ++j)
+                mbar_wait_bounded(smem_addr(&full[lane * S + j % S]), (j / S) & 1u, kSpinLimit);
+        }
+        return;
+    }
+
+    // ---- computing warps: stream `st`, heads [hp * GS, hp * GS + nh)
+    const int st = wid % NS, hp = wid / NS;
+    const int nh = max(0, min(GS, G - hp * GS));
+    Block blk(lane, join + wid * GM * D);
+    auto head_row = [&](int u) { return (size_t)(u / a.Hkv) * a.Hq + (size_t)(u % a.Hkv) * G; };
+    // units without rows: zeros, lse = -inf
+    for (int u = c * NW + wid; u < P; u += (int)gridDim.x * NW) {
+        if (rows_of(a, a.lens[u]) > 0) continue;
+        const size_t q0 = head_row(u);
+        for (int x = lane; x < G * D / 4; x += 32) store_out4(a, q0 * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (lane < G) put_lse(a, q0 + lane, -INFINITY);
+    }
+    bool dead = false;
+    uint32_t slot = 0, par = 0;
+    int n = 0;
+    Walk w = start;
+    Piece p = {};
+    auto begin_piece = [&]() {
+        while (next_piece<KB>(a, w, p)) {
+            if (whole && (n++ & (NS - 1)) != st) continue;
+            blk.load_q(a.q, (long)head_row(p.u) + hp * GS, nh);
+            blk.start();
+            return true;
+        }
+        return false;
+    };
+    bool have = begin_piece();
+    int parity = 0;
+    while (have) {
+        bool bad = false;
+        const size_t q0 = head_row(p.u);
+        const int Lapp = a.append && p.hi == p.nb ? p.le - 1 : -1;  // the new row, in its unit's last block
+        float *lg = a.logits ? a.logits + (q0 + hp * GS) * a.cap : nullptr;
+        for (int i = whole ? p.lo : p.lo + ((st - p.at) & (NS - 1)); i < p.hi; i += whole ? 1 : NS) {
+            const int at = st * S + (int)slot;
+            const bool app = Lapp >= 0 && i == p.nb - 1;
+            uint4 rows[Block::APP];  // this lane's chunks of the new rows, K's then V's
+            if (app) {
+#pragma unroll
+                for (int x = 0; x < Block::APP; ++x) {
+                    const int t = lane + 32 * x;
+                    rows[x] = make_uint4(0, 0, 0, 0);
+                    if (t < 2 * CPR)
+                        rows[x] = reinterpret_cast<const uint4 *>(t < CPR ? a.k_new : a.v_new)[(long)p.u * CPR + t % CPR];
+                }
+            }
+            if (!dead && !mbar_wait_bounded(smem_addr(&full[at]), par, kSpinLimit)) {  // a copy never landed
+                dead = true;
+                if (lane == 0) {
+                    raise_error(a.err, ERR_INTERNAL);
+                    atomicOr(&sm_flags, 1);
+                }
+            }
+            if (!dead) {
+                const int row = sm_row[at];
+                const int kb = KB * (i + (i >= p.sg.head ? p.sg.gap : 0));
+                const uint32_t Ks = ring0 + (uint32_t)at * STAGE, Vs = Ks + STAGE / 2;
+                bad |= row < 0;
+                // zero the V rows that are not seen (their weights are zero, but NaN times zero is not) and put
+                // the new row, which is not in the cache yet, in place
+                const bool border = kb < p.sg.h1 && kb + KB > p.sg.h0;
+                if (border || kb + KB > p.le || app) {
+                    for (int t = lane; t < KB * CPR; t += 32) {
+                        const int k = kb + t / CPR;
+                        if (k >= p.le || (k >= p.sg.h0 && k < p.sg.h1))
+                            sts_u4(Vs + Block::chunk(t / CPR, t % CPR), make_uint4(0, 0, 0, 0));
+                    }
+                    if (app) {
+#pragma unroll
+                        for (int x = 0; x < Block::APP; ++x) {
+                            const int t = lane + 32 * x;
+                            if (t < 2 * CPR) sts_u4((t < CPR ? Ks : Vs) + Block::chunk(Lapp - kb, t % CPR), rows[x]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                blk.consume(Ks, Vs, kb, p.le, a.c2, p.sg.h0, p.sg.h1, lg, a.cap, nh);
+                if (app && row >= 0 && hp == 0) {  // and into the cache
+                    const long r = (long)row + (Lapp - kb);
+#pragma unroll
+                    for (int x = 0; x < Block::APP; ++x) {
+                        const int t = lane + 32 * x;
+                        if (t < 2 * CPR) reinterpret_cast<uint4 *>(t < CPR ? a.K : a.V)[r * CPR + t % CPR] = rows[x];
+                    }
+                    if (lane == 0 && a.weights) a.weights[(size_t)p.u * a.cap + Lapp] = 0.f;
+                }
+                fence_async_shared();  // the stage's reads and writes come before the copy that fills it next
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&empty[at]));
+            }
+            if (++slot == (uint32_t)S) {
+                slot = 0;
+                par ^= 1u;
+            }
+        }
+        blk.finish();
+        if (bad && lane == 0) {
+            raise_error(a.err, ERR_PAGE);
+            atomicOr(&sm_flags, 2);
+        }
+        if (whole) {
+            if (bad) {
+                for (int x = lane; x < nh * D / 4; x += 32)
+                    store_out4(a, (q0 + hp * GS) * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f));
+                if (lane < nh) put_lse(a, q0 + hp * GS + lane, -INFINITY);
+            } else {
+                blk.store(a.out, a.out_bf16 != 0, (long)q0 + hp * GS, nh);
+                blk.each_lse(nh, [&](int q, float m, float l) {
+                    put_lse(a, q0 + hp * GS + q, l > 0.f ? m + log2f(l) : -INFINITY);
+                });
+            }
+            have = begin_piece();
+            continue;
+        }
+
+        // ---- join: one barrier after the warps' results are in shared memory, one after they have been read
+        blk.store_partial(join + wid * GM * D, nh);
+        blk.each_lse(nh, [&](int q, float m, float l) { sm_ml[parity][wid][q] = make_float2(m, bad ? -1.f : l); });
+        const Piece d = p;  // done
+        have = begin_piece();  // the next piece's queries load meanwhile
+        bar_compute();
+        const bool all = d.lo == 0 && d.hi == d.nb;
+        const int out_slot = 2 * c + (d.lo == 0 ? 1 : 0);
+        for (int x = tid; x < G * D / 4; x += kPagedThreads) {
+            const int q = x / (D / 4), d4 = x % (D / 4), part = HS == 1 ? 0 : q / GS, ql = q - part * GS;
+            float M = -INFINITY, Ls = 0.f;
+            bool err = false;
+            float2 ml[NS];
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                ml[s] = sm_ml[parity][part * NS + s][ql];
+                M = fmaxf(M, ml[s].x);
+                err |= ml[s].y < 0.f;
+            }
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (!err && M != -INFINITY) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const float f = fast_exp2(ml[s].x - M);
+                    const float4 v = *reinterpret_cast<const float4 *>(join + ((part * NS + s) * GM + ql) * D + 4 * d4);
+                    Ls += ml[s].y * f;
+                    o.x += v.x * f;
+                    o.y += v.y * f;
+                    o.z += v.z * f;
+                    o.w += v.w * f;
+                }
+            }
+            if (all) {
+                const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+                store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+                if (d4 == 0) put_lse(a, q0 + q, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
+            } else {
+                *reinterpret_cast<float4 *>(a.part_o + ((size_t)out_slot * G + q) * D + 4 * d4) = o;
+                if (d4 == 0)
+                    reinterpret_cast<float2 *>(a.part_ml)[(size_t)out_slot * G + q] = make_float2(M, err ? -1.f : Ls);
+            }
+        }
+        bar_compute();
+        parity ^= 1;
+        if (all) continue;
+
+        // ---- a unit cut between CTAs: publish; the last one joins the pieces
+        // Cuts inside [ub, ue) stay where they fall from ub + T to ue - T; piece 0 is the CTA's before the first.
+        const long long ub = start.begin + d.at - d.lo, ue = ub + d.nb;
+        auto first_at = [&](long long b) { return (int)((b * W + NB - 1) / NB); };  // first CTA whose ideal start is >= b
+        const int c1 = first_at(ub + T), pieces = 1 + max(0, first_at(ue - T + 1) - c1);
+        if (tid == 0) {
+            __threadfence();
+            sm_old = atom_add_acq_rel(&a.counters[2 + d.u], 1);
+        }
+        bar_compute();
+        if (sm_old == pieces - 1) {
+            if (tid == 0) a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
+            for (int x = tid; x < G * D / 4; x += kPagedThreads) {
+                const int q = x / (D / 4), d4 = x % (D / 4);
+                auto slot_of = [&](int s) { return (size_t)(2 * (c1 - 1 + s) + (s == 0 ? 1 : 0)) * G + q; };
+                float M = -INFINITY, Ls = 0.f;
+                bool err = false;
+#pragma unroll 4
+                for (int s = 0; s < pieces; ++s) {
+                    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + slot_of(s));
+                    M = fmaxf(M, ml.x);
+                    err |= ml.y < 0.f;
+                }
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!err && M != -INFINITY) {
+#pragma unroll 4
+                    for (int s = 0; s < pieces; ++s) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + slot_of(s));
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o + slot_of(s) * D + 4 * d4));
+                        const float f = fast_exp2(ml.x - M);
+                        Ls += ml.y * f;
+                        o.x += v.x * f;
+                        o.y += v.y * f;
+                        o.z += v.z * f;
+                        o.w += v.w * f;
+                    }
+                }
+                const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+                store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+                if (d4 == 0) put_lse(a, q0 + q, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
+            }
+        }
+    }
+
+    // ---- the last CTA to finish advances the lengths (every plan has been read by then) and leaves the
+    // counters zero, as it found them
+    bar_compute();
+    if (tid == 0) {
+        const unsigned f = (unsigned)sm_flags;
+        const unsigned long long add = (1ull << 32) | (f & 1u ? 1ull : 0ull) | (f & 2u ? 1ull << 16 : 0ull);
+        const unsigned long long old = atom_add_acq_rel_u64(reinterpret_cast<unsigned long long *>(a.counters), add);
+        const unsigned seen = (unsigned)(old + add);
+        sm_old = (int)(old >> 32) == (int)gridDim.x - 1 ? 1 | (seen & 0xffffu ? 2 : 0) | (seen >> 16 ? 4 : 0) : 0;
+    }
+    bar_compute();
+    const int last = sm_old;
+    if (last == 0) return;
+    if (last & 2) {  // tickets of units whose pieces stopped early may still count
+        for (int u = tid; u < P; u += kPagedThreads) a.counters[2 + u] = 0;
+    } else if (a.append) {
+#pragma unroll 4
+        for (int u = tid; u < P; u += kPagedThreads) {
+            const int L = __ldcg(a.lens + u);
+            bool ok = unit_ok(L, a.cap, a.append);
+            if (ok && (last & 4)) {  // units whose table names no page for a row in sight keep their length
+                const Sight sg = sight_of<KB>(a, L + 1);
+                const Pages pg = pages_of(a, u);
+                for (int k = 0; k <= L; k += KB)
+                    if (k < KB * sg.head || k >= KB * (sg.head + sg.gap)) ok &= paged_row(a, pg, k, page_entry(a, pg, k)) >= 0;
+            }
+            if (ok) a.lens[u] = L + 1;
+        }
+    }
+    if (tid == 0) *reinterpret_cast<unsigned long long *>(a.counters) = 0ull;
 }
 
 // weights[u, j] += (1/G) sum_g 2^(logit - lse2) for the rows in sight.  Threads take four rows at a time
@@ -77,69 +630,78 @@ __global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__r
     }
 }
 
+// ---------------------------------------------------------------- host side
+typedef void (*PagedKernel)(CUtensorMap, CUtensorMap, PagedArgs);
+struct PagedLaunch {
+    PagedKernel fn;
+    int smem;
+};
+template <class Block, int HS> static PagedLaunch with()
+{
+    static_assert(paged_smem<Block>() + 2048 <= 227 * 1024, "shared memory of a CTA (2 KB of it static)");
+    return PagedLaunch{paged_decode<Block, HS>, paged_smem<Block>()};
+}
+template <int D> static PagedLaunch paged_kernel(bool f32, int G)
+{
+    if (!f32) return G > 8 ? with<Bf16Block<D, 1>, 2>() : with<Bf16Block<D, 1>, 1>();
+    // four heads per warp at most: their queries take D / 8 registers each
+    if (G > 8) return with<F32Block<D, 4>, 4>();
+    if (G > 4) return with<F32Block<D, 4>, 2>();
+    return G > 2 ? with<F32Block<D, 4>, 1>() : with<F32Block<D, 2>, 1>();
+}
+
 cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new,
                                 int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
                                 float *lse, float *weights, const PagedDecodeWs &ws, unsigned *err, cudaStream_t s)
 {
     const bool f32 = kv.dtype == RECO_F32;
-    const int cap = paged_cap(kv);
-    DecodeArgs a = {};
+    const int cap = paged_cap(kv), units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv;
+    PagedArgs a = {};
     a.K = kv.k;
     a.V = kv.v;
-    a.counters = ws.dec.counters;
-    a.part_ml = ws.dec.part_ml;
-    a.part_o = ws.dec.part_o;
+    a.table = kv.table;
+    a.q = q;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.lens = lens;
+    a.out = out;
+    a.lse = lse;
+    a.lse2 = ws.lse2;
+    a.logits = ws.logits;
+    a.weights = weights;
+    a.counters = ws.counters;
+    a.part_ml = ws.part_ml;
+    a.part_o = ws.part_o;
+    a.units = units;
+    a.B = kv.B;
     a.Hq = kv.H_q;
     a.Hkv = kv.H_kv;
-    a.G = kv.H_q / kv.H_kv;
-    a.L_cap = cap;
-    a.append = k_new ? 1 : 0;
-    a.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;
-    a.c2 = scale * kLog2e;
-    a.err = err;
-    a.table = kv.table;
-    a.B = kv.B;
+    a.G = G;
+    a.cap = cap;
     a.n_pages = kv.n_pages;
     a.max_pages = kv.max_pages;
-    a.page_shift = __builtin_ctz((unsigned)kv.page);
+    a.shift = __builtin_ctz((unsigned)kv.page);
+    a.append = k_new ? 1 : 0;
+    a.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;
     a.window = window;
     a.sinks = sinks;
-    const int units = kv.n_layers * kv.B * kv.H_kv;
-    const StreamKernel k = stream_kernel<true>(kv.d, f32, units, a.G, cap);
-    a.hs_min = k.hs;
+    a.c2 = scale * kLog2e;
+    a.err = err;
     CUtensorMap mk = {}, mv = {};
     const unsigned long long rows = (unsigned long long)kv.n_layers * kv.n_pages * kv.H_kv * kv.page;
-    if (!f32 && (!encode_cache_map(&mk, kv.k, rows, kv.d) || !encode_cache_map(&mv, kv.v, rows, kv.d)))
+    if (!f32 && (!encode_bf16_2d(&mk, kv.k, rows, kv.d, 64, 16) || !encode_bf16_2d(&mv, kv.v, rows, kv.d, 64, 16)))
         return cudaErrorInvalidValue;
-    const size_t row_b = (size_t)kv.d * (f32 ? 4 : 2), out_b = (size_t)kv.d * (a.out_bf16 ? 2 : 4);
-    for (long long u0 = 0; u0 < units; u0 += k.part_units) {  // as many units as one plan holds
-        const int cu = (int)std::min(k.part_units, units - u0);
-        const size_t q0 = (size_t)u0 * a.G;
-        DecodeArgs at = a;
-        at.u0 = (int)u0;
-        at.units = cu;
-        at.hs_max = k.most_halves(cu, a.G);
-        at.q = static_cast<const char *>(q) + q0 * row_b;
-        at.k_new = k_new ? static_cast<const char *>(k_new) + (size_t)u0 * row_b : nullptr;
-        at.v_new = v_new ? static_cast<const char *>(v_new) + (size_t)u0 * row_b : nullptr;
-        at.lens = lens + u0;
-        at.out = static_cast<char *>(out) + q0 * out_b;
-        at.lse = lse ? lse + q0 : nullptr;
-        if (weights) {
-            at.lse2 = ws.lse2 + q0;
-            at.logits = ws.logits + q0 * cap;
-            at.weights = weights + (size_t)u0 * cap;
-        }
-        const cudaError_t e = launch_stream(k.fn, kv.d, mk, mv, at, ws.dec.part_slots, s);
-        if (e != cudaSuccess) return e;
-    }
-    if (!weights) return cudaSuccess;
+    const PagedLaunch k = kv.d == 64 ? paged_kernel<64>(f32, G) : paged_kernel<128>(f32, G);
+    cudaError_t e = allow_smem((const void *)k.fn, k.smem);
+    if (e != cudaSuccess) return e;
+    const int grid = std::min(device_sm_count(), kPagedMaxGrid);
+    e = launch_pdl(k.fn, dim3(grid), dim3(kPagedThreads + 32), k.smem, s, mk, mv, a);
+    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights) return e;
     // CTAs over a unit's rows: enough that all units together fill the GPU four times over, never more than
     // the rows of a unit need (lengths are not known here, and CTAs without rows cost time too)
     const int need = (cap + kWeightRows - 1) / kWeightRows, fill = 4 * 8 * device_sm_count() / units;
-    const cudaError_t e = launch_pdl(paged_weights, dim3(std::max(1, std::min(need, fill)), units), dim3(kWeightThreads),
-                                     0, s, (const float *)ws.logits, (const float *)ws.lse2, (const int32_t *)lens, a.G,
-                                     cap, window, sinks, weights);
+    e = launch_pdl(paged_weights, dim3(std::max(1, std::min(need, fill)), units), dim3(kWeightThreads), 0, s,
+                   (const float *)ws.logits, (const float *)ws.lse2, (const int32_t *)lens, G, cap, window, sinks, weights);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
