@@ -30,13 +30,12 @@ namespace reco {
 
 constexpr int kPagedWarps = 8;               // computing warps per CTA
 constexpr int kPagedThreads = 32 * kPagedWarps;  // and their threads; 32 more copy
-constexpr int kPagedStages = 24;             // ring stages per CTA
+constexpr int kRingBytes = 24 * 8192;         // ring of a CTA
 constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
-constexpr int kStageBytes = 8192;            // a block of K and V rows at d = 128 (half of it at d = 64)
-constexpr int kMinBlocks = 16;               // blocks per working CTA at least (fewer CTAs rather than less)
-constexpr int kSnapDiv = 8;                  // a cut within this part of a CTA's range of a unit's end moves there
-constexpr int kWholeBlocks = 16;             // units of at most this many blocks go whole to a warp ...
-constexpr int kWholeUnits = 4;               // ... where every CTA has this many of them
+constexpr int kStageBytes = 8192;            // a block of K and V rows at d = 128 (half of it, and twice as many, at d = 64)
+constexpr int kMinBlocks = 16;               // blocks per working CTA (fewer CTAs rather than less)
+constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
+constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
 
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base)
 {
@@ -145,6 +144,23 @@ template <int KB> __device__ __forceinline__ bool next_piece(const PagedArgs &a,
     return false;
 }
 
+// Whole units: those of a CTA's units [w.u, w.end) that fall to stream s, every NS-th one (w.u is moved there
+// before the first call).
+template <int KB, int NS> __device__ __forceinline__ bool next_whole(const PagedArgs &a, Walk &w, Piece &p)
+{
+    while (w.u < w.end) {
+        p.u = w.u;
+        w.u += NS;
+        p.le = rows_of(a, a.lens[p.u]);
+        if (p.le == 0) continue;
+        p.nb = p.hi = blocks_of<KB>(a, p.le);
+        p.lo = p.at = 0;
+        p.sg = sight_of<KB>(a, p.le);
+        return true;
+    }
+    return false;
+}
+
 __device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;" ::"n"(kPagedThreads) : "memory"); }
 
 __device__ __forceinline__ void put_lse(const PagedArgs &a, size_t row, float l2)
@@ -168,7 +184,7 @@ __device__ __forceinline__ void store_out4(const PagedArgs &a, size_t i, float4 
 // Ring, then [warp][head][D] floats: the warps' outputs as they join (and, until then, each warp's scratch).
 template <class Block> constexpr int paged_smem()
 {
-    return 1024 + kPagedStages * (kStageBytes * Block::D / 128) + kPagedWarps * Block::GM * Block::D * 4;
+    return 1024 + kRingBytes + kPagedWarps * Block::GM * Block::D * 4;
 }
 
 template <class Block, int HS>
@@ -176,25 +192,26 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     paged_decode(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, PagedArgs a)
 {
     constexpr int D = Block::D, KB = Block::KB, GM = Block::GM;
-    constexpr int NW = kPagedWarps, NS = NW / HS, S = kPagedStages / NS, STAGE = kStageBytes * D / 128;
+    constexpr int STAGE = kStageBytes * D / 128, STAGES = kRingBytes / STAGE;
+    constexpr int NW = kPagedWarps, NS = NW / HS, S = STAGES / NS;
     constexpr int NT = kPagedThreads + 32, CPR = Block::ROW / 16;
     static_assert(Block::SCRATCH <= GM * D, "a warp's scratch lies in its part of the join buffer");
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t full[kPagedStages], empty[kPagedStages];
-    __shared__ int sm_row[kPagedStages];  // pool row of a stage's block, -1: none
+    __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
+    __shared__ int sm_row[STAGES];  // pool row of a stage's block, -1: none
     __shared__ float2 sm_ml[2][NW][GM];   // joins: the warps' (max, sum), a sum of -1 for a piece in error
     __shared__ int sm_scan[3][NT / 32];
-    __shared__ int sm_cut[2][3];  // unit, its first block and its number, at the start and the end of the range
+    __shared__ int sm_cut[2][4];  // unit, its first block (or CTA), blocks and rows, at the start and the end of the range
     __shared__ int sm_flags, sm_old;
     const uint32_t raw0 = smem_addr(smem_raw), ring0 = (raw0 + 1023u) & ~1023u;
-    float *join = reinterpret_cast<float *>(smem_raw + (ring0 - raw0) + kPagedStages * STAGE);
+    float *join = reinterpret_cast<float *>(smem_raw + (ring0 - raw0) + kRingBytes);
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int P = a.units, G = a.G, GS = (G + HS - 1) / HS;
     if (Block::TENSOR_MAPS && tid == 0) {
         prefetch_tensormap(&tmK);
         prefetch_tensormap(&tmV);
     }
-    if (tid < kPagedStages) {
+    if (tid < STAGES) {
         mbar_init(smem_addr(&full[tid]), 1);
         mbar_init(smem_addr(&empty[tid]), HS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -202,67 +219,126 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     if (tid == 0) sm_flags = 0;
     wait_prior_grid();  // lens, the table, q and the new rows may come from the previous kernels
 
-    // ---- plan, the same in every CTA: blocks of all units, this CTA's range of them
+    // ---- plan, the same in every CTA
     const int seg = (P + NT - 1) / NT, u_lo = min(P, tid * seg), u_hi = min(P, u_lo + seg);
-    int my_b = 0, my_max = 0, my_ne = 0;
+    int my_b = 0, my_max = 0, my_ne = 0, le0 = 0;
 #pragma unroll 4
     for (int u = u_lo; u < u_hi; ++u) {
         const int L = __ldcg(a.lens + u);
         if (blockIdx.x == 0 && !unit_ok(L, a.cap, a.append))
             raise_error(a.err, (a.append && L == a.cap) ? ERR_ROOM : ERR_LEN);
-        const int nb = blocks_of<KB>(a, rows_of(a, L));
+        const int le = rows_of(a, L), nb = blocks_of<KB>(a, le);
+        if (u == u_lo) le0 = le;
         my_b += nb;
         my_max = max(my_max, nb);
         my_ne += nb > 0;
     }
-    int incl = my_b;
+    auto rows_again = [&](int u) { return u == u_lo ? le0 : rows_of(a, __ldcg(a.lens + u)); };
+    // exclusive prefix of x over the CTA's threads, and its sum
+    auto scan = [&](int x, int &total) {
+        int incl = x;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-    }
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) sm_scan[0][wid] = incl;
+        __syncthreads();
+        int before = incl - x;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) {
+            before += w < wid ? sm_scan[0][w] : 0;
+            total += sm_scan[0][w];
+        }
+        return before;
+    };
     my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
     my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
-    if (lane == 31) sm_scan[0][wid] = incl;
     if (lane == 0) {
         sm_scan[1][wid] = my_max;
         sm_scan[2][wid] = my_ne;
     }
-    __syncthreads();
-    int NB = 0, before = incl - my_b, max_nb = 0, n_ne = 0;
+    int NB;
+    const int before = scan(my_b, NB);
+    int max_nb = 0, n_ne = 0;
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) {
-        before += w < wid ? sm_scan[0][w] : 0;
-        NB += sm_scan[0][w];
         max_nb = max(max_nb, sm_scan[1][w]);
         n_ne += sm_scan[2][w];
     }
-    const int W = max(1, min((int)gridDim.x, NB / kMinBlocks));  // CTAs with work
-    const bool whole = max_nb <= kWholeBlocks && n_ne >= kWholeUnits * W;
-    const int T = whole ? 1 << 30 : max(1, NB / W / kSnapDiv);  // a cut nearer to a unit's end moves there
-    const int c = blockIdx.x;
-    auto ideal = [&](int k) { return (int)((long long)k * NB / W); };
-    if (c < W && NB > 0) {
+    const int c = blockIdx.x, grid = gridDim.x;
+    const bool split = n_ne <= grid;
+    const bool whole = !split && max_nb <= kWholeBlocks;
+    const int T = whole ? 1 << 30 : min(kSnapBlocks, max(1, NB / grid / 4));
+    int c1 = 0, pieces = 1;  // split: the CTA after the first piece's, the pieces of the unit
+    Walk start;
+    start.begin = start.end = start.u = 0;
+    if (split && NB > 0) {
+        // Units that fit the grid: every one is cut into equal pieces of at most `per` blocks, a CTA each, so that a
+        // CTA joins and publishes once.  `per` is the longest unit's share when it is cut as often as its part of
+        // all blocks allows, or once, twice or three times less, whichever leaves no more pieces than CTAs, and
+        // failing those one that cannot leave more.
+        const int target = max(n_ne, min(grid, NB / kMinBlocks));
+        const int j0 = max(1, (int)((long long)max_nb * target / NB));
+        int per = 0, total = 0, at = 0;
+        for (int j = 0; j < 5; ++j) {
+            const int div = max(1, j0 - j), room = max(1, grid - n_ne);
+            per = j < 4 ? (max_nb + div - 1) / div : (NB + room - 1) / room;
+            int my_k = 0;
+            for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, rows_again(u)) + per - 1) / per;
+            __syncthreads();  // the last scan has been read
+            at = scan(my_k, total);
+            if (total <= grid) {
+                if (c >= at && c < at + my_k) {
+                    for (int u = u_lo; u < u_hi; ++u) {
+                        const int le = rows_again(u), nb = blocks_of<KB>(a, le), k = (nb + per - 1) / per;
+                        if (c < at + k) {
+                            sm_cut[0][0] = u;
+                            sm_cut[0][1] = at;
+                            sm_cut[0][2] = nb;
+                            sm_cut[0][3] = le;
+                            break;
+                        }
+                        at += k;
+                    }
+                }
+                break;
+            }
+        }
+        __syncthreads();
+        if (c < total) {
+            start.u = sm_cut[0][0];
+            start.ub = 0;
+            start.nb = sm_cut[0][2];
+            start.le = sm_cut[0][3];
+            const int s = c - sm_cut[0][1];
+            c1 = sm_cut[0][1] + 1;
+            pieces = (start.nb + per - 1) / per;
+            start.begin = (int)((long long)start.nb * s / pieces);
+            start.end = (int)((long long)start.nb * (s + 1) / pieces);
+        }
+    } else if (NB > 0) {
+        // More units than CTAs: equal ranges of the blocks laid end to end
+        auto ideal = [&](int k) { return (int)((long long)k * NB / grid); };
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int t = ideal(c + k);
             if (t >= before && t < before + my_b) {  // in one of this thread's units
-                int ub = before, u = u_lo, nb = 0;
+                int ub = before, u = u_lo, nb = 0, le = 0;
                 for (; u < u_hi; ++u) {
-                    nb = blocks_of<KB>(a, rows_of(a, __ldcg(a.lens + u)));
+                    le = rows_again(u);
+                    nb = blocks_of<KB>(a, le);
                     if (t < ub + nb) break;
                     ub += nb;
                 }
                 sm_cut[k][0] = u;
                 sm_cut[k][1] = ub;
                 sm_cut[k][2] = nb;
+                sm_cut[k][3] = le;
             }
         }
-    }
-    __syncthreads();
-    Walk start;
-    start.begin = start.end = 0;
-    if (c < W && NB > 0) {
+        __syncthreads();
         auto cut = [&](int k) {
             const int t = ideal(c + k), ub = sm_cut[k][1], ue = ub + sm_cut[k][2];
             if (t >= NB) return NB;
@@ -272,9 +348,13 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         start.begin = cut(0);
         start.end = cut(1);
         start.u = sm_cut[0][0];
+        if (whole) {  // the units [start.u, start.end)
+            start.u += start.begin == sm_cut[0][1] ? 0 : 1;
+            start.end = ideal(c + 1) >= NB ? P : sm_cut[1][0] + (start.end == sm_cut[1][1] ? 0 : 1);
+        }
         start.ub = sm_cut[0][1];
         start.nb = sm_cut[0][2];
-        start.le = rows_of(a, __ldcg(a.lens + start.u));
+        start.le = sm_cut[0][3];
     }
     start.b = start.begin;
 
@@ -286,13 +366,13 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             Walk w = start;
             Piece p = {};
             Pages pg = {};
-            int i = 0, e = 0, n = 0;  // next block of the piece, its table entry, pieces seen
+            int i = 0, e = 0;  // next block of the piece, and its table entry
+            if (whole) w.u += lane;
             auto first_row = [&]() { return KB * (i + (i >= p.sg.head ? p.sg.gap : 0)); };
             auto begin_piece = [&]() {
-                while (next_piece<KB>(a, w, p)) {
-                    const int k = n++;
-                    i = whole ? p.lo : p.lo + ((lane - p.at) & (NS - 1));
-                    if (whole ? (k & (NS - 1)) != lane : i >= p.hi) continue;
+                while (whole ? next_whole<KB, NS>(a, w, p) : next_piece<KB>(a, w, p)) {
+                    i = whole ? 0 : p.lo + ((lane - p.at) & (NS - 1));
+                    if (i >= p.hi) continue;
                     pg = pages_of(a, p.u);
                     e = page_entry(a, pg, first_row());
                     return true;
@@ -357,17 +437,24 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     }
     bool dead = false;
     uint32_t slot = 0, par = 0;
-    int n = 0;
     Walk w = start;
     Piece p = {};
+    if (whole) w.u += st;
+    int q_of = -1;  // whole: the unit whose queries were loaded ahead
+    auto load_q = [&](int u) { blk.load_q(a.q, (long)head_row(u) + hp * GS, nh); };
     auto begin_piece = [&]() {
-        while (next_piece<KB>(a, w, p)) {
-            if (whole && (n++ & (NS - 1)) != st) continue;
-            blk.load_q(a.q, (long)head_row(p.u) + hp * GS, nh);
+        if (whole) {
+            if (!next_whole<KB, NS>(a, w, p)) return false;
+            if (q_of != p.u) load_q(p.u);
             blk.start();
+            q_of = w.u < w.end ? w.u : -1;
+            if (q_of >= 0) load_q(q_of);
             return true;
         }
-        return false;
+        if (!next_piece<KB>(a, w, p)) return false;
+        load_q(p.u);
+        blk.start();
+        return true;
     };
     bool have = begin_piece();
     int parity = 0;
@@ -376,7 +463,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         const size_t q0 = head_row(p.u);
         const int Lapp = a.append && p.hi == p.nb ? p.le - 1 : -1;  // the new row, in its unit's last block
         float *lg = a.logits ? a.logits + (q0 + hp * GS) * a.cap : nullptr;
-        for (int i = whole ? p.lo : p.lo + ((st - p.at) & (NS - 1)); i < p.hi; i += whole ? 1 : NS) {
+        for (int i = whole ? 0 : p.lo + ((st - p.at) & (NS - 1)); i < p.hi; i += whole ? 1 : NS) {
             const int at = st * S + (int)slot;
             const bool app = Lapp >= 0 && i == p.nb - 1;
             uint4 rows[Block::APP];  // this lane's chunks of the new rows, K's then V's
@@ -505,10 +592,12 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         if (all) continue;
 
         // ---- a unit cut between CTAs: publish; the last one joins the pieces
-        // Cuts inside [ub, ue) stay where they fall from ub + T to ue - T; piece 0 is the CTA's before the first.
-        const long long ub = start.begin + d.at - d.lo, ue = ub + d.nb;
-        auto first_at = [&](long long b) { return (int)((b * W + NB - 1) / NB); };  // first CTA whose ideal start is >= b
-        const int c1 = first_at(ub + T), pieces = 1 + max(0, first_at(ue - T + 1) - c1);
+        if (!split) {  // cuts inside [ub, ue) stay where they fall from ub + T to ue - T; piece 0 is the CTA's before the first
+            const long long ub = start.begin + d.at - d.lo, ue = ub + d.nb;
+            auto first_at = [&](long long b) { return (int)((b * grid + NB - 1) / NB); };  // first CTA whose ideal start is >= b
+            c1 = first_at(ub + T);
+            pieces = 1 + max(0, first_at(ue - T + 1) - c1);
+        }
         if (tid == 0) {
             __threadfence();
             sm_old = atom_add_acq_rel(&a.counters[2 + d.u], 1);
@@ -519,27 +608,50 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             for (int x = tid; x < G * D / 4; x += kPagedThreads) {
                 const int q = x / (D / 4), d4 = x % (D / 4);
                 auto slot_of = [&](int s) { return (size_t)(2 * (c1 - 1 + s) + (s == 0 ? 1 : 0)) * G + q; };
+                // four pieces at a time, their loads in flight together, with a running maximum
                 float M = -INFINITY, Ls = 0.f;
                 bool err = false;
-#pragma unroll 4
-                for (int s = 0; s < pieces; ++s) {
-                    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + slot_of(s));
-                    M = fmaxf(M, ml.x);
-                    err |= ml.y < 0.f;
-                }
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!err && M != -INFINITY) {
-#pragma unroll 4
-                    for (int s = 0; s < pieces; ++s) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + slot_of(s));
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(a.part_o + slot_of(s) * D + 4 * d4));
-                        const float f = fast_exp2(ml.x - M);
-                        Ls += ml.y * f;
-                        o.x += v.x * f;
-                        o.y += v.y * f;
-                        o.z += v.z * f;
-                        o.w += v.w * f;
+                for (int s0 = 0; s0 < pieces; s0 += 4) {
+                    float2 ml[4];
+                    float4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool in = s0 + k < pieces;
+                        const size_t at = slot_of(in ? s0 + k : s0);
+                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + at);
+                        v[k] = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * d4));
+                        if (!in) {
+                            ml[k] = make_float2(-INFINITY, 0.f);
+                            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        }
                     }
+                    float Mn = M;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        Mn = fmaxf(Mn, ml[k].x);
+                        err |= ml[k].y < 0.f;
+                    }
+                    const float base = Mn == -INFINITY ? 0.f : Mn, f0 = fast_exp2(M - base);
+                    Ls *= f0;
+                    o.x *= f0;
+                    o.y *= f0;
+                    o.z *= f0;
+                    o.w *= f0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float f = fast_exp2(ml[k].x - base);
+                        Ls += ml[k].y * f;
+                        o.x += v[k].x * f;
+                        o.y += v[k].y * f;
+                        o.z += v[k].z * f;
+                        o.w += v[k].w * f;
+                    }
+                    M = Mn;
+                }
+                if (err) {
+                    Ls = 0.f;
+                    o = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
                 const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
                 store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
@@ -607,14 +719,21 @@ __global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__r
         const float *src = logits + u * G * cap + j0;
         const float4 old = *dst;
         float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int g = 0; g < G; ++g) {
-            const float4 x = __ldcs(reinterpret_cast<const float4 *>(src + (long)g * cap));
-            const float z = sm_lse[g];
-            if (z == -INFINITY) continue;
-            p.x += fast_exp2(x.x - z);
-            p.y += fast_exp2(x.y - z);
-            p.z += fast_exp2(x.z - z);
-            p.w += fast_exp2(x.w - z);
+        for (int g0 = 0; g0 < G; g0 += 8) {  // eight heads' loads in flight
+            float4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = g0 + k < G ? __ldcs(reinterpret_cast<const float4 *>(src + (long)(g0 + k) * cap))
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float z = g0 + k < G ? sm_lse[g0 + k] : INFINITY;  // (2^-inf is 0)
+                if (z == -INFINITY) continue;
+                p.x += fast_exp2(x[k].x - z);
+                p.y += fast_exp2(x[k].y - z);
+                p.z += fast_exp2(x[k].z - z);
+                p.w += fast_exp2(x[k].w - z);
+            }
         }
         const float4 sum = make_float4(fmaf(p.x, inv, old.x), fmaf(p.y, inv, old.y), fmaf(p.z, inv, old.z),
                                        fmaf(p.w, inv, old.w));
@@ -694,7 +813,9 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     const PagedLaunch k = kv.d == 64 ? paged_kernel<64>(f32, G) : paged_kernel<128>(f32, G);
     cudaError_t e = allow_smem((const void *)k.fn, k.smem);
     if (e != cudaSuccess) return e;
-    const int grid = std::min(device_sm_count(), kPagedMaxGrid);
+    // no more CTAs than the cache can hold work for
+    const long long most = (long long)units * ((cap + (f32 ? 7 : 15)) / (f32 ? 8 : 16));
+    const int grid = (int)std::min<long long>(std::min(device_sm_count(), kPagedMaxGrid), std::max<long long>(units, most / kMinBlocks));
     e = launch_pdl(k.fn, dim3(grid), dim3(kPagedThreads + 32), k.smem, s, mk, mv, a);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights) return e;
     // CTAs over a unit's rows: enough that all units together fill the GPU four times over, never more than
