@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
     __shared__ int sm_row[STAGES];  // pool row of a stage's block, -1: none
     __shared__ float2 sm_ml[2][NW][GM];   // joins: the warps' (max, sum), a sum of -1 for a piece in error
-    __shared__ int sm_scan[3][NT / 32];
+    __shared__ int sm_scan[4][NT / 32];
     __shared__ int sm_cut[2][4];  // unit, its first block (or CTA), blocks and rows, at the start and the end of the range
     __shared__ int sm_flags, sm_old;
     const uint32_t raw0 = smem_addr(smem_raw), ring0 = (raw0 + 1023u) & ~1023u;
@@ -234,6 +234,22 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         my_ne += nb > 0;
     }
     auto rows_again = [&](int u) { return u == u_lo ? le0 : rows_of(a, __ldcg(a.lens + u)); };
+    my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
+    my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
+    const int warp_b = __reduce_add_sync(0xffffffffu, (unsigned)my_b);
+    if (lane == 0) {
+        sm_scan[0][wid] = warp_b;
+        sm_scan[1][wid] = my_max;
+        sm_scan[2][wid] = my_ne;
+    }
+    __syncthreads();
+    int NB = 0, max_nb = 0, n_ne = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+        NB += sm_scan[0][w];
+        max_nb = max(max_nb, sm_scan[1][w]);
+        n_ne += sm_scan[2][w];
+    }
     // exclusive prefix of x over the CTA's threads, and its sum
     auto scan = [&](int x, int &total) {
         int incl = x;
@@ -242,35 +258,24 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             const int v = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += v;
         }
-        if (lane == 31) sm_scan[0][wid] = incl;
+        if (lane == 31) sm_scan[3][wid] = incl;
         __syncthreads();
         int before = incl - x;
         total = 0;
 #pragma unroll
         for (int w = 0; w < NT / 32; ++w) {
-            before += w < wid ? sm_scan[0][w] : 0;
-            total += sm_scan[0][w];
+            const int v = sm_scan[3][w];
+            before += w < wid ? v : 0;
+            total += v;
         }
         return before;
     };
-    my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
-    my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
-    if (lane == 0) {
-        sm_scan[1][wid] = my_max;
-        sm_scan[2][wid] = my_ne;
-    }
-    int NB;
-    const int before = scan(my_b, NB);
-    int max_nb = 0, n_ne = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        max_nb = max(max_nb, sm_scan[1][w]);
-        n_ne += sm_scan[2][w];
-    }
+    // (64-bit products and divisions here cost a short call 0.5 us: equal parts are cut as quotient and rest)
     const int c = blockIdx.x, grid = gridDim.x;
     const bool split = n_ne <= grid;
     const bool whole = !split && max_nb <= kWholeBlocks;
-    const int T = whole ? 1 << 30 : min(kSnapBlocks, max(1, NB / grid / 4));
+    const int quot = NB / grid, rest = NB - quot * grid;  // (more units than CTAs: quot > 0)
+    const int T = whole ? 1 << 30 : min(kSnapBlocks, max(1, quot / 4));
     int c1 = 0, pieces = 1;  // split: the CTA after the first piece's, the pieces of the unit
     Walk start;
     start.begin = start.end = start.u = 0;
@@ -280,14 +285,14 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         // all blocks allows, or once, twice or three times less, whichever leaves no more pieces than CTAs, and
         // failing those one that cannot leave more.
         const int target = max(n_ne, min(grid, NB / kMinBlocks));
-        const int j0 = max(1, (int)((long long)max_nb * target / NB));
+        const int j0 = max(1, (int)((float)max_nb * (float)target / (float)NB));
         int per = 0, total = 0, at = 0;
         for (int j = 0; j < 5; ++j) {
             const int div = max(1, j0 - j), room = max(1, grid - n_ne);
             per = j < 4 ? (max_nb + div - 1) / div : (NB + room - 1) / room;
             int my_k = 0;
             for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, rows_again(u)) + per - 1) / per;
-            __syncthreads();  // the last scan has been read
+            if (j > 0) __syncthreads();  // the last scan has been read
             at = scan(my_k, total);
             if (total <= grid) {
                 if (c >= at && c < at + my_k) {
@@ -315,12 +320,15 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             const int s = c - sm_cut[0][1];
             c1 = sm_cut[0][1] + 1;
             pieces = (start.nb + per - 1) / per;
-            start.begin = (int)((long long)start.nb * s / pieces);
-            start.end = (int)((long long)start.nb * (s + 1) / pieces);
+            const int pq = start.nb / pieces, pr = start.nb - pq * pieces;
+            start.begin = pq * s + min(s, pr);
+            start.end = pq * (s + 1) + min(s + 1, pr);
         }
     } else if (NB > 0) {
         // More units than CTAs: equal ranges of the blocks laid end to end
-        auto ideal = [&](int k) { return (int)((long long)k * NB / grid); };
+        int total;
+        const int before = scan(my_b, total);
+        auto ideal = [&](int k) { return quot * k + min(k, rest); };
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int t = ideal(c + k);
@@ -429,7 +437,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     Block blk(lane, join + wid * GM * D);
     auto head_row = [&](int u) { return (size_t)(u / a.Hkv) * a.Hq + (size_t)(u % a.Hkv) * G; };
     // units without rows: zeros, lse = -inf
-    for (int u = c * NW + wid; u < P; u += (int)gridDim.x * NW) {
+    for (int u = n_ne < P ? c * NW + wid : P; u < P; u += grid * NW) {
         if (rows_of(a, a.lens[u]) > 0) continue;
         const size_t q0 = head_row(u);
         for (int x = lane; x < G * D / 4; x += 32) store_out4(a, q0 * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f));
@@ -593,13 +601,15 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
 
         // ---- a unit cut between CTAs: publish; the last one joins the pieces
         if (!split) {  // cuts inside [ub, ue) stay where they fall from ub + T to ue - T; piece 0 is the CTA's before the first
-            const long long ub = start.begin + d.at - d.lo, ue = ub + d.nb;
-            auto first_at = [&](long long b) { return (int)((b * grid + NB - 1) / NB); };  // first CTA whose ideal start is >= b
+            const int ub = start.begin + d.at - d.lo, ue = ub + d.nb;
+            auto first_at = [&](int b) {  // first CTA whose ideal start is >= b
+                const int big = rest * (quot + 1);
+                return b <= big ? (b + quot) / (quot + 1) : rest + (b - big + quot - 1) / quot;
+            };
             c1 = first_at(ub + T);
             pieces = 1 + max(0, first_at(ue - T + 1) - c1);
         }
         if (tid == 0) {
-            __threadfence();
             sm_old = atom_add_acq_rel(&a.counters[2 + d.u], 1);
         }
         bar_compute();

@@ -131,6 +131,7 @@ def test_workspace_sizes(L):
     (dict(page=512), reco.RECO_EUNSUPPORTED), (dict(page=0), reco.RECO_EUNSUPPORTED),
     (dict(page=-16), reco.RECO_EUNSUPPORTED), (dict(n_layers=70000, B=70000), reco.RECO_EUNSUPPORTED),
     (dict(n_layers=100, B=400), reco.RECO_EUNSUPPORTED), (dict(max_pages=1 << 27), reco.RECO_EUNSUPPORTED),
+    (dict(B=8192, max_pages=1 << 16), reco.RECO_EUNSUPPORTED),
     (dict(n_pages=1 << 25), reco.RECO_EUNSUPPORTED)])
 def test_descriptors_that_are_refused(L, bad, status):
     kv, vp, big = _kv(**bad), ctypes.c_void_p, 1 << 40
