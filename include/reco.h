@@ -369,7 +369,9 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  *   w, sinks : >= 0, w + sinks <= max_pages * page
  *   kept_idx : [n_layers][B][H_kv][max_pages * page] int32 (device) or NULL; if given,
  *              the first m entries of each unit that is cut receive `kept`
- *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes
+ *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes, of which the
+ *              first 256 are zero-filled before its first use; every call leaves it
+ *              reusable; calls that share one must not overlap on the GPU
  * No two table entries for rows of live sequences may name the same page.  A unit with a
  * length outside [0, max_pages * page], one to be cut below sinks + w, or one to be cut
  * whose table names a page outside [0, n_pages) for one of its rows is left untouched

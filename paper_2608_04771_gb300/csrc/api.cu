@@ -271,7 +271,7 @@ reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size
     if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS)
         *bytes_out = reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
     else if (op == RECO_OP_PAGED_EVICT)
-        *bytes_out = reco::paged_evict_ws_layout(*kv, nullptr).bytes;
+        *bytes_out = reco::evict_ws_layout(*kv, nullptr).bytes;
     else
         return fail(RECO_EINVAL, "op %d is not a paged call", (int)op);
     return RECO_OK;
@@ -517,7 +517,7 @@ reco_status reco_paged_evict(const reco_paged_kv *kv, float *weights, int32_t *l
     const int cap = reco::paged_cap(*kv);
     if (w < 0 || sinks < 0 || w > cap || sinks > cap - w)
         return fail(RECO_EINVAL, "w = %d and sinks = %d must be >= 0 and together at most the %d rows of a sequence", w, sinks, cap);
-    reco::SelectWs lay = reco::paged_evict_ws_layout(*kv, ws);
+    reco::EvictWs lay = reco::evict_ws_layout(*kv, ws);
     if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK) return st;
     unsigned *err;
     if ((st = error_word(&err)) != RECO_OK) return st;

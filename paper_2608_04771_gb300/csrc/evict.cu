@@ -1,0 +1,251 @@
+// evict.cu -- eviction of a paged cache down to a budget by accumulated attention weight (the selection
+// and in-place compaction of Sec. 3.2 with running sums in place of Eq. 2's scores).
+//
+// The selection (select.cu) writes every cut unit's kept rows in ascending order, compacts the weights and
+// lists the units and their chunks.  kept[r] >= r, so a destination row is the source of rows at or below it
+// only, and the rows can move in place.  With many cut units a CTA walks a column of a unit in order
+// (compact_columns).  With few, their chunks of 16 KB of K and 16 KB of V move in parallel (compact_chunks: 32
+// units of 3900 rows 69 -> 32 us): a CTA reads its chunk's rows into registers, says so in the chunk's flag, and
+// writes them once the chunks have been read whose sources lie in its destination rows.  Those are known from the
+// kept rows counted before the chunk's first row and its end (`rank`): no more than a chunk has, so two chunks at
+// most.  CTAs claim chunks in the order of the list, a unit's own in ascending order: the chunks that a CTA
+// waits for were claimed before its own, and reading never waits, so every wait ends.  The chunks would do for
+// many units too, but slower: 896 units of 3900 rows 881 us (each chunk's chain of index, table, row and flag),
+// by columns 595, 0.90 of the copy rate.
+#include <algorithm>
+
+#include "common.cuh"
+#include "internal.h"
+
+namespace reco {
+
+EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base)
+{
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char *r = base ? (char *)base + off : nullptr;
+        off += align256(bytes);
+        return r;
+    };
+    const size_t units = (size_t)kv.n_layers * kv.B * kv.H_kv, chunks = evict_chunks(kv);
+    EvictWs ws;
+    ws.counters = (int32_t *)take(16);
+    ws.idx = (int32_t *)take(units * paged_cap(kv) * 4);
+    ws.rank = (int32_t *)take(units * (chunks + 1) * 4);
+    ws.flags = (int32_t *)take(units * chunks * 4);
+    ws.list = (int2 *)take(units * chunks * 8);
+    ws.ulist = (int32_t *)take(units * 4);
+    ws.bytes = off;
+    return ws;
+}
+
+struct CompactArgs {
+    char *K, *V;
+    const int32_t *table, *idx, *lens;
+    EvictWs ws;
+    int units, B, Hkv, n_pages, max_pages, page_shift, cap, chunks;
+    int column_ctas;  // CTAs of compact_columns, 0: not launched
+    unsigned *err;
+};
+
+constexpr int kCompactThreads = 256;
+constexpr long long kFlagSpin = 1LL << 22;  // polls of a chunk's flag (about a second)
+
+__device__ __forceinline__ int ld_acquire(const int *p)
+{
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_release(int *p, int v)
+{
+    asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+
+// Where the rows of a unit lie.  The selection has checked the table entries of all its rows; an entry is
+// held inside the pool all the same, and a kept row inside the cache, so that a workspace or an index array that
+// something else has written to costs no access out of bounds.
+template <int ROW> struct UnitRows {
+    const int32_t *table;
+    int base, pitch, shift;  // pool row of the unit's row 0 in page 0, rows from page to page
+    unsigned last;           // the last page of the pool
+    __device__ __forceinline__ UnitRows(const CompactArgs &a, int u) : shift(a.page_shift), last(a.n_pages - 1)
+    {
+        const int lb = u / a.Hkv, layer = lb / a.B;
+        table = a.table + (long)(lb - layer * a.B) * a.max_pages;
+        pitch = a.Hkv << shift;
+        base = layer * a.n_pages * pitch + ((u - lb * a.Hkv) << shift);
+    }
+    __device__ __forceinline__ size_t at(int r) const  // byte of row r in the pool
+    {
+        const int e = (int)min((unsigned)__ldg(table + (r >> shift)), last);
+        return (size_t)(unsigned)(base + e * pitch + (r & ((1 << shift) - 1))) * ROW;
+    }
+};
+
+// Many cut units: a CTA moves a unit's 128-byte column slice of K or of V, its destinations in order in steps of
+// 32 U rows, U rows per thread: a step's reads, a barrier, its writes, with the next step's reads issued before this
+// one's writes (two steps in registers).  kept[r] >= r, so no source is a row that an earlier step has written.
+template <int ROW> __device__ __forceinline__ void compact_column(const CompactArgs &a, int u, bool is_v, int slice)
+{
+    constexpr int U = 2, RPP = kCompactThreads / 8, STEP = U * RPP;
+    const UnitRows<ROW> rows(a, u);
+    const int m = min(a.lens[u], a.cap), sub = threadIdx.x / 8;
+    const int32_t *idx = a.idx + (size_t)u * a.cap;
+    char *pool = (is_v ? a.V : a.K) + slice * 128 + (threadIdx.x % 8) * 16;
+    auto load = [&](int r0, uint4 (&v)[U], int (&dst)[U]) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int r = r0 + i * RPP + sub;
+            dst[i] = -1;
+            if (r < m) {
+                const int src = __ldg(idx + r);
+                if (src > r && src < a.cap) {  // else already in place
+                    v[i] = *reinterpret_cast<const uint4 *>(pool + rows.at(src));
+                    dst[i] = r;
+                }
+            }
+        }
+    };
+    auto store = [&](const uint4 (&v)[U], const int (&dst)[U]) {
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (dst[i] >= 0) *reinterpret_cast<uint4 *>(pool + rows.at(dst[i])) = v[i];
+    };
+    uint4 va[U], vb[U];
+    int da[U], db[U];
+    load(0, va, da);
+    for (int r0 = 0; r0 < m; r0 += 2 * STEP) {
+        load(r0 + STEP, vb, db);
+        __syncthreads();
+        store(va, da);
+        if (r0 + STEP >= m) break;
+        load(r0 + 2 * STEP, va, da);
+        __syncthreads();
+        store(vb, db);
+    }
+}
+
+// Few cut units: chunk `c` of a unit, 16 KB of K and 16 KB of V, four pieces of 16 bytes of each per thread.
+template <int ROW> __device__ __forceinline__ void compact_chunk(const CompactArgs &a, int u, int c)
+{
+    constexpr int PIECES = ROW / 16, RPP = kCompactThreads / PIECES, U = 4, R = RPP * U;
+    const UnitRows<ROW> rows(a, u);
+    const int m = min(a.lens[u], a.cap), r0 = c * R, sub = threadIdx.x / PIECES;
+    const int32_t *idx = a.idx + (size_t)u * a.cap;
+    char *K = a.K + (threadIdx.x % PIECES) * 16, *V = a.V + (threadIdx.x % PIECES) * 16;
+    uint4 k[U], v[U];
+    int src[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int r = r0 + i * RPP + sub;
+        src[i] = r < m ? __ldg(idx + r) : r;
+        if (src[i] < r || src[i] >= a.cap) src[i] = r;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        if (src[i] == r0 + i * RPP + sub) continue;  // already in place, or behind the last row
+        const size_t p = rows.at(src[i]);
+        k[i] = __ldcs(reinterpret_cast<const uint4 *>(K + p));
+        v[i] = __ldcs(reinterpret_cast<const uint4 *>(V + p));
+    }
+    __syncthreads();  // the chunk has been read
+    if (threadIdx.x == 0) {
+        int *flags = a.ws.flags + (size_t)u * a.chunks;
+        st_release(flags + c, 1);
+        // kept rows in this chunk's destination rows: their destinations' chunks have to have been read
+        const int32_t *rank = a.ws.rank + (size_t)u * (a.chunks + 1);
+        const int lo = max(0, __ldg(rank + c)), hi = __ldg(rank + c + 1);
+        for (int b = lo / R; b < c && b * R < hi; ++b) {
+            long long spin = 0;
+            while (ld_acquire(flags + b) == 0 && spin < kFlagSpin) ++spin;
+            if (spin >= kFlagSpin) {
+                raise_error(a.err, ERR_INTERNAL);
+                break;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int r = r0 + i * RPP + sub;
+        if (src[i] == r) continue;
+        const size_t p = rows.at(r);
+        *reinterpret_cast<uint4 *>(K + p) = k[i];
+        *reinterpret_cast<uint4 *>(V + p) = v[i];
+    }
+}
+
+// Whether the columns of the cut units keep most of the `ctas` of compact_columns busy: then they move, and
+// else the chunks.
+__device__ __forceinline__ bool by_columns(const CompactArgs &a, int columns)
+{
+    return a.column_ctas > 0 && 4LL * columns >= 3LL * a.column_ctas;
+}
+
+template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 8) compact_columns(CompactArgs a)
+{
+    wait_prior_grid();  // the selection's results
+    const int cut = min(a.ws.counters[3], a.units);
+    if (!by_columns(a, cut * 2 * (ROW / 128))) return;
+    for (int i = blockIdx.x; i < cut; i += gridDim.x) {
+        const int u = a.ws.ulist[i];
+        if ((unsigned)u >= (unsigned)a.units) continue;
+        compact_column<ROW>(a, u, blockIdx.y != 0, blockIdx.z);
+        __syncthreads();
+    }
+}
+
+template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact_chunks(CompactArgs a)
+{
+    wait_prior_grid();  // the selection's results
+    const int columns = min(a.ws.counters[3], a.units) * 2 * (ROW / 128);
+    const int chunks = min(a.ws.counters[1], a.units * a.chunks);
+    const int total = by_columns(a, columns) ? 0 : chunks;
+    __shared__ int sm_next;
+    if (threadIdx.x == 0) sm_next = total > 0 ? atomicAdd(&a.ws.counters[0], 1) : 0;
+    __syncthreads();
+    int t = sm_next;
+    while (t < total) {
+        int claimed = 0;
+        if (threadIdx.x == 0) claimed = atomicAdd(&a.ws.counters[0], 1);  // the next one, while this one moves
+        const int2 it = a.ws.list[t];
+        if ((unsigned)it.x < (unsigned)a.units && (unsigned)it.y < (unsigned)a.chunks) compact_chunk<ROW>(a, it.x, it.y);
+        else if (threadIdx.x == 0) raise_error(a.err, ERR_INTERNAL);
+        __syncthreads();
+        if (threadIdx.x == 0) sm_next = claimed;
+        __syncthreads();
+        t = sm_next;
+    }
+    // the last CTA to finish leaves the counters zero, as the call found them
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&a.ws.counters[2], 1) == (int)gridDim.x - 1)
+            *reinterpret_cast<int4 *>(a.ws.counters) = make_int4(0, 0, 0, 0);
+    }
+}
+
+cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                               int sinks, int32_t *kept_idx, const EvictWs &ws, unsigned *err, cudaStream_t s)
+{
+    int32_t *idx = kept_idx ? kept_idx : ws.idx;
+    cudaError_t e = launch_select_budget(kv, weights, lens, budget, w, sinks, idx, ws, err, s);
+    if (e != cudaSuccess) return e;
+    const int units = kv.n_layers * kv.B * kv.H_kv;
+    const int row = kv.d * (kv.dtype == RECO_F32 ? 4 : 2), sms = device_sm_count();
+    const long long columns = (long long)units * 2 * (row / 128);
+    CompactArgs a{(char *)kv.k, (char *)kv.v, kv.table, idx, lens, ws, units, kv.B, kv.H_kv, kv.n_pages, kv.max_pages,
+                  __builtin_ctz((unsigned)kv.page), paged_cap(kv), evict_chunks(kv), 0, err};
+    if (4 * columns >= 3LL * 8 * sms) {  // (else not even all units' columns would do)
+        a.column_ctas = 8 * sms;
+        e = launch_pdl(row == 128 ? compact_columns<128> : (row == 256 ? compact_columns<256> : compact_columns<512>),
+                       dim3(a.column_ctas / (2 * (row / 128)), 2, row / 128), dim3(kCompactThreads), 0, s, a);
+        if (e != cudaSuccess) return e;
+    }
+    const dim3 grid((unsigned)std::min<long long>((long long)units * a.chunks, 4LL * sms));
+    e = launch_pdl(row == 128 ? compact_chunks<128> : (row == 256 ? compact_chunks<256> : compact_chunks<512>), grid,
+                   dim3(kCompactThreads), 0, s, a);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace reco

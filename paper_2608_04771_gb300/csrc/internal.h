@@ -72,14 +72,32 @@ struct PagedDecodeWs {
     size_t bytes;
 };
 
+// Regions of the paged eviction's workspace.  The compaction moves chunks of 2^evict_shift rows.
+struct EvictWs {
+    int32_t *counters;  // [0] items claimed, [1] chunks and [3] units listed, [2] CTAs done: zero between calls
+    int32_t *idx;       // [units][cap] kept rows (when the caller passes none)
+    int32_t *rank;      // [units][chunks + 1] kept rows before row i << shift
+    int32_t *flags;     // [units][chunks] the chunk's rows have been read
+    int2 *list;         // [units * chunks] (unit, chunk) to move, a unit's chunks in order
+    int32_t *ulist;     // [units] units that are cut
+    size_t bytes;
+};
+
 ScoreWs score_ws_layout(const reco_kv &kv, int w, void *base);
 SelectWs select_ws_layout(const reco_kv &kv, void *base);
 DecodeWs decode_ws_layout(const reco_kv &kv, void *base);
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base);
-SelectWs paged_evict_ws_layout(const reco_paged_kv &kv, void *base);
+EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base);
 
 // Rows a unit of the paged cache may hold.
 inline int paged_cap(const reco_paged_kv &kv) { return kv.max_pages * kv.page; }
+// Chunks of the eviction's compaction: 16 KB of K and 16 KB of V, 128 to 32 rows.
+inline int evict_shift(const reco_paged_kv &kv)
+{
+    const int row = kv.d * (kv.dtype == RECO_F32 ? 4 : 2);
+    return row == 128 ? 7 : (row == 256 ? 6 : 5);
+}
+inline int evict_chunks(const reco_paged_kv &kv) { return (paged_cap(kv) + (1 << evict_shift(kv)) - 1) >> evict_shift(kv); }
 
 // Launchers return cudaSuccess or the launch error.  All arguments validated by the caller.
 cudaError_t launch_score(const reco_kv &kv, const void *q_win, const int32_t *lens, const int32_t *keep, int w,
@@ -109,7 +127,10 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
                                 int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
                                 float *lse, float *weights, const PagedDecodeWs &ws, unsigned *err, cudaStream_t s);
 cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
-                               int sinks, int32_t *kept_idx, const SelectWs &ws, unsigned *err, cudaStream_t s);
+                               int sinks, int32_t *kept_idx, const EvictWs &ws, unsigned *err, cudaStream_t s);
+// The eviction's selection: kept rows into idx, weights compacted, lens cut, the compaction's list.
+cudaError_t launch_select_budget(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                                 int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s);
 cudaError_t launch_penalty(float *logits, int B, int V, const int32_t *ids, int n_ids,
                            const float *rewards, float tau_l, float tau_h, float beta, float *beta_out,
                            unsigned *err, cudaStream_t s);

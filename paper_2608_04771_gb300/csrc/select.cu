@@ -42,14 +42,6 @@ SelectWs select_ws_layout(const reco_kv &kv, void *base)
     return ws;
 }
 
-// The paged cache as the selection sees it: units of at most cap rows.
-static reco_kv paged_units(const reco_paged_kv &kv)
-{
-    return reco_kv{kv.k, kv.v, kv.n_layers, kv.B, kv.H_q, kv.H_kv, paged_cap(kv), kv.d, kv.dtype};
-}
-
-SelectWs paged_evict_ws_layout(const reco_paged_kv &kv, void *base) { return select_ws_layout(paged_units(kv), base); }
-
 // Most candidates a unit may have for the shared-memory selection (192 KB of keys).
 constexpr int kSelectSmemKeys = 48 * 1024;
 
@@ -85,31 +77,63 @@ struct KeepRule {
     {
         return (L < w || L > L_cap) ? ERR_LEN : ((m < w || m > L) ? ERR_KEEP : 0u);
     }
-    __device__ __forceinline__ bool leave(int, int) const { return false; }
-    __device__ __forceinline__ bool bad_page(int, int) const { return false; }
-    __device__ __forceinline__ int entries(int) const { return 0; }
+    __device__ __forceinline__ float load(const float *p) const { return *p; }
     __device__ __forceinline__ uint32_t key(float f) const { return order_key(f); }
 };
 
 // Down to at most budget[b] rows of a paged cache: a unit within its budget is left alone, one whose
-// table names a page that the pool does not have is refused before anything moves.
+// table names a page that the pool does not have is refused before anything moves.  The selection also
+// moves the weights themselves (the one score array that is compacted: every kernel holds or has read a unit's
+// weights by the time it writes them, and writes none above the row it read last), and prepares the
+// compaction: its list of (unit, chunk of 2^shift rows), the chunks' flags cleared, and rank[i], the kept rows
+// before row i << shift.
 struct BudgetRule {
     static constexpr bool BUDGET = true;
     int w, first;
     const int32_t *table;
     int max_pages, n_pages, page;
+    float *weights;
+    int32_t *rank, *flags;
+    int2 *list;
+    int32_t *ulist, *counters;
+    int shift, chunks, units;
     __device__ __forceinline__ unsigned error(int L, int m, int L_cap) const
     {
         return (L < 0 || L > L_cap) ? ERR_LEN : ((L > m && m < first + w) ? ERR_KEEP : 0u);
     }
-    __device__ __forceinline__ bool leave(int L, int m) const { return L <= m; }
-    __device__ __forceinline__ bool bad_page(int b, int i) const
+    // the unit's table entries i = from, from + step, ... are looked at: any that names no page
+    __device__ __forceinline__ bool bad_page(int b, int L, int from, int step) const
     {
-        return (unsigned)table[(long)b * max_pages + i] >= (unsigned)n_pages;
+        bool any = false;
+        for (int i = from; i < (L + page - 1) / page; i += step)
+            any |= (unsigned)table[(long)b * max_pages + i] >= (unsigned)n_pages;
+        return any;
     }
-    __device__ __forceinline__ int entries(int L) const { return (L + page - 1) / page; }
+    __device__ __forceinline__ float load(const float *p) const { return __ldcg(p); }
     // -0 equals +0, and NaN lies above everything
     __device__ __forceinline__ uint32_t key(float f) const { return f == f ? order_key(f + 0.f) : 0xffffffffu; }
+    __device__ __forceinline__ float value(uint32_t k) const { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+    // row j, with `before` kept rows below it
+    __device__ __forceinline__ void passed(long u, int j, int before) const
+    {
+        if ((j & ((1 << shift) - 1)) == 0) rank[u * (chunks + 1) + (j >> shift)] = before;
+    }
+    // lists the unit; the first place of its chunks in their list
+    __device__ __forceinline__ int claim(long u, int m) const
+    {
+        const int at = atomicAdd(&counters[3], 1);
+        if ((unsigned)at < (unsigned)units) ulist[at] = (int)u;
+        return atomicAdd(&counters[1], (m + (1 << shift) - 1) >> shift);
+    }
+    // a thread's share of the unit's chunks (and, by one, the rank of the end of its rows)
+    __device__ __forceinline__ void enlist(long u, int L, int m, int at, int from, int step) const
+    {
+        if (from == 0) rank[u * (chunks + 1) + ((L - 1) >> shift) + 1] = m;
+        for (int i = from; i < (m + (1 << shift) - 1) >> shift; i += step) {
+            flags[u * chunks + i] = 0;
+            if ((unsigned)(at + i) < (unsigned)(units * chunks)) list[at + i] = make_int2((int)u, i);
+        }
+    }
 };
 
 // Exclusive block scan of a 0/1 flag.  `tot` must hold NT/32 + 1 ints.
@@ -160,20 +184,14 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
         const int w = rule.w, first = rule.first;
         unsigned bad = rule.error(L, m, L_cap);
         if constexpr (Rule::BUDGET) {
-            if (bad == 0u && rule.leave(L, m)) {
-                if (tid == 0) count[u] = 0;
-                continue;
-            }
+            if (bad == 0u && L <= m) continue;
             if (bad == 0u) {
-                const int b = (int)((u / Hkv) % B), n = rule.entries(L);
-                bool any = false;
-                for (int i = tid; i < n; i += NT) any |= rule.bad_page(b, i);
-                if (__syncthreads_or(any)) bad = ERR_PAGE;
+                if (__syncthreads_or(rule.bad_page((int)((u / Hkv) % B), L, tid, NT))) bad = ERR_PAGE;
             }
         }
         if (bad != 0u) {
             if (tid == 0) {
-                count[u] = 0;
+                if constexpr (!Rule::BUDGET) count[u] = 0;
                 raise_error(err, bad);
             }
             continue;
@@ -187,7 +205,10 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
             continue;
         }
         if constexpr (Rule::BUDGET) {
-            for (int j = tid; j < first; j += NT) idx[j] = j;
+            for (int j = tid; j < first; j += NT) {
+                idx[j] = j;
+                rule.passed(u, j, j);
+            }
             idx += first;
         }
         uint32_t T = 0xffffffffu;
@@ -206,7 +227,7 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
                 for (int jb = 0; jb < nc; jb += NT) {
                     const int j = jb + tid;
                     const bool valid = j < nc;
-                    const uint32_t key = valid ? rule.key(s[j]) : 0u;
+                    const uint32_t key = valid ? rule.key(rule.load(s + j)) : 0u;
                     const bool match = valid && (key & mask) == prefix;
                     const uint32_t bin = (key >> shift) & 255u;
                     if (match) atomicAdd(&hist[bin], 1);
@@ -248,7 +269,8 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
         for (int jb = 0; jb < nc; jb += NT) {
             const int j = jb + tid;
             const bool valid = j < nc;
-            const uint32_t key = valid ? rule.key(s[j]) : 0u;
+            const float x = valid ? rule.load(s + j) : 0.f;
+            const uint32_t key = valid ? rule.key(x) : 0u;
             const bool gt = valid && key > T;
             const bool eq = valid && key == T;
             int eq_tot, f_tot;
@@ -256,12 +278,32 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
             const bool flag = gt || (eq && eq_rank < need);
             const int pos = block_scan_flag<NT>(flag, tot, f_tot) + base_pos;
             if (flag) idx[pos] = first + j;
+            if constexpr (Rule::BUDGET) {  // (the scans' barriers: every thread has read its weight)
+                if (flag) rule.weights[u * L_cap + first + pos] = x;
+                if (valid) rule.passed(u, first + j, first + pos);
+            }
             base_eq += eq_tot;
             base_pos += f_tot;
         }
+        if constexpr (Rule::BUDGET) {
+            __shared__ int s_at;
+            if (tid == 0) s_at = rule.claim(u, m);
+            float *wt = rule.weights + u * L_cap;
+            for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
+                const int t = t0 + tid;
+                const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+                __syncthreads();
+                if (t < w) {
+                    wt[m - w + t] = x;
+                    rule.passed(u, L - w + t, m - w + t);
+                }
+            }
+            __syncthreads();
+            rule.enlist(u, L, m, s_at, tid, NT);
+        }
         for (int t = tid; t < w; t += NT) idx[kc + t] = first + nc + t;
         if (tid == 0) {
-            count[u] = m;
+            if constexpr (!Rule::BUDGET) count[u] = m;
             if (lens_out) lens_out[u] = m;
         }
         __syncthreads();  // this unit's shared memory is read out before the next unit's fill
@@ -311,20 +353,14 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
         const int w = rule.w, first = rule.first;
         unsigned bad = rule.error(L, m, L_cap);
         if constexpr (Rule::BUDGET) {
-            if (bad == 0u && rule.leave(L, m)) {
-                if (tid == 0) count[u] = 0;
-                continue;
-            }
+            if (bad == 0u && L <= m) continue;
             if (bad == 0u) {
-                const int b = (int)((u / Hkv) % B), n = rule.entries(L);
-                bool any = false;
-                for (int i = tid; i < n; i += NT) any |= rule.bad_page(b, i);
-                if (__syncthreads_or(any)) bad = ERR_PAGE;
+                if (__syncthreads_or(rule.bad_page((int)((u / Hkv) % B), L, tid, NT))) bad = ERR_PAGE;
             }
         }
         if (bad != 0u) {
             if (tid == 0) {
-                count[u] = 0;
+                if constexpr (!Rule::BUDGET) count[u] = 0;
                 raise_error(err, bad);
             }
             continue;
@@ -338,7 +374,10 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
             continue;
         }
         if constexpr (Rule::BUDGET) {
-            for (int j = tid; j < first; j += NT) idx[j] = j;
+            for (int j = tid; j < first; j += NT) {
+                idx[j] = j;
+                rule.passed(u, j, j);
+            }
             idx += first;
         }
         uint32_t lo = 0xffffffffu, hi = 0;
@@ -481,12 +520,33 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
             const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
             const unsigned fb = __ballot_sync(0xffffffffu, flag);
             if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
+            if constexpr (Rule::BUDGET) {
+                const int p = rule.first + pos + __popc(fb & below);
+                if (flag) rule.weights[u * L_cap + p] = rule.value(key);
+                if (valid) rule.passed(u, rule.first + j, p);
+            }
             e_run += __popc(eb);
             pos += __popc(fb);
         }
+        if constexpr (Rule::BUDGET) {
+            __shared__ int s_at;
+            if (tid == 0) s_at = rule.claim(u, m);
+            float *wt = rule.weights + u * L_cap;
+            for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
+                const int t = t0 + tid;
+                const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+                __syncthreads();
+                if (t < w) {
+                    wt[m - w + t] = x;
+                    rule.passed(u, L - w + t, m - w + t);
+                }
+            }
+            __syncthreads();
+            rule.enlist(u, L, m, s_at, tid, NT);
+        }
         for (int t = tid; t < w; t += NT) idx[kc + t] = first + nc + t;
         if (tid == 0) {
-            count[u] = m;
+            if constexpr (!Rule::BUDGET) count[u] = m;
             if (lens_out) lens_out[u] = m;
         }
         __syncthreads();  // this unit's shared memory is read out before the next unit's fill
@@ -502,8 +562,8 @@ constexpr int kWarpThreads = 256;
 
 // The kept candidates of a unit, kc of its nc <= 32 * K, into idx.
 template <int K, class Rule>
-__device__ __forceinline__ void select_in_warp(const Rule &rule, const float *__restrict__ s, int nc, int kc,
-                                               int32_t *__restrict__ idx, int lane)
+__device__ __forceinline__ void select_in_warp(const Rule &rule, long u, int L_cap, const float *__restrict__ s, int nc,
+                                               int kc, int32_t *__restrict__ idx, int lane)
 {
     uint32_t key[K], lo = 0xffffffffu, hi = 0;
 #pragma unroll
@@ -552,6 +612,11 @@ __device__ __forceinline__ void select_in_warp(const Rule &rule, const float *__
         const bool flag = (j < nc && key[i] > T) || (is_eq && e_run + __popc(eb & below) < need);
         const unsigned fb = __ballot_sync(0xffffffffu, flag);
         if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
+        if constexpr (Rule::BUDGET) {
+            const int p = rule.first + pos + __popc(fb & below);
+            if (flag) rule.weights[u * L_cap + p] = rule.value(key[i]);
+            if (j < nc) rule.passed(u, rule.first + j, p);
+        }
         e_run += __popc(eb);
         pos += __popc(fb);
     }
@@ -572,20 +637,12 @@ __global__ void __launch_bounds__(kWarpThreads) select_topm_warp(const float *__
     const int w = rule.w, first = rule.first;
     unsigned bad = rule.error(L, m, L_cap);
     if constexpr (Rule::BUDGET) {
-        if (bad == 0u && rule.leave(L, m)) {
-            if (lane == 0) count[u] = 0;
-            return;
-        }
-        if (bad == 0u) {
-            const int b = (u / Hkv) % B, n = rule.entries(L);
-            bool any = false;
-            for (int i = lane; i < n; i += 32) any |= rule.bad_page(b, i);
-            if (__any_sync(0xffffffffu, any)) bad = ERR_PAGE;
-        }
+        if (bad == 0u && L <= m) return;
+        if (bad == 0u && __any_sync(0xffffffffu, rule.bad_page((u / Hkv) % B, L, lane, 32))) bad = ERR_PAGE;
     }
     if (bad != 0u) {
         if (lane == 0) {
-            count[u] = 0;
+            if constexpr (!Rule::BUDGET) count[u] = 0;
             raise_error(err, bad);
         }
         return;
@@ -599,20 +656,38 @@ __global__ void __launch_bounds__(kWarpThreads) select_topm_warp(const float *__
         return;
     }
     if constexpr (Rule::BUDGET) {
-        for (int j = lane; j < first; j += 32) idx[j] = j;
+        for (int j = lane; j < first; j += 32) {
+            idx[j] = j;
+            rule.passed(u, j, j);
+        }
         idx += first;
     }
     // a cache's units are often far shorter than its rows (the trace's boundaries, units of 70 to 240
     // rows in a cache of up to 1024: 9.4 -> 5.8 us each)
     if (K > 8 && nc <= 32 * 8)
-        select_in_warp<8>(rule, s, nc, kc, idx, lane);
+        select_in_warp<8>(rule, u, L_cap, s, nc, kc, idx, lane);
     else if (K > 16 && nc <= 32 * 16)
-        select_in_warp<16>(rule, s, nc, kc, idx, lane);
+        select_in_warp<16>(rule, u, L_cap, s, nc, kc, idx, lane);
     else
-        select_in_warp<K>(rule, s, nc, kc, idx, lane);
+        select_in_warp<K>(rule, u, L_cap, s, nc, kc, idx, lane);
+    if constexpr (Rule::BUDGET) {
+        const int at = __shfl_sync(0xffffffffu, lane == 0 ? rule.claim(u, m) : 0, 0);
+        float *wt = rule.weights + (long)u * L_cap;
+        for (int t0 = 0; t0 < w; t0 += 32) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
+            const int t = t0 + lane;
+            const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+            __syncwarp();
+            if (t < w) {
+                wt[m - w + t] = x;
+                rule.passed(u, L - w + t, m - w + t);
+            }
+            __syncwarp();
+        }
+        rule.enlist(u, L, m, at, lane, 32);
+    }
     for (int t = lane; t < w; t += 32) idx[kc + t] = first + nc + t;
     if (lane == 0) {
-        count[u] = m;
+        if constexpr (!Rule::BUDGET) count[u] = m;
         if (lens_out) lens_out[u] = m;
     }
 }
@@ -646,45 +721,8 @@ struct CountFromKeep {
     }
 };
 
-// Where the rows of a unit lie: one after another, or in the pages that its sequence's table names
-// (of which the selection has checked all that hold rows).
-struct ContiguousRows {
-    char *K, *V;
-    struct Unit {
-        char *base;
-        int row_bytes;
-        __device__ __forceinline__ char *row(int r) const { return base + (long)r * row_bytes; }
-    };
-    __device__ __forceinline__ Unit unit(bool v, long u, int L_cap, int row_bytes) const
-    {
-        return Unit{(v ? V : K) + u * (long)L_cap * row_bytes, row_bytes};
-    }
-};
-struct PagedRows {
-    char *K, *V;
-    const int32_t *table;
-    int B, Hkv, n_pages, max_pages, shift;
-    struct Unit {
-        char *base;  // row 0 of page 0 of the unit's layer and head
-        const int32_t *table;
-        long page_bytes;  // from one page of the layer to the next
-        int row_bytes, shift;
-        __device__ __forceinline__ char *row(int r) const
-        {
-            return base + (long)__ldg(table + (r >> shift)) * page_bytes + (long)(r & ((1 << shift) - 1)) * row_bytes;
-        }
-    };
-    __device__ __forceinline__ Unit unit(bool v, long u, int, int row_bytes) const
-    {
-        const long lb = u / Hkv, layer = lb / B;
-        const long head_bytes = (long)row_bytes << shift;
-        return Unit{(v ? V : K) + (layer * n_pages * Hkv + u % Hkv) * head_bytes, table + (lb % B) * max_pages,
-                    Hkv * head_bytes, row_bytes, shift};
-    }
-};
-
-template <class Count, class Rows>
-__global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t *__restrict__ idx_all,
+template <class Count>
+__global__ void __launch_bounds__(256, 8) compact_rows(char *K, char *V, const int32_t *__restrict__ idx_all,
                                                     Count cnt, int L_cap, int row_bytes, long units, unsigned *err)
 {
     constexpr int P = 8;  // 16-byte pieces per 128-byte slice
@@ -704,7 +742,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t 
     for (long u = blockIdx.x; u < units; u += gridDim.x, ++it) {  // a few CTAs per SM walk the units
         const int m = s_ml[it].x, lim = s_ml[it].y;  // the grid gives no CTA more than kWalkAhead units
         if (m == 0) continue;
-        const auto unit = rows.unit(blockIdx.y != 0, u, L_cap, row_bytes);
+        char *base = (blockIdx.y == 0 ? K : V) + u * (long)L_cap * row_bytes;
         const int32_t *idx = idx_all + u * L_cap;
         const int rows_per_pass = blockDim.x / P;
         const int my_row = threadIdx.x / P;
@@ -720,7 +758,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t 
                     if (src < r || src >= lim) {  // never trust an index outside [r, lim)
                         raise_error(err, ERR_INTERNAL);
                     } else if (src != r) {
-                        v[i] = *reinterpret_cast<const uint4 *>(unit.row(src) + off);
+                        v[i] = *reinterpret_cast<const uint4 *>(base + (long)src * row_bytes + off);
                         dst[i] = r;
                     }
                 }
@@ -729,7 +767,7 @@ __global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t 
         auto store = [&](const uint4 (&v)[U], const int (&dst)[U]) {
     #pragma unroll
             for (int i = 0; i < U; ++i)
-                if (dst[i] >= 0) *reinterpret_cast<uint4 *>(unit.row(dst[i]) + off) = v[i];
+                if (dst[i] >= 0) *reinterpret_cast<uint4 *>(base + (long)dst[i] * row_bytes + off) = v[i];
         };
         // Two chunks in registers: the next chunk's reads are issued before this chunk's
         // writes (its sources lie at or above its first destination, above every row this
@@ -745,35 +783,6 @@ __global__ void __launch_bounds__(256, 8) compact_rows(Rows rows, const int32_t 
             load(r0 + 2 * step, va, da);
             __syncthreads();
             store(vb, db);
-        }
-    }
-}
-
-// weights[u, r] = weights[u, idx[r]] for the units that the selection cut, in place: a chunk's reads, a
-// barrier, then its writes, as in compact_rows.
-__global__ void __launch_bounds__(256) compact_weights(float *weights, const int32_t *__restrict__ idx_all,
-                                                       const int32_t *__restrict__ count, int L_cap, long units)
-{
-    constexpr int U = 4;
-    wait_prior_grid();
-    for (long u = blockIdx.x; u < units; u += gridDim.x) {
-        const int m = count[u];
-        float *wt = weights + u * L_cap;
-        const int32_t *idx = idx_all + u * L_cap;
-        for (int r0 = 0; r0 < m; r0 += U * (int)blockDim.x) {
-            float x[U];
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int r = r0 + i * (int)blockDim.x + (int)threadIdx.x;
-                if (r < m) x[i] = wt[idx[r]];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int r = r0 + i * (int)blockDim.x + (int)threadIdx.x;
-                if (r < m) wt[r] = x[i];
-            }
-            __syncthreads();
         }
     }
 }
@@ -865,13 +874,13 @@ static cudaError_t launch_select(const reco_kv &kv, const float *scores, const i
     return cudaGetLastError();
 }
 
-template <class Count, class Rows>
+template <class Count>
 static dim3 compact_grid(const reco_kv &kv, int &row_bytes, long &units)
 {
     row_bytes = kv.d * (kv.dtype == RECO_F32 ? 4 : 2);
     units = (long)kv.n_layers * kv.B * kv.H_kv;
     const int per_unit = 2 * (row_bytes / 128);  // K and V, 128-byte column slices
-    return dim3(walk_grid(compact_rows<Count, Rows>, 256, 0, units, per_unit), 2, row_bytes / 128);
+    return dim3(walk_grid(compact_rows<Count>, 256, 0, units, per_unit), 2, row_bytes / 128);
 }
 
 cudaError_t launch_select_compact(const reco_kv &kv, const float *scores, int32_t *lens,
@@ -883,9 +892,8 @@ cudaError_t launch_select_compact(const reco_kv &kv, const float *scores, int32_
     if (e != cudaSuccess) return e;
     int row_bytes;
     long units;
-    const dim3 grid = compact_grid<CountFromSelect, ContiguousRows>(kv, row_bytes, units);
-    e = launch_pdl(compact_rows<CountFromSelect, ContiguousRows>, grid, dim3(256), 0, s,
-                   ContiguousRows{(char *)kv.k, (char *)kv.v}, (const int32_t *)idx,
+    const dim3 grid = compact_grid<CountFromSelect>(kv, row_bytes, units);
+    e = launch_pdl(compact_rows<CountFromSelect>, grid, dim3(256), 0, s, (char *)kv.k, (char *)kv.v, (const int32_t *)idx,
                    CountFromSelect{ws.count, kv.L_cap}, kv.L_cap, row_bytes, units, err);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -901,9 +909,9 @@ cudaError_t launch_compact(const reco_kv &kv, const int32_t *kept_idx, int32_t *
 {
     int row_bytes;
     long units;
-    const dim3 grid = compact_grid<CountFromKeep, ContiguousRows>(kv, row_bytes, units);
-    cudaError_t e = launch_pdl(compact_rows<CountFromKeep, ContiguousRows>, grid, dim3(256), 0, s,
-                               ContiguousRows{(char *)kv.k, (char *)kv.v}, kept_idx, CountFromKeep{lens, keep, w, kv.B, kv.H_kv, kv.L_cap}, kv.L_cap, row_bytes,
+    const dim3 grid = compact_grid<CountFromKeep>(kv, row_bytes, units);
+    cudaError_t e = launch_pdl(compact_rows<CountFromKeep>, grid, dim3(256), 0, s, (char *)kv.k, (char *)kv.v,
+                               kept_idx, CountFromKeep{lens, keep, w, kv.B, kv.H_kv, kv.L_cap}, kv.L_cap, row_bytes,
                                units, err);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
     e = launch_pdl(compact_set_lens, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, lens, keep, units, w, kv.B,
@@ -911,25 +919,13 @@ cudaError_t launch_compact(const reco_kv &kv, const int32_t *kept_idx, int32_t *
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-cudaError_t launch_paged_evict(const reco_paged_kv &pkv, float *weights, int32_t *lens, const int32_t *budget, int w,
-                               int sinks, int32_t *kept_idx, const SelectWs &ws, unsigned *err, cudaStream_t s)
+cudaError_t launch_select_budget(const reco_paged_kv &pkv, float *weights, int32_t *lens, const int32_t *budget, int w,
+                                 int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s)
 {
-    const reco_kv kv = paged_units(pkv);
-    int32_t *idx = kept_idx ? kept_idx : ws.idx;
-    const BudgetRule rule{w, sinks, pkv.table, pkv.max_pages, pkv.n_pages, pkv.page};
-    cudaError_t e = launch_select(kv, weights, lens, lens, budget, rule, idx, ws.count, err, s);
-    if (e != cudaSuccess) return e;
-    const int shift = __builtin_ctz((unsigned)pkv.page);
-    const PagedRows rows{(char *)pkv.k, (char *)pkv.v, pkv.table, pkv.B, pkv.H_kv, pkv.n_pages, pkv.max_pages, shift};
-    int row_bytes;
-    long units;
-    const dim3 grid = compact_grid<CountFromSelect, PagedRows>(kv, row_bytes, units);
-    e = launch_pdl(compact_rows<CountFromSelect, PagedRows>, grid, dim3(256), 0, s, rows, (const int32_t *)idx,
-                   CountFromSelect{ws.count, kv.L_cap}, kv.L_cap, row_bytes, units, err);
-    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess) return e;
-    e = launch_pdl(compact_weights, dim3(walk_grid(compact_weights, 256, 0, units, 1)), dim3(256), 0, s, weights,
-                   (const int32_t *)idx, (const int32_t *)ws.count, kv.L_cap, units);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    const reco_kv kv{pkv.k, pkv.v, pkv.n_layers, pkv.B, pkv.H_q, pkv.H_kv, paged_cap(pkv), pkv.d, pkv.dtype};
+    const BudgetRule rule{w, sinks, pkv.table, pkv.max_pages, pkv.n_pages, pkv.page, weights, ws.rank, ws.flags, ws.list,
+                          ws.ulist, ws.counters, evict_shift(pkv), evict_chunks(pkv), kv.n_layers * kv.B * kv.H_kv};
+    return launch_select(kv, weights, lens, lens, budget, rule, idx, nullptr, err, s);
 }
 
 }  // namespace reco

@@ -306,8 +306,7 @@ def paged_workspace(op: int, kv: reco_paged_kv, device="cuda") -> torch.Tensor:
     """A workspace for a paged call, with its counters zero as the decode needs them before its first use
     (the logits of a call with weights lie behind what a call without needs, and need no fill)."""
     ws = torch.empty(max(reco_paged_workspace_bytes(op, kv), 256), dtype=torch.uint8, device=device)
-    if op != RECO_OP_PAGED_EVICT:
-        ws[:reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv)].zero_()
+    ws[:256 if op == RECO_OP_PAGED_EVICT else reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv)].zero_()
     return ws
 
 

@@ -382,7 +382,7 @@ def test_captured_and_replayed_on_streams_of_their_own():
         with torch.cuda.graph(graph, stream=st, capture_error_mode="relaxed"):
             reco.reco_paged_decode_attn_weights(c.kv, q, kn, vn, c.lens, c.scale, out, lse, c.weights, ws, 2000, 4)
             reco.reco_paged_evict(c.kv, c.weights, c.lens, budget, 16, 4, None, wse)
-        runs.append((c, eager, graph, st, out, lse, (q, kn, vn), budget))
+        runs.append((c, eager, graph, st, out, lse, (q, kn, vn), budget, ws, wse))  # (a graph keeps no workspace alive)
     torch.cuda.synchronize()
     for _ in range(5):
         for c, eager, graph, st, *_ in runs:
@@ -390,7 +390,7 @@ def test_captured_and_replayed_on_streams_of_their_own():
                 graph.replay()
     torch.cuda.synchronize()
     reco.reco_check()
-    for c, eager, graph, st, out, lse, (q, kn, vn), budget in runs:
+    for c, eager, graph, st, out, lse, (q, kn, vn), budget, *_ in runs:
         e_out, e_lse = eager.outputs(BF)
         ws, wse = eager.workspace(reco.RECO_OP_PAGED_WEIGHTS), eager.workspace(reco.RECO_OP_PAGED_EVICT)
         for _ in range(5):
