@@ -43,7 +43,7 @@ struct CompactArgs {
     char *K, *V;
     const int32_t *table, *idx, *lens;
     EvictWs ws;
-    int units, B, Hkv, n_pages, max_pages, page_shift, cap, chunks;
+    int units, B, Hkv, n_pages, max_pages, page_shift, page_mask, pitch, cap, chunks;  // pitch: pool rows from page to page
     int column_ctas;  // CTAs of compact_columns, 0: not launched
     unsigned *err;
 };
@@ -65,21 +65,19 @@ __device__ __forceinline__ void st_release(int *p, int v)
 // Where the rows of a unit lie.  The selection has checked the table entries of all its rows; an entry is
 // held inside the pool all the same, and a kept row inside the cache, so that a workspace or an index array that
 // something else has written to costs no access out of bounds.
-template <int ROW> struct UnitRows {
+struct UnitRows {
     const int32_t *table;
-    int base, pitch, shift;  // pool row of the unit's row 0 in page 0, rows from page to page
-    unsigned last;           // the last page of the pool
-    __device__ __forceinline__ UnitRows(const CompactArgs &a, int u) : shift(a.page_shift), last(a.n_pages - 1)
+    int base;  // pool row of the unit's row 0 in page 0
+    __device__ __forceinline__ UnitRows(const CompactArgs &a, int u)
     {
         const int lb = u / a.Hkv, layer = lb / a.B;
         table = a.table + (long)(lb - layer * a.B) * a.max_pages;
-        pitch = a.Hkv << shift;
-        base = layer * a.n_pages * pitch + ((u - lb * a.Hkv) << shift);
+        base = layer * a.n_pages * a.pitch + ((u - lb * a.Hkv) << a.page_shift);
     }
-    __device__ __forceinline__ size_t at(int r) const  // byte of row r in the pool
+    template <int ROW> __device__ __forceinline__ size_t at(const CompactArgs &a, int r) const  // byte of row r in the pool
     {
-        const int e = (int)min((unsigned)__ldg(table + (r >> shift)), last);
-        return (size_t)(unsigned)(base + e * pitch + (r & ((1 << shift) - 1))) * ROW;
+        const int e = (int)min((unsigned)__ldg(table + (r >> a.page_shift)), (unsigned)a.n_pages - 1u);
+        return (size_t)(unsigned)(base + e * a.pitch + (r & a.page_mask)) * ROW;
     }
 };
 
@@ -89,40 +87,40 @@ template <int ROW> struct UnitRows {
 template <int ROW> __device__ __forceinline__ void compact_column(const CompactArgs &a, int u, bool is_v, int slice)
 {
     constexpr int U = 2, RPP = kCompactThreads / 8, STEP = U * RPP;
-    const UnitRows<ROW> rows(a, u);
+    const UnitRows rows(a, u);
     const int m = min(a.lens[u], a.cap), sub = threadIdx.x / 8;
     const int32_t *idx = a.idx + (size_t)u * a.cap;
     char *pool = (is_v ? a.V : a.K) + slice * 128 + (threadIdx.x % 8) * 16;
-    auto load = [&](int r0, uint4 (&v)[U], int (&dst)[U]) {
+    auto load = [&](int r0, uint4 (&v)[U]) {  // which of the thread's rows move, a bit each
+        unsigned moves = 0;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int r = r0 + i * RPP + sub;
-            dst[i] = -1;
             if (r < m) {
                 const int src = __ldg(idx + r);
                 if (src > r && src < a.cap) {  // else already in place
-                    v[i] = *reinterpret_cast<const uint4 *>(pool + rows.at(src));
-                    dst[i] = r;
+                    v[i] = *reinterpret_cast<const uint4 *>(pool + rows.at<ROW>(a, src));
+                    moves |= 1u << i;
                 }
             }
         }
+        return moves;
     };
-    auto store = [&](const uint4 (&v)[U], const int (&dst)[U]) {
+    auto store = [&](int r0, const uint4 (&v)[U], unsigned moves) {
 #pragma unroll
         for (int i = 0; i < U; ++i)
-            if (dst[i] >= 0) *reinterpret_cast<uint4 *>(pool + rows.at(dst[i])) = v[i];
+            if (moves & (1u << i)) *reinterpret_cast<uint4 *>(pool + rows.at<ROW>(a, r0 + i * RPP + sub)) = v[i];
     };
     uint4 va[U], vb[U];
-    int da[U], db[U];
-    load(0, va, da);
+    unsigned ma = load(0, va);
     for (int r0 = 0; r0 < m; r0 += 2 * STEP) {
-        load(r0 + STEP, vb, db);
+        const unsigned mb = load(r0 + STEP, vb);
         __syncthreads();
-        store(va, da);
+        store(r0, va, ma);
         if (r0 + STEP >= m) break;
-        load(r0 + 2 * STEP, va, da);
+        ma = load(r0 + 2 * STEP, va);
         __syncthreads();
-        store(vb, db);
+        store(r0 + STEP, vb, mb);
     }
 }
 
@@ -130,7 +128,7 @@ template <int ROW> __device__ __forceinline__ void compact_column(const CompactA
 template <int ROW> __device__ __forceinline__ void compact_chunk(const CompactArgs &a, int u, int c)
 {
     constexpr int PIECES = ROW / 16, RPP = kCompactThreads / PIECES, U = 4, R = RPP * U;
-    const UnitRows<ROW> rows(a, u);
+    const UnitRows rows(a, u);
     const int m = min(a.lens[u], a.cap), r0 = c * R, sub = threadIdx.x / PIECES;
     const int32_t *idx = a.idx + (size_t)u * a.cap;
     char *K = a.K + (threadIdx.x % PIECES) * 16, *V = a.V + (threadIdx.x % PIECES) * 16;
@@ -145,7 +143,7 @@ template <int ROW> __device__ __forceinline__ void compact_chunk(const CompactAr
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         if (src[i] == r0 + i * RPP + sub) continue;  // already in place, or behind the last row
-        const size_t p = rows.at(src[i]);
+        const size_t p = rows.at<ROW>(a, src[i]);
         k[i] = __ldcs(reinterpret_cast<const uint4 *>(K + p));
         v[i] = __ldcs(reinterpret_cast<const uint4 *>(V + p));
     }
@@ -170,7 +168,7 @@ template <int ROW> __device__ __forceinline__ void compact_chunk(const CompactAr
     for (int i = 0; i < U; ++i) {
         const int r = r0 + i * RPP + sub;
         if (src[i] == r) continue;
-        const size_t p = rows.at(r);
+        const size_t p = rows.at<ROW>(a, r);
         *reinterpret_cast<uint4 *>(K + p) = k[i];
         *reinterpret_cast<uint4 *>(V + p) = v[i];
     }
@@ -235,7 +233,7 @@ cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t 
     const int row = kv.d * (kv.dtype == RECO_F32 ? 4 : 2), sms = device_sm_count();
     const long long columns = (long long)units * 2 * (row / 128);
     CompactArgs a{(char *)kv.k, (char *)kv.v, kv.table, idx, lens, ws, units, kv.B, kv.H_kv, kv.n_pages, kv.max_pages,
-                  __builtin_ctz((unsigned)kv.page), paged_cap(kv), evict_chunks(kv), 0, err};
+                  __builtin_ctz((unsigned)kv.page), kv.page - 1, kv.H_kv * kv.page, paged_cap(kv), evict_chunks(kv), 0, err};
     if (4 * columns >= 3LL * 8 * sms) {  // (else not even all units' columns would do)
         a.column_ctas = 8 * sms;
         e = launch_pdl(row == 128 ? compact_columns<128> : (row == 256 ? compact_columns<256> : compact_columns<512>),

@@ -275,21 +275,28 @@ def make_paged_kv(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, H_q: in
     kv = reco_paged_kv(K.data_ptr(), V.data_ptr(), table.data_ptr(), Ly, B, H_q, Hkv, n_pages, max_pages, page, d,
                        _dtype_code(K.dtype))
     kv.tensors = (K, V, table)
+    # what a call checks its tensors against: device, dtype, queries, new rows, lse, units, rows of all units
+    kv.expect = (K.get_device(), K.dtype, (Ly, B, H_q, d), (Ly, B, Hkv, d), (Ly, B, H_q), (Ly, B, Hkv),
+                 (Ly, B, Hkv, max_pages * page))
     return kv
 
 
-def _paged_args(kv: reco_paged_kv, ws, args):
-    """args: (name, tensor or None, shape, dtype or None).  The library takes bare pointers: a tensor
-    of another shape, type or device, or with gaps, would be read out of place."""
-    dev = kv.tensors[0].get_device()
-    for name, t, shape, dtype in args:
-        if t is None:
-            continue
-        if t.shape != shape or (dtype is not None and t.dtype != dtype):
-            raise ValueError(f"{name} must be {list(shape)}" + (f" of {dtype}" if dtype else "") +
-                             f", not {list(t.shape)} of {t.dtype}")
-        if not t.is_contiguous() or t.get_device() != dev:
-            raise ValueError(f"{name} must be contiguous and on the cache's device")
+def _tensor_error(name, t, shape, dtype, dev):
+    """What is wrong with a tensor that the library would read out of place: it takes bare pointers."""
+    if t.shape != shape or (dtype is not None and t.dtype != dtype):
+        return ValueError(f"{name} must be {list(shape)}" + (f" of {dtype}" if dtype else "") +
+                          f", not {list(t.shape)} of {t.dtype}")
+    if not t.is_contiguous() or t.get_device() != dev:
+        return ValueError(f"{name} must be contiguous and on the cache's device")
+    return None
+
+
+def _check_tensor(name, t, shape, dtype, dev):
+    if t.shape != shape or (dtype is not None and t.dtype != dtype) or not t.is_contiguous() or t.get_device() != dev:
+        raise _tensor_error(name, t, shape, dtype, dev)
+
+
+def _check_place(ws, dev):
     if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != dev:
         raise ValueError("ws must be a contiguous uint8 tensor on the cache's device")
     if dev < 0 or dev != torch.cuda.current_device():
@@ -303,27 +310,34 @@ def reco_paged_workspace_bytes(op: int, kv: reco_paged_kv) -> int:
 
 
 def paged_workspace(op: int, kv: reco_paged_kv, device="cuda") -> torch.Tensor:
-    """A workspace for a paged call, with its counters zero as the decode needs them before its first use
+    """A workspace for a paged call, with its counters zero as the calls need them before its first use
     (the logits of a call with weights lie behind what a call without needs, and need no fill)."""
     ws = torch.empty(max(reco_paged_workspace_bytes(op, kv), 256), dtype=torch.uint8, device=device)
     ws[:256 if op == RECO_OP_PAGED_EVICT else reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv)].zero_()
     return ws
 
 
-def _paged_decode_args(kv, q, k_new, v_new, lens, out, lse):
-    if (k_new is None) != (v_new is None):
+def _check_paged_decode(kv, q, k_new, v_new, lens, out, lse, ws):
+    dev, dt, qs, new, heads, units, _ = kv.expect
+    if k_new is not None and v_new is not None:
+        _check_tensor("k_new", k_new, new, dt, dev)
+        _check_tensor("v_new", v_new, new, dt, dev)
+    elif k_new is not v_new:
         raise ValueError("k_new and v_new must both be given or both be None")
-    qs, new, dt = (kv.n_layers, kv.B, kv.H_q, kv.d), (kv.n_layers, kv.B, kv.H_kv, kv.d), kv.tensors[0].dtype
-    return [("q", q, qs, dt), ("k_new", k_new, new, dt), ("v_new", v_new, new, dt), ("lens", lens, new[:3], torch.int32),
-            ("out", out, qs, None), ("lse", lse, qs[:3], torch.float32)]
+    _check_tensor("q", q, qs, dt, dev)
+    _check_tensor("lens", lens, units, torch.int32, dev)
+    _check_tensor("out", out, qs, None, dev)
+    if lse is not None:
+        _check_tensor("lse", lse, heads, torch.float32, dev)
+    _check_place(ws, dev)
 
 
 def reco_paged_decode_attn(kv: reco_paged_kv, q, k_new, v_new, lens, scale: float, out, lse, ws, window: int = 0,
                            sinks: int = 0, stream=None):
     """window > 0: a query sees the first `sinks` rows and the latest `window` rows (the new one included)."""
-    _paged_args(kv, ws, _paged_decode_args(kv, q, k_new, v_new, lens, out, lse))
-    _ok(lib().reco_paged_decode_attn(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(lens), float(scale),
-                                     int(window), int(sinks), _ptr(out), _dtype_code(out.dtype), _ptr(lse), _ptr(ws),
+    _check_paged_decode(kv, q, k_new, v_new, lens, out, lse, ws)
+    _ok(lib().reco_paged_decode_attn(ctypes.byref(kv), q.data_ptr(), _ptr(k_new), _ptr(v_new), lens.data_ptr(), scale,
+                                     window, sinks, out.data_ptr(), _dtype_code(out.dtype), _ptr(lse), ws.data_ptr(),
                                      ws.numel(), _stream(stream)))
 
 
@@ -331,22 +345,25 @@ def reco_paged_decode_attn_weights(kv: reco_paged_kv, q, k_new, v_new, lens, sca
                                    window: int = 0, sinks: int = 0, stream=None):
     """reco_paged_decode_attn that also adds each row's attention weight (the mean over the query heads of
     its KV head) to weights [layers, B, H_kv, max_pages * page] float32."""
-    _paged_args(kv, ws, _paged_decode_args(kv, q, k_new, v_new, lens, out, lse) +
-                [("weights", weights, (kv.n_layers, kv.B, kv.H_kv, kv.max_pages * kv.page), torch.float32)])
-    _ok(lib().reco_paged_decode_attn_weights(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(lens),
-                                             float(scale), int(window), int(sinks), _ptr(out), _dtype_code(out.dtype),
-                                             _ptr(lse), _ptr(weights), _ptr(ws), ws.numel(), _stream(stream)))
+    _check_paged_decode(kv, q, k_new, v_new, lens, out, lse, ws)
+    _check_tensor("weights", weights, kv.expect[6], torch.float32, kv.expect[0])
+    _ok(lib().reco_paged_decode_attn_weights(ctypes.byref(kv), q.data_ptr(), _ptr(k_new), _ptr(v_new), lens.data_ptr(),
+                                             scale, window, sinks, out.data_ptr(), _dtype_code(out.dtype), _ptr(lse),
+                                             weights.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def reco_paged_evict(kv: reco_paged_kv, weights, lens, budget, w: int, sinks: int, kept_idx, ws, stream=None):
     """Cuts every unit longer than budget[b] down to it: the first `sinks` rows, the latest `w` rows and the
     rows of the largest weights between them stay, in order."""
-    unit = (kv.n_layers, kv.B, kv.H_kv)
-    rows = unit + (kv.max_pages * kv.page,)
-    _paged_args(kv, ws, [("weights", weights, rows, torch.float32), ("lens", lens, unit, torch.int32),
-                     ("budget", budget, (kv.B,), torch.int32), ("kept_idx", kept_idx, rows, torch.int32)])
-    _ok(lib().reco_paged_evict(ctypes.byref(kv), _ptr(weights), _ptr(lens), _ptr(budget), int(w), int(sinks),
-                               _ptr(kept_idx), _ptr(ws), ws.numel(), _stream(stream)))
+    dev, _, _, _, _, units, rows = kv.expect
+    _check_tensor("weights", weights, rows, torch.float32, dev)
+    _check_tensor("lens", lens, units, torch.int32, dev)
+    _check_tensor("budget", budget, (kv.B,), torch.int32, dev)
+    if kept_idx is not None:
+        _check_tensor("kept_idx", kept_idx, rows, torch.int32, dev)
+    _check_place(ws, dev)
+    _ok(lib().reco_paged_evict(ctypes.byref(kv), weights.data_ptr(), lens.data_ptr(), budget.data_ptr(), w, sinks,
+                               _ptr(kept_idx), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def reco_reflect_penalty(logits, ids, rewards, tau_l=0.4, tau_h=0.8, beta=4.0, beta_out=None,
