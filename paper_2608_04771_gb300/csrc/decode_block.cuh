@@ -306,22 +306,26 @@ template <int D_, int NT_, int HALVES_ = 1> struct Bf16Block {
     __device__ __forceinline__ void store_partial(float *po, int G) const
     {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int q0 = 8 * n + 2 * c, q1 = q0 + 1;
+        for (int n = 0; n < NT; ++n) store_tile(n, po + (size_t)8 * n * D, G - 8 * n);
+    }
+
+    // heads 8 n .. 8 n + 7, of which the first G are there
+    __device__ __forceinline__ void store_tile(int n, float *po, int G) const
+    {
+        const int q0 = 2 * c, q1 = q0 + 1;
 #pragma unroll
-            for (int hh = 0; hh < HALVES; ++hh) {
-                const int d0 = 64 * hh + 8 * g;
-                const float(*v)[4] = &o[n][4 * hh];
-                if (q0 < G) {
-                    float4 *dst = reinterpret_cast<float4 *>(po + (size_t)q0 * D + d0);
-                    dst[0] = make_float4(v[0][0], v[0][2], v[1][0], v[1][2]);
-                    dst[1] = make_float4(v[2][0], v[2][2], v[3][0], v[3][2]);
-                }
-                if (q1 < G) {
-                    float4 *dst = reinterpret_cast<float4 *>(po + (size_t)q1 * D + d0);
-                    dst[0] = make_float4(v[0][1], v[0][3], v[1][1], v[1][3]);
-                    dst[1] = make_float4(v[2][1], v[2][3], v[3][1], v[3][3]);
-                }
+        for (int hh = 0; hh < HALVES; ++hh) {
+            const int d0 = 64 * hh + 8 * g;
+            const float(*v)[4] = &o[n][4 * hh];
+            if (q0 < G) {
+                float4 *dst = reinterpret_cast<float4 *>(po + (size_t)q0 * D + d0);
+                dst[0] = make_float4(v[0][0], v[0][2], v[1][0], v[1][2]);
+                dst[1] = make_float4(v[2][0], v[2][2], v[3][0], v[3][2]);
+            }
+            if (q1 < G) {
+                float4 *dst = reinterpret_cast<float4 *>(po + (size_t)q1 * D + d0);
+                dst[0] = make_float4(v[0][1], v[0][3], v[1][1], v[1][3]);
+                dst[1] = make_float4(v[2][1], v[2][3], v[3][1], v[3][3]);
             }
         }
     }
@@ -567,6 +571,226 @@ template <int D_, int GT_> struct F32Block {
     }
 
     __device__ __forceinline__ void store_partial(float *po, int G) const
+    {
+#pragma unroll
+        for (int g = 0; g < GT; ++g)
+            if (g < G) {
+                float *dst = po + (size_t)g * D + lane * E;
+                if constexpr (E == 4) *reinterpret_cast<float4 *>(dst) = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
+                else *reinterpret_cast<float2 *>(dst) = make_float2(o[g][0], o[g][1]);
+            }
+    }
+};
+
+
+// float32 in blocks of 16 rows, two or four heads a warp: what a warp spends on a block besides its products (the
+// exchanges, the maximum, the vote, the barrier around the probabilities) is latency, and costs the same for
+// 16 rows as F32Block's for eight.  Lane (kq = lane / 8, part = lane % 8) multiplies rows kq, kq + 4, kq + 8 and
+// kq + 12; halving exchanges over the parts leave each (row, head) sum in one lane.
+template <int D_, int GT_> struct F32Wide {
+    static constexpr int D = D_, KB = 16, GM = GT_, GT = GT_, E = D / 32, QE = D / 8;
+    static constexpr int ROW = 4 * D, APP = (2 * ROW / 16 + 31) / 32, SCRATCH = KB * GT;
+    static constexpr bool TENSOR_MAPS = false;
+    using RowIndex = size_t;
+    static constexpr int VPL = GT / 2;  // heads per lane after the exchanges
+    static_assert(GT == 2 || GT == 4, "two or four heads");
+
+    float q[GT][QE], o[GT][E], m[VPL], l[VPL];
+    const float *q_src = nullptr;
+    int nh_src = 0;
+    float *const p_sm;  // [KB][GT] probabilities of the block
+    const int lane;
+
+    __device__ __forceinline__ F32Wide(int lane_, float *scratch) : p_sm(scratch), lane(lane_) {}
+
+    __device__ static __forceinline__ uint32_t chunk(int row, int ch) { return row * ROW + ch * 16; }
+
+    // `rows` rows of K, then of V, each one contiguous copy (none when only the appended row is left)
+    __device__ static __forceinline__ void load(uint32_t dst, uint32_t bar, const CUtensorMap *, const CUtensorMap *,
+                                                const void *K, const void *V, size_t row, int rows, uint64_t policy)
+    {
+        const uint32_t bytes = (uint32_t)max(rows, 0) * ROW;
+        mbar_expect_tx(bar, 2 * bytes);
+        if (bytes == 0) return;
+        bulk_load_hint(dst, static_cast<const char *>(K) + row * ROW, bytes, bar, policy);
+        bulk_load_hint(dst + KB * ROW, static_cast<const char *>(V) + row * ROW, bytes, bar, policy);
+    }
+
+    __device__ __forceinline__ void load_q(const void *qp, long qrow, int nh)
+    {
+        q_src = reinterpret_cast<const float *>(qp) + qrow * D;
+        nh_src = nh;
+    }
+
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+#pragma unroll
+            for (int i = 0; i < QE / 4; ++i) {
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (g < nh_src) x = *reinterpret_cast<const float4 *>(q_src + (long)g * D + 32 * i + 4 * (lane & 7));
+                q[g][4 * i] = x.x;
+                q[g][4 * i + 1] = x.y;
+                q[g][4 * i + 2] = x.z;
+                q[g][4 * i + 3] = x.w;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[g][e] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            m[v] = -INFINITY;
+            l[v] = 0.f;
+        }
+    }
+
+    // head v of this lane; the lane (of row 0) and the value that hold head g
+    __device__ __forceinline__ int head_of(int v) const { return (lane & 1) * VPL + v; }
+    __device__ static __forceinline__ constexpr int lane_of(int g) { return g / VPL; }
+    __device__ static __forceinline__ constexpr int value_of(int g) { return g % VPL; }
+
+    template <int N> __device__ __forceinline__ void halve(float *s, int bit) const
+    {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float send = up ? s[i] : s[i + N];
+            const float keep = up ? s[i + N] : s[i];
+            s[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+        }
+    }
+
+    __device__ __forceinline__ void consume(uint32_t Ks, uint32_t Vs, int kb, int k1, float c2, int h0, int h1, float *lg,
+                                            int cap, int nh)
+    {
+        float s[4 * GT];  // rows kq, kq + 4, kq + 8, kq + 12
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t row = Ks + ((lane >> 3) + 4 * k) * ROW + (lane & 7) * 16;
+#pragma unroll
+            for (int g = 0; g < GT; ++g) s[k * GT + g] = 0.f;
+#pragma unroll
+            for (int i = 0; i < QE / 4; ++i) {
+                const float4 x = lds_f4(row + 128 * i);
+#pragma unroll
+                for (int g = 0; g < GT; ++g) {
+                    float t = s[k * GT + g];
+                    t = fmaf(q[g][4 * i], x.x, t);
+                    t = fmaf(q[g][4 * i + 1], x.y, t);
+                    t = fmaf(q[g][4 * i + 2], x.z, t);
+                    s[k * GT + g] = fmaf(q[g][4 * i + 3], x.w, t);
+                }
+            }
+        }
+        halve<2 * GT>(s, 4);   // lane bit 2: rows + 8
+        halve<GT>(s, 2);       // bit 1: rows + 4
+        halve<GT / 2>(s, 1);   // bit 0: the upper heads
+        const int kk = (lane >> 3) + 2 * (lane & 6);  // this lane's row of the block
+        const int k = kb + kk;
+        const bool seen = k < k1 && (k < h0 || k >= h1);
+        float x[VPL], mb[VPL];
+        bool any = false;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            x[v] = seen ? s[v] * c2 : -INFINITY;
+            if (lg != nullptr && head_of(v) < nh) lg[(size_t)head_of(v) * cap + k] = x[v];
+            mb[v] = x[v];
+#pragma unroll
+            for (int o2 = 2; o2 <= 16; o2 <<= 1) mb[v] = fmaxf(mb[v], __shfl_xor_sync(0xffffffffu, mb[v], o2));
+            any |= mb[v] > m[v] + kLazyLog2;
+        }
+        if (__any_sync(0xffffffffu, any)) {  // lazy rescale, as in the bf16 consumer
+            float al[VPL];
+#pragma unroll
+            for (int v = 0; v < VPL; ++v) {
+                const float mn = mb[v] > m[v] + kLazyLog2 ? mb[v] : m[v];
+                al[v] = mn == m[v] ? 1.f : fast_exp2(m[v] - mn);  // m = -inf gives 0
+                l[v] *= al[v];
+                m[v] = mn;
+            }
+#pragma unroll
+            for (int g = 0; g < GT; ++g) {
+                const float f = __shfl_sync(0xffffffffu, al[value_of(g)], lane_of(g));
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[g][e] *= f;
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            const float p = fast_exp2(x[v] - (m[v] == -INFINITY ? 0.f : m[v]));
+            l[v] += p;
+            p_sm[kk * GT + head_of(v)] = p;
+        }
+        __syncwarp();
+        // a block's products are summed before they join the output (F32Block)
+        float acc[GT][E];
+#pragma unroll
+        for (int r = 0; r < KB; ++r) {
+            float p[GT], y[E];
+            if constexpr (GT == 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(p_sm + r * GT);
+                p[0] = f.x;
+                p[1] = f.y;
+                p[2] = f.z;
+                p[3] = f.w;
+            } else {
+                const float2 f = *reinterpret_cast<const float2 *>(p_sm + r * GT);
+                p[0] = f.x;
+                p[1] = f.y;
+            }
+            if constexpr (E == 4) {
+                const float4 f = lds_f4(Vs + r * ROW + lane * 16);
+                y[0] = f.x;
+                y[1] = f.y;
+                y[2] = f.z;
+                y[3] = f.w;
+            } else {
+                const float2 f = lds_f2(Vs + r * ROW + lane * 8);
+                y[0] = f.x;
+                y[1] = f.y;
+            }
+#pragma unroll
+            for (int g = 0; g < GT; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[g][e] = r ? fmaf(p[g], y[e], acc[g][e]) : p[g] * y[e];
+        }
+#pragma unroll
+        for (int g = 0; g < GT; ++g)
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[g][e] += acc[g][e];
+        __syncwarp();  // the probabilities have been read
+    }
+
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v)
+#pragma unroll
+            for (int o2 = 2; o2 <= 16; o2 <<= 1) l[v] += __shfl_xor_sync(0xffffffffu, l[v], o2);
+    }
+
+    template <typename F> __device__ __forceinline__ void each_lse(int G, F f) const
+    {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v)
+            if (lane < 2 && head_of(v) < G) f(head_of(v), m[v], l[v]);
+    }
+
+    __device__ __forceinline__ void store(void *out, bool bf16, long qrow0, int G) const
+    {
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+            const float lg = __shfl_sync(0xffffffffu, l[value_of(g)], lane_of(g));
+            if (g < G) {
+                const float inv = lg > 0.f ? 1.f / lg : 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) store_out(out, bf16, (qrow0 + g) * D + lane * E + e, o[g][e] * inv);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void store_tile(int, float *po, int G) const
     {
 #pragma unroll
         for (int g = 0; g < GT; ++g)

@@ -28,11 +28,8 @@
 
 namespace reco {
 
-constexpr int kPagedWarps = 8;               // computing warps per CTA
-constexpr int kPagedThreads = 32 * kPagedWarps;  // and their threads; 32 more copy
 constexpr int kRingBytes = 24 * 8192;         // ring of a CTA
 constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
-constexpr int kStageBytes = 8192;            // a block of K and V rows at d = 128 (half of it, and twice as many, at d = 64)
 constexpr int kMinBlocks = 16;               // blocks per working CTA (fewer CTAs rather than less)
 constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
 constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
@@ -161,7 +158,8 @@ template <int KB, int NS> __device__ __forceinline__ bool next_whole(const Paged
     return false;
 }
 
-__device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;" ::"n"(kPagedThreads) : "memory"); }
+// Barrier of the computing warps.
+template <int THREADS> __device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 
 __device__ __forceinline__ void put_lse(const PagedArgs &a, size_t row, float l2)
 {
@@ -182,24 +180,28 @@ __device__ __forceinline__ void store_out4(const PagedArgs &a, size_t i, float4 
 }
 
 // Ring, then [warp][head][D] floats: the warps' outputs as they join (and, until then, each warp's scratch).
-template <class Block> constexpr int paged_smem()
+template <class Block, int NW> constexpr int paged_smem()
 {
-    return 1024 + kRingBytes + kPagedWarps * Block::GM * Block::D * 4;
+    return 1024 + kRingBytes + NW * (Block::GM < 8 ? Block::GM : 8) * Block::D * 4;
 }
 
-template <class Block, int HS>
-__global__ void __launch_bounds__(kPagedThreads + 32, 1)
+// NW computing warps in NS = NW / HS streams of HS warps: each takes a part of a unit's query heads.
+template <class Block, int HS, int NW>
+__global__ void __launch_bounds__(32 * NW + 32, 1)
     paged_decode(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, PagedArgs a)
 {
     constexpr int D = Block::D, KB = Block::KB, GM = Block::GM;
-    constexpr int STAGE = kStageBytes * D / 128, STAGES = kRingBytes / STAGE;
-    constexpr int NW = kPagedWarps, NS = NW / HS, S = STAGES / NS;
-    constexpr int NT = kPagedThreads + 32, CPR = Block::ROW / 16;
-    static_assert(Block::SCRATCH <= GM * D, "a warp's scratch lies in its part of the join buffer");
+    constexpr int STAGE = 2 * KB * Block::ROW, STAGES = kRingBytes / STAGE;  // a stage holds a block of K and V rows
+    constexpr int NS = NW / HS, S = STAGES / NS;
+    constexpr int JH = GM < 8 ? GM : 8;  // heads that join at a time
+    constexpr int NC = 32 * NW, NT = NC + 32, CPR = Block::ROW / 16;
+    static_assert(NS * HS == NW && S * NS == STAGES, "equal streams");
+    static_assert(GM % JH == 0 && (GM == JH || HS == 1), "heads join in whole tiles");
+    static_assert(Block::SCRATCH <= JH * D, "a warp's scratch lies in its part of the join buffer");
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
     __shared__ int sm_row[STAGES];  // pool row of a stage's block, -1: none
-    __shared__ float2 sm_ml[2][NW][GM];   // joins: the warps' (max, sum), a sum of -1 for a piece in error
+    __shared__ float2 sm_ml[NW][GM];      // joins: the warps' (max, sum), a sum of -1 for a piece in error
     __shared__ int sm_scan[4][NT / 32];
     __shared__ int sm_cut[2][4];  // unit, its first block (or CTA), blocks and rows, at the start and the end of the range
     __shared__ int sm_flags, sm_old;
@@ -221,19 +223,41 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
 
     // ---- plan, the same in every CTA
     const int seg = (P + NT - 1) / NT, u_lo = min(P, tid * seg), u_hi = min(P, u_lo + seg);
-    int my_b = 0, my_max = 0, my_ne = 0, le0 = 0;
-#pragma unroll 4
-    for (int u = u_lo; u < u_hi; ++u) {
-        const int L = __ldcg(a.lens + u);
+    int le0 = 0;  // with a unit per thread at most: its rows; with more, the rows of all lie in the (still idle) ring
+    int *sm_le = reinterpret_cast<int *>(smem_raw + (ring0 - raw0));
+    const bool staged = seg > 1 && P <= kRingBytes / 4;
+    auto look = [&](int L) {
         if (blockIdx.x == 0 && !unit_ok(L, a.cap, a.append))
             raise_error(a.err, (a.append && L == a.cap) ? ERR_ROOM : ERR_LEN);
-        const int le = rows_of(a, L), nb = blocks_of<KB>(a, le);
-        if (u == u_lo) le0 = le;
+        return rows_of(a, L);
+    };
+    if (seg == 1) {
+        if (tid < P) le0 = look(__ldcg(a.lens + tid));
+    } else {
+        for (int u0 = tid; u0 < P; u0 += 8 * NT) {  // eight loads in flight
+            int L[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) L[k] = u0 + k * NT < P ? __ldcg(a.lens + u0 + k * NT) : 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int u = u0 + k * NT;
+                if (u < P) {
+                    const int le = look(L[k]);
+                    if (staged) sm_le[u] = le;
+                }
+            }
+        }
+        __syncthreads();
+    }
+    // rows of a unit of this thread's share
+    auto le_of = [&](int u) { return seg == 1 ? le0 : (staged ? sm_le[u] : rows_of(a, __ldcg(a.lens + u))); };
+    int my_b = 0, my_max = 0, my_ne = 0;
+    for (int u = u_lo; u < u_hi; ++u) {
+        const int nb = blocks_of<KB>(a, le_of(u));
         my_b += nb;
         my_max = max(my_max, nb);
         my_ne += nb > 0;
     }
-    auto rows_again = [&](int u) { return u == u_lo ? le0 : rows_of(a, __ldcg(a.lens + u)); };
     my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
     my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
     const int warp_b = __reduce_add_sync(0xffffffffu, (unsigned)my_b);
@@ -291,13 +315,13 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             const int div = max(1, j0 - j), room = max(1, grid - n_ne);
             per = j < 4 ? (max_nb + div - 1) / div : (NB + room - 1) / room;
             int my_k = 0;
-            for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, rows_again(u)) + per - 1) / per;
+            for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, le_of(u)) + per - 1) / per;
             if (j > 0) __syncthreads();  // the last scan has been read
             at = scan(my_k, total);
             if (total <= grid) {
                 if (c >= at && c < at + my_k) {
                     for (int u = u_lo; u < u_hi; ++u) {
-                        const int le = rows_again(u), nb = blocks_of<KB>(a, le), k = (nb + per - 1) / per;
+                        const int le = le_of(u), nb = blocks_of<KB>(a, le), k = (nb + per - 1) / per;
                         if (c < at + k) {
                             sm_cut[0][0] = u;
                             sm_cut[0][1] = at;
@@ -335,7 +359,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             if (t >= before && t < before + my_b) {  // in one of this thread's units
                 int ub = before, u = u_lo, nb = 0, le = 0;
                 for (; u < u_hi; ++u) {
-                    le = rows_again(u);
+                    le = le_of(u);
                     nb = blocks_of<KB>(a, le);
                     if (t < ub + nb) break;
                     ub += nb;
@@ -366,6 +390,9 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     }
     start.b = start.begin;
 
+    // the first block of a piece that falls to stream s (block x of the CTA's range falls to stream x % NS)
+    auto first_of = [](int s, int at) { return (int)((unsigned)(s + NS - at % NS) % (unsigned)NS); };
+
     if (wid == NW) {
         // ---- copies: lane s feeds stream s
         if (lane < NS) {
@@ -379,7 +406,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             auto first_row = [&]() { return KB * (i + (i >= p.sg.head ? p.sg.gap : 0)); };
             auto begin_piece = [&]() {
                 while (whole ? next_whole<KB, NS>(a, w, p) : next_piece<KB>(a, w, p)) {
-                    i = whole ? 0 : p.lo + ((lane - p.at) & (NS - 1));
+                    i = whole ? 0 : p.lo + first_of(lane, p.at);
                     if (i >= p.hi) continue;
                     pg = pages_of(a, p.u);
                     e = page_entry(a, pg, first_row());
@@ -434,7 +461,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
     // ---- computing warps: stream `st`, heads [hp * GS, hp * GS + nh)
     const int st = wid % NS, hp = wid / NS;
     const int nh = max(0, min(GS, G - hp * GS));
-    Block blk(lane, join + wid * GM * D);
+    Block blk(lane, join + wid * JH * D);
     auto head_row = [&](int u) { return (size_t)(u / a.Hkv) * a.Hq + (size_t)(u % a.Hkv) * G; };
     // units without rows: zeros, lse = -inf
     for (int u = n_ne < P ? c * NW + wid : P; u < P; u += grid * NW) {
@@ -465,13 +492,12 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         return true;
     };
     bool have = begin_piece();
-    int parity = 0;
     while (have) {
         bool bad = false;
         const size_t q0 = head_row(p.u);
         const int Lapp = a.append && p.hi == p.nb ? p.le - 1 : -1;  // the new row, in its unit's last block
         float *lg = a.logits ? a.logits + (q0 + hp * GS) * a.cap : nullptr;
-        for (int i = whole ? 0 : p.lo + ((st - p.at) & (NS - 1)); i < p.hi; i += whole ? 1 : NS) {
+        for (int i = whole ? 0 : p.lo + first_of(st, p.at); i < p.hi; i += whole ? 1 : NS) {
             const int at = st * S + (int)slot;
             const bool app = Lapp >= 0 && i == p.nb - 1;
             uint4 rows[Block::APP];  // this lane's chunks of the new rows, K's then V's
@@ -512,6 +538,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
                             if (t < 2 * CPR) sts_u4((t < CPR ? Ks : Vs) + Block::chunk(Lapp - kb, t % CPR), rows[x]);
                         }
                     }
+                    fence_async_shared();  // these writes come before the copy that fills the stage next
                     __syncwarp();
                 }
                 blk.consume(Ks, Vs, kb, p.le, a.c2, p.sg.h0, p.sg.h1, lg, a.cap, nh);
@@ -524,7 +551,6 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
                     }
                     if (lane == 0 && a.weights) a.weights[(size_t)p.u * a.cap + Lapp] = 0.f;
                 }
-                fence_async_shared();  // the stage's reads and writes come before the copy that fills it next
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&empty[at]));
             }
@@ -553,50 +579,55 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
             continue;
         }
 
-        // ---- join: one barrier after the warps' results are in shared memory, one after they have been read
-        blk.store_partial(join + wid * GM * D, nh);
-        blk.each_lse(nh, [&](int q, float m, float l) { sm_ml[parity][wid][q] = make_float2(m, bad ? -1.f : l); });
+        // ---- join, eight heads at a time: one barrier after the warps' results are in shared memory, one after
+        // they have been read
         const Piece d = p;  // done
-        have = begin_piece();  // the next piece's queries load meanwhile
-        bar_compute();
         const bool all = d.lo == 0 && d.hi == d.nb;
         const int out_slot = 2 * c + (d.lo == 0 ? 1 : 0);
-        for (int x = tid; x < G * D / 4; x += kPagedThreads) {
-            const int q = x / (D / 4), d4 = x % (D / 4), part = HS == 1 ? 0 : q / GS, ql = q - part * GS;
-            float M = -INFINITY, Ls = 0.f;
-            bool err = false;
-            float2 ml[NS];
+        blk.each_lse(nh, [&](int q, float m, float l) { sm_ml[wid][q] = make_float2(m, bad ? -1.f : l); });
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                ml[s] = sm_ml[parity][part * NS + s][ql];
-                M = fmaxf(M, ml[s].x);
-                err |= ml[s].y < 0.f;
-            }
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (!err && M != -INFINITY) {
+        for (int tile = 0; tile < GM / JH; ++tile) {
+            blk.store_tile(tile, join + wid * JH * D, nh - tile * JH);
+            if (tile == GM / JH - 1) have = begin_piece();  // the next piece's queries load meanwhile
+            bar_compute<NC>();
+            const int tile0 = tile * JH, heads = HS == 1 ? min(JH, G - tile0) : G;
+            for (int x = tid; x < heads * D / 4; x += NC) {
+                const int q = x / (D / 4), d4 = x % (D / 4), part = HS == 1 ? 0 : q / GS, ql = q - part * GS;
+                float M = -INFINITY, Ls = 0.f;
+                bool err = false;
+                float2 ml[NS];
 #pragma unroll
                 for (int s = 0; s < NS; ++s) {
-                    const float f = fast_exp2(ml[s].x - M);
-                    const float4 v = *reinterpret_cast<const float4 *>(join + ((part * NS + s) * GM + ql) * D + 4 * d4);
-                    Ls += ml[s].y * f;
-                    o.x += v.x * f;
-                    o.y += v.y * f;
-                    o.z += v.z * f;
-                    o.w += v.w * f;
+                    ml[s] = sm_ml[part * NS + s][tile0 + ql];
+                    M = fmaxf(M, ml[s].x);
+                    err |= ml[s].y < 0.f;
+                }
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (!err && M != -INFINITY) {
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const float f = fast_exp2(ml[s].x - M);
+                        const float4 v = *reinterpret_cast<const float4 *>(join + ((part * NS + s) * JH + ql) * D + 4 * d4);
+                        Ls += ml[s].y * f;
+                        o.x += v.x * f;
+                        o.y += v.y * f;
+                        o.z += v.z * f;
+                        o.w += v.w * f;
+                    }
+                }
+                const int head = tile0 + q;
+                if (all) {
+                    const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+                    store_out4(a, (q0 + head) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+                    if (d4 == 0) put_lse(a, q0 + head, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
+                } else {
+                    *reinterpret_cast<float4 *>(a.part_o + ((size_t)out_slot * G + head) * D + 4 * d4) = o;
+                    if (d4 == 0)
+                        reinterpret_cast<float2 *>(a.part_ml)[(size_t)out_slot * G + head] = make_float2(M, err ? -1.f : Ls);
                 }
             }
-            if (all) {
-                const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
-                store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-                if (d4 == 0) put_lse(a, q0 + q, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
-            } else {
-                *reinterpret_cast<float4 *>(a.part_o + ((size_t)out_slot * G + q) * D + 4 * d4) = o;
-                if (d4 == 0)
-                    reinterpret_cast<float2 *>(a.part_ml)[(size_t)out_slot * G + q] = make_float2(M, err ? -1.f : Ls);
-            }
+            bar_compute<NC>();
         }
-        bar_compute();
-        parity ^= 1;
         if (all) continue;
 
         // ---- a unit cut between CTAs: publish; the last one joins the pieces
@@ -612,10 +643,10 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         if (tid == 0) {
             sm_old = atom_add_acq_rel(&a.counters[2 + d.u], 1);
         }
-        bar_compute();
+        bar_compute<NC>();
         if (sm_old == pieces - 1) {
             if (tid == 0) a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
-            for (int x = tid; x < G * D / 4; x += kPagedThreads) {
+            for (int x = tid; x < G * D / 4; x += NC) {
                 const int q = x / (D / 4), d4 = x % (D / 4);
                 auto slot_of = [&](int s) { return (size_t)(2 * (c1 - 1 + s) + (s == 0 ? 1 : 0)) * G + q; };
                 // four pieces at a time, their loads in flight together, with a running maximum
@@ -672,7 +703,7 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
 
     // ---- the last CTA to finish advances the lengths (every plan has been read by then) and leaves the
     // counters zero, as it found them
-    bar_compute();
+    bar_compute<NC>();
     if (tid == 0) {
         const unsigned f = (unsigned)sm_flags;
         const unsigned long long add = (1ull << 32) | (f & 1u ? 1ull : 0ull) | (f & 2u ? 1ull << 16 : 0ull);
@@ -680,14 +711,14 @@ __global__ void __launch_bounds__(kPagedThreads + 32, 1)
         const unsigned seen = (unsigned)(old + add);
         sm_old = (int)(old >> 32) == (int)gridDim.x - 1 ? 1 | (seen & 0xffffu ? 2 : 0) | (seen >> 16 ? 4 : 0) : 0;
     }
-    bar_compute();
+    bar_compute<NC>();
     const int last = sm_old;
     if (last == 0) return;
     if (last & 2) {  // tickets of units whose pieces stopped early may still count
-        for (int u = tid; u < P; u += kPagedThreads) a.counters[2 + u] = 0;
+        for (int u = tid; u < P; u += NC) a.counters[2 + u] = 0;
     } else if (a.append) {
 #pragma unroll 4
-        for (int u = tid; u < P; u += kPagedThreads) {
+        for (int u = tid; u < P; u += NC) {
             const int L = __ldcg(a.lens + u);
             bool ok = unit_ok(L, a.cap, a.append);
             if (ok && (last & 4)) {  // units whose table names no page for a row in sight keep their length
@@ -763,20 +794,23 @@ __global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__r
 typedef void (*PagedKernel)(CUtensorMap, CUtensorMap, PagedArgs);
 struct PagedLaunch {
     PagedKernel fn;
-    int smem;
+    int smem, threads;
 };
-template <class Block, int HS> static PagedLaunch with()
+template <class Block, int HS, int NW> static PagedLaunch with()
 {
-    static_assert(paged_smem<Block>() + 2048 <= 227 * 1024, "shared memory of a CTA (2 KB of it static)");
-    return PagedLaunch{paged_decode<Block, HS>, paged_smem<Block>()};
+    static_assert(paged_smem<Block, NW>() + 2048 <= 227 * 1024, "shared memory of a CTA (2 KB of it static)");
+    return PagedLaunch{paged_decode<Block, HS, NW>, paged_smem<Block, NW>(), 32 * NW + 32};
 }
 template <int D> static PagedLaunch paged_kernel(bool f32, int G)
 {
-    if (!f32) return G > 8 ? with<Bf16Block<D, 1>, 2>() : with<Bf16Block<D, 1>, 1>();
-    // four heads per warp at most: their queries take D / 8 registers each
-    if (G > 8) return with<F32Block<D, 4>, 4>();
-    if (G > 4) return with<F32Block<D, 4>, 2>();
-    return G > 2 ? with<F32Block<D, 4>, 1>() : with<F32Block<D, 2>, 1>();
+    if (!f32) return G > 8 ? with<Bf16Block<D, 2>, 1, 8>() : with<Bf16Block<D, 1>, 1, 8>();
+    // float32: two heads per warp, whose queries and sums leave registers for twelve warps (plain FMAs wait for
+    // each other: 224 units of 1150 rows, 6 heads, eight warps of four heads 82 us, XX)
+    if (G > 12) return with<F32Wide<D, 4>, 4, 8>();
+    if (G > 8) return with<F32Wide<D, 2>, 6, 12>();
+    if (G > 6) return with<F32Wide<D, 2>, 4, 12>();
+    if (G > 4) return with<F32Wide<D, 2>, 3, 12>();
+    return G > 2 ? with<F32Wide<D, 2>, 2, 12>() : with<F32Wide<D, 2>, 1, 12>();
 }
 
 cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new,
@@ -824,9 +858,9 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     cudaError_t e = allow_smem((const void *)k.fn, k.smem);
     if (e != cudaSuccess) return e;
     // no more CTAs than the cache can hold work for
-    const long long most = (long long)units * ((cap + (f32 ? 7 : 15)) / (f32 ? 8 : 16));
+    const long long most = (long long)units * ((cap + 15) / 16);
     const int grid = (int)std::min<long long>(std::min(device_sm_count(), kPagedMaxGrid), std::max<long long>(units, most / kMinBlocks));
-    e = launch_pdl(k.fn, dim3(grid), dim3(kPagedThreads + 32), k.smem, s, mk, mv, a);
+    e = launch_pdl(k.fn, dim3(grid), dim3(k.threads), k.smem, s, mk, mv, a);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights) return e;
     // CTAs over a unit's rows: enough that all units together fill the GPU four times over, never more than
     // the rows of a unit need (lengths are not known here, and CTAs without rows cost time too)
