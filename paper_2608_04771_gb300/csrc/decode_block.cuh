@@ -74,6 +74,11 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int x)
 // Byte offset of 16-byte chunk ch (0..7) of row rr inside a 128B-swizzled 16-row box.
 __device__ __forceinline__ uint32_t swz(int rr, int ch) { return rr * 128 + ((ch ^ (rr & 7)) << 4); }
 
+// Where row k of a block of 16 lies among a head's 16 logits: as the bf16 product leaves them, four to a lane (rows
+// 2 c, 2 c + 1, 2 c + 8, 2 c + 9), so that a warp stores a block of all its heads in whole lines (the 7B-class stack
+// of 4K rows, calls with weights, from 8-byte stores a head apart: 345 -> 342 us).
+__host__ __device__ constexpr int logit_place(int k) { return 4 * ((k & 7) >> 1) + 2 * (k >> 3) + (k & 1); }
+
 // A block consumer holds one item's queries, running (max, sum) and output in a warp's registers
 // and takes the item's keys in blocks of KB rows from the warp's ring.  It says how a block is
 // copied (load), where a 16-byte chunk of a row lies in a stage (chunk), and how results leave.
@@ -170,10 +175,10 @@ template <int D_, int NT_, int HALVES_ = 1> struct Bf16Block {
         }
     }
 
-    // The block of rows kb, kb + 1, ... below k1, rows [h0, h1) out of sight.  `lg`: or nullptr, where the
-    // base-2 logits of head 0 go (those of the next of nh heads `cap` floats on).
+    // The block of rows kb, kb + 1, ... below k1, rows [h0, h1) out of sight.  `lg`: or nullptr, where the block's
+    // base-2 logits go: 16 floats per head, of nh, in the order of logit_place.
     __device__ __forceinline__ void consume(uint32_t Ks, uint32_t Vs, int kb, int k1, float c2, int h0 = 0, int h1 = 0,
-                                            float *lg = nullptr, int cap = 0, int nh = 0)
+                                            float *lg = nullptr, int nh = 0)
     {
         // four accumulators (keys 0-7 / 8-15, even / odd k-steps): dependent MMA chains
         // of D/32 instead of D/16
@@ -203,11 +208,8 @@ template <int D_, int NT_, int HALVES_ = 1> struct Bf16Block {
             const float x1 = seen(kA + 1) ? (s0[2 * n + 1] + t0[2 * n + 1]) * c2 : -INFINITY;
             const float x2 = seen(kB) ? (s1[2 * n] + t1[2 * n]) * c2 : -INFINITY;
             const float x3 = seen(kB + 1) ? (s1[2 * n + 1] + t1[2 * n + 1]) * c2 : -INFINITY;
-            if (lg != nullptr && g + 8 * n < nh) {
-                float2 *dst = reinterpret_cast<float2 *>(lg + (size_t)(g + 8 * n) * cap + kA);
-                dst[0] = make_float2(x0, x1);
-                dst[4] = make_float2(x2, x3);
-            }
+            if (lg != nullptr && g + 8 * n < nh)
+                *reinterpret_cast<float4 *>(lg + 16 * (g + 8 * n) + 4 * c) = make_float4(x0, x1, x2, x3);
             float mb = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
             mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 1));
             mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 2));
@@ -423,8 +425,7 @@ template <int D_, int GT_> struct F32Block {
         }
     }
 
-    __device__ __forceinline__ void consume(uint32_t Ks, uint32_t Vs, int kb, int k1, float c2, int h0 = 0, int h1 = 0,
-                                            float *lg = nullptr, int cap = 0, int nh = 0)
+    __device__ __forceinline__ void consume(uint32_t Ks, uint32_t Vs, int kb, int k1, float c2)
     {
         float s[2 * GT];  // keys kq, then kq + 4
 #pragma unroll
@@ -458,9 +459,7 @@ template <int D_, int GT_> struct F32Block {
         bool any = false;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const int k = kb + kk;
-            x[v] = k < k1 && (k < h0 || k >= h1) ? s[v] * c2 : -INFINITY;
-            if (lg != nullptr && head_of(v) < nh) lg[(size_t)head_of(v) * cap + k] = x[v];
+            x[v] = kb + kk < k1 ? s[v] * c2 : -INFINITY;
             mb[v] = x[v];
 #pragma unroll
             for (int o2 = 4; o2 <= 16; o2 <<= 1) mb[v] = fmaxf(mb[v], __shfl_xor_sync(0xffffffffu, mb[v], o2));
@@ -662,7 +661,7 @@ template <int D_, int GT_> struct F32Wide {
     }
 
     __device__ __forceinline__ void consume(uint32_t Ks, uint32_t Vs, int kb, int k1, float c2, int h0, int h1, float *lg,
-                                            int cap, int nh)
+                                            int nh)
     {
         float s[4 * GT];  // rows kq, kq + 4, kq + 8, kq + 12
 #pragma unroll
@@ -694,7 +693,7 @@ template <int D_, int GT_> struct F32Wide {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
             x[v] = seen ? s[v] * c2 : -INFINITY;
-            if (lg != nullptr && head_of(v) < nh) lg[(size_t)head_of(v) * cap + k] = x[v];
+            if (lg != nullptr && head_of(v) < nh) lg[16 * head_of(v) + logit_place(kk)] = x[v];
             mb[v] = x[v];
 #pragma unroll
             for (int o2 = 2; o2 <= 16; o2 <<= 1) mb[v] = fmaxf(mb[v], __shfl_xor_sync(0xffffffffu, mb[v], o2));

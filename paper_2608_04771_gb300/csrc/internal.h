@@ -65,10 +65,11 @@ struct DecodeWs {
 // normalisers and logits.
 struct PagedDecodeWs {
     int32_t *counters;  // [2 + units]: [0] stops and errors, [1] CTAs done, [2 + u] tickets
+    int32_t *cuts;      // [2 + CTAs]: calls with weights: the units cut between CTAs
     float *part_ml;     // [2 * CTAs][G][2]   (m log2, l)
     float *part_o;      // [2 * CTAs][G][d]   unnormalised output
     float *lse2;    // [n_layers * B * H_q]         log2 of the softmax sums
-    float *logits;  // [n_layers * B * H_q][cap]    scale * log2(e) * q . k, rows a multiple of 16 floats
+    float *logits;  // [units][cap / 16][G][16]     scale * log2(e) * q . k of a block of 16 rows
     size_t bytes;
 };
 

@@ -20,7 +20,8 @@
 // are the unit's list, in which everything above counts; a block that a border crosses masks its rows.
 //
 // A call with weights has the kernel leave its logits (4 G bytes a row, against 4 d bytes of K and V in
-// bf16) in the workspace; paged_weights turns them into weights once the units' log-sum-exps are known.
+// bf16) in the workspace.  A unit that one CTA or warp sees through turns them into weights there, while they are
+// still in L2 and the copies of the next unit run; paged_weights does the rest, the units cut between CTAs.
 #include <algorithm>
 
 #include "decode_block.cuh"
@@ -30,6 +31,7 @@ namespace reco {
 
 constexpr int kRingBytes = 24 * 8192;         // ring of a CTA
 constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
+constexpr int kWeightWarps = 3;              // warps that turn the logits of finished units into weights
 constexpr int kMinBlocks = 16;               // blocks per working CTA (fewer CTAs rather than less)
 constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
 constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
@@ -46,6 +48,7 @@ PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void
     const size_t G = kv.H_q / kv.H_kv;
     PagedDecodeWs ws;
     ws.counters = (int32_t *)take((2 + units) * 4);
+    ws.cuts = (int32_t *)take((2 + kPagedMaxGrid) * 4);
     ws.part_ml = (float *)take(2 * kPagedMaxGrid * G * 2 * 4);
     ws.part_o = (float *)take(2 * kPagedMaxGrid * G * kv.d * 4);
     ws.lse2 = weights ? (float *)take(heads * 4) : nullptr;
@@ -61,11 +64,12 @@ struct PagedArgs {
     int32_t *lens;
     void *out;
     float *lse;      // or nullptr
-    float *lse2;     // or nullptr: log2 of the softmax sums
-    float *logits;   // or nullptr: [query head][cap] base-2 logits of the rows seen
+    float *lse2;     // with logits: log2 of the softmax sums of the units that are cut between CTAs
+    float *logits;   // or nullptr: [unit][cap / 16][G][16] base-2 logits of the rows seen (logit_place)
     float *weights;  // with logits: the running sums; an appended row's starts at zero
     int32_t *counters;  // [0] warps that stopped and units in error, [1] CTAs done, [2 + u] tickets
     float *part_ml, *part_o;
+    int32_t *cuts;  // units cut between CTAs: [0] counted, [1] their number once the launch is done, [2 ...] the units
     int units, B, Hq, Hkv, G, cap, n_pages, max_pages, shift, append, out_bf16, window, sinks;
     float c2;  // scale * log2(e)
     unsigned *err;
@@ -158,13 +162,14 @@ template <int KB, int NS> __device__ __forceinline__ bool next_whole(const Paged
     return false;
 }
 
+// Barrier of the warps of a stream (one barrier per stream).
+template <int THREADS> __device__ __forceinline__ void bar_stream(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
 // Barrier of the computing warps.
 template <int THREADS> __device__ __forceinline__ void bar_compute() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 
 __device__ __forceinline__ void put_lse(const PagedArgs &a, size_t row, float l2)
 {
     if (a.lse) a.lse[row] = l2 * kLn2;
-    if (a.lse2) a.lse2[row] = l2;
 }
 
 __device__ __forceinline__ void store_out4(const PagedArgs &a, size_t i, float4 v)
@@ -179,6 +184,52 @@ __device__ __forceinline__ void store_out4(const PagedArgs &a, size_t i, float4 
     }
 }
 
+// weights[j] += (1/G) sum_g 2^(logit_g[j] - z_g) for the rows in sight of a unit of n rows, by `step` threads of
+// which this is number `from`, the loads of GB heads in flight.  A thread takes four rows of a block at a time, as
+// they lie among the logits: rows 2 c, 2 c + 1, 2 c + 8 and 2 c + 9 (logit_place).
+template <int GB>
+__device__ __forceinline__ void add_weights(const float *logits, const float *z, float *weights, int G, int n, int window,
+                                            int sinks, int from, int step)
+{
+    const int start = window > 0 && n > window ? n - window : 0, head = min(sinks, start);
+    const float inv = 1.f / (float)G;
+    auto seen = [&](int j) { return j < n && (j < head || j >= start); };
+    for (int i = from; 16 * (i >> 2) < n; i += step) {
+        const int k = 16 * (i >> 2), j0 = k + 2 * (i & 3), j1 = j0 + 8;
+        if (k >= head && k + 16 <= start) continue;  // a block out of sight
+        const float *src = logits + (size_t)k * G + 4 * (i & 3);
+        float2 *w0 = reinterpret_cast<float2 *>(weights + j0), *w1 = reinterpret_cast<float2 *>(weights + j1);
+        const float2 a = *w0, b = *w1;
+        float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int g0 = 0; g0 < G; g0 += GB) {
+            float4 x[GB];
+#pragma unroll
+            for (int h = 0; h < GB; ++h)
+                x[h] = g0 + h < G ? __ldcg(reinterpret_cast<const float4 *>(src + 16 * (g0 + h))) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int h = 0; h < GB; ++h) {
+                const float zh = g0 + h < G ? z[g0 + h] : INFINITY;  // (2^-inf is 0)
+                if (zh == -INFINITY) continue;
+                p.x += fast_exp2(x[h].x - zh);
+                p.y += fast_exp2(x[h].y - zh);
+                p.z += fast_exp2(x[h].z - zh);
+                p.w += fast_exp2(x[h].w - zh);
+            }
+        }
+        const float2 s0 = make_float2(fmaf(p.x, inv, a.x), fmaf(p.y, inv, a.y));
+        const float2 s1 = make_float2(fmaf(p.z, inv, b.x), fmaf(p.w, inv, b.y));
+        if (k + 16 <= n && (k + 16 <= head || k >= start)) {
+            *w0 = s0;
+            *w1 = s1;
+        } else {
+            if (seen(j0)) w0->x = s0.x;
+            if (seen(j0 + 1)) w0->y = s0.y;
+            if (seen(j1)) w1->x = s1.x;
+            if (seen(j1 + 1)) w1->y = s1.y;
+        }
+    }
+}
+
 // Ring, then [warp][head][D] floats: the warps' outputs as they join (and, until then, each warp's scratch).
 template <class Block, int NW> constexpr int paged_smem()
 {
@@ -187,20 +238,24 @@ template <class Block, int NW> constexpr int paged_smem()
 
 // NW computing warps in NS = NW / HS streams of HS warps: each takes a part of a unit's query heads.
 template <class Block, int HS, int NW>
-__global__ void __launch_bounds__(32 * NW + 32, 1)
+__global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
     paged_decode(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, PagedArgs a)
 {
     constexpr int D = Block::D, KB = Block::KB, GM = Block::GM;
     constexpr int STAGE = 2 * KB * Block::ROW, STAGES = kRingBytes / STAGE;  // a stage holds a block of K and V rows
     constexpr int NS = NW / HS, S = STAGES / NS;
     constexpr int JH = GM < 8 ? GM : 8;  // heads that join at a time
-    constexpr int NC = 32 * NW, NT = NC + 32, CPR = Block::ROW / 16;
+    constexpr int NC = 32 * NW, NT = NC + 32 * (1 + kWeightWarps), CPR = Block::ROW / 16;
     static_assert(NS * HS == NW && S * NS == STAGES, "equal streams");
     static_assert(GM % JH == 0 && (GM == JH || HS == 1), "heads join in whole tiles");
-    static_assert(Block::SCRATCH <= JH * D, "a warp's scratch lies in its part of the join buffer");
+    static_assert(Block::SCRATCH <= JH * D - 16, "a warp's scratch lies in its part of the join buffer");
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
     __shared__ int sm_row[STAGES];  // pool row of a stage's block, -1: none
+    // calls with weights: units that are done, for the weight warps (log2 of the sums; unit and rows, -1: no more)
+    __shared__ __align__(8) uint64_t job_full[2], job_empty[2];
+    __shared__ float sm_lse[2][16];
+    __shared__ int2 sm_job[2];
     __shared__ float2 sm_ml[NW][GM];      // joins: the warps' (max, sum), a sum of -1 for a piece in error
     __shared__ int sm_scan[4][NT / 32];
     __shared__ int sm_cut[2][4];  // unit, its first block (or CTA), blocks and rows, at the start and the end of the range
@@ -218,7 +273,14 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
         mbar_init(smem_addr(&empty[tid]), HS);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (tid == 0) sm_flags = 0;
+    if (tid == 0) {
+        sm_flags = 0;
+        for (int k = 0; k < 2; ++k) {
+            mbar_init(smem_addr(&job_full[k]), 1);
+            mbar_init(smem_addr(&job_empty[k]), kWeightWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     wait_prior_grid();  // lens, the table, q and the new rows may come from the previous kernels
 
     // ---- plan, the same in every CTA
@@ -458,6 +520,25 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
         return;
     }
 
+    if (wid > NW) {
+        // ---- weights of units that the CTA sees through, while the computing warps go on with the next
+        if (a.logits == nullptr || split || whole) return;
+        for (int k = 0;; ++k) {
+            const int slot = k & 1;
+            if (!mbar_wait_bounded(smem_addr(&job_full[slot]), (k >> 1) & 1, kSpinLimit)) {
+                if (lane == 0) raise_error(a.err, ERR_INTERNAL);
+                return;
+            }
+            const int2 job = sm_job[slot];
+            if (job.x < 0) return;
+            const size_t at = (size_t)job.x * a.cap;
+            add_weights<8>(a.logits + at * G, sm_lse[slot], a.weights + at, G, job.y, a.window, a.sinks,
+                           tid - NC - 32, 32 * kWeightWarps);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&job_empty[slot]));
+        }
+    }
+
     // ---- computing warps: stream `st`, heads [hp * GS, hp * GS + nh)
     const int st = wid % NS, hp = wid / NS;
     const int nh = max(0, min(GS, G - hp * GS));
@@ -492,11 +573,28 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
         return true;
     };
     bool have = begin_piece();
+    // jobs given to the weight warps: the next one's place is free once the one before the last is done
+    int jobs = 0;
+    auto give = [&](int2 job) {
+        sm_job[jobs & 1] = job;
+        mbar_arrive(smem_addr(&job_full[jobs & 1]));
+    };
+    auto place_free = [&]() {
+        if (!mbar_wait_bounded(smem_addr(&job_empty[jobs & 1]), ((jobs >> 1) & 1) ^ 1, kSpinLimit)) {
+            raise_error(a.err, ERR_INTERNAL);
+            atomicOr(&sm_flags, 1);
+        }
+    };
+    auto list_cut = [&](int u) {  // for paged_weights
+        const int at = atomicAdd(&a.cuts[0], 1);
+        if (at < kPagedMaxGrid) a.cuts[2 + at] = u;
+    };
+    const bool hand_on = a.logits != nullptr && !split && !whole;
     while (have) {
         bool bad = false;
         const size_t q0 = head_row(p.u);
         const int Lapp = a.append && p.hi == p.nb ? p.le - 1 : -1;  // the new row, in its unit's last block
-        float *lg = a.logits ? a.logits + (q0 + hp * GS) * a.cap : nullptr;
+        float *lg = a.logits ? a.logits + (size_t)p.u * G * a.cap + 16 * hp * GS : nullptr;  // of the unit's row 0
         for (int i = whole ? 0 : p.lo + first_of(st, p.at); i < p.hi; i += whole ? 1 : NS) {
             const int at = st * S + (int)slot;
             const bool app = Lapp >= 0 && i == p.nb - 1;
@@ -541,7 +639,7 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
                     fence_async_shared();  // these writes come before the copy that fills the stage next
                     __syncwarp();
                 }
-                blk.consume(Ks, Vs, kb, p.le, a.c2, p.sg.h0, p.sg.h1, lg, a.cap, nh);
+                blk.consume(Ks, Vs, kb, p.le, a.c2, p.sg.h0, p.sg.h1, lg ? lg + (size_t)kb * G : nullptr, nh);
                 if (app && row >= 0 && hp == 0) {  // and into the cache
                     const long r = (long)row + (Lapp - kb);
 #pragma unroll
@@ -565,6 +663,7 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
             atomicOr(&sm_flags, 2);
         }
         if (whole) {
+            float *z = join + (st + 1) * JH * D - 16;  // log2 of the sums (the join buffer is not used otherwise)
             if (bad) {
                 for (int x = lane; x < nh * D / 4; x += 32)
                     store_out4(a, (q0 + hp * GS) * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f));
@@ -572,8 +671,19 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
             } else {
                 blk.store(a.out, a.out_bf16 != 0, (long)q0 + hp * GS, nh);
                 blk.each_lse(nh, [&](int q, float m, float l) {
-                    put_lse(a, q0 + hp * GS + q, l > 0.f ? m + log2f(l) : -INFINITY);
+                    const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
+                    put_lse(a, q0 + hp * GS + q, l2);
+                    if (a.logits) z[hp * GS + q] = l2;
                 });
+            }
+            if (a.logits) {
+                if constexpr (HS > 1) bar_stream<32 * HS>(2 + st);  // the warps of this stream have all their heads' sums
+                else __syncwarp();
+                const size_t at = (size_t)p.u * a.cap;
+                if (!bad) add_weights<4>(a.logits + at * G, z, a.weights + at, G, p.le, a.window, a.sinks,
+                                      hp * 32 + lane, 32 * HS);
+                if constexpr (HS > 1) bar_stream<32 * HS>(2 + st);
+                else __syncwarp();
             }
             have = begin_piece();
             continue;
@@ -589,6 +699,7 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
         for (int tile = 0; tile < GM / JH; ++tile) {
             blk.store_tile(tile, join + wid * JH * D, nh - tile * JH);
             if (tile == GM / JH - 1) have = begin_piece();  // the next piece's queries load meanwhile
+            if (tile == 0 && tid == 0 && hand_on && all) place_free();
             bar_compute<NC>();
             const int tile0 = tile * JH, heads = HS == 1 ? min(JH, G - tile0) : G;
             for (int x = tid; x < heads * D / 4; x += NC) {
@@ -619,7 +730,12 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
                 if (all) {
                     const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
                     store_out4(a, (q0 + head) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-                    if (d4 == 0) put_lse(a, q0 + head, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
+                    if (d4 == 0) {
+                        const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
+                        put_lse(a, q0 + head, l2);
+                        sm_lse[jobs & 1][head] = l2;
+                        if (a.lse2) a.lse2[q0 + head] = l2;
+                    }
                 } else {
                     *reinterpret_cast<float4 *>(a.part_o + ((size_t)out_slot * G + head) * D + 4 * d4) = o;
                     if (d4 == 0)
@@ -628,7 +744,18 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
             }
             bar_compute<NC>();
         }
-        if (all) continue;
+        if (all) {
+            if (a.logits && split) {  // (nothing left to hide it behind: the launch that follows has all CTAs for it)
+                if (tid == 0) list_cut(d.u);
+            } else if (a.logits && have) {
+                if (tid == 0) give(make_int2(d.u, d.le));
+                ++jobs;
+            } else if (a.logits) {  // the CTA's last unit (in error: sums of -inf, nothing is added)
+                const size_t at = (size_t)d.u * a.cap;
+                add_weights<4>(a.logits + at * G, sm_lse[jobs & 1], a.weights + at, G, d.le, a.window, a.sinks, tid, NC);
+            }
+            continue;
+        }
 
         // ---- a unit cut between CTAs: publish; the last one joins the pieces
         if (!split) {  // cuts inside [ub, ue) stay where they fall from ub + T to ue - T; piece 0 is the CTA's before the first
@@ -645,7 +772,10 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
         }
         bar_compute<NC>();
         if (sm_old == pieces - 1) {
-            if (tid == 0) a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
+            if (tid == 0) {
+                a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
+                if (a.logits) list_cut(d.u);
+            }
             for (int x = tid; x < G * D / 4; x += NC) {
                 const int q = x / (D / 4), d4 = x % (D / 4);
                 auto slot_of = [&](int s) { return (size_t)(2 * (c1 - 1 + s) + (s == 0 ? 1 : 0)) * G + q; };
@@ -696,9 +826,18 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
                 }
                 const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
                 store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-                if (d4 == 0) put_lse(a, q0 + q, Ls > 0.f ? M + log2f(Ls) : -INFINITY);
+                if (d4 == 0) {
+                    const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
+                    put_lse(a, q0 + q, l2);
+                    if (a.lse2) a.lse2[q0 + q] = l2;
+                }
             }
         }
+    }
+
+    if (tid == 0 && hand_on) {
+        place_free();
+        give(make_int2(-1, 0));
     }
 
     // ---- the last CTA to finish advances the lengths (every plan has been read by then) and leaves the
@@ -730,63 +869,43 @@ __global__ void __launch_bounds__(32 * NW + 32, 1)
             if (ok) a.lens[u] = L + 1;
         }
     }
-    if (tid == 0) *reinterpret_cast<unsigned long long *>(a.counters) = 0ull;
+    if (tid == 0) {
+        *reinterpret_cast<unsigned long long *>(a.counters) = 0ull;
+        if (a.logits) {
+            a.cuts[1] = min(__ldcg(a.cuts), kPagedMaxGrid);
+            a.cuts[0] = 0;
+        }
+    }
 }
 
-// weights[u, j] += (1/G) sum_g 2^(logit - lse2) for the rows in sight.  Threads take four rows at a time
-// (a block of the decode holds all four or none).
-constexpr int kWeightThreads = 256, kWeightRows = 4 * kWeightThreads;
+// The weights of the units that were cut between CTAs: their sums are known once all their pieces are.  The CTAs
+// share the units out evenly, an equal part of each unit's rows per CTA.
+constexpr int kWeightThreads = 256;
 
 __global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__restrict__ logits,
                                                                 const float *__restrict__ lse2,
-                                                                const int32_t *__restrict__ lens, int G, int cap,
+                                                                const int32_t *__restrict__ lens,
+                                                                const int32_t *__restrict__ cuts, int units, int G, int cap,
                                                                 int window, int sinks, float *weights)
 {
-    wait_prior_grid();
-    const long u = blockIdx.y;
-    const int n = lens[u];
-    if (n < 0 || n > cap) return;  // reported by the decode
     __shared__ float sm_lse[16];
-    if (threadIdx.x < G) sm_lse[threadIdx.x] = lse2[u * G + threadIdx.x];
-    __syncthreads();
-    bool any = false;
-    for (int g = 0; g < G; ++g) any |= sm_lse[g] != -INFINITY;
-    if (!any) return;  // no rows, or in error
-    const int start = window > 0 && n > window ? n - window : 0, head = min(sinks, start);
-    const float inv = 1.f / (float)G;
-    for (int j0 = (blockIdx.x * kWeightThreads + threadIdx.x) * 4; j0 < n; j0 += gridDim.x * kWeightRows) {
-        if (j0 >= head && j0 + 4 <= start) continue;
-        float4 *dst = reinterpret_cast<float4 *>(weights + u * cap + j0);
-        const float *src = logits + u * G * cap + j0;
-        const float4 old = *dst;
-        float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int g0 = 0; g0 < G; g0 += 8) {  // eight heads' loads in flight
-            float4 x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                x[k] = g0 + k < G ? __ldcs(reinterpret_cast<const float4 *>(src + (long)(g0 + k) * cap))
-                                  : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float z = g0 + k < G ? sm_lse[g0 + k] : INFINITY;  // (2^-inf is 0)
-                if (z == -INFINITY) continue;
-                p.x += fast_exp2(x[k].x - z);
-                p.y += fast_exp2(x[k].y - z);
-                p.z += fast_exp2(x[k].z - z);
-                p.w += fast_exp2(x[k].w - z);
-            }
-        }
-        const float4 sum = make_float4(fmaf(p.x, inv, old.x), fmaf(p.y, inv, old.y), fmaf(p.z, inv, old.z),
-                                       fmaf(p.w, inv, old.w));
-        if (j0 + 4 <= n && (j0 + 4 <= head || j0 >= start)) {
-            *dst = sum;
-        } else {
-            auto seen = [&](int j) { return j < n && (j < head || j >= start); };
-            if (seen(j0)) dst->x = sum.x;
-            if (seen(j0 + 1)) dst->y = sum.y;
-            if (seen(j0 + 2)) dst->z = sum.z;
-            if (seen(j0 + 3)) dst->w = sum.w;
-        }
+    wait_prior_grid();
+    const int n_cut = cuts[1];
+    if (n_cut == 0) return;
+    const int parts = max(1, (int)gridDim.x / n_cut);  // CTAs per unit
+    for (int i = blockIdx.x; i < n_cut * parts; i += gridDim.x) {
+        const int u = cuts[2 + i / parts];
+        if ((unsigned)u >= (unsigned)units) continue;
+        const int n = lens[u];
+        __syncthreads();
+        if (threadIdx.x < G) sm_lse[threadIdx.x] = lse2[(size_t)u * G + threadIdx.x];
+        __syncthreads();
+        bool any = false;
+        for (int g = 0; g < G; ++g) any |= sm_lse[g] != -INFINITY;
+        if (!any || n < 0 || n > cap) continue;  // in error
+        const size_t at = (size_t)u * cap;
+        add_weights<8>(logits + at * G, sm_lse, weights + at, G, n, window, sinks,
+                    (i % parts) * kWeightThreads + threadIdx.x, parts * kWeightThreads);
     }
 }
 
@@ -799,7 +918,7 @@ struct PagedLaunch {
 template <class Block, int HS, int NW> static PagedLaunch with()
 {
     static_assert(paged_smem<Block, NW>() + 2048 <= 227 * 1024, "shared memory of a CTA (2 KB of it static)");
-    return PagedLaunch{paged_decode<Block, HS, NW>, paged_smem<Block, NW>(), 32 * NW + 32};
+    return PagedLaunch{paged_decode<Block, HS, NW>, paged_smem<Block, NW>(), 32 * (NW + 1 + kWeightWarps)};
 }
 template <int D> static PagedLaunch paged_kernel(bool f32, int G)
 {
@@ -834,6 +953,7 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     a.weights = weights;
     a.counters = ws.counters;
     a.part_ml = ws.part_ml;
+    a.cuts = ws.cuts;
     a.part_o = ws.part_o;
     a.units = units;
     a.B = kv.B;
@@ -862,11 +982,9 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     const int grid = (int)std::min<long long>(std::min(device_sm_count(), kPagedMaxGrid), std::max<long long>(units, most / kMinBlocks));
     e = launch_pdl(k.fn, dim3(grid), dim3(k.threads), k.smem, s, mk, mv, a);
     if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights) return e;
-    // CTAs over a unit's rows: enough that all units together fill the GPU four times over, never more than
-    // the rows of a unit need (lengths are not known here, and CTAs without rows cost time too)
-    const int need = (cap + kWeightRows - 1) / kWeightRows, fill = 4 * 8 * device_sm_count() / units;
-    e = launch_pdl(paged_weights, dim3(std::max(1, std::min(need, fill)), units), dim3(kWeightThreads), 0, s,
-                   (const float *)ws.logits, (const float *)ws.lse2, (const int32_t *)lens, G, cap, window, sinks, weights);
+    e = launch_pdl(paged_weights, dim3(4 * device_sm_count()), dim3(kWeightThreads), 0, s, (const float *)ws.logits,
+                   (const float *)ws.lse2, (const int32_t *)lens, (const int32_t *)ws.cuts, units, G, cap, window, sinks,
+                   weights);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
