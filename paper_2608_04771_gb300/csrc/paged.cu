@@ -32,7 +32,9 @@ namespace reco {
 constexpr int kRingBytes = 24 * 8192;         // ring of a CTA
 constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
 constexpr int kWeightWarps = 3;              // warps that turn the logits of finished units into weights
-constexpr int kMinBlocks = 16;               // blocks per working CTA (fewer CTAs rather than less)
+constexpr int kMinBlocks = 8;                // blocks per working CTA (fewer CTAs rather than less: a layer of two units of 512
+                                             // rows 10.9 us, with 16 12.1; 8 units of 1000 rows 11.5 and 13.1)
+constexpr int kInlineRows = 1024;            // calls whose units are no longer than this make their weights where pieces join
 constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
 constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
 
@@ -71,6 +73,7 @@ struct PagedArgs {
     float *part_ml, *part_o;
     int32_t *cuts;  // units cut between CTAs: [0] counted, [1] their number once the launch is done, [2 ...] the units
     int units, B, Hq, Hkv, G, cap, n_pages, max_pages, shift, append, out_bf16, window, sinks;
+    int inline_weights;  // no paged_weights follows: pieces become weights where they join
     float c2;  // scale * log2(e)
     unsigned *err;
 };
@@ -745,7 +748,7 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
             bar_compute<NC>();
         }
         if (all) {
-            if (a.logits && split) {  // (nothing left to hide it behind: the launch that follows has all CTAs for it)
+            if (a.logits && split && !a.inline_weights) {  // (nothing to hide it behind: the next launch has all CTAs)
                 if (tid == 0) list_cut(d.u);
             } else if (a.logits && have) {
                 if (tid == 0) give(make_int2(d.u, d.le));
@@ -774,7 +777,7 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
         if (sm_old == pieces - 1) {
             if (tid == 0) {
                 a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
-                if (a.logits) list_cut(d.u);
+                if (a.logits && !a.inline_weights) list_cut(d.u);
             }
             for (int x = tid; x < G * D / 4; x += NC) {
                 const int q = x / (D / 4), d4 = x % (D / 4);
@@ -830,7 +833,13 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
                     const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
                     put_lse(a, q0 + q, l2);
                     if (a.lse2) a.lse2[q0 + q] = l2;
+                    if (a.inline_weights) sm_lse[0][q] = l2;
                 }
+            }
+            if (a.inline_weights) {
+                bar_compute<NC>();
+                const size_t at = (size_t)d.u * a.cap;
+                add_weights<4>(a.logits + at * G, sm_lse[0], a.weights + at, G, d.le, a.window, a.sinks, tid, NC);
             }
         }
     }
@@ -974,6 +983,8 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     const unsigned long long rows = (unsigned long long)kv.n_layers * kv.n_pages * kv.H_kv * kv.page;
     if (!f32 && (!encode_bf16_2d(&mk, kv.k, rows, kv.d, 64, 16) || !encode_bf16_2d(&mv, kv.v, rows, kv.d, 64, 16)))
         return cudaErrorInvalidValue;
+    // (units that fit the grid are cut one piece per CTA: no unit is left for the weight warps)
+    a.inline_weights = weights && units <= std::min(device_sm_count(), kPagedMaxGrid) && cap <= kInlineRows ? 1 : 0;
     const PagedLaunch k = kv.d == 64 ? paged_kernel<64>(f32, G) : paged_kernel<128>(f32, G);
     cudaError_t e = allow_smem((const void *)k.fn, k.smem);
     if (e != cudaSuccess) return e;
@@ -981,7 +992,7 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     const long long most = (long long)units * ((cap + 15) / 16);
     const int grid = (int)std::min<long long>(std::min(device_sm_count(), kPagedMaxGrid), std::max<long long>(units, most / kMinBlocks));
     e = launch_pdl(k.fn, dim3(grid), dim3(k.threads), k.smem, s, mk, mv, a);
-    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights) return e;
+    if (e != cudaSuccess || (e = cudaGetLastError()) != cudaSuccess || !weights || a.inline_weights) return e;
     e = launch_pdl(paged_weights, dim3(4 * device_sm_count()), dim3(kWeightThreads), 0, s, (const float *)ws.logits,
                    (const float *)ws.lse2, (const int32_t *)lens, (const int32_t *)ws.cuts, units, G, cap, window, sinks,
                    weights);
