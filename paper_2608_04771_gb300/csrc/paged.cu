@@ -34,6 +34,7 @@ constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots 
 constexpr int kWeightWarps = 3;              // warps that turn the logits of finished units into weights
 constexpr int kMinBlocks = 8;                // blocks per working CTA (fewer CTAs rather than less: a layer of two units of 512
                                              // rows 10.9 us, with 16 12.1; 8 units of 1000 rows 11.5 and 13.1)
+constexpr int kWarpUnits = 128;              // up to this many units (that fit the grid) every warp plans by itself
 constexpr int kInlineRows = 1024;            // calls whose units are no longer than this make their weights where pieces join
 constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
 constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
@@ -285,173 +286,248 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     wait_prior_grid();  // lens, the table, q and the new rows may come from the previous kernels
-
-    // ---- plan, the same in every CTA
-    const int seg = (P + NT - 1) / NT, u_lo = min(P, tid * seg), u_hi = min(P, u_lo + seg);
-    int le0 = 0;  // with a unit per thread at most: its rows; with more, the rows of all lie in the (still idle) ring
-    int *sm_le = reinterpret_cast<int *>(smem_raw + (ring0 - raw0));
-    const bool staged = seg > 1 && P <= kRingBytes / 4;
     auto look = [&](int L) {
         if (blockIdx.x == 0 && !unit_ok(L, a.cap, a.append))
             raise_error(a.err, (a.append && L == a.cap) ? ERR_ROOM : ERR_LEN);
         return rows_of(a, L);
     };
-    if (seg == 1) {
-        if (tid < P) le0 = look(__ldcg(a.lens + tid));
-    } else {
-        for (int u0 = tid; u0 < P; u0 += 8 * NT) {  // eight loads in flight
-            int L[8];
+    // Few units: every warp plans by itself, up to kWarpUnits / 32 of them in a row per lane
+    const bool by_warp = P <= kWarpUnits && P <= (int)gridDim.x;
+    constexpr int UL = kWarpUnits / 32;
+    const int per_lane = (P + 31) / 32;
+    int le_w[UL];
+    if (by_warp) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) L[k] = u0 + k * NT < P ? __ldcg(a.lens + u0 + k * NT) : 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int u = u0 + k * NT;
-                if (u < P) {
-                    const int le = look(L[k]);
-                    if (staged) sm_le[u] = le;
-                }
-            }
+        for (int i = 0; i < UL; ++i) {
+            const int u = lane * per_lane + i;
+            le_w[i] = i < per_lane && u < P ? __ldcg(a.lens + u) : 0;
         }
-        __syncthreads();
     }
-    // rows of a unit of this thread's share
-    auto le_of = [&](int u) { return seg == 1 ? le0 : (staged ? sm_le[u] : rows_of(a, __ldcg(a.lens + u))); };
-    int my_b = 0, my_max = 0, my_ne = 0;
-    for (int u = u_lo; u < u_hi; ++u) {
-        const int nb = blocks_of<KB>(a, le_of(u));
-        my_b += nb;
-        my_max = max(my_max, nb);
-        my_ne += nb > 0;
-    }
-    my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
-    my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
-    const int warp_b = __reduce_add_sync(0xffffffffu, (unsigned)my_b);
-    if (lane == 0) {
-        sm_scan[0][wid] = warp_b;
-        sm_scan[1][wid] = my_max;
-        sm_scan[2][wid] = my_ne;
-    }
-    __syncthreads();
-    int NB = 0, max_nb = 0, n_ne = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        NB += sm_scan[0][w];
-        max_nb = max(max_nb, sm_scan[1][w]);
-        n_ne += sm_scan[2][w];
-    }
-    // exclusive prefix of x over the CTA's threads, and its sum
-    auto scan = [&](int x, int &total) {
-        int incl = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
-        }
-        if (lane == 31) sm_scan[3][wid] = incl;
-        __syncthreads();
-        int before = incl - x;
-        total = 0;
-#pragma unroll
-        for (int w = 0; w < NT / 32; ++w) {
-            const int v = sm_scan[3][w];
-            before += w < wid ? v : 0;
-            total += v;
-        }
-        return before;
-    };
-    // (64-bit products and divisions here cost a short call 0.5 us: equal parts are cut as quotient and rest)
+    __syncthreads();  // the barriers are ready
+
+    // ---- plan, the same in every CTA
     const int c = blockIdx.x, grid = gridDim.x;
-    const bool split = n_ne <= grid;
-    const bool whole = !split && max_nb <= kWholeBlocks;
-    const int quot = NB / grid, rest = NB - quot * grid;  // (more units than CTAs: quot > 0)
-    const int T = whole ? 1 << 30 : min(kSnapBlocks, max(1, quot / 4));
-    int c1 = 0, pieces = 1;  // split: the CTA after the first piece's, the pieces of the unit
+    int NB = 0, max_nb = 0, n_ne = 0, c1 = 0, pieces = 1;  // c1, pieces: split: the CTA after the first piece's, the pieces
+    bool split = true, whole = false;
+    int quot = 0, rest = 0, T = 0;
     Walk start;
     start.begin = start.end = start.u = 0;
-    if (split && NB > 0) {
-        // Units that fit the grid: every one is cut into equal pieces of at most `per` blocks, a CTA each, so that a
-        // CTA joins and publishes once.  `per` is the longest unit's share when it is cut as often as its part of
-        // all blocks allows, or once, twice or three times less, whichever leaves no more pieces than CTAs, and
-        // failing those one that cannot leave more.
+    // Units that fit the grid are cut into equal pieces of at most `per` blocks, a CTA each, so that a CTA joins
+    // and publishes once.  `per` is the longest unit's share when it is cut as often as its part of all blocks allows,
+    // or once, twice or three times less, whichever leaves no more pieces than CTAs, and failing those one that
+    // cannot leave more.
+    auto share = [&](int j) {
         const int target = max(n_ne, min(grid, NB / kMinBlocks));
         const int j0 = max(1, (int)((float)max_nb * (float)target / (float)NB));
-        int per = 0, total = 0, at = 0;
-        for (int j = 0; j < 5; ++j) {
-            const int div = max(1, j0 - j), room = max(1, grid - n_ne);
-            per = j < 4 ? (max_nb + div - 1) / div : (NB + room - 1) / room;
+        const int div = max(1, j0 - j), room = max(1, grid - n_ne);
+        return j < 4 ? (max_nb + div - 1) / div : (NB + room - 1) / room;
+    };
+    auto take = [&](int u, int nb, int le, int first, int per) {  // this CTA's piece of unit u, whose first CTA is `first`
+        start.u = u;
+        start.ub = 0;
+        start.nb = nb;
+        start.le = le;
+        c1 = first + 1;
+        pieces = (nb + per - 1) / per;
+        const int s = c - first, pq = nb / pieces, pr = nb - pq * pieces;
+        start.begin = pq * s + min(s, pr);
+        start.end = pq * (s + 1) + min(s + 1, pr);
+    };
+    if (by_warp) {
+        int my_b = 0, my_max = 0, my_ne = 0, nb[UL];
+#pragma unroll
+        for (int i = 0; i < UL; ++i) {
+            const bool mine = i < per_lane && lane * per_lane + i < P;
+            le_w[i] = mine ? (wid == 0 ? look(le_w[i]) : rows_of(a, le_w[i])) : 0;
+            nb[i] = blocks_of<KB>(a, le_w[i]);
+            my_b += nb[i];
+            my_max = max(my_max, nb[i]);
+            my_ne += nb[i] > 0;
+        }
+        NB = __reduce_add_sync(0xffffffffu, (unsigned)my_b);
+        max_nb = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
+        n_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
+        for (int j = 0; NB > 0 && j < 5; ++j) {
+            const int per = share(j);
             int my_k = 0;
-            for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, le_of(u)) + per - 1) / per;
-            if (j > 0) __syncthreads();  // the last scan has been read
-            at = scan(my_k, total);
-            if (total <= grid) {
-                if (c >= at && c < at + my_k) {
-                    for (int u = u_lo; u < u_hi; ++u) {
-                        const int le = le_of(u), nb = blocks_of<KB>(a, le), k = (nb + per - 1) / per;
-                        if (c < at + k) {
-                            sm_cut[0][0] = u;
-                            sm_cut[0][1] = at;
-                            sm_cut[0][2] = nb;
-                            sm_cut[0][3] = le;
-                            break;
-                        }
-                        at += k;
+#pragma unroll
+            for (int i = 0; i < UL; ++i) my_k += (nb[i] + per - 1) / per;
+            int at = my_k;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, at, o);
+                if (lane >= o) at += v;
+            }
+            const int total = __shfl_sync(0xffffffffu, at, 31);
+            at -= my_k;
+            if (total > grid) continue;
+            int u = 0, unb = 0, le = 0;
+            const bool mine = c >= at && c < at + my_k;
+            if (mine) {
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < UL; ++i) {
+                    const int k = (nb[i] + per - 1) / per;
+                    if (!found && c < at + k) {
+                        found = true;
+                        u = lane * per_lane + i;
+                        unb = nb[i];
+                        le = le_w[i];
+                    }
+                    at += found ? 0 : k;
+                }
+            }
+            const unsigned who = __ballot_sync(0xffffffffu, mine);
+            if (who != 0u) {
+                const int src = __ffs(who) - 1;
+                u = __shfl_sync(0xffffffffu, u, src);
+                unb = __shfl_sync(0xffffffffu, unb, src);
+                le = __shfl_sync(0xffffffffu, le, src);
+                at = __shfl_sync(0xffffffffu, at, src);
+                take(u, unb, le, at, per);
+            }
+            break;
+        }
+    } else {
+        const int seg = (P + NT - 1) / NT, u_lo = min(P, tid * seg), u_hi = min(P, u_lo + seg);
+        int le0 = 0;  // with a unit per thread at most: its rows; with more, the rows of all lie in the (still idle) ring
+        int *sm_le = reinterpret_cast<int *>(smem_raw + (ring0 - raw0));
+        const bool staged = seg > 1 && P <= kRingBytes / 4;
+        if (seg == 1) {
+            if (tid < P) le0 = look(__ldcg(a.lens + tid));
+        } else {
+            for (int u0 = tid; u0 < P; u0 += 8 * NT) {  // eight loads in flight
+                int L[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) L[k] = u0 + k * NT < P ? __ldcg(a.lens + u0 + k * NT) : 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int u = u0 + k * NT;
+                    if (u < P) {
+                        const int le = look(L[k]);
+                        if (staged) sm_le[u] = le;
                     }
                 }
-                break;
             }
+            __syncthreads();
+        }
+        // rows of a unit of this thread's share
+        auto le_of = [&](int u) { return seg == 1 ? le0 : (staged ? sm_le[u] : rows_of(a, __ldcg(a.lens + u))); };
+        int my_b = 0, my_max = 0, my_ne = 0;
+        for (int u = u_lo; u < u_hi; ++u) {
+            const int nb = blocks_of<KB>(a, le_of(u));
+            my_b += nb;
+            my_max = max(my_max, nb);
+            my_ne += nb > 0;
+        }
+        my_max = __reduce_max_sync(0xffffffffu, (unsigned)my_max);
+        my_ne = __reduce_add_sync(0xffffffffu, (unsigned)my_ne);
+        const int warp_b = __reduce_add_sync(0xffffffffu, (unsigned)my_b);
+        if (lane == 0) {
+            sm_scan[0][wid] = warp_b;
+            sm_scan[1][wid] = my_max;
+            sm_scan[2][wid] = my_ne;
         }
         __syncthreads();
-        if (c < total) {
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) {
+            NB += sm_scan[0][w];
+            max_nb = max(max_nb, sm_scan[1][w]);
+            n_ne += sm_scan[2][w];
+        }
+        // exclusive prefix of x over the CTA's threads, and its sum
+        auto scan = [&](int x, int &total) {
+            int incl = x;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            if (lane == 31) sm_scan[3][wid] = incl;
+            __syncthreads();
+            int before = incl - x;
+            total = 0;
+#pragma unroll
+            for (int w = 0; w < NT / 32; ++w) {
+                const int v = sm_scan[3][w];
+                before += w < wid ? v : 0;
+                total += v;
+            }
+            return before;
+        };
+        // (64-bit products and divisions here cost a short call 0.5 us: equal parts are cut as quotient and rest)
+        split = n_ne <= grid;
+        whole = !split && max_nb <= kWholeBlocks;
+        quot = NB / grid;  // (more units than CTAs: at least 1)
+        rest = NB - quot * grid;
+        T = whole ? 1 << 30 : min(kSnapBlocks, max(1, quot / 4));
+        if (split && NB > 0) {
+            int per = 0, total = 0, at = 0;
+            for (int j = 0; j < 5; ++j) {
+                per = share(j);
+                int my_k = 0;
+                for (int u = u_lo; u < u_hi; ++u) my_k += (blocks_of<KB>(a, le_of(u)) + per - 1) / per;
+                if (j > 0) __syncthreads();  // the last scan has been read
+                at = scan(my_k, total);
+                if (total <= grid) {
+                    if (c >= at && c < at + my_k) {
+                        for (int u = u_lo; u < u_hi; ++u) {
+                            const int le = le_of(u), nb = blocks_of<KB>(a, le), k = (nb + per - 1) / per;
+                            if (c < at + k) {
+                                sm_cut[0][0] = u;
+                                sm_cut[0][1] = at;
+                                sm_cut[0][2] = nb;
+                                sm_cut[0][3] = le;
+                                break;
+                            }
+                            at += k;
+                        }
+                    }
+                    break;
+                }
+            }
+            __syncthreads();
+            if (c < total) take(sm_cut[0][0], sm_cut[0][2], sm_cut[0][3], sm_cut[0][1], per);
+        } else if (NB > 0) {
+            // More units than CTAs: equal ranges of the blocks laid end to end
+            int total;
+            const int before = scan(my_b, total);
+            auto ideal = [&](int k) { return quot * k + min(k, rest); };
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int t = ideal(c + k);
+                if (t >= before && t < before + my_b) {  // in one of this thread's units
+                    int ub = before, u = u_lo, nb = 0, le = 0;
+                    for (; u < u_hi; ++u) {
+                        le = le_of(u);
+                        nb = blocks_of<KB>(a, le);
+                        if (t < ub + nb) break;
+                        ub += nb;
+                    }
+                    sm_cut[k][0] = u;
+                    sm_cut[k][1] = ub;
+                    sm_cut[k][2] = nb;
+                    sm_cut[k][3] = le;
+                }
+            }
+            __syncthreads();
+            auto cut = [&](int k) {
+                const int t = ideal(c + k), ub = sm_cut[k][1], ue = ub + sm_cut[k][2];
+                if (t >= NB) return NB;
+                if (min(t - ub, ue - t) >= T) return t;
+                return t - ub <= ue - t ? ub : ue;
+            };
+            start.begin = cut(0);
+            start.end = cut(1);
             start.u = sm_cut[0][0];
-            start.ub = 0;
+            if (whole) {  // the units [start.u, start.end)
+                start.u += start.begin == sm_cut[0][1] ? 0 : 1;
+                start.end = ideal(c + 1) >= NB ? P : sm_cut[1][0] + (start.end == sm_cut[1][1] ? 0 : 1);
+            }
+            start.ub = sm_cut[0][1];
             start.nb = sm_cut[0][2];
             start.le = sm_cut[0][3];
-            const int s = c - sm_cut[0][1];
-            c1 = sm_cut[0][1] + 1;
-            pieces = (start.nb + per - 1) / per;
-            const int pq = start.nb / pieces, pr = start.nb - pq * pieces;
-            start.begin = pq * s + min(s, pr);
-            start.end = pq * (s + 1) + min(s + 1, pr);
         }
-    } else if (NB > 0) {
-        // More units than CTAs: equal ranges of the blocks laid end to end
-        int total;
-        const int before = scan(my_b, total);
-        auto ideal = [&](int k) { return quot * k + min(k, rest); };
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int t = ideal(c + k);
-            if (t >= before && t < before + my_b) {  // in one of this thread's units
-                int ub = before, u = u_lo, nb = 0, le = 0;
-                for (; u < u_hi; ++u) {
-                    le = le_of(u);
-                    nb = blocks_of<KB>(a, le);
-                    if (t < ub + nb) break;
-                    ub += nb;
-                }
-                sm_cut[k][0] = u;
-                sm_cut[k][1] = ub;
-                sm_cut[k][2] = nb;
-                sm_cut[k][3] = le;
-            }
-        }
-        __syncthreads();
-        auto cut = [&](int k) {
-            const int t = ideal(c + k), ub = sm_cut[k][1], ue = ub + sm_cut[k][2];
-            if (t >= NB) return NB;
-            if (min(t - ub, ue - t) >= T) return t;
-            return t - ub <= ue - t ? ub : ue;
-        };
-        start.begin = cut(0);
-        start.end = cut(1);
-        start.u = sm_cut[0][0];
-        if (whole) {  // the units [start.u, start.end)
-            start.u += start.begin == sm_cut[0][1] ? 0 : 1;
-            start.end = ideal(c + 1) >= NB ? P : sm_cut[1][0] + (start.end == sm_cut[1][1] ? 0 : 1);
-        }
-        start.ub = sm_cut[0][1];
-        start.nb = sm_cut[0][2];
-        start.le = sm_cut[0][3];
     }
     start.b = start.begin;
 
