@@ -35,7 +35,8 @@ constexpr int kWeightWarps = 3;              // warps that turn the logits of fi
 constexpr int kMinBlocks = 8;                // blocks per working CTA (fewer CTAs rather than less: a layer of two units of 512
                                              // rows 10.9 us, with 16 12.1; 8 units of 1000 rows 11.5 and 13.1)
 constexpr int kWarpUnits = 128;              // up to this many units (that fit the grid) every warp plans by itself
-constexpr int kInlineRows = 1024;            // calls whose units are no longer than this make their weights where pieces join
+constexpr int kInlineRows = 2560;            // calls with no more rows in sight than this (and units that fit the grid) make their weights
+                                             // where pieces join: 32 units of 2000 rows 16.9 us, with a launch for them 19.1, 4 of 4000 19.3 and 18.5
 constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
 constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
 
@@ -1060,7 +1061,8 @@ cudaError_t launch_paged_decode(const reco_paged_kv &kv, const void *q, const vo
     if (!f32 && (!encode_bf16_2d(&mk, kv.k, rows, kv.d, 64, 16) || !encode_bf16_2d(&mv, kv.v, rows, kv.d, 64, 16)))
         return cudaErrorInvalidValue;
     // (units that fit the grid are cut one piece per CTA: no unit is left for the weight warps)
-    a.inline_weights = weights && units <= std::min(device_sm_count(), kPagedMaxGrid) && cap <= kInlineRows ? 1 : 0;
+    const int most_seen = window > 0 ? (int)std::min<long long>(cap, (long long)window + sinks) : cap;
+    a.inline_weights = weights && units <= std::min(device_sm_count(), kPagedMaxGrid) && most_seen <= kInlineRows ? 1 : 0;
     const PagedLaunch k = kv.d == 64 ? paged_kernel<64>(f32, G) : paged_kernel<128>(f32, G);
     cudaError_t e = allow_smem((const void *)k.fn, k.smem);
     if (e != cudaSuccess) return e;
