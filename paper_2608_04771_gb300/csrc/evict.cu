@@ -33,7 +33,7 @@ EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base)
     ws.idx = (int32_t *)take(units * paged_cap(kv) * 4);
     ws.rank = (int32_t *)take(units * (chunks + 1) * 4);
     ws.flags = (int32_t *)take(units * chunks * 4);
-    ws.list = (int2 *)take(units * chunks * 8);
+    ws.list = (int4 *)take(units * chunks * 16);
     ws.ulist = (int32_t *)take(units * 4);
     ws.bytes = off;
     return ws;
@@ -124,55 +124,31 @@ template <int ROW> __device__ __forceinline__ void compact_column(const CompactA
     }
 }
 
-// Few cut units: chunk `c` of a unit, 16 KB of K and 16 KB of V, four pieces of 16 bytes of each per thread.
-template <int ROW> __device__ __forceinline__ void compact_chunk(const CompactArgs &a, int u, int c)
-{
-    constexpr int PIECES = ROW / 16, RPP = kCompactThreads / PIECES, U = 4, R = RPP * U;
-    const UnitRows rows(a, u);
-    const int m = min(a.lens[u], a.cap), r0 = c * R, sub = threadIdx.x / PIECES;
-    const int32_t *idx = a.idx + (size_t)u * a.cap;
-    char *K = a.K + (threadIdx.x % PIECES) * 16, *V = a.V + (threadIdx.x % PIECES) * 16;
-    uint4 k[U], v[U];
-    int src[U];
+// Few cut units: a chunk of a unit, 16 KB of K and 16 KB of V, four pieces of 16 bytes of each per thread.
+template <int ROW> struct Chunk {
+    static constexpr int PIECES = ROW / 16, RPP = kCompactThreads / PIECES, U = 4, R = RPP * U;
+    int u, c;     // unit and chunk
+    int src[U];   // the rows that move to this thread's rows (those rows themselves: nothing moves)
+
+    __device__ __forceinline__ int row(int i) const { return c * R + i * RPP + (int)threadIdx.x / PIECES; }
+
+    // entry t of the list
+    __device__ __forceinline__ void find(const CompactArgs &a, int t)
+    {
+        const int4 it = __ldg(a.ws.list + t);  // (unit, chunk, kept rows)
+        const bool ok = (unsigned)it.x < (unsigned)a.units && (unsigned)it.y < (unsigned)a.chunks;
+        if (!ok && threadIdx.x == 0) raise_error(a.err, ERR_INTERNAL);
+        u = ok ? it.x : 0;
+        c = ok ? it.y : 0;
+        const int m = ok ? min(it.z, a.cap) : 0;
+        const int32_t *idx = a.idx + (size_t)u * a.cap;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int r = r0 + i * RPP + sub;
-        src[i] = r < m ? __ldg(idx + r) : r;
-        if (src[i] < r || src[i] >= a.cap) src[i] = r;
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        if (src[i] == r0 + i * RPP + sub) continue;  // already in place, or behind the last row
-        const size_t p = rows.at<ROW>(a, src[i]);
-        k[i] = __ldcs(reinterpret_cast<const uint4 *>(K + p));
-        v[i] = __ldcs(reinterpret_cast<const uint4 *>(V + p));
-    }
-    __syncthreads();  // the chunk has been read
-    if (threadIdx.x == 0) {
-        int *flags = a.ws.flags + (size_t)u * a.chunks;
-        st_release(flags + c, 1);
-        // kept rows in this chunk's destination rows: their destinations' chunks have to have been read
-        const int32_t *rank = a.ws.rank + (size_t)u * (a.chunks + 1);
-        const int lo = max(0, __ldg(rank + c)), hi = __ldg(rank + c + 1);
-        for (int b = lo / R; b < c && b * R < hi; ++b) {
-            long long spin = 0;
-            while (ld_acquire(flags + b) == 0 && spin < kFlagSpin) ++spin;
-            if (spin >= kFlagSpin) {
-                raise_error(a.err, ERR_INTERNAL);
-                break;
-            }
+        for (int i = 0; i < U; ++i) {
+            const int r = row(i), s = r < m ? __ldg(idx + r) : r;
+            src[i] = s < r || s >= a.cap ? r : s;
         }
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int r = r0 + i * RPP + sub;
-        if (src[i] == r) continue;
-        const size_t p = rows.at<ROW>(a, r);
-        *reinterpret_cast<uint4 *>(K + p) = k[i];
-        *reinterpret_cast<uint4 *>(V + p) = v[i];
-    }
-}
+};
 
 // Whether the columns of the cut units keep most of the `ctas` of compact_columns busy: then they move, and
 // else the chunks.
@@ -196,24 +172,59 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 8) compact
 
 template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact_chunks(CompactArgs a)
 {
+    constexpr int U = Chunk<ROW>::U, R = Chunk<ROW>::R;
+    __shared__ int sm_next;
     wait_prior_grid();  // the selection's results
     const int columns = min(a.ws.counters[3], a.units) * 2 * (ROW / 128);
     const int chunks = min(a.ws.counters[1], a.units * a.chunks);
     const int total = by_columns(a, columns) ? 0 : chunks;
-    __shared__ int sm_next;
+    const int off = (threadIdx.x % Chunk<ROW>::PIECES) * 16;
     if (threadIdx.x == 0) sm_next = total > 0 ? atomicAdd(&a.ws.counters[0], 1) : 0;
     __syncthreads();
     int t = sm_next;
+    Chunk<ROW> cur, nxt;
+    if (t < total) cur.find(a, t);
     while (t < total) {
         int claimed = 0;
-        if (threadIdx.x == 0) claimed = atomicAdd(&a.ws.counters[0], 1);  // the next one, while this one moves
-        const int2 it = a.ws.list[t];
-        if ((unsigned)it.x < (unsigned)a.units && (unsigned)it.y < (unsigned)a.chunks) compact_chunk<ROW>(a, it.x, it.y);
-        else if (threadIdx.x == 0) raise_error(a.err, ERR_INTERNAL);
-        __syncthreads();
+        if (threadIdx.x == 0) claimed = atomicAdd(&a.ws.counters[0], 1);  // the next chunk, while this one moves
+        const UnitRows rows(a, cur.u);
+        uint4 k[U], v[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (cur.src[i] == cur.row(i)) continue;  // already in place, or behind the last row
+            const size_t p = rows.at<ROW>(a, cur.src[i]) + off;
+            k[i] = __ldcs(reinterpret_cast<const uint4 *>(a.K + p));
+            v[i] = __ldcs(reinterpret_cast<const uint4 *>(a.V + p));
+        }
         if (threadIdx.x == 0) sm_next = claimed;
-        __syncthreads();
+        __syncthreads();  // the chunk has been read
         t = sm_next;
+        if (t < total) nxt.find(a, t);  // its rows are looked up while this chunk waits for its turn
+        if (threadIdx.x == 0) {
+            int *flags = a.ws.flags + (size_t)cur.u * a.chunks;
+            st_release(flags + cur.c, 1);
+            // kept rows in this chunk's destination rows: their destinations' chunks have to have been read
+            const int32_t *rank = a.ws.rank + (size_t)cur.u * (a.chunks + 1);
+            const int lo = max(0, __ldg(rank + cur.c)), hi = __ldg(rank + cur.c + 1);
+            for (int b = lo / R; b < cur.c && b * R < hi; ++b) {
+                long long spin = 0;
+                while (ld_acquire(flags + b) == 0 && spin < kFlagSpin) ++spin;
+                if (spin >= kFlagSpin) {
+                    raise_error(a.err, ERR_INTERNAL);
+                    break;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int r = cur.row(i);
+            if (cur.src[i] == r) continue;
+            const size_t p = rows.at<ROW>(a, r) + off;
+            *reinterpret_cast<uint4 *>(a.K + p) = k[i];
+            *reinterpret_cast<uint4 *>(a.V + p) = v[i];
+        }
+        cur = nxt;
     }
     // the last CTA to finish leaves the counters zero, as the call found them
     if (threadIdx.x == 0) {

@@ -79,7 +79,7 @@ struct EvictWs {
     int32_t *idx;       // [units][cap] kept rows (when the caller passes none)
     int32_t *rank;      // [units][chunks + 1] kept rows before row i << shift
     int32_t *flags;     // [units][chunks] the chunk's rows have been read
-    int2 *list;         // [units * chunks] (unit, chunk) to move, a unit's chunks in order
+    int4 *list;         // [units * chunks] (unit, chunk, kept rows) to move, a unit's chunks in order
     int32_t *ulist;     // [units] units that are cut
     size_t bytes;
 };

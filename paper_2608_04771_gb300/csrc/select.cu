@@ -94,7 +94,7 @@ struct BudgetRule {
     int max_pages, n_pages, page;
     float *weights;
     int32_t *rank, *flags;
-    int2 *list;
+    int4 *list;
     int32_t *ulist, *counters;
     int shift, chunks, units;
     __device__ __forceinline__ unsigned error(int L, int m, int L_cap) const
@@ -131,7 +131,7 @@ struct BudgetRule {
         if (from == 0) rank[u * (chunks + 1) + ((L - 1) >> shift) + 1] = m;
         for (int i = from; i < (m + (1 << shift) - 1) >> shift; i += step) {
             flags[u * chunks + i] = 0;
-            if ((unsigned)(at + i) < (unsigned)(units * chunks)) list[at + i] = make_int2((int)u, i);
+            if ((unsigned)(at + i) < (unsigned)(units * chunks)) list[at + i] = make_int4((int)u, i, m, 0);
         }
     }
 };
