@@ -186,6 +186,31 @@ CASES = [
     (1, 1, 6, 1, 64, F32, 32, (7001, 7001), 0, 0, True),
     (1, 2, 16, 1, 128, BF, 32, (100, 6000), 0, 0, False),
     (1, 1, 5, 1, 128, BF, 16, (9001, 9001), 4097, 5, True),
+    # more units than CTAs: ranges of blocks cut across units, joined in tiles of eight heads, heads shared by
+    # the warps of a stream
+    (10, 10, 6, 2, 128, BF, 16, (200, 900), 0, 0, True),
+    (10, 10, 6, 2, 64, F32, 32, (200, 700), 0, 0, True),
+    (9, 9, 24, 2, 128, BF, 16, (280, 600), 0, 0, True),
+    (9, 9, 11, 1, 64, BF, 16, (280, 600), 300, 7, False),
+    (9, 9, 14, 2, 128, F32, 16, (270, 500), 0, 0, True),
+    (10, 16, 13, 1, 64, F32, 64, (270, 400), 0, 0, False),
+    (10, 16, 3, 1, 128, BF, 64, (1, 3000), 200, 20, True),
+    # and short units, each of which goes to the warps of one stream
+    (12, 10, 6, 2, 128, BF, 16, (0, 200), 0, 0, True),
+    (12, 10, 22, 2, 64, BF, 32, (0, 200), 30, 5, True),
+    (12, 10, 8, 2, 128, F32, 16, (0, 200), 0, 0, True),
+    (12, 10, 14, 2, 64, F32, 16, (0, 200), 50, 0, True),
+    (9, 18, 10, 1, 128, F32, 16, (0, 100), 0, 0, True),
+    (9, 18, 16, 1, 128, F32, 16, (0, 100), 0, 0, True),
+    (9, 18, 1, 1, 64, F32, 16, (0, 100), 0, 0, True),
+    # as many units as plan by warps, as fit a CTA each, and one more of each
+    (4, 32, 2, 1, 64, BF, 16, (0, 300), 0, 0, True),
+    (3, 43, 2, 1, 64, BF, 16, (0, 300), 0, 0, True),
+    (8, 19, 2, 1, 64, BF, 16, (0, 600), 0, 0, True),
+    (9, 17, 2, 1, 64, BF, 16, (0, 600), 0, 0, True),
+    # units that one CTA sees through, one after another, and rows enough for the weights of cut ones to
+    # take a launch of their own
+    (5, 40, 7, 1, 128, BF, 64, (2000, 3500), 0, 0, True),
 ]
 
 
@@ -277,6 +302,13 @@ def test_more_units_than_one_plan_holds():
     check(c, q, kn, vn, weights=True)
 
 
+def test_more_units_than_lengths_staged_in_shared_memory():
+    Ly, B, H = 50, 125, 8  # 50000 units
+    c = Cache(14, Ly, B, H, H, 64, BF, 16, _lens(14, Ly, B, H, 0, 3, 16))
+    q, kn, vn = c.token()
+    check(c, q, kn, vn, weights=True)
+
+
 def test_offsets_beyond_32_bits():
     """Rows behind the first 2^31 elements of the pools, in the last layer and the last pages."""
     H, page, d, n = 2, 64, 128, 200
@@ -349,6 +381,45 @@ def test_units_in_error_are_skipped_and_the_others_are_right(dtype, weights, wha
     # the call after it is sound
     c2 = Cache(21, 1, 2, 10, 2, 128, dtype, 16, 300)
     check(c2, *c2.token())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hi", [100, 700])  # units that go whole to warps, and ranges cut across units
+@pytest.mark.parametrize("what", ["length", "page"])
+def test_errors_among_many_units(dtype, hi, what):
+    lens = _lens(24, 10, 20, 2, 60, hi, 16)
+    good, c = (Cache(24, 10, 20, 14, 2, 128, dtype, 16, lens) for _ in range(2))
+    q, kn, vn = c.token()
+    bad = torch.zeros((10, 20, 2), dtype=torch.bool)
+    if what == "length":
+        c.lens[3, 5, 1] = c.cap + 7
+        c.lens[9, 19, 0] = -1
+        bad[3, 5, 1] = bad[9, 19, 0] = True
+    else:
+        c.table[7, 3] = -1  # rows 48 to 63, which every unit has
+        bad[:, 7] = True
+    before = (c.lens.clone(), c.weights.clone())
+    ws = c.workspace(reco.RECO_OP_PAGED_WEIGHTS)
+    out, lse = decode(c, q, kn, vn, ws=ws)
+    assert what in _refused()
+    wo, wl = decode(good, q, kn, vn)
+    reco.reco_check()
+    bq, bad = bad.to(DEV).repeat_interleave(7, 2), bad.to(DEV)
+    assert (out[bq] == 0).all() and torch.isneginf(lse[bq]).all()
+    assert torch.allclose(out[~bq], wo[~bq], rtol=1e-4, atol=2e-5) and torch.allclose(lse[~bq], wl[~bq], rtol=1e-5)
+    assert torch.equal(c.lens[bad], before[0][bad]) and torch.equal(c.lens[~bad], good.lens[~bad])
+    live = torch.arange(c.cap, device=DEV) < torch.from_numpy(lens).to(DEV).unsqueeze(-1)
+    assert torch.equal(c.weights[bad.unsqueeze(-1) & live], before[1][bad.unsqueeze(-1) & live])
+    assert torch.allclose(c.weights[~bad], good.weights[~bad], rtol=1e-4, atol=1e-7)
+    # the next call through the same workspace
+    if what == "page":
+        c.table[7, 3] = good.table[7, 3]
+    c.lens.copy_(good.lens)
+    c.K.copy_(good.K), c.V.copy_(good.V), c.weights.copy_(good.weights)
+    o1, l1 = decode(c, q, None, None, ws=ws)
+    o2, l2 = decode(good, q, None, None)
+    reco.reco_check()
+    assert torch.equal(o1, o2) and torch.equal(l1, l2) and torch.equal(c.weights, good.weights)
 
 
 def test_a_workspace_survives_an_error():
@@ -459,6 +530,10 @@ EVICT = [
     (1, 1, 1, 64, BF, 64, (60000, 60000), [41111], 128, 4),   # more candidates than shared memory holds
     (28, 8, 4, 64, BF, 16, (30, 250), [60, 10 ** 6, 100, 10 ** 6, 10 ** 6, 10 ** 6, 33, 10 ** 6], 32, 1),
     (28, 10, 5, 64, BF, 16, (500, 1000), [600] * 10, 3, 3),   # a warp per unit
+    # many cut units, by columns: rows of 256 and 512 bytes, and of so few that a step does not fill
+    (10, 10, 3, 128, BF, 32, (100, 300), [90] * 10, 8, 2),
+    (8, 6, 3, 128, F32, 16, (100, 300), [40, 77, 90, 33, 50, 10 ** 6], 8, 2),
+    (20, 10, 3, 64, BF, 16, (20, 60), [17] * 10, 2, 1),
 ]
 
 
