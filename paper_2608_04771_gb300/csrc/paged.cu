@@ -2,26 +2,34 @@
 // Sec. 1, 2.2 and 4.2, rows in pages), and the accumulation of the rows' attention weights (Eq. 2's
 // sums, taken token by token as the tokens are decoded).
 //
-// paged_decode: persistent, one CTA per SM of eight warps that compute and one that copies.  The
-// blocks of rows of all units (8 KB of K and V at d = 128) are laid end to end and every CTA takes
-// an equal range of them; inside it the blocks go to the warps in turn, each into its own ring of
-// three stages, filled by TMA copies (bf16) or bulk copies (float32).  Lane w of the copying warp
-// feeds warp w: it walks the same units, looks the pages up (a block never straddles two), and waits
-// for free stages, so that the computing warps spend nothing on either.  What a warp does with a
-// block is decode_block.cuh's.  At the end of a unit's piece the warps join their (max, sum, output)
-// through shared memory; a unit cut between CTAs leaves one partial per CTA, which the last CTA to
-// finish (atomic ticket, no waiting) joins.  Units of many query heads (bf16 9 to 16, float32 5 to 16)
-// run on fewer streams of two or four warps each, a part of the heads per warp, all reading the stage
-// that was copied once.
+// x_gj = scale q_g . k_j over the rows j in sight, an online softmax (running max and sum in float32, to base 2),
+// out_g = sum_j p_gj v_j.  A row's 4 d bytes (bf16) serve 4 G d operations, G at most 16: the bytes of K and V are the
+// bound, and everything here is there to keep them coming.
 //
-// Many short units would spend their time joining: there every unit goes whole to one warp.
+// paged_decode: persistent, one CTA per SM of eight computing warps (float32: twelve), one that copies and, for
+// calls with weights, three more.  The blocks of 16 rows (bf16: 8 KB of K and V at d = 128) of all units are shared out
+// to the CTAs:
+//   units that fit the grid are cut into equal pieces, one piece per CTA, so that every CTA joins and publishes once;
+//   more units: the blocks are laid end to end and every CTA takes an equal range, cut across units;
+//   many short units would spend their time joining: each goes whole to one stream of its CTA.
+// Inside a CTA's range the blocks go round the streams.  A stream is a ring of stages, filled by TMA copies (bf16) or
+// bulk copies (float32), and the warps that read it: one, or several that take a part of the query heads each (float32
+// of more than two heads: F32Wide).  Lane s of the copying warp feeds stream s: it walks the same units, looks the pages
+// up (a block never straddles two; the next block's entry loads while this one's copies go out) and waits for free
+// stages, so that the computing warps spend nothing on either: with the copies and the look-ups in the computing warps,
+// as the contiguous decode has its copies, the 7B-class stack of 16K rows took 1308 us, so 1015 (7.1 TB/s, 1.04 of the
+// copy rate).  What a warp does with a block is decode_block.cuh's.  At the end of a piece the streams join their (max,
+// sum, output) through shared memory; a unit cut between CTAs leaves one partial per CTA, which the last CTA to
+// finish (atomic ticket, no waiting) joins in the order of the pieces: the same inputs give the same bits.
 //
 // A window leaves the blocks that hold rows in sight: the first `head` ones and those `gap` further on
 // are the unit's list, in which everything above counts; a block that a border crosses masks its rows.
 //
 // A call with weights has the kernel leave its logits (4 G bytes a row, against 4 d bytes of K and V in
-// bf16) in the workspace.  A unit that one CTA or warp sees through turns them into weights there, while they are
-// still in L2 and the copies of the next unit run; paged_weights does the rest, the units cut between CTAs.
+// bf16) in the workspace: a second product with K would read half of the cache again.  The three warps turn those of a
+// unit that the CTA sees through into weights while they are still in L2 and the next unit streams; with few rows in
+// sight the CTA that joins a unit's pieces does it; paged_weights does the rest.  (7B-class stack of 4K rows: 287 us
+// without weights; 370 with all of them in paged_weights, 342 so, of which some 40 go with the logits' stores.)
 #include <algorithm>
 
 #include "decode_block.cuh"
@@ -29,16 +37,23 @@
 
 namespace reco {
 
-constexpr int kRingBytes = 24 * 8192;         // ring of a CTA
-constexpr int kPagedMaxGrid = 256;           // CTAs at most (two partial slots each in the workspace)
-constexpr int kWeightWarps = 3;              // warps that turn the logits of finished units into weights
-constexpr int kMinBlocks = 8;                // blocks per working CTA (fewer CTAs rather than less: a layer of two units of 512
-                                             // rows 10.9 us, with 16 12.1; 8 units of 1000 rows 11.5 and 13.1)
-constexpr int kWarpUnits = 128;              // up to this many units (that fit the grid) every warp plans by itself
-constexpr int kInlineRows = 2560;            // calls with no more rows in sight than this (and units that fit the grid) make their weights
-                                             // where pieces join: 32 units of 2000 rows 16.9 us, with a launch for them 19.1, 4 of 4000 19.3 and 18.5
-constexpr int kSnapBlocks = 8;               // a cut this near to a unit's end moves there
-constexpr int kWholeBlocks = 16;             // more units than CTAs, none longer than this, go whole to a warp
+constexpr int kRingBytes = 24 * 8192;  // ring of a CTA, all streams
+constexpr int kPagedMaxGrid = 256;     // CTAs at most (two partial slots each in the workspace)
+constexpr int kWeightWarps = 3;        // they cost no registers: 9 warps or 12, an SM's quarter holds three of 168
+// Blocks per working CTA at least (fewer CTAs rather than less): two units of 512 rows 10.9 us, with 16 12.1, with 2
+// 10.9; 8 units of 1000 rows 11.5, 13.1 and 11.9.
+constexpr int kMinBlocks = 8;
+// Up to this many units, if they fit the grid, every warp plans by itself, without barriers (a Tiny layer 10.7 -> 10.1).
+constexpr int kWarpUnits = 128;
+// A cut this near to a unit's end moves there.  From an eighth of a CTA's range: window of 4000 over 32K rows 185 ->
+// 165 us; 4, 16 and 32 blocks within 1% but for 448 units of 300 to 2000 rows (32: 47 -> 50).
+constexpr int kSnapBlocks = 8;
+// More units than CTAs, none longer than this, go whole to a stream: 1792 units of 60 to 200 rows 33.8 us, cut 51; the
+// same of 200 to 400 rows 73.7 whole, 64.7 cut.
+constexpr int kWholeBlocks = 16;
+// Calls with no more rows in sight than this, whose units fit the grid, make their weights where pieces join: 32 units
+// of 2000 rows 16.9 us, with a launch for them 19.1; 4 units of 4000 rows 19.3 and 18.5.
+constexpr int kInlineRows = 2560;
 
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base)
 {
@@ -1009,8 +1024,9 @@ template <class Block, int HS, int NW> static PagedLaunch with()
 template <int D> static PagedLaunch paged_kernel(bool f32, int G)
 {
     if (!f32) return G > 8 ? with<Bf16Block<D, 2>, 1, 8>() : with<Bf16Block<D, 1>, 1, 8>();
-    // float32: two heads per warp, whose queries and sums leave registers for twelve warps (plain FMAs wait for
-    // each other: 224 units of 1150 rows, 6 heads, eight warps of four heads 82 us, XX)
+    // float32: two heads per warp, whose queries and sums leave registers for twelve warps (plain FMAs wait for each
+    // other and for shared memory: 224 units of 1150 rows, 6 heads, eight warps of four heads 82 us, so 68, in blocks
+    // of 16 rows 58; pairs of FMAs in one instruction 61)
     if (G > 12) return with<F32Wide<D, 4>, 4, 8>();
     if (G > 8) return with<F32Wide<D, 2>, 6, 12>();
     if (G > 6) return with<F32Wide<D, 2>, 4, 12>();
