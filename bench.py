@@ -161,9 +161,10 @@ def decode_traffic(wl):
     c = re.search(r"capture:\s*(.+)", text)
     if not m or not h:
         return None, f"none: profiles/{name} carries no per-launch DRAM bytes"
-    src = open(os.path.join(ROOT, "paper_2608_04771_gb300", "csrc", "decode.cu")).read()
+    csrc = os.path.join(ROOT, "paper_2608_04771_gb300", "csrc")
+    src = "".join(open(os.path.join(csrc, f)).read() for f in ("decode.cu", "decode_block.cuh"))
     if decode_code_hash(src) != h.group(1)[:16]:
-        return None, f"none: profiles/{name} was taken on another decode.cu"
+        return None, f"none: profiles/{name} was taken on another decode.cu or decode_block.cuh"
     return float(m.group(1)), (f"profile-derived, not measured in this run: profiles/{name} "
                                f"(ncu dram__bytes_read.sum + dram__bytes_write.sum; {c.group(1).strip() if c else ''})")
 
