@@ -2,7 +2,7 @@
 // highest-scoring tokens with the latest w always retained, then compress the L
 // cached tokens down to m_i).
 //
-// Three selections, by the most candidates a unit may have (L_cap - w), all with the same rule: a
+// Selections, by the most candidates a unit may have (L_cap - w), all with the same rule: a
 // radix or bit search over order-preserving uint32 keys of the float32 scores finds the (m-w)-th
 // largest key T and how many keys equal to T are still needed; one ordered pass then emits every
 // candidate with key > T plus the first `need` with key == T in index order.  The result is
@@ -10,6 +10,8 @@
 //   select_topm_warp  up to 256, and up to 1024 where there are many units: one warp per unit, keys in registers
 //   select_topm_smem  up to kSelectSmemKeys: CTAs walk the units, keys in shared memory
 //   select_topm       longer: CTAs walk the units, keys read from global memory
+//   select_topm_cluster  (reco_paged_evict) few long units: a cluster of CTAs per unit, a part of its keys in the
+//                     shared memory of each, one histogram read across the cluster
 // A unit whose sequence keeps its whole cache is an identity, skipped by the compaction.
 //
 // compact_rows: CTAs per (K|V, 128-byte column slice) that walk the units, one at a
@@ -22,6 +24,7 @@
 
 #include "common.cuh"
 #include "internal.h"
+#include "tma.cuh"
 
 namespace reco {
 
@@ -553,6 +556,230 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
     }
 }
 
+// The same selection with a unit's keys spread over the CTAs of a cluster: few long units would leave most SMs idle
+// (an eviction of one unit of 131072 rows took 270 us with one CTA that reads its keys from global memory pass by pass,
+// 45 us so; 8 of them 429 and 174).  Each CTA counts its part; every CTA reads the others' counts and finds the same bin, so a digit takes one cluster barrier (two
+// histograms in turn: the one before last has been read by everyone at that barrier, and is cleared after it).
+constexpr int kClusterThreads = 512;
+// Units of that many candidates at least: two units of 30000 rows 53.8 -> 45.4 us, 32 of 16000 75.5 -> 72.2, but 64 of
+// 4500 61.8 -> 63.6 and 16 of 2500 20.5 -> 22.3 (a cluster barrier per digit costs more than the keys' passes there).
+constexpr int kClusterMin = 8192;
+template <class Rule>
+__global__ void __launch_bounds__(kClusterThreads) select_topm_cluster(const float *__restrict__ scores, const int32_t *lens,
+                                                                       int32_t *lens_out, const int32_t *__restrict__ keep,
+                                                                       Rule rule, int B, int Hkv, int L_cap, int ctas,
+                                                                       int32_t *__restrict__ idx_out, unsigned *err)
+{
+    constexpr int NT = kClusterThreads, NW = NT / 32;
+    extern __shared__ uint32_t keys[];  // this CTA's part
+    __shared__ __align__(16) int hist[2][256], sum[256];
+    __shared__ int w_gt[NW], w_eq[NW];
+    __shared__ uint32_t w_min[NW], w_max[NW];
+    __shared__ int part[4];  // smallest and largest key of the part; keys above T and equal to it
+    __shared__ uint32_t s_prefix;
+    __shared__ int s_remaining, s_at;
+    wait_prior_grid();
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int r = (int)cluster_rank();
+    const long u = blockIdx.x / ctas;
+    const int b = (int)((u / Hkv) % B);
+    const int L = lens[u], m = keep[b], w = rule.w, first = rule.first;
+    // (the same in every CTA of the cluster)
+    unsigned bad = rule.error(L, m, L_cap);
+    if (bad == 0u && L <= m) return;
+    if (bad == 0u && __syncthreads_or(rule.bad_page(b, L, tid, NT))) bad = ERR_PAGE;
+    if (bad != 0u) {
+        if (tid == 0 && r == 0) raise_error(err, bad);
+        return;
+    }
+    const int nc = L - w - first, kc = m - w - first;
+    const int seg = (nc + ctas - 1) / ctas, c0 = min(nc, r * seg), n = min(nc, c0 + seg) - c0;  // candidates [c0, c0 + n)
+    const float *s = scores + u * L_cap + first + c0;
+    int32_t *idx = idx_out + u * L_cap;
+    uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll 8
+    for (int j = tid; j < n; j += NT) {
+        const uint32_t key = rule.key(rule.load(s + j));
+        keys[j] = key;
+        lo = min(lo, key);
+        hi = max(hi, key);
+    }
+    for (int i = tid; i < 512; i += NT) hist[i >> 8][i & 255] = 0;
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) {
+        w_min[wid] = lo;
+        w_max[wid] = hi;
+    }
+    __syncthreads();
+    if (wid == 0) {
+        lo = __reduce_min_sync(0xffffffffu, lane < NW ? w_min[lane] : 0xffffffffu);
+        hi = __reduce_max_sync(0xffffffffu, lane < NW ? w_max[lane] : 0u);
+        if (lane == 0) {
+            part[0] = (int)lo;
+            part[1] = (int)hi;
+        }
+    }
+    cluster_sync();  // (and every weight of the unit has been read)
+    lo = 0xffffffffu;
+    hi = 0;
+    const uint32_t part_a = smem_addr(part);
+    for (int c = 0; c < ctas; ++c) {
+        lo = min(lo, (uint32_t)ld_cluster_s32(cluster_addr(part_a, c)));
+        hi = max(hi, (uint32_t)ld_cluster_s32(cluster_addr(part_a + 4, c)));
+    }
+    uint32_t T = 0xffffffffu;
+    int need = 0;
+    if (kc > 0) {
+        int bits = 32 - __clz(lo ^ hi), buf = 0;
+        uint32_t prefix = bits < 32 ? hi >> bits << bits : 0u;
+        uint32_t mask = bits < 32 ? ~0u << bits : 0u;
+        int remaining = kc;
+        while (bits > 0) {
+            const int shift = max(0, bits - 8);
+            for (int j = tid; j < n; j += NT) {
+                const uint32_t key = keys[j];
+                if ((key & mask) == prefix) atomicAdd(&hist[buf][(key >> shift) & 255u], 1);
+            }
+            cluster_sync();
+            if (tid < 256) {
+                const uint32_t at = smem_addr(&hist[buf][tid]);
+                int x = 0;
+                for (int c = 0; c < ctas; ++c) x += ld_cluster_s32(cluster_addr(at, c));
+                sum[tid] = x;
+                hist[buf ^ 1][tid] = 0;
+            }
+            __syncthreads();
+            if (wid == 0) {  // find the bin holding the remaining-th largest key
+                const int4 *h4 = reinterpret_cast<const int4 *>(sum) + 62 - 2 * lane;  // bins 255 - 8 * lane and the seven below
+                const int4 x = h4[1], y = h4[0];
+                const int c8[8] = {x.w, x.z, x.y, x.x, y.w, y.z, y.y, y.x};
+                const int all = (x.x + x.y) + (x.z + x.w) + (y.x + y.y) + (y.z + y.w);
+                int incl = all;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += v;
+                }
+                int cum = incl - all;
+                if (cum < remaining && remaining <= incl) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (cum + c8[i] >= remaining) {
+                            s_prefix = (uint32_t)(255 - 8 * lane - i) << shift;
+                            s_remaining = c8[i] == remaining - cum ? kWholeBin : remaining - cum;
+                            break;
+                        }
+                        cum += c8[i];
+                    }
+                }
+            }
+            __syncthreads();
+            prefix |= s_prefix;
+            remaining = s_remaining;
+            if (remaining == kWholeBin) break;
+            mask |= 255u << shift;
+            bits = shift;
+            buf ^= 1;
+        }
+        T = prefix;
+        need = remaining;
+    }
+    // emit in index order: keys > T, then the first `need` keys == T
+    const int wseg = (n + NW - 1) / NW;
+    const int j0 = min(n, wid * wseg), j1 = min(n, j0 + wseg);
+    int n_gt = 0, n_eq = 0;
+    for (int j = j0 + lane; j < j1; j += 32) {
+        const uint32_t key = keys[j];
+        n_gt += key > T;
+        n_eq += key == T;
+    }
+    n_gt = __reduce_add_sync(0xffffffffu, n_gt);
+    n_eq = __reduce_add_sync(0xffffffffu, n_eq);
+    if (lane == 0) {
+        w_gt[wid] = n_gt;
+        w_eq[wid] = n_eq;
+    }
+    __syncthreads();
+    if (wid == 0) {
+        const int g = __reduce_add_sync(0xffffffffu, lane < NW ? w_gt[lane] : 0);
+        const int e = __reduce_add_sync(0xffffffffu, lane < NW ? w_eq[lane] : 0);
+        if (lane == 0) {
+            part[2] = g;
+            part[3] = e;
+        }
+    }
+    cluster_sync();
+    int eq0 = 0, out0 = 0;  // equal keys and output rows before this CTA's part
+    for (int c = 0; c < r; ++c) {
+        const int g = ld_cluster_s32(cluster_addr(part_a + 8, c)), e = ld_cluster_s32(cluster_addr(part_a + 12, c));
+        out0 += g + min(max(need - eq0, 0), e);
+        eq0 += e;
+    }
+    if (wid == 0) {  // per warp: equal keys before its segment, and output rows before it
+        const int e = lane < NW ? w_eq[lane] : 0, g = lane < NW ? w_gt[lane] : 0;
+        int e_inc = e;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, e_inc, o);
+            if (lane >= o) e_inc += v;
+        }
+        const int e_base = eq0 + e_inc - e;
+        const int f = g + min(max(need - e_base, 0), e);
+        int f_inc = f;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, f_inc, o);
+            if (lane >= o) f_inc += v;
+        }
+        if (lane < NW) {
+            w_eq[lane] = e_base;
+            w_gt[lane] = out0 + f_inc - f;
+        }
+    }
+    if (tid == 0 && r == 0) s_at = rule.claim(u, m);
+    __syncthreads();
+    int e_run = w_eq[wid], pos = w_gt[wid];
+    const unsigned below = (1u << lane) - 1u;
+    for (int jb = j0; jb < j1; jb += 32) {
+        const int j = jb + lane;
+        const bool valid = j < j1;
+        const uint32_t key = valid ? keys[j] : 0u;
+        const bool is_eq = valid && key == T;
+        const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
+        const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
+        const unsigned fb = __ballot_sync(0xffffffffu, flag);
+        const int p = first + pos + __popc(fb & below);
+        if (flag) {
+            idx[p] = first + c0 + j;
+            rule.weights[u * L_cap + p] = rule.value(key);
+        }
+        if (valid) rule.passed(u, first + c0 + j, p);
+        e_run += __popc(eb);
+        pos += __popc(fb);
+    }
+    if (r == 0) {
+        for (int j = tid; j < first; j += NT) {
+            idx[j] = j;
+            rule.passed(u, j, j);
+        }
+        float *wt = rule.weights + u * L_cap;
+        for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
+            const int t = t0 + tid;
+            const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+            __syncthreads();
+            if (t < w) {
+                wt[m - w + t] = x;
+                idx[m - w + t] = L - w + t;
+                rule.passed(u, L - w + t, m - w + t);
+            }
+        }
+        rule.enlist(u, L, m, s_at, tid, NT);
+        if (tid == 0) lens_out[u] = m;
+    }
+    cluster_sync();  // the parts have been read out of every CTA
+}
+
 // The same selection for short units (L_cap - w <= 32 * K): one warp per unit, its keys in
 // registers (lane l holds candidates l, l + 32, ...), the threshold found bit by bit from the top
 // one in which keys differ: a count of the keys at or above each trial value, no shared memory and
@@ -923,8 +1150,34 @@ cudaError_t launch_select_budget(const reco_paged_kv &pkv, float *weights, int32
                                  int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s)
 {
     const reco_kv kv{pkv.k, pkv.v, pkv.n_layers, pkv.B, pkv.H_q, pkv.H_kv, paged_cap(pkv), pkv.d, pkv.dtype};
+    const int units = kv.n_layers * kv.B * kv.H_kv, sms = device_sm_count(), most = kv.L_cap - w - sinks;
     const BudgetRule rule{w, sinks, pkv.table, pkv.max_pages, pkv.n_pages, pkv.page, weights, ws.rank, ws.flags, ws.list,
-                          ws.ulist, ws.counters, evict_shift(pkv), evict_chunks(pkv), kv.n_layers * kv.B * kv.H_kv};
+                          ws.ulist, ws.counters, evict_shift(pkv), evict_chunks(pkv), units};
+    // few long units: as many CTAs per unit (2, 4 or 8) as the GPU holds at once
+    int ctas = 1;
+    while (ctas < 8 && 2 * ctas * units <= sms && most >= kClusterMin) ctas *= 2;
+    const int part = (most + ctas - 1) / ctas;  // keys of a CTA
+    if (ctas > 1 && part <= kSelectSmemKeys) {
+        auto fn = select_topm_cluster<BudgetRule>;
+        const cudaError_t e = allow_smem((const void *)fn, kSelectSmemKeys * (int)sizeof(uint32_t));
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(units * ctas));
+        cfg.blockDim = dim3(kClusterThreads);
+        cfg.dynamicSmemBytes = (size_t)part * sizeof(uint32_t);
+        cfg.stream = s;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)ctas;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        return cudaLaunchKernelEx(&cfg, fn, (const float *)weights, (const int32_t *)lens, lens, budget, rule, kv.B, kv.H_kv,
+                                  kv.L_cap, ctas, idx, err);
+    }
     return launch_select(kv, weights, lens, lens, budget, rule, idx, nullptr, err, s);
 }
 

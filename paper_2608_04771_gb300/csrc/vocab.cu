@@ -303,21 +303,6 @@ constexpr int kSampleClusterRecs = 48;    // records per CTA at most (192 KB of 
 constexpr int kSampleCluster = 8;         // CTAs per row at most (the portable cluster size)
 constexpr long long kSampleSpin = 1LL << 24;  // bounded wait on the bulk copies (about a second)
 
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-
-// Address of the same shared-memory location in CTA `rank` of the cluster.
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-
 __device__ __forceinline__ void st_cluster_f2(uint32_t addr, float x, float y)
 {
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
@@ -331,13 +316,6 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr)
                  : "r"(addr)
                  : "memory");
     return v;
-}
-
-// All threads of all CTAs of the cluster; shared-memory writes before it (local or
-// remote) are visible to every CTA after it.
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Untiled bulk copy global -> shared (both 16-byte aligned, bytes a multiple of 16).

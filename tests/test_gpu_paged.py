@@ -530,6 +530,13 @@ EVICT = [
     (1, 1, 1, 64, BF, 64, (60000, 60000), [41111], 128, 4),   # more candidates than shared memory holds
     (28, 8, 4, 64, BF, 16, (30, 250), [60, 10 ** 6, 100, 10 ** 6, 10 ** 6, 10 ** 6, 33, 10 ** 6], 32, 1),
     (28, 10, 5, 64, BF, 16, (500, 1000), [600] * 10, 3, 3),   # a warp per unit
+    # few long units: clusters of CTAs
+    (1, 1, 1, 64, BF, 16, (131000, 131000), [50000], 32, 4),
+    (1, 2, 1, 64, F32, 64, (2100, 9000), [2000, 1500], 0, 0),
+    (2, 2, 2, 128, BF, 256, (9000, 30000), [8000, 29000], 64, 16),
+    (1, 5, 4, 64, BF, 32, (5000, 8300), [4000, 10 ** 6, 64, 4999, 7000], 60, 4),
+    (1, 3, 1, 64, BF, 16, (60000, 90000), [59999, 2, 41111], 1, 1),
+    (1, 1, 2, 64, BF, 128, (400000, 400000), [100000], 128, 4),  # more keys than the cluster holds
     # many cut units, by columns: rows of 256 and 512 bytes, and of so few that a step does not fill
     (10, 10, 3, 128, BF, 32, (100, 300), [90] * 10, 8, 2),
     (8, 6, 3, 128, F32, 16, (100, 300), [40, 77, 90, 33, 50, 10 ** 6], 8, 2),
