@@ -127,7 +127,8 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
 /* Workspace bytes a paged call needs for this cache: RECO_OP_PAGED_DECODE,
  * RECO_OP_PAGED_WEIGHTS (it holds the logits of a token, 4 bytes per query head and row
  * of max_pages * page) or RECO_OP_PAGED_EVICT.  Only the sizes in kv are read.  The size
- * does not depend on the device or on lens.  Alignment: 256 bytes.                   */
+ * does not depend on the device or on lens.  Alignment: 256 bytes.  The decode's two
+ * are refused for more than 16 query heads per KV head, as the calls are.            */
 reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size_t *bytes_out);
 
 /* Thread-local message describing the last non-OK status ("" if none).        */

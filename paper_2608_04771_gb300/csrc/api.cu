@@ -268,9 +268,11 @@ reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size
     if (!bytes_out) return fail(RECO_EINVAL, "NULL pointer");
     reco_status st = check_paged(kv, false);
     if (st != RECO_OK) return st;
-    if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS)
+    if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS) {
+        const int G = kv->H_q / kv->H_kv;
+        if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
         *bytes_out = reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
-    else if (op == RECO_OP_PAGED_EVICT)
+    } else if (op == RECO_OP_PAGED_EVICT)
         *bytes_out = reco::evict_ws_layout(*kv, nullptr).bytes;
     else
         return fail(RECO_EINVAL, "op %d is not a paged call", (int)op);

@@ -114,6 +114,11 @@ def test_workspace_sizes(L):
     # beyond 32 bits: 28 x 8 x 28 heads of 131072 rows
     big = dict(n_layers=28, B=8, H_q=28, H_kv=4, max_pages=8192, n_pages=9000)
     assert size(reco.RECO_OP_PAGED_WEIGHTS, **big) > 28 * 8 * 28 * 131072 * 4
+    for op in (reco.RECO_OP_PAGED_DECODE, reco.RECO_OP_PAGED_WEIGHTS):  # no size for heads that the call refuses
+        for H_q in (34, 2 ** 31 - 2):
+            with pytest.raises(reco.RecoError) as e:
+                size(op, H_q=H_q)
+            assert e.value.status == reco.RECO_EUNSUPPORTED
     with pytest.raises(reco.RecoError) as e:
         size(reco.RECO_OP_DECODE)
     assert e.value.status == reco.RECO_EINVAL
@@ -165,7 +170,7 @@ def test_decode_arguments_that_are_refused(L, kw, text, status):
         if "weights" in kw and not wts:
             continue
         op = reco.RECO_OP_PAGED_WEIGHTS if wts else reco.RECO_OP_PAGED_DECODE
-        n = reco.reco_paged_workspace_bytes(op, kv) + a["ws_bytes"]
+        n = reco.reco_paged_workspace_bytes(op, _kv()) + a["ws_bytes"]
         args = [ctypes.byref(kv), p(a["q"]), p(a["k_new"]), p(a["v_new"]), p(a["lens"]), a["scale"], a["window"],
                 a["sinks"], p(a["out"]), a["out_dtype"], p(a["lse"])] + ([p(a["weights"])] if wts else []) + \
             [p(a["ws"]), n, None]
