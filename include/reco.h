@@ -5,15 +5,18 @@
  * (Eq. 2), per-head top-m selection with in-place compaction (Sec. 3.2), decode
  * attention over the ragged compacted cache, the reward-banded reflection
  * penalty (Eq. 3-4) with the draw of the next token from the penalised logits
- * (Sec. 3.3), and the answer-perplexity stop test (Eq. 5-6).
+ * (Sec. 3.3), and the answer-perplexity stop test (Eq. 5-6).  Beside them, for caches
+ * whose rows lie in pages of a shared pool: decode attention, the running sums of its
+ * weights, and eviction down to a budget by those sums (the reco_paged_ calls).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - Pointers are DEVICE pointers owned by the caller unless marked "host".
  *    The library never allocates device memory: calls that need scratch take a
- *    caller-owned workspace sized by reco_workspace_bytes() (the decode's must
- *    be zero-filled before its first use; each call leaves it reusable), except
- *    reco_answer_ppl_static, which uses a fixed array inside the library.
+ *    caller-owned workspace sized by reco_workspace_bytes() or, for the paged
+ *    calls, reco_paged_workspace_bytes() (the decode's must be zero-filled
+ *    before its first use, the paged calls' in the parts that they name; each
+ *    call leaves it reusable), except reco_answer_ppl_static, which uses a fixed array inside the library.
  *  - Device calls are asynchronous on the given stream and return after the
  *    launches are queued.  They return RECO_OK, or an error status before
  *    launching anything when a host-side check fails (nothing is modified then).
