@@ -599,6 +599,50 @@ def test_evict_leaves_units_in_error_untouched(what):
             assert torch.equal(got[i[0], pages, i[2]].view(torch.int16), ref[i[0], pages, i[2]].view(torch.int16))
 
 
+@pytest.mark.parametrize("what", ["negative", "long", "budget", "page"])
+def test_evict_of_long_units_leaves_those_in_error_untouched(what):
+    lens = np.array([[[9000, 8700], [8193, 8900], [12, 8888]]])
+    c, good = (Cache(231, 1, 3, 4, 2, 64, BF, 64, lens) for _ in range(2))
+    budget, bad = [150, 8192, 8000], [(0, 1, 1)]
+    if what in ("negative", "long"):
+        c.lens[0, 1, 1] = -1 if what == "negative" else c.cap + 1
+    elif what == "budget":
+        budget, bad = [150, 11, 8000], [(0, 1, 0), (0, 1, 1)]
+    else:
+        c.table[1, 100] = -1
+        bad = [(0, 1, 0), (0, 1, 1)]
+    before = (c.K.clone(), c.V.clone(), c.weights.clone(), c.lens.clone())
+    ws = c.workspace(reco.RECO_OP_PAGED_EVICT)
+    reco.reco_paged_evict(c.kv, c.weights, c.lens, torch.tensor(budget, dtype=torch.int32, device=DEV), 8, 4, None, ws)
+    text = _refused()
+    assert {"budget": "keep", "page": "page"}.get(what, "length") in text
+    reco.reco_paged_evict(good.kv, good.weights, good.lens, torch.tensor([150, 8192, 8000], dtype=torch.int32, device=DEV),
+                          8, 4, None, ws)
+    reco.reco_check()
+    assert good.lens.flatten().tolist() == [150, 150, 8192, 8192, 12, 8000]
+    t = good.table.cpu().numpy()
+    for i in np.ndindex(1, 3, 2):
+        want = before if i in bad else (good.K, good.V, good.weights, good.lens)
+        assert c.lens[i] == want[3][i] and torch.equal(c.weights[i], want[2][i])
+        pages = torch.from_numpy(t[i[1]][:(int(lens[i]) + 63) // 64].astype(np.int64)).to(DEV)
+        for got, ref in ((c.K, want[0]), (c.V, want[1])):
+            assert torch.equal(got[i[0], pages, i[2]].view(torch.int16), ref[i[0], pages, i[2]].view(torch.int16))
+
+
+def test_evict_of_long_units_ranks_infinities_and_nan():
+    c = Cache(221, 1, 1, 2, 1, 64, F32, 16, 20000)
+    c.weights[..., 5000:5010] = float("inf")
+    c.weights[..., 30:40] = float("-inf")
+    c.weights[0, 0, 0, 19999] = float("nan")
+    c.weights[0, 0, 0, 51] = -float("nan")
+    rows = [51] + list(range(5000, 5010)) + [19999]
+    idx = torch.zeros((1, 1, 1, c.cap), dtype=torch.int32, device=DEV)
+    reco.reco_paged_evict(c.kv, c.weights, c.lens, torch.tensor([12], dtype=torch.int32, device=DEV), 0, 0, idx,
+                          c.workspace(reco.RECO_OP_PAGED_EVICT))
+    reco.reco_check()
+    assert idx[0, 0, 0, :12].tolist() == rows
+
+
 # ---------------------------------------------------------------- together
 @pytest.mark.parametrize("dtype,window", [(BF, 0), (F32, 0), (BF, 60)])
 def test_a_run_of_tokens_with_evictions(dtype, window):
