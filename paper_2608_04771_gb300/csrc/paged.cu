@@ -964,8 +964,9 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
             if (ok && (last & 4)) {  // units whose table names no page for a row in sight keep their length
                 const Sight sg = sight_of<KB>(a, L + 1);
                 const Pages pg = pages_of(a, u);
-                for (int k = 0; k <= L; k += KB)
-                    if (k < KB * sg.head || k >= KB * (sg.head + sg.gap)) ok &= paged_row(a, pg, k, page_entry(a, pg, k)) >= 0;
+                const int page = 1 << a.shift;
+                for (int k = 0; k <= L; k += page)
+                    if (k < KB * sg.head || k + page > KB * (sg.head + sg.gap)) ok &= paged_row(a, pg, k, page_entry(a, pg, k)) >= 0;
             }
             if (ok) a.lens[u] = L + 1;
         }
