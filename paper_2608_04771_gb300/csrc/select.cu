@@ -558,8 +558,9 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
 
 // The same selection with a unit's keys spread over the CTAs of a cluster: few long units would leave most SMs idle
 // (an eviction of one unit of 131072 rows took 270 us with one CTA that reads its keys from global memory pass by pass,
-// 42 us so; 8 of them 429 and 170; with 512 threads 45 and 173).  Each CTA counts its part; every CTA reads the others' counts and finds the same bin, so a digit takes one cluster barrier (two
-// histograms in turn: the one before last has been read by everyone at that barrier, and is cleared after it).
+// 42 us so; 8 of them 429 and 170; with 512 threads 45 and 173).  Each CTA counts its part; every CTA reads the others'
+// counts and finds the same bin, so a digit takes one cluster barrier (two histograms in turn: the one before last has
+// been read by everyone at that barrier, and is cleared after it).
 constexpr int kClusterThreads = 1024;
 // Units of that many candidates at least: eight units of 30000 rows 53.8 -> 44.4 us, 32 of 16000 75.5 -> 71.6, but 64
 // of 4500 61.8 -> 63.6 and 16 of 2500 20.5 -> 22.3 (a cluster barrier per digit costs more than the keys' passes there).
