@@ -15,7 +15,7 @@
  *    The library never allocates device memory: calls that need scratch take a
  *    caller-owned workspace sized by reco_workspace_bytes() or, for the paged
  *    calls, reco_paged_workspace_bytes() (the decode's must be zero-filled
- *    before its first use, the paged calls' in the parts that they name; each
+ *    before its first use, the paged calls' in its first 4096 bytes; each
  *    call leaves it reusable), except reco_answer_ppl_static, which uses a fixed array inside the library.
  *  - Device calls are asynchronous on the given stream and return after the
  *    launches are queued.  They return RECO_OK, or an error status before
@@ -324,8 +324,10 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
  *   window, sinks: window 0 sees every row (sinks must be 0 then)
  *   out          : [n_layers][B][H_q][d] of out_dtype (RECO_F32 or RECO_BF16)
  *   lse          : [n_layers][B][H_q] float32 or NULL
- *   ws           : reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) bytes,
- *                  zero-filled before its first use; every call leaves it reusable;
+ *   ws           : reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) bytes, of which
+ *                  the first 4096 are zero-filled before its first use; every call leaves
+ *                  it reusable, by any paged call and descriptor that it is large enough
+ *                  for (another number of sequences, layers or heads, another type);
  *                  calls (captured graphs too) that share one must not overlap on the GPU
  * Sequences may share pages that are only read; a page that receives a new row belongs
  * to one sequence.  A unit without rows gives zeros and lse = -inf.  A unit with a length
@@ -346,9 +348,8 @@ reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const
  * those of all rows of a unit that is in error.
  *   weights : [n_layers][B][H_kv][max_pages * page] float32, 16-byte aligned (device,
  *             in/out)
- *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, of which the
- *             first reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) are zero-filled
- *             before its first use; otherwise as reco_paged_decode_attn's
+ *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, otherwise as
+ *             reco_paged_decode_attn's
  * Every other argument and result is that of reco_paged_decode_attn.  The same inputs
  * give the same sums bit for bit.                                                    */
 reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *q, const void *k_new,
@@ -373,9 +374,8 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  *   w, sinks : >= 0, w + sinks <= max_pages * page
  *   kept_idx : [n_layers][B][H_kv][max_pages * page] int32 (device) or NULL; if given,
  *              the first m entries of each unit that is cut receive `kept`
- *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes, of which the
- *              first 256 are zero-filled before its first use; every call leaves it
- *              reusable; calls that share one must not overlap on the GPU
+ *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes, otherwise as
+ *              reco_paged_decode_attn's
  * No two table entries for rows of live sequences may name the same page.  A unit with a
  * length outside [0, max_pages * page], one to be cut below sinks + w, or one to be cut
  * whose table names a page outside [0, n_pages) for one of its rows is left untouched

@@ -29,7 +29,7 @@ EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base)
     };
     const size_t units = (size_t)kv.n_layers * kv.B * kv.H_kv, chunks = evict_chunks(kv);
     EvictWs ws;
-    ws.counters = (int32_t *)take(16);
+    ws.counters = (int32_t *)take(kPagedZeroBytes);  // (16 bytes of them)
     ws.idx = (int32_t *)take(units * paged_cap(kv) * 4);
     ws.rank = (int32_t *)take(units * (chunks + 1) * 4);
     ws.flags = (int32_t *)take(units * chunks * 4);

@@ -18,7 +18,11 @@ constexpr int kDecodePartSlots = 4096;
 constexpr int kSampleSeg = 4096;
 constexpr int kSampleMaxSeg = 1024;
 
-inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+constexpr size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// First bytes of a paged call's workspace, zero between calls where the call counts in them: nothing else lies
+// there, whatever the call and its descriptor, so that one workspace serves them all.
+constexpr size_t kPagedZeroBytes = 4096;
 
 struct ScoreWs {  // regions carved from the caller's workspace
     float *part_m, *part_z;  // [units][parts][R]     a part's row reference (log2) / row sum: up to two parts per 2048
@@ -64,7 +68,7 @@ struct DecodeWs {
 // Regions of the paged decode's workspace; the last two for calls with weights: the token's
 // normalisers and logits.
 struct PagedDecodeWs {
-    int32_t *counters;  // [2 + units]: [0] stops and errors, [1] CTAs done, [2 + u] tickets
+    int32_t *counters;  // [2 + CTAs]: [0] stops and errors, [1] CTAs done, [2 + c] ticket of the unit that CTA c starts
     int32_t *cuts;      // [2 + CTAs]: calls with weights: the units cut between CTAs
     float *part_ml;     // [2 * CTAs][G][2]   (m log2, l)
     float *part_o;      // [2 * CTAs][G][d]   unnormalised output

@@ -63,11 +63,14 @@ PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void
         off += align256(bytes);
         return r;
     };
-    const size_t units = (size_t)kv.n_layers * kv.B * kv.H_kv, heads = (size_t)kv.n_layers * kv.B * kv.H_q;
+    const size_t heads = (size_t)kv.n_layers * kv.B * kv.H_q;
     const size_t G = kv.H_q / kv.H_kv;
     PagedDecodeWs ws;
-    ws.counters = (int32_t *)take((2 + units) * 4);
+    // what has to be zero on entry, in a place that no descriptor moves: whatever call used the workspace last left it zero
+    ws.counters = (int32_t *)take((2 + kPagedMaxGrid) * 4);
     ws.cuts = (int32_t *)take((2 + kPagedMaxGrid) * 4);
+    static_assert(2 * align256((2 + kPagedMaxGrid) * 4) <= kPagedZeroBytes, "counters and cuts");
+    off = kPagedZeroBytes;
     ws.part_ml = (float *)take(2 * kPagedMaxGrid * G * 2 * 4);
     ws.part_o = (float *)take(2 * kPagedMaxGrid * G * kv.d * 4);
     ws.lse2 = weights ? (float *)take(heads * 4) : nullptr;
@@ -86,7 +89,7 @@ struct PagedArgs {
     float *lse2;     // with logits: log2 of the softmax sums of the units that are cut between CTAs
     float *logits;   // or nullptr: [unit][cap / 16][G][16] base-2 logits of the rows seen (logit_place)
     float *weights;  // with logits: the running sums; an appended row's starts at zero
-    int32_t *counters;  // [0] warps that stopped and units in error, [1] CTAs done, [2 + u] tickets
+    int32_t *counters;  // [0] warps that stopped and units in error, [1] CTAs done, [2 + c] ticket of the unit that CTA c starts
     float *part_ml, *part_o;
     int32_t *cuts;  // units cut between CTAs: [0] counted, [1] their number once the launch is done, [2 ...] the units
     int units, B, Hq, Hkv, G, cap, n_pages, max_pages, shift, append, out_bf16, window, sinks;
@@ -682,7 +685,7 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
     };
     auto list_cut = [&](int u) {  // for paged_weights
         const int at = atomicAdd(&a.cuts[0], 1);
-        if (at < kPagedMaxGrid) a.cuts[2 + at] = u;
+        if ((unsigned)at < (unsigned)kPagedMaxGrid) a.cuts[2 + at] = u;
     };
     const bool hand_on = a.logits != nullptr && !split && !whole;
     while (have) {
@@ -862,13 +865,13 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
             c1 = first_at(ub + T);
             pieces = 1 + max(0, first_at(ue - T + 1) - c1);
         }
-        if (tid == 0) {
-            sm_old = atom_add_acq_rel(&a.counters[2 + d.u], 1);
-        }
+        // the unit's ticket is that of the CTA with its first piece, which starts no other unit that is cut
+        int32_t *ticket = &a.counters[2 + c1 - 1];
+        if (tid == 0) sm_old = atom_add_acq_rel(ticket, 1);
         bar_compute<NC>();
         if (sm_old == pieces - 1) {
             if (tid == 0) {
-                a.counters[2 + d.u] = 0;  // every piece has counted: clear for the next launch
+                *ticket = 0;  // every piece has counted: clear for the next launch
                 if (a.logits && !a.inline_weights) list_cut(d.u);
             }
             for (int x = tid; x < G * D / 4; x += NC) {
@@ -955,7 +958,7 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
     const int last = sm_old;
     if (last == 0) return;
     if (last & 2) {  // tickets of units whose pieces stopped early may still count
-        for (int u = tid; u < P; u += NC) a.counters[2 + u] = 0;
+        for (int k = tid; k < kPagedMaxGrid; k += NC) a.counters[2 + k] = 0;
     } else if (a.append) {
 #pragma unroll 4
         for (int u = tid; u < P; u += NC) {
@@ -993,7 +996,7 @@ __global__ void __launch_bounds__(kWeightThreads) paged_weights(const float *__r
     __shared__ float sm_lse[16];
     wait_prior_grid();
     const int n_cut = cuts[1];
-    if (n_cut == 0) return;
+    if (n_cut <= 0) return;
     const int parts = max(1, (int)gridDim.x / n_cut);  // CTAs per unit
     for (int i = blockIdx.x; i < n_cut * parts; i += gridDim.x) {
         const int u = cuts[2 + i / parts];

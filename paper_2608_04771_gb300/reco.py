@@ -310,10 +310,10 @@ def reco_paged_workspace_bytes(op: int, kv: reco_paged_kv) -> int:
 
 
 def paged_workspace(op: int, kv: reco_paged_kv, device="cuda") -> torch.Tensor:
-    """A workspace for a paged call, with its counters zero as the calls need them before its first use
-    (the logits of a call with weights lie behind what a call without needs, and need no fill)."""
+    """A workspace for a paged call, with its counters, which lie in its first bytes, zero as the calls need them
+    before its first use.  It serves every paged call, with any cache, that it is large enough for."""
     ws = torch.empty(max(reco_paged_workspace_bytes(op, kv), 256), dtype=torch.uint8, device=device)
-    ws[:256 if op == RECO_OP_PAGED_EVICT else reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv)].zero_()
+    ws[:4096].zero_()
     return ws
 
 
