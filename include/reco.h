@@ -277,7 +277,8 @@ reco_status reco_compact(const reco_kv *kv, const int32_t *kept_idx, int32_t *le
  *   lse          : [n_layers][B][H_q] float32 or NULL
  *   ws           : workspace of reco_workspace_bytes(RECO_OP_DECODE, kv, 0) bytes,
  *                  zero-filled before its first use (e.g. cudaMemset); every call
- *                  leaves its counters zero again, so it can be reused as it is;
+ *                  leaves its counters zero again, so it can be reused as it is, with
+ *                  any descriptor that it is large enough for;
  *                  calls sharing one workspace must not overlap on the GPU
  * A unit with a length outside [0, L_cap] (or no room to append) writes zeros
  * and lse = -inf, and sets the device error word.                              */

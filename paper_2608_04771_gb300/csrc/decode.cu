@@ -50,8 +50,10 @@ DecodeWs decode_ws_layout(const reco_kv &kv, void *base)
     };
     DecodeWs ws;
     ws.part_slots = kDecodePartSlots;
-    // merge tickets per unit; a unit of G > 8 heads may run as two
-    ws.counters = (int32_t *)take((2 + units * (G > 8 ? 2 : 1)) * 4);
+    // Merge tickets, one per warp of the grid (of the unit that it starts), first: no call's partials lie where
+    // another's tickets have to be zero, whatever the descriptors.  (Room for the unit tickets of more units than
+    // warps is kept: sizes do not shrink.)
+    ws.counters = (int32_t *)take((2 + std::max<size_t>(ws.part_slots / 2, units * (G > 8 ? 2 : 1))) * 4);
     ws.part_ml = (float *)take((size_t)ws.part_slots * G * 2 * 4);
     ws.part_o = (float *)take((size_t)ws.part_slots * G * kv.d * 4);
     ws.bytes = off;
@@ -663,7 +665,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
     }
 
     while (cur.nblk >= 0) {
-        const int u = cur.u, k0 = cur.k0, k1 = cur.k1, Lapp = cur.Lapp;
+        const int k0 = cur.k0, k1 = cur.k1, Lapp = cur.Lapp;
         const int nsplit = cur.nsplit, item = cur.slot, wf = cur.wf, slot0 = cur.slot0;  // partial slots
         const int pu = cur.pu;  // the cache unit
         const long lb = pu / a.Hkv;
@@ -750,15 +752,16 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
             blk.each_lse(G, [&](int q, float m, float l) {
                 reinterpret_cast<float2 *>(a.part_ml)[(size_t)item * GS + q] = make_float2(m, l);
             });
+            // The unit's ticket is its first warp's, which starts no other unit that is cut.
             // publish: the warp barrier orders every lane's partial writes before lane 0's
             // release; the last arriver's acquire (and the barrier after it) orders its reads
             __syncwarp();
             int old = 0;
-            if (lane == 0) old = atom_add_acq_rel(&a.counters[2 + u], 1);
+            if (lane == 0) old = atom_add_acq_rel(&a.counters[2 + wf], 1);
             old = __shfl_sync(0xffffffffu, old, 0);
             __syncwarp();
             if (old == nsplit - 1) {  // last item of this unit: merge the partials
-                if (lane == 0) a.counters[2 + u] = 0;  // every piece has counted: clear for the next launch
+                if (lane == 0) a.counters[2 + wf] = 0;  // every piece has counted: clear for the next launch
                 // pass 1: per-query-head maxima, lanes over splits (independent loads)
                 float Mq[GM];
 #pragma unroll
@@ -858,7 +861,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
     if ((int)(dc >> 32) == total_warps - 1) {
         const bool any_stop = stopped || (uint32_t)dc != 0u;
         if (any_stop) {  // tickets of units whose pieces stopped early may still count
-            for (int u = lane; u < units; u += 32) a.counters[2 + u] = 0;
+            for (int w2 = lane; w2 < total_warps; w2 += 32) a.counters[2 + w2] = 0;
         } else if (a.append) {
             // 16 independent loads per lane in flight before any store, of 4 lengths each
             // when lens is 16-byte aligned: one L2 round trip for up to 2048 units

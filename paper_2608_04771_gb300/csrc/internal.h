@@ -57,8 +57,8 @@ struct SelectWs {
 };
 
 struct DecodeWs {
-    int32_t *counters;  // [2 + units], or [2 + 2 * units] for G > 8: [0] warps stopped early, [1] finished warps,
-                        // [2 + u] merge tickets (of halves: [2 + units + u] too)
+    int32_t *counters;  // [0] warps stopped early, [1] finished warps, [2 + w] merge ticket of the unit (or half of one)
+                        // that warp w of the grid starts
     float *part_ml;     // [part_slots][G][2]  (m log2, l)
     float *part_o;      // [part_slots][G][d]  unnormalised output
     int part_slots;
