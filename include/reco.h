@@ -281,7 +281,9 @@ reco_status reco_compact(const reco_kv *kv, const int32_t *kept_idx, int32_t *le
  *                  any descriptor that it is large enough for;
  *                  calls sharing one workspace must not overlap on the GPU
  * A unit with a length outside [0, L_cap] (or no room to append) writes zeros
- * and lse = -inf, and sets the device error word.                              */
+ * and lse = -inf, and sets the device error word.  A head with a NaN among its
+ * logits (in its query or in a row), or one that is +inf, gives NaN in out and
+ * lse; one whose logits are all -inf gives zeros and lse = -inf.               */
 reco_status reco_decode_attn(const reco_kv *kv, const void *q, const void *k_new, const void *v_new,
                              int32_t *lens, float scale, void *out, reco_dtype out_dtype, float *lse,
                              void *ws, size_t ws_bytes, cudaStream_t stream);
@@ -331,7 +333,9 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
  *                  for (another number of sequences, layers or heads, another type);
  *                  calls (captured graphs too) that share one must not overlap on the GPU
  * Sequences may share pages that are only read; a page that receives a new row belongs
- * to one sequence.  A unit without rows gives zeros and lse = -inf.  A unit with a length
+ * to one sequence.  A unit without rows gives zeros and lse = -inf, and so does a head
+ * whose logits are all -inf; a NaN among a head's logits (in its query or in a row seen),
+ * or one that is +inf, gives NaN in its out and lse.  A unit with a length
  * outside [0, max_pages * page], with no room to append, or whose table names a page
  * outside [0, n_pages) for a row it needs, writes zeros and lse = -inf, keeps its length
  * and sets the device error word.  At most 16 query heads per KV head.                */
@@ -346,7 +350,8 @@ reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const
  *   weights[unit, j] += (1/G) * sum_g softmax_j(scale * q[layer,b,h*G+g,:] . K_j)
  * for the rows j seen; an appended row starts at its own weight (what its entry held
  * before does not count).  The entries of other rows are left as they are, and so are
- * those of all rows of a unit that is in error.
+ * those of all rows of a unit that is in error.  A head whose lse is NaN makes the entries
+ * of all rows seen NaN; one whose logits are all -inf adds nothing.
  *   weights : [n_layers][B][H_kv][max_pages * page] float32, 16-byte aligned (device,
  *             in/out)
  *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, otherwise as

@@ -158,8 +158,8 @@ __global__ void __launch_bounds__(128) decode_simt(DecodeArgs a)
                 for (int i = 0; i < PER; ++i) s = fmaf(q[g][i], kk[i], s);
                 s = warp_sum(s) * a.c2;
                 const float mn = fmaxf(m[g], s);
-                const float al = fast_exp2(m[g] - mn);
-                const float p = fast_exp2(s - mn);
+                const float al = part_factor(m[g], mn);
+                const float p = part_factor(s, mn);
                 l[g] = l[g] * al + p;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) o[g][i] = fmaf(o[g][i], al, p * vv[i]);
@@ -184,16 +184,14 @@ __global__ void __launch_bounds__(128) decode_simt(DecodeArgs a)
         float M = -INFINITY;
         for (int w = 0; w < NW; ++w) M = fmaxf(M, sm_m[w][g]);
         float Ls = 0.f, O = 0.f;
-        if (M != -INFINITY) {
-            for (int w = 0; w < NW; ++w) {
-                const float wt = fast_exp2(sm_m[w][g] - M);
-                Ls += sm_l[w][g] * wt;
-                O += sm_o[w][g][dd] * wt;
-            }
+        for (int w = 0; w < NW; ++w) {
+            const float wt = part_factor(sm_m[w][g], M);
+            Ls += sm_l[w][g] * wt;
+            O += sm_o[w][g][dd] * wt;
         }
         const size_t row = (size_t)(lb * a.Hq + (long)h * G + g);
-        store_out(a.out, a.out_bf16, row * D + dd, Ls > 0.f ? O / Ls : 0.f);
-        if (dd == 0) put_lse(a, rs, row, Ls > 0.f ? (M + log2f(Ls)) * kLn2 : -INFINITY);
+        store_out(a.out, a.out_bf16, row * D + dd, Ls == 0.f ? 0.f : O / Ls);
+        if (dd == 0) put_lse(a, rs, row, sum_log2(M, Ls) * kLn2);
     }
     if (ok && a.append) {
         for (int e = threadIdx.x; e < D; e += blockDim.x) {
@@ -745,7 +743,7 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
         if (nsplit == 1) {
             blk.store(a.out, out_bf16, qrow0, G);
             blk.each_lse(G, [&](int q, float m, float l) {
-                put_lse(a, rs, qrow0 + q, l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY);
+                put_lse(a, rs, qrow0 + q, sum_log2(m, l) * kLn2);
             });
         } else {
             blk.store_partial(a.part_o + (size_t)item * GS * D, G);
@@ -792,9 +790,9 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
                     const size_t it0 = (size_t)(s2 ? 2 * (wf + s2) : slot0) * GS;
 #pragma unroll
                     for (int qq = 0; qq < GM; ++qq) {
-                        if (qq < G && Mq[qq] != -INFINITY) {
+                        if (qq < G) {
                             const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml) + it0 + qq);
-                            const float wt = fast_exp2(ml.x - Mq[qq]);
+                            const float wt = part_factor(ml.x, Mq[qq]);
                             Lq[qq] += ml.y * wt;
                             const float *src = a.part_o + (it0 + qq) * D + lane * PER;
                             if constexpr (PER == 4) {
@@ -813,13 +811,13 @@ __global__ void __launch_bounds__(kDecodeWarps * 32, 1)
 #pragma unroll
                 for (int qq = 0; qq < GM; ++qq) {
                     if (qq < G) {
-                        const float inv = Lq[qq] > 0.f ? 1.f / Lq[qq] : 0.f;
+                        const float inv = sum_inverse(Lq[qq]);
 #pragma unroll
                         for (int e = 0; e < PER; ++e)
                             store_out(a.out, out_bf16, (qrow0 + qq) * D + lane * PER + e,
                                                      acc[qq][e] * inv);
                         if (lane == 0)
-                            put_lse(a, rs, qrow0 + qq, Lq[qq] > 0.f ? (Mq[qq] + log2f(Lq[qq])) * kLn2 : -INFINITY);
+                            put_lse(a, rs, qrow0 + qq, sum_log2(Mq[qq], Lq[qq]) * kLn2);
                     }
                 }
             }

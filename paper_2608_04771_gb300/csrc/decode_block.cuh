@@ -33,6 +33,15 @@ __device__ __forceinline__ bool unit_ok(int L, int L_cap, int append)
     return L >= 0 && L <= L_cap && (!append || L < L_cap);
 }
 
+// What the sum of a softmax (l, of maximum m, to base 2) leaves: the factor of the output, and the sum's logarithm.  A
+// sum of zero is that of no rows, or of logits that are all -inf: zeros and -inf.  Anything else goes by its value,
+// so that a NaN among the logits (of a query, of a row in sight; an infinite logit is one of them when its maximum is
+// taken away) comes out as NaN.  m may still be -inf then: NaN raises no maximum.
+__device__ __forceinline__ float sum_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float sum_log2(float m, float l) { return l == 0.f ? -INFINITY : m + log2f(l); }
+// What a part's sum and output, of maximum m, are multiplied by where parts of maximum M, the largest, join.
+__device__ __forceinline__ float part_factor(float m, float M) { return fast_exp2(m - (M == -INFINITY ? 0.f : M)); }
+
 __device__ __forceinline__ void store_out(void *out, bool bf16, size_t i, float v)
 {
     if (bf16)
@@ -285,7 +294,7 @@ template <int D_, int NT_, int HALVES_ = 1> struct Bf16Block {
         for (int n = 0; n < NT; ++n) {
             const int q0 = 8 * n + 2 * c, q1 = q0 + 1;
             const float l0 = __shfl_sync(0xffffffffu, l[n], 8 * c), l1 = __shfl_sync(0xffffffffu, l[n], 8 * c + 4);
-            const float inv0 = l0 > 0.f ? 1.f / l0 : 0.f, inv1 = l1 > 0.f ? 1.f / l1 : 0.f;
+            const float inv0 = sum_inverse(l0), inv1 = sum_inverse(l1);
 #pragma unroll
             for (int hh = 0; hh < HALVES; ++hh) {
                 const long d0 = 64 * hh + 8 * g;
@@ -562,7 +571,7 @@ template <int D_, int GT_> struct F32Block {
         for (int g = 0; g < GT; ++g) {
             const float lg = __shfl_sync(0xffffffffu, l[value_of(g)], lane_of(g));
             if (g < G) {
-                const float inv = lg > 0.f ? 1.f / lg : 0.f;
+                const float inv = sum_inverse(lg);
 #pragma unroll
                 for (int e = 0; e < E; ++e) store_out(out, bf16, (qrow0 + g) * D + lane * E + e, o[g][e] * inv);
             }
@@ -782,7 +791,7 @@ template <int D_, int GT_> struct F32Wide {
         for (int g = 0; g < GT; ++g) {
             const float lg = __shfl_sync(0xffffffffu, l[value_of(g)], lane_of(g));
             if (g < G) {
-                const float inv = lg > 0.f ? 1.f / lg : 0.f;
+                const float inv = sum_inverse(lg);
 #pragma unroll
                 for (int e = 0; e < E; ++e) store_out(out, bf16, (qrow0 + g) * D + lane * E + e, o[g][e] * inv);
             }

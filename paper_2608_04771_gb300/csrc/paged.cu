@@ -769,7 +769,7 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
             } else {
                 blk.store(a.out, a.out_bf16 != 0, (long)q0 + hp * GS, nh);
                 blk.each_lse(nh, [&](int q, float m, float l) {
-                    const float l2 = l > 0.f ? m + log2f(l) : -INFINITY;
+                    const float l2 = sum_log2(m, l);
                     put_lse(a, q0 + hp * GS + q, l2);
                     if (a.logits) z[hp * GS + q] = l2;
                 });
@@ -812,10 +812,10 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
                     err |= ml[s].y < 0.f;
                 }
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (!err && M != -INFINITY) {
+                if (!err) {
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        const float f = fast_exp2(ml[s].x - M);
+                        const float f = part_factor(ml[s].x, M);
                         const float4 v = *reinterpret_cast<const float4 *>(join + ((part * NS + s) * JH + ql) * D + 4 * d4);
                         Ls += ml[s].y * f;
                         o.x += v.x * f;
@@ -826,10 +826,10 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
                 }
                 const int head = tile0 + q;
                 if (all) {
-                    const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+                    const float inv = sum_inverse(Ls);
                     store_out4(a, (q0 + head) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
                     if (d4 == 0) {
-                        const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
+                        const float l2 = sum_log2(M, Ls);
                         put_lse(a, q0 + head, l2);
                         sm_lse[jobs & 1][head] = l2;
                         if (a.lse2) a.lse2[q0 + head] = l2;
@@ -922,10 +922,10 @@ __global__ void __launch_bounds__(32 * (NW + 1 + kWeightWarps), 1)
                     Ls = 0.f;
                     o = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-                const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+                const float inv = sum_inverse(Ls);
                 store_out4(a, (q0 + q) * D + 4 * d4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
                 if (d4 == 0) {
-                    const float l2 = Ls > 0.f ? M + log2f(Ls) : -INFINITY;
+                    const float l2 = sum_log2(M, Ls);
                     put_lse(a, q0 + q, l2);
                     if (a.lse2) a.lse2[q0 + q] = l2;
                     if (a.inline_weights) sm_lse[0][q] = l2;
