@@ -8,9 +8,11 @@
 // units of 3900 rows 69 -> 32 us): a CTA reads its chunk's rows into registers, says so in the chunk's flag, and
 // writes them once the chunks have been read whose sources lie in its destination rows.  Those are known from the
 // kept rows counted before the chunk's first row and its end (`rank`): no more than a chunk has, so two chunks at
-// most.  CTAs claim chunks in the order of the list, a unit's own in ascending order: the chunks that a CTA
-// waits for were claimed before its own, and reading never waits, so every wait ends.  The chunks would do for
-// many units too, but slower: 896 units of 3900 rows 881 us (each chunk's chain of index, table, row and flag),
+// most.  CTAs claim chunks in the order of the list, a unit's own in ascending order, each the next one before the
+// present one is done.  Every wait ends: the first unread chunk of the list is some CTA's present one, which it reads at
+// once, or the next one of a CTA whose present chunk lies further up the list, has been read, and waits only for chunks
+// above itself, all read.  (A wait that runs out all the same reports it, and the chunk's rows are not written: they
+// could lie over rows that nobody has read.)  The chunks would do for many units too, but slower: 896 units of 3900 rows 881 us (each chunk's chain of index, table, row and flag),
 // by columns 595, 0.90 of the copy rate.
 #include <algorithm>
 
@@ -173,7 +175,7 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 8) compact
 template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact_chunks(CompactArgs a)
 {
     constexpr int U = Chunk<ROW>::U, R = Chunk<ROW>::R;
-    __shared__ int sm_next;
+    __shared__ int sm_next, sm_late;
     wait_prior_grid();  // the selection's results
     const int columns = min(a.ws.counters[3], a.units) * 2 * (ROW / 128);
     const int chunks = min(a.ws.counters[1], a.units * a.chunks);
@@ -206,20 +208,21 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact
             // kept rows in this chunk's destination rows: their destinations' chunks have to have been read
             const int32_t *rank = a.ws.rank + (size_t)cur.u * (a.chunks + 1);
             const int lo = max(0, __ldg(rank + cur.c)), hi = __ldg(rank + cur.c + 1);
-            for (int b = lo / R; b < cur.c && b * R < hi; ++b) {
+            int late = 0;
+            for (int b = lo / R; b < cur.c && b * R < hi && !late; ++b) {
                 long long spin = 0;
                 while (ld_acquire(flags + b) == 0 && spin < kFlagSpin) ++spin;
-                if (spin >= kFlagSpin) {
-                    raise_error(a.err, ERR_INTERNAL);
-                    break;
-                }
+                late = spin >= kFlagSpin;
             }
+            if (late) raise_error(a.err, ERR_INTERNAL);
+            sm_late = late;
         }
         __syncthreads();
+        const bool late = sm_late != 0;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int r = cur.row(i);
-            if (cur.src[i] == r) continue;
+            if (late || cur.src[i] == r) continue;
             const size_t p = rows.at<ROW>(a, r) + off;
             *reinterpret_cast<uint4 *>(a.K + p) = k[i];
             *reinterpret_cast<uint4 *>(a.V + p) = v[i];
