@@ -175,7 +175,7 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 8) compact
 template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact_chunks(CompactArgs a)
 {
     constexpr int U = Chunk<ROW>::U, R = Chunk<ROW>::R;
-    __shared__ int sm_next, sm_late;
+    __shared__ int sm_next;
     wait_prior_grid();  // the selection's results
     const int columns = min(a.ws.counters[3], a.units) * 2 * (ROW / 128);
     const int chunks = min(a.ws.counters[1], a.units * a.chunks);
@@ -202,23 +202,21 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact
         __syncthreads();  // the chunk has been read
         t = sm_next;
         if (t < total) nxt.find(a, t);  // its rows are looked up while this chunk waits for its turn
+        bool late = false;
         if (threadIdx.x == 0) {
             int *flags = a.ws.flags + (size_t)cur.u * a.chunks;
             st_release(flags + cur.c, 1);
             // kept rows in this chunk's destination rows: their destinations' chunks have to have been read
             const int32_t *rank = a.ws.rank + (size_t)cur.u * (a.chunks + 1);
             const int lo = max(0, __ldg(rank + cur.c)), hi = __ldg(rank + cur.c + 1);
-            int late = 0;
             for (int b = lo / R; b < cur.c && b * R < hi && !late; ++b) {
                 long long spin = 0;
                 while (ld_acquire(flags + b) == 0 && spin < kFlagSpin) ++spin;
                 late = spin >= kFlagSpin;
             }
             if (late) raise_error(a.err, ERR_INTERNAL);
-            sm_late = late;
         }
-        __syncthreads();
-        const bool late = sm_late != 0;
+        late = __syncthreads_or(late);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int r = cur.row(i);
