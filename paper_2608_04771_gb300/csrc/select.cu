@@ -21,6 +21,7 @@
 // the next chunk's reads are issued before the current chunk's writes, since their
 // sources lie above every row written so far.  Rows with kept[r] == r are not moved.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "internal.h"
@@ -68,6 +69,14 @@ __device__ __forceinline__ uint32_t order_key(float f)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// A load that stays before the barrier it stands before: what it reads is written over after that.
+__device__ __forceinline__ float ld_cg(const float *p)
+{
+    float v;
+    asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // What a selection does with a unit of L rows and a count m, and how a score is ordered.  Rows
 // before `first` and the last w are kept; the candidates lie between.
 
@@ -82,6 +91,7 @@ struct KeepRule {
     }
     __device__ __forceinline__ float load(const float *p) const { return *p; }
     __device__ __forceinline__ uint32_t key(float f) const { return order_key(f); }
+    __device__ __forceinline__ bool odd(float) const { return false; }
 };
 
 // Down to at most budget[b] rows of a paged cache: a unit within its budget is left alone, one whose
@@ -115,7 +125,10 @@ struct BudgetRule {
     __device__ __forceinline__ float load(const float *p) const { return __ldcg(p); }
     // -0 equals +0, and NaN lies above everything
     __device__ __forceinline__ uint32_t key(float f) const { return f == f ? order_key(f + 0.f) : 0xffffffffu; }
+    // The weight that a key was made of, but for these two, whose key is another value's too.  A kernel that meets one
+    // among a unit's weights takes the unit's weights themselves when it writes them.
     __device__ __forceinline__ float value(uint32_t k) const { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+    __device__ __forceinline__ bool odd(float f) const { return f != f || __float_as_uint(f) == 0x80000000u; }
     // row j, with `before` kept rows below it
     __device__ __forceinline__ void passed(long u, int j, int before) const
     {
@@ -330,8 +343,11 @@ constexpr int kWholeBin = 0x7fffffff;
 // Where there are more units than SMs, smaller CTAs share an SM and one counts
 // while another waits at a barrier (512 units of 15000 to 16384 candidates: 54 -> 45 us).
 constexpr int kFewKeys = 8;  // keys per thread
+// CTAs that are to share an SM in an eviction, 0: as many as ptxas leaves room for (it takes 51 registers for 512 threads, and 48
+// for 256, where 40 do and three and six CTAs fit).
+template <int NT, bool FEW, class Rule> constexpr int select_ctas() { return !Rule::BUDGET || NT > 512 ? 0 : (NT == 512 ? 3 : (FEW ? 5 : 6)); }
 template <int NT, bool FEW, class Rule>
-__global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__ scores, const int32_t *lens,
+__global__ void __launch_bounds__(NT, select_ctas<NT, FEW, Rule>()) select_topm_smem(const float *__restrict__ scores, const int32_t *lens,
                                                        int32_t *lens_out, const int32_t *__restrict__ keep, Rule rule, int B, int Hkv,
                                                        int L_cap, int32_t *__restrict__ idx_out,
                                                        int32_t *__restrict__ count, long units, unsigned *err)
@@ -343,11 +359,12 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
     __shared__ int w_gt[NW], w_eq[NW];
     __shared__ uint32_t w_min[NW], w_max[NW];
     __shared__ uint32_t s_prefix;
-    __shared__ int s_remaining;
+    __shared__ int s_remaining, s_raw;
     __shared__ int2 s_lm[kWalkAhead];
     wait_prior_grid();  // scores, lens and keep may come from the previous kernels
     walk_headers(s_lm, lens, keep, units, B, Hkv);
     for (int i = threadIdx.x; i < 256; i += NT) hist[i] = 0;
+    if (threadIdx.x == 0) s_raw = 0;
     __syncthreads();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     int it = 0;
@@ -386,7 +403,9 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
         uint32_t lo = 0xffffffffu, hi = 0;
 #pragma unroll 8
         for (int j = tid; j < nc; j += NT) {
-            const uint32_t key = rule.key(__ldcg(s + j));
+            const float x = __ldcg(s + j);
+            const uint32_t key = rule.key(x);
+            if (rule.odd(x)) s_raw = 1;
             keys[j] = key;
             lo = min(lo, key);
             hi = max(hi, key);
@@ -511,25 +530,39 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
                 w_gt[lane] = f_inc - f;
             }
         }
+        const bool raw = Rule::BUDGET && s_raw != 0;  // keys[] takes the weights themselves
+        if (raw) {
+#pragma unroll 1
+            for (int j = tid; j < nc; j += NT) keys[j] = __float_as_uint(__ldcg(s + j));
+        }
         __syncthreads();
-        int e_run = w_eq[wid], pos = w_gt[wid];
         const unsigned below = (1u << lane) - 1u;
-        for (int jb = j0; jb < j1; jb += 32) {
-            const int j = jb + lane;
-            const bool valid = j < j1;
-            const uint32_t key = valid ? keys[j] : 0u;
-            const bool is_eq = valid && key == T;
-            const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
-            const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
-            const unsigned fb = __ballot_sync(0xffffffffu, flag);
-            if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
-            if constexpr (Rule::BUDGET) {
-                const int p = rule.first + pos + __popc(fb & below);
-                if (flag) rule.weights[u * L_cap + p] = rule.value(key);
-                if (valid) rule.passed(u, rule.first + j, p);
+        auto emit = [&](auto weights) {  // whether keys[] holds the weights
+            constexpr bool RAW = decltype(weights)::value;
+            int e_run = w_eq[wid], pos = w_gt[wid];
+            for (int jb = j0; jb < j1; jb += 32) {
+                const int j = jb + lane;
+                const bool valid = j < j1;
+                const uint32_t word = valid ? keys[j] : 0u, key = RAW && valid ? rule.key(__uint_as_float(word)) : word;
+                const bool is_eq = valid && key == T;
+                const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
+                const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
+                const unsigned fb = __ballot_sync(0xffffffffu, flag);
+                if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
+                if constexpr (Rule::BUDGET) {
+                    const int p = rule.first + pos + __popc(fb & below);
+                    if (flag) rule.weights[u * L_cap + p] = RAW ? __uint_as_float(word) : rule.value(key);
+                    if (valid) rule.passed(u, rule.first + j, p);
+                }
+                e_run += __popc(eb);
+                pos += __popc(fb);
             }
-            e_run += __popc(eb);
-            pos += __popc(fb);
+        };
+        if constexpr (Rule::BUDGET) {
+            if (raw) emit(std::true_type{});
+            else emit(std::false_type{});
+        } else {
+            emit(std::false_type{});
         }
         if constexpr (Rule::BUDGET) {
             __shared__ int s_at;
@@ -551,6 +584,9 @@ __global__ void __launch_bounds__(NT) select_topm_smem(const float *__restrict__
         if (tid == 0) {
             if constexpr (!Rule::BUDGET) count[u] = m;
             if (lens_out) lens_out[u] = m;
+        }
+        if constexpr (Rule::BUDGET) {
+            if (tid == 0) s_raw = 0;
         }
         __syncthreads();  // this unit's shared memory is read out before the next unit's fill
     }
@@ -598,9 +634,12 @@ __global__ void __launch_bounds__(kClusterThreads) select_topm_cluster(const flo
     const float *s = scores + u * L_cap + first + c0;
     int32_t *idx = idx_out + u * L_cap;
     uint32_t lo = 0xffffffffu, hi = 0;
+    bool odd = false;
 #pragma unroll 8
     for (int j = tid; j < n; j += NT) {
-        const uint32_t key = rule.key(rule.load(s + j));
+        const float x = rule.load(s + j);
+        const uint32_t key = rule.key(x);
+        odd |= rule.odd(x);
         keys[j] = key;
         lo = min(lo, key);
         hi = max(hi, key);
@@ -701,7 +740,9 @@ __global__ void __launch_bounds__(kClusterThreads) select_topm_cluster(const flo
         w_gt[wid] = n_gt;
         w_eq[wid] = n_eq;
     }
-    __syncthreads();
+    const bool raw = __syncthreads_or(odd);  // keys[] will hold the weights themselves
+    if (raw)  // (before the cluster's barrier: no CTA has written a weight)
+        for (int j = tid; j < n; j += NT) keys[j] = __float_as_uint(rule.load(s + j));
     if (wid == 0) {
         const int g = __reduce_add_sync(0xffffffffu, lane < NW ? w_gt[lane] : 0);
         const int e = __reduce_add_sync(0xffffffffu, lane < NW ? w_eq[lane] : 0);
@@ -740,25 +781,30 @@ __global__ void __launch_bounds__(kClusterThreads) select_topm_cluster(const flo
     }
     if (tid == 0 && r == 0) s_at = rule.claim(u, m);
     __syncthreads();
-    int e_run = w_eq[wid], pos = w_gt[wid];
     const unsigned below = (1u << lane) - 1u;
-    for (int jb = j0; jb < j1; jb += 32) {
-        const int j = jb + lane;
-        const bool valid = j < j1;
-        const uint32_t key = valid ? keys[j] : 0u;
-        const bool is_eq = valid && key == T;
-        const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
-        const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
-        const unsigned fb = __ballot_sync(0xffffffffu, flag);
-        const int p = first + pos + __popc(fb & below);
-        if (flag) {
-            idx[p] = first + c0 + j;
-            rule.weights[u * L_cap + p] = rule.value(key);
+    auto emit = [&](auto weights) {  // whether keys[] holds the weights
+        constexpr bool RAW = decltype(weights)::value;
+        int e_run = w_eq[wid], pos = w_gt[wid];
+        for (int jb = j0; jb < j1; jb += 32) {
+            const int j = jb + lane;
+            const bool valid = j < j1;
+            const uint32_t word = valid ? keys[j] : 0u, key = RAW && valid ? rule.key(__uint_as_float(word)) : word;
+            const bool is_eq = valid && key == T;
+            const unsigned eb = __ballot_sync(0xffffffffu, is_eq);
+            const bool flag = (valid && key > T) || (is_eq && e_run + __popc(eb & below) < need);
+            const unsigned fb = __ballot_sync(0xffffffffu, flag);
+            const int p = first + pos + __popc(fb & below);
+            if (flag) {
+                idx[p] = first + c0 + j;
+                rule.weights[u * L_cap + p] = RAW ? __uint_as_float(word) : rule.value(key);
+            }
+            if (valid) rule.passed(u, first + c0 + j, p);
+            e_run += __popc(eb);
+            pos += __popc(fb);
         }
-        if (valid) rule.passed(u, first + c0 + j, p);
-        e_run += __popc(eb);
-        pos += __popc(fb);
-    }
+    };
+    if (raw) emit(std::true_type{});
+    else emit(std::false_type{});
     if (r == 0) {
         for (int j = tid; j < first; j += NT) {
             idx[j] = j;
@@ -794,10 +840,12 @@ __device__ __forceinline__ void select_in_warp(const Rule &rule, long u, int L_c
                                                int kc, int32_t *__restrict__ idx, int lane)
 {
     uint32_t key[K], lo = 0xffffffffu, hi = 0;
+    bool odd = false;
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         const int j = 32 * i + lane;
         const float x = j < nc ? __ldcg(s + j) : 0.f;
+        odd |= rule.odd(x);
         key[i] = j < nc ? rule.key(x) : 0u;  // order_key is 0 for no score but the NaN of all ones
         if (j < nc) {
             lo = min(lo, key[i]);
@@ -832,6 +880,7 @@ __device__ __forceinline__ void select_in_warp(const Rule &rule, long u, int L_c
     }
     const unsigned below = (1u << lane) - 1u;
     int e_run = 0, pos = 0;
+    if constexpr (Rule::BUDGET) odd = __any_sync(0xffffffffu, odd);
 #pragma unroll
     for (int i = 0; i < K; ++i) {
         const int j = 32 * i + lane;
@@ -842,7 +891,12 @@ __device__ __forceinline__ void select_in_warp(const Rule &rule, long u, int L_c
         if (flag) idx[pos + __popc(fb & below)] = rule.first + j;
         if constexpr (Rule::BUDGET) {
             const int p = rule.first + pos + __popc(fb & below);
-            if (flag) rule.weights[u * L_cap + p] = rule.value(key[i]);
+            float x = rule.value(key[i]);
+            if (odd) {  // (what has been written so far lies below these)
+                if (j < nc) x = ld_cg(s + j);
+                __syncwarp();
+            }
+            if (flag) rule.weights[u * L_cap + p] = x;
             if (j < nc) rule.passed(u, rule.first + j, p);
         }
         e_run += __popc(eb);
