@@ -64,6 +64,14 @@ __device__ __forceinline__ void st_release(int *p, int v)
     asm volatile("st.release.gpu.global.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 
+// 16 bytes that are read once (streamed past what L2 holds), before the barrier behind which they may be written over.
+__device__ __forceinline__ uint4 ld_once(const char *p)
+{
+    uint4 v;
+    asm volatile("ld.global.cs.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
 // Where the rows of a unit lie.  The selection has checked the table entries of all its rows; an entry is
 // held inside the pool all the same, and a kept row inside the cache, so that a workspace or an index array that
 // something else has written to costs no access out of bounds.
@@ -195,8 +203,8 @@ template <int ROW> __global__ void __launch_bounds__(kCompactThreads, 4) compact
         for (int i = 0; i < U; ++i) {
             if (cur.src[i] == cur.row(i)) continue;  // already in place, or behind the last row
             const size_t p = rows.at<ROW>(a, cur.src[i]) + off;
-            k[i] = __ldcs(reinterpret_cast<const uint4 *>(a.K + p));
-            v[i] = __ldcs(reinterpret_cast<const uint4 *>(a.V + p));
+            k[i] = ld_once(a.K + p);
+            v[i] = ld_once(a.V + p);
         }
         if (threadIdx.x == 0) sm_next = claimed;
         __syncthreads();  // the chunk has been read

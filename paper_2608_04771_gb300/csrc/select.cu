@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(NT) select_topm(const float *__restrict__ scor
             float *wt = rule.weights + u * L_cap;
             for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
                 const int t = t0 + tid;
-                const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+                const float x = t < w ? ld_cg(wt + (L - w + t)) : 0.f;
                 __syncthreads();
                 if (t < w) {
                     wt[m - w + t] = x;
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(NT, select_ctas<NT, FEW, Rule>()) select_topm_
             float *wt = rule.weights + u * L_cap;
             for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
                 const int t = t0 + tid;
-                const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+                const float x = t < w ? ld_cg(wt + (L - w + t)) : 0.f;
                 __syncthreads();
                 if (t < w) {
                     wt[m - w + t] = x;
@@ -813,7 +813,7 @@ __global__ void __launch_bounds__(kClusterThreads) select_topm_cluster(const flo
         float *wt = rule.weights + u * L_cap;
         for (int t0 = 0; t0 < w; t0 += NT) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
             const int t = t0 + tid;
-            const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+            const float x = t < w ? ld_cg(wt + (L - w + t)) : 0.f;
             __syncthreads();
             if (t < w) {
                 wt[m - w + t] = x;
@@ -957,7 +957,7 @@ __global__ void __launch_bounds__(kWarpThreads) select_topm_warp(const float *__
         float *wt = rule.weights + (long)u * L_cap;
         for (int t0 = 0; t0 < w; t0 += 32) {  // rows L - w .. L - 1 move to m - w .. m - 1: read, then written
             const int t = t0 + lane;
-            const float x = t < w ? __ldcg(wt + (L - w + t)) : 0.f;
+            const float x = t < w ? ld_cg(wt + (L - w + t)) : 0.f;
             __syncwarp();
             if (t < w) {
                 wt[m - w + t] = x;
