@@ -15,7 +15,7 @@
  *    The library never allocates device memory: calls that need scratch take a
  *    caller-owned workspace sized by reco_workspace_bytes() or, for the paged
  *    calls, reco_paged_workspace_bytes() (the decode's must be zero-filled
- *    before its first use, the paged calls' in its first 4096 bytes; each
+ *    before its first use, the paged calls' in its first 8192 bytes; each
  *    call leaves it reusable), except reco_answer_ppl_static, which uses a fixed array inside the library.
  *  - Device calls are asynchronous on the given stream and return after the
  *    launches are queued.  They return RECO_OK, or an error status before
@@ -328,7 +328,7 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
  *   out          : [n_layers][B][H_q][d] of out_dtype (RECO_F32 or RECO_BF16)
  *   lse          : [n_layers][B][H_q] float32 or NULL
  *   ws           : reco_paged_workspace_bytes(RECO_OP_PAGED_DECODE, kv) bytes, of which
- *                  the first 4096 are zero-filled before its first use; every call leaves
+ *                  the first 8192 are zero-filled before its first use; every call leaves
  *                  it reusable, by any paged call and descriptor that it is large enough
  *                  for (another number of sequences, layers or heads, another type);
  *                  calls (captured graphs too) that share one must not overlap on the GPU

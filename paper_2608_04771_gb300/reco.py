@@ -313,7 +313,7 @@ def paged_workspace(op: int, kv: reco_paged_kv, device="cuda") -> torch.Tensor:
     """A workspace for a paged call, with its counters, which lie in its first bytes, zero as the calls need them
     before its first use.  It serves every paged call, with any cache, that it is large enough for."""
     ws = torch.empty(max(reco_paged_workspace_bytes(op, kv), 256), dtype=torch.uint8, device=device)
-    ws[:4096].zero_()
+    ws[:8192].zero_()
     return ws
 
 

@@ -43,12 +43,12 @@ def test_growing_and_shrinking_batches_share_a_workspace(weights):
 
 def test_every_paged_call_shares_a_workspace_zero_in_its_first_bytes():
     """Decode with and without weights and evictions in turn, through a buffer that is no more than its first
-    4096 bytes zero."""
+    8192 bytes zero."""
     caches = _caches()
     ops = (reco.RECO_OP_PAGED_DECODE, reco.RECO_OP_PAGED_WEIGHTS, reco.RECO_OP_PAGED_EVICT)
     ws = torch.full((max(reco.reco_paged_workspace_bytes(op, c.kv) for c in caches for op in ops),), 0xA5,
                     dtype=torch.uint8, device=DEV)
-    ws[:4096] = 0
+    ws[:8192] = 0
     for step, i in enumerate(ORDER):
         c = caches[i]
         check(c, *c.token(), weights=step % 2 == 0, ws=ws, exact_pool=False)
@@ -63,5 +63,5 @@ def test_a_workspace_from_the_binding_is_zero_where_it_must_be():
     c = Cache(66, 1, 1, 2, 1, 64, BF, 16, 20)
     for op in (reco.RECO_OP_PAGED_DECODE, reco.RECO_OP_PAGED_WEIGHTS, reco.RECO_OP_PAGED_EVICT):
         ws = reco.paged_workspace(op, c.kv, DEV)
-        assert ws.numel() >= reco.reco_paged_workspace_bytes(op, c.kv) >= 4096 and not ws[:4096].any()
+        assert ws.numel() >= reco.reco_paged_workspace_bytes(op, c.kv) >= 8192 and not ws[:8192].any()
     assert np.isfinite(float(c.scale))
