@@ -283,7 +283,10 @@ reco_status reco_compact(const reco_kv *kv, const int32_t *kept_idx, int32_t *le
  * A unit with a length outside [0, L_cap] (or no room to append) writes zeros
  * and lse = -inf, and sets the device error word.  A head with a NaN among its
  * logits (in its query or in a row), or one that is +inf, gives NaN in out and
- * lse; one whose logits are all -inf gives zeros and lse = -inf.               */
+ * lse; one whose logits are all -inf gives zeros and lse = -inf.
+ * Products, sums and lse are float32; over bf16 caches the probabilities enter
+ * their product with V in two bf16 parts (2^-17 of each: with out_dtype RECO_F32
+ * the largest error of a short sum, with RECO_BF16 half a step hides it).       */
 reco_status reco_decode_attn(const reco_kv *kv, const void *q, const void *k_new, const void *v_new,
                              int32_t *lens, float scale, void *out, reco_dtype out_dtype, float *lse,
                              void *ws, size_t ws_bytes, cudaStream_t stream);
@@ -338,7 +341,9 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
  * or one that is +inf, gives NaN in its out and lse.  A unit with a length
  * outside [0, max_pages * page], with no room to append, or whose table names a page
  * outside [0, n_pages) for a row it needs, writes zeros and lse = -inf, keeps its length
- * and sets the device error word.  At most 16 query heads per KV head.                */
+ * and sets the device error word (where the fault is a page of older rows, the new row may
+ * be in the pool all the same, behind that length).  At most 16 query heads per KV head.
+ * Precision as reco_decode_attn's.                                                    */
 reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
                                    int32_t *lens, float scale, int window, int sinks, void *out,
                                    reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes,
@@ -350,8 +355,9 @@ reco_status reco_paged_decode_attn(const reco_paged_kv *kv, const void *q, const
  *   weights[unit, j] += (1/G) * sum_g softmax_j(scale * q[layer,b,h*G+g,:] . K_j)
  * for the rows j seen; an appended row starts at its own weight (what its entry held
  * before does not count).  The entries of other rows are left as they are, and so are
- * those of all rows of a unit that is in error.  A head whose lse is NaN makes the entries
- * of all rows seen NaN; one whose logits are all -inf adds nothing.
+ * those of all rows of a unit that is in error (that of its new row may have become 0).
+ * A head whose lse is NaN makes the entries of all rows seen NaN; one whose logits are all
+ * -inf adds nothing.
  *   weights : [n_layers][B][H_kv][max_pages * page] float32, 16-byte aligned (device,
  *             in/out)
  *   ws      : reco_paged_workspace_bytes(RECO_OP_PAGED_WEIGHTS, kv) bytes, otherwise as
@@ -382,7 +388,10 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  *              the first m entries of each unit that is cut receive `kept`
  *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_EVICT, kv) bytes, otherwise as
  *              reco_paged_decode_attn's
- * No two table entries for rows of live sequences may name the same page.  A unit with a
+ * Pages that a cut sequence shares with another (a common prefix) must be copied first: rows
+ * move inside the pages that the table names, so the other sequence would read moved rows.
+ * The call does not look for them: others than this call's sequences may hold a page too.
+ * A weight moves with its bits (the sign of a zero, a NaN's payload).  A unit with a
  * length outside [0, max_pages * page], one to be cut below sinks + w, or one to be cut
  * whose table names a page outside [0, n_pages) for one of its rows is left untouched
  * (device error word set).                                                           */

@@ -92,7 +92,7 @@ reco_status check_paged(const reco_paged_kv *kv, bool need_ptrs = true)
     if (units > 65535 || units * kv->H_kv > 65535) return fail(RECO_EUNSUPPORTED, "%lld units exceed 65535", units * kv->H_kv);
     if ((long long)kv->max_pages * kv->page > (1LL << 30))
         return fail(RECO_EUNSUPPORTED, "%lld rows per sequence exceed 2^30", (long long)kv->max_pages * kv->page);
-    // blocks of eight rows are counted in 32 bits
+    // blocks of 16 rows, of all units, are counted in 32 bits
     if (units * kv->H_kv * kv->max_pages * kv->page >= (1LL << 34))
         return fail(RECO_EUNSUPPORTED, "%lld units of up to %lld rows (2^34 rows in all)", units * kv->H_kv, (long long)kv->max_pages * kv->page);
     // rows of a pool are addressed by tensor-map coordinates, 32-bit integers

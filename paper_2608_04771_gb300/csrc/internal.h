@@ -22,8 +22,8 @@ constexpr size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // First bytes of a paged call's workspace, zero between calls where the call counts in them: nothing else lies
 // there, whatever the call and its descriptor, so that one workspace serves them all.  (2560 would do.  What follows
-// is read across the GPU, and where it falls in L2 is felt: the eviction of one unit of 131072 rows took 43.2 us with
-// 256, 1024 or 8192 bytes here and 46.4 with 2048, 4096 or 4352.)
+// is read across the GPU, and where it falls in L2 is felt: the eviction of one unit of 131072 rows takes 37.4 us with
+// 256, 1024 or 8192 bytes here, 39 to 40.4 with 2048, 4352, 12288 or 16384; other evictions stay within 3%.)
 constexpr size_t kPagedZeroBytes = 8192;
 
 struct ScoreWs {  // regions carved from the caller's workspace

@@ -17,7 +17,7 @@
 // of more than two heads: F32Wide).  Lane s of the copying warp feeds stream s: it walks the same units, looks the pages
 // up (a block never straddles two; the next block's entry loads while this one's copies go out) and waits for free
 // stages, so that the computing warps spend nothing on either: with the copies and the look-ups in the computing warps,
-// as the contiguous decode has its copies, the 7B-class stack of 16K rows took 1308 us, so 1015 (7.1 TB/s, 1.04 of the
+// as the contiguous decode has its copies, the 7B-class stack of 16K rows took 1308 us, so 1020 (7.05 TB/s, 1.04 of the
 // copy rate).  What a warp does with a block is decode_block.cuh's.  At the end of a piece the streams join their (max,
 // sum, output) through shared memory; a unit cut between CTAs leaves one partial per CTA, which the last CTA to
 // finish (atomic ticket, no waiting) joins in the order of the pieces: the same inputs give the same bits.
@@ -41,7 +41,7 @@ constexpr int kRingBytes = 24 * 8192;  // ring of a CTA, all streams
 constexpr int kPagedMaxGrid = 256;     // CTAs at most (two partial slots each in the workspace)
 constexpr int kWeightWarps = 3;        // they cost no registers: 9 warps or 12, an SM's quarter holds three of 168
 // Blocks per working CTA at least (fewer CTAs rather than less): two units of 512 rows 10.9 us, with 16 12.1, with 2
-// 10.9; 8 units of 1000 rows 11.5, 13.1 and 11.9.
+// 10.9; 8 units of 1000 rows 11.5, 13.1 and 11.9 (with the plan of before kWarpUnits: now 10.1 and 11.1).
 constexpr int kMinBlocks = 8;
 // Up to this many units, if they fit the grid, every warp plans by itself, without barriers (a Tiny layer 10.7 -> 10.1).
 constexpr int kWarpUnits = 128;
