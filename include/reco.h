@@ -7,7 +7,8 @@
  * penalty (Eq. 3-4) with the draw of the next token from the penalised logits
  * (Sec. 3.3), and the answer-perplexity stop test (Eq. 5-6).  Beside them, for caches
  * whose rows lie in pages of a shared pool: decode attention, the running sums of its
- * weights, and eviction down to a budget by those sums (the reco_paged_ calls).
+ * weights, eviction down to a budget by those sums, and the append of new tokens with their
+ * position rotation (the reco_paged_ calls).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -75,7 +76,8 @@ typedef enum {
     RECO_OP_SAMPLE = 4,
     RECO_OP_PAGED_DECODE = 5, /* the paged calls: sized by reco_paged_workspace_bytes */
     RECO_OP_PAGED_WEIGHTS = 6,
-    RECO_OP_PAGED_EVICT = 7
+    RECO_OP_PAGED_EVICT = 7,
+    RECO_OP_PAGED_APPEND = 8
 } reco_op;
 
 /* A paged cache: the rows of a sequence lie in pages of one pool that all sequences
@@ -99,6 +101,15 @@ typedef struct {
     int d;                /* head dimension: 64 or 128 */
     reco_dtype dtype;     /* RECO_F32 or RECO_BF16 */
 } reco_paged_kv;
+
+/* Rows of d elements, [n_layers][tokens][heads], as a view: element (layer, t, h, i) lies at
+ * p + layer * `layer` + t * `token` + h * `head` + i elements.  p and the strides (of
+ * dimensions larger than one) are multiples of 16 bytes; strides may be zero or negative.
+ * Keys, queries and values inside the output of one projection are such views.          */
+typedef struct {
+    void *p;                    /* device */
+    int64_t layer, token, head; /* strides, in elements */
+} reco_rows;
 
 /* ---------------------------------------------------------------- host helpers */
 
@@ -129,7 +140,7 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
 
 /* Workspace bytes a paged call needs for this cache: RECO_OP_PAGED_DECODE,
  * RECO_OP_PAGED_WEIGHTS (it holds the logits of a token, 4 bytes per query head and row
- * of max_pages * page) or RECO_OP_PAGED_EVICT.  Only the sizes in kv are read.  The size
+ * of max_pages * page), RECO_OP_PAGED_EVICT or RECO_OP_PAGED_APPEND.  Only the sizes in kv are read.  The size
  * does not depend on the device or on lens.  Alignment: 256 bytes.  The decode's two
  * are refused for more than 16 query heads per KV head, as the calls are.            */
 reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size_t *bytes_out);
@@ -368,6 +379,43 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
                                            const void *v_new, int32_t *lens, float scale, int window, int sinks,
                                            void *out, reco_dtype out_dtype, float *lse, float *weights, void *ws,
                                            size_t ws_bytes, cudaStream_t stream);
+
+/* Appends the keys and values of new tokens to a paged cache, the keys (and queries) rotated by
+ * the tokens' positions on the way: prompts, pieces of prompts, or one token per sequence.  The
+ * tokens of all sequences lie one after the other: those of sequence b are
+ * t = starts[b] .. starts[b+1] - 1.  For every layer, KV head h and token of sequence b, with
+ * L = lens[layer, b, h]:
+ *   K[unit, L + t - starts[b]] = rotate(k[layer, t, h], pos[t]),   V[...] = v[layer, t, h]
+ * in the pages that the table names; then lens[layer, b, h] = L + starts[b+1] - starts[b].  If
+ * q is given, q_out[layer, t, hq] = rotate(q[layer, t, hq], pos[t]) for the same tokens.
+ *   rotate(x, s) turns the pairs (x_i, x_{i + rot/2}), or with `interleaved` the pairs
+ *   (x_{2i}, x_{2i+1}), i < rot / 2, by the angle s * inv_freq[i]:
+ *     (x, y) -> (x cos - y sin, y cos + x sin);   elements from rot on stay as they are.
+ *   The angle is that of the exact product, reduced to a turn before it is rounded (far
+ *   positions lose nothing); the rest is float32, rounded once to the cache's type.
+ *   k, v     : [n_layers][T][H_kv] rows, cache dtype
+ *   q, q_out : [n_layers][T][H_q] rows, cache dtype, or both NULL.  q_out may be q itself (the
+ *              same view); otherwise it overlaps no input
+ *   T        : tokens that k, v, q and pos have room for, 0 <= T <= 2^30 (0: nothing to do)
+ *   starts   : [B + 1] int32 (device), 0 <= starts[b] <= starts[b+1] <= T; tokens of no
+ *              sequence (behind starts[B], say) are not read, nor their rows of q_out written
+ *   pos      : [T] int32 (device), any values; may be NULL if rot == 0
+ *   inv_freq : [rot / 2] float32 (device); may be NULL if rot == 0.  An entry that is not
+ *              finite makes its pairs NaN
+ *   rot      : a multiple of 16, 0 <= rot <= d
+ *   lens     : [n_layers][B][H_kv] int32 (device, advanced)
+ *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_APPEND, kv) bytes, otherwise as
+ *              reco_paged_decode_attn's
+ * A page that receives a row belongs to one sequence.  A unit whose length is outside
+ * [0, max_pages * page], or that has no room for its new rows, is left as it is; one whose
+ * table names a page outside [0, n_pages) for a new row keeps its length (other new rows may
+ * be in the pool behind it).  If starts decreases or leaves [0, T], no length advances (rows
+ * behind the lengths, and rows of q_out, may have been written).  Each sets the device error
+ * word.  Sequences without new tokens are not looked at.                               */
+reco_status reco_paged_append(const reco_paged_kv *kv, const reco_rows *k, const reco_rows *v, const reco_rows *q,
+                              const reco_rows *q_out, int T, const int32_t *starts, const int32_t *pos,
+                              const float *inv_freq, int rot, int interleaved, int32_t *lens, void *ws,
+                              size_t ws_bytes, cudaStream_t stream);
 
 /* Eviction of a paged cache down to a budget by accumulated attention weight (the
  * selection and compaction of Sec. 3.2 with running sums of reco_paged_decode_attn_weights

@@ -79,3 +79,31 @@ def evict(K, V, weights, table, lens, budget, w, sinks):
                 lens[ly, b, h] = m
                 kept[ly, b, h] = np.array(rows)
     return kept
+
+
+def rotate(x, pos, inv_freq, interleaved):
+    """Rows x [..., d] turned by the position pos: pairs (i, i + rot / 2), or neighbours; float64."""
+    x = np.array(x, np.float64)
+    half = len(inv_freq)
+    a = float(pos) * np.asarray(inv_freq, np.float64)
+    c, s = np.cos(a), np.sin(a)
+    lo, hi = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    u, v = x[..., lo].copy(), x[..., hi].copy()
+    x[..., lo], x[..., hi] = u * c - v * s, v * c + u * s
+    return x
+
+
+def append(K, V, table, lens, k, v, starts, pos=None, inv_freq=(), interleaved=False, q=None, q_out=None):
+    """New tokens' rows into K and V (and q_out), updated in place with lens; k, v, q are [layers, T, heads, d]."""
+    Ly, H, page = K.shape[0], K.shape[2], K.shape[3]
+    for b in range(len(starts) - 1):
+        for t in range(starts[b], starts[b + 1]):
+            s = 0 if pos is None else pos[t]
+            for ly in range(Ly):
+                if q is not None:
+                    q_out[ly, t] = rotate(q[ly, t], s, inv_freq, interleaved)
+                for h in range(H):
+                    r = lens[ly, b, h] + t - starts[b]
+                    K[ly, table[b, r // page], h, r % page] = rotate(k[ly, t, h], s, inv_freq, interleaved)
+                    V[ly, table[b, r // page], h, r % page] = v[ly, t, h]
+        lens[:, b] += starts[b + 1] - starts[b]

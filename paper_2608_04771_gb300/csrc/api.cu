@@ -258,6 +258,7 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
     case RECO_OP_PAGED_DECODE:
     case RECO_OP_PAGED_WEIGHTS:
     case RECO_OP_PAGED_EVICT:
+    case RECO_OP_PAGED_APPEND:
         return fail(RECO_EINVAL, "op %d is sized by reco_paged_workspace_bytes", (int)op);
     }
     return fail(RECO_EINVAL, "unknown op %d", (int)op);
@@ -274,6 +275,8 @@ reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size
         *bytes_out = reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
     } else if (op == RECO_OP_PAGED_EVICT)
         *bytes_out = reco::evict_ws_layout(*kv, nullptr).bytes;
+    else if (op == RECO_OP_PAGED_APPEND)
+        *bytes_out = reco::kPagedZeroBytes;
     else
         return fail(RECO_EINVAL, "op %d is not a paged call", (int)op);
     return RECO_OK;
@@ -545,6 +548,42 @@ reco_status reco_decode_attn_ring(const reco_kv *kv, const void *q, const void *
     if (q_ring && !al16(q_ring)) return fail(RECO_EINVAL, "q_ring must be 16-byte aligned");
     return decode_checked(kv, q, k_new, v_new, lens, scale, out, out_dtype, nullptr, ring, slots, slot, q_ring, ws,
                           ws_bytes, stream, "reco_decode_attn_ring launch");
+}
+
+// A view of rows: its start and the strides of dimensions larger than one at 16-byte boundaries.
+static reco_status check_rows(const reco_rows *r, const char *name, const reco_paged_kv *kv, int T, int heads)
+{
+    if (!r || !r->p) return fail(RECO_EINVAL, "NULL %s", name);
+    const int64_t chunk = kv->dtype == RECO_F32 ? 4 : 8;
+    if (!al16(r->p) || (kv->n_layers > 1 && r->layer % chunk) || (T > 1 && r->token % chunk) || (heads > 1 && r->head % chunk))
+        return fail(RECO_EINVAL, "%s and its strides must be multiples of 16 bytes", name);
+    return RECO_OK;
+}
+
+reco_status reco_paged_append(const reco_paged_kv *kv, const reco_rows *k, const reco_rows *v, const reco_rows *q,
+                              const reco_rows *q_out, int T, const int32_t *starts, const int32_t *pos,
+                              const float *inv_freq, int rot, int interleaved, int32_t *lens, void *ws, size_t ws_bytes,
+                              cudaStream_t stream)
+{
+    reco_status st = check_paged(kv);
+    if (st != RECO_OK) return st;
+    if (T < 0 || T > (1 << 30)) return fail(RECO_EINVAL, "T = %d tokens outside [0, 2^30]", T);
+    if (!starts || !lens) return fail(RECO_EINVAL, "NULL starts or lens");
+    if (((uintptr_t)starts | (uintptr_t)lens | (uintptr_t)pos | (uintptr_t)inv_freq) & 3u)
+        return fail(RECO_EINVAL, "starts, pos, inv_freq and lens must be 4-byte aligned");
+    if (rot < 0 || rot > kv->d || rot % 16) return fail(RECO_EINVAL, "rot = %d must be a multiple of 16 in [0, d = %d]", rot, kv->d);
+    if (interleaved != 0 && interleaved != 1) return fail(RECO_EINVAL, "interleaved must be 0 or 1");
+    if ((st = check_ws(ws, ws_bytes, reco::kPagedZeroBytes)) != RECO_OK) return st;
+    if ((q == nullptr) != (q_out == nullptr)) return fail(RECO_EINVAL, "q and q_out must both be given or both be NULL");
+    if (T == 0) return RECO_OK;
+    if (rot > 0 && (!pos || !inv_freq)) return fail(RECO_EINVAL, "NULL pos or inv_freq");
+    if ((st = check_rows(k, "k", kv, T, kv->H_kv)) != RECO_OK || (st = check_rows(v, "v", kv, T, kv->H_kv)) != RECO_OK) return st;
+    if (q && ((st = check_rows(q, "q", kv, T, kv->H_q)) != RECO_OK || (st = check_rows(q_out, "q_out", kv, T, kv->H_q)) != RECO_OK))
+        return st;
+    unsigned *err;
+    if ((st = error_word(&err)) != RECO_OK) return st;
+    cudaError_t e = reco::launch_paged_append(*kv, *k, *v, q, q_out, T, starts, pos, inv_freq, rot, interleaved, lens, ws, err, stream);
+    return e == cudaSuccess ? RECO_OK : cuda_fail(e, "reco_paged_append launch");
 }
 
 reco_status reco_reflect_penalty(float *logits, int B, int V, const int32_t *ids, int n_ids, const float *rewards,

@@ -26,6 +26,11 @@ constexpr size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 // 256, 1024 or 8192 bytes here, 39 to 40.4 with 2048, 4352, 12288 or 16384; other evictions stay within 3%.)
 constexpr size_t kPagedZeroBytes = 8192;
 
+// The append's counters, one per group of layers, in that place behind those of the other calls.
+constexpr size_t kAppendCounters = 4096;
+constexpr int kAppendGroups = 512;
+static_assert(kAppendCounters + 8 * kAppendGroups <= kPagedZeroBytes, "the append's counters");
+
 struct ScoreWs {  // regions carved from the caller's workspace
     float *part_m, *part_z;  // [units][parts][R]     a part's row reference (log2) / row sum: up to two parts per 2048
                              // keys on the tensor cores, one per 128 keys otherwise
@@ -138,6 +143,11 @@ cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t 
 // The eviction's selection: kept rows into idx, weights compacted, lens cut, the compaction's list.
 cudaError_t launch_select_budget(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
                                  int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s);
+// q, q_out: nullptr or both.
+cudaError_t launch_paged_append(const reco_paged_kv &kv, const reco_rows &k, const reco_rows &v, const reco_rows *q,
+                                const reco_rows *q_out, int T, const int32_t *starts, const int32_t *pos,
+                                const float *inv_freq, int rot, int interleaved, int32_t *lens, void *ws, unsigned *err,
+                                cudaStream_t s);
 cudaError_t launch_penalty(float *logits, int B, int V, const int32_t *ids, int n_ids,
                            const float *rewards, float tau_l, float tau_h, float beta, float *beta_out,
                            unsigned *err, cudaStream_t s);

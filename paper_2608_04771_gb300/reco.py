@@ -17,14 +17,14 @@ _lib = None
 RECO_OK, RECO_EINVAL, RECO_EUNSUPPORTED, RECO_ECUDA, RECO_EDEVICE = range(5)
 RECO_F32, RECO_BF16 = 0, 1
 RECO_OP_SCORE, RECO_OP_SELECT, RECO_OP_DECODE, RECO_OP_PPL, RECO_OP_SAMPLE = range(5)
-RECO_OP_PAGED_DECODE, RECO_OP_PAGED_WEIGHTS, RECO_OP_PAGED_EVICT = range(5, 8)
+RECO_OP_PAGED_DECODE, RECO_OP_PAGED_WEIGHTS, RECO_OP_PAGED_EVICT, RECO_OP_PAGED_APPEND = range(5, 9)
 
 EXPORTS = ("reco_retention_ratio", "reco_keep_count", "reco_penalty_band", "reco_probe_trigger",
            "reco_workspace_bytes", "reco_last_error", "reco_check", "reco_score_cache",
            "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact", "reco_select_topm", "reco_compact",
            "reco_decode_attn", "reco_decode_attn_ring", "reco_reflect_penalty", "reco_penalty_sample", "reco_answer_ppl",
            "reco_answer_ppl_static", "reco_paged_workspace_bytes", "reco_paged_decode_attn",
-           "reco_paged_decode_attn_weights", "reco_paged_evict")
+           "reco_paged_decode_attn_weights", "reco_paged_evict", "reco_paged_append")
 RECO_PPL_STATIC_MAX_ROWS = 65536
 
 
@@ -45,6 +45,10 @@ class reco_paged_kv(ctypes.Structure):
                 ("n_layers", ctypes.c_int), ("B", ctypes.c_int), ("H_q", ctypes.c_int), ("H_kv", ctypes.c_int),
                 ("n_pages", ctypes.c_int), ("max_pages", ctypes.c_int), ("page", ctypes.c_int), ("d", ctypes.c_int),
                 ("dtype", ctypes.c_int)]
+
+
+class reco_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("layer", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 def library_path() -> Path:
@@ -90,7 +94,9 @@ def lib():
     L.reco_paged_decode_attn.argtypes = [pkvp, vp, vp, vp, vp, f32, i32, i32, vp, i32, vp, vp, sz, vp]
     L.reco_paged_decode_attn_weights.argtypes = [pkvp, vp, vp, vp, vp, f32, i32, i32, vp, i32, vp, vp, vp, sz, vp]
     L.reco_paged_evict.argtypes = [pkvp, vp, vp, vp, i32, i32, vp, vp, sz, vp]
-    for name in ("reco_paged_workspace_bytes", "reco_paged_decode_attn", "reco_paged_decode_attn_weights",
+    rows = ctypes.POINTER(reco_rows)
+    L.reco_paged_append.argtypes = [pkvp, rows, rows, rows, rows, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]
+    for name in ("reco_paged_append", "reco_paged_workspace_bytes", "reco_paged_decode_attn", "reco_paged_decode_attn_weights",
                  "reco_paged_evict", "reco_retention_ratio", "reco_keep_count", "reco_workspace_bytes", "reco_check",
                  "reco_score_cache", "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact",
                  "reco_select_topm", "reco_compact",
@@ -364,6 +370,48 @@ def reco_paged_evict(kv: reco_paged_kv, weights, lens, budget, w: int, sinks: in
     _check_place(ws, dev)
     _ok(lib().reco_paged_evict(ctypes.byref(kv), weights.data_ptr(), lens.data_ptr(), budget.data_ptr(), w, sinks,
                                _ptr(kept_idx), ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def _rows(name, t, shape, kv):
+    """A [layers, T, heads, d] tensor of the cache's type as a view with its strides."""
+    if t.shape != shape or t.dtype != kv.expect[1] or t.get_device() != kv.expect[0]:
+        raise ValueError(f"{name} must be {list(shape)} of {kv.expect[1]} on the cache's device, not {list(t.shape)} of {t.dtype}")
+    layer, token, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the elements of a row of {name} must lie next to each other")
+    return reco_rows(t.data_ptr(), layer, token, head)
+
+
+def reco_paged_append(kv: reco_paged_kv, k, v, starts, lens, ws, pos=None, inv_freq=None, q=None, q_out=None,
+                      interleaved: bool = False, stream=None):
+    """Appends the rows of new tokens, keys (and queries, into q_out) rotated by their positions.  k and v are
+    [layers, T, H_kv, d], q and q_out [layers, T, H_q, d], of any strides but the last; tokens starts[b] to
+    starts[b + 1] - 1 are sequence b's.  inv_freq [rot / 2] float32 gives the angles per position (None: no
+    rotation), pos [T] int32 the positions; pairs are (i, i + rot / 2), or neighbours if interleaved."""
+    dev, _, (Ly, B, H_q, d), _, _, units, _ = kv.expect
+    if k.dim() != 4:
+        raise ValueError("k must be [layers, T, H_kv, d]")
+    T = k.shape[1]
+    kr, vr = _rows("k", k, (Ly, T, kv.H_kv, d), kv), _rows("v", v, (Ly, T, kv.H_kv, d), kv)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out must both be given or both be None")
+    qr = qor = None
+    if q is not None:
+        qr, qor = ctypes.byref(_rows("q", q, (Ly, T, H_q, d), kv)), ctypes.byref(_rows("q_out", q_out, (Ly, T, H_q, d), kv))
+    _check_tensor("starts", starts, (B + 1,), torch.int32, dev)
+    _check_tensor("lens", lens, units, torch.int32, dev)
+    rot = 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+        _check_tensor("inv_freq", inv_freq, (rot // 2,), torch.float32, dev)
+        if pos is None:
+            raise ValueError("inv_freq needs pos")
+    if pos is not None:
+        _check_tensor("pos", pos, (T,), torch.int32, dev)
+    _check_place(ws, dev)
+    _ok(lib().reco_paged_append(ctypes.byref(kv), ctypes.byref(kr), ctypes.byref(vr), qr, qor, T, starts.data_ptr(),
+                                _ptr(pos), _ptr(inv_freq) if rot else None, rot, 1 if interleaved else 0, lens.data_ptr(),
+                                ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def reco_reflect_penalty(logits, ids, rewards, tau_l=0.4, tau_h=0.8, beta=4.0, beta_out=None,
