@@ -7,8 +7,8 @@
  * penalty (Eq. 3-4) with the draw of the next token from the penalised logits
  * (Sec. 3.3), and the answer-perplexity stop test (Eq. 5-6).  Beside them, for caches
  * whose rows lie in pages of a shared pool: decode attention, the running sums of its
- * weights, eviction down to a budget by those sums, and the append of new tokens with their
- * position rotation (the reco_paged_ calls).
+ * weights, eviction down to a budget by those sums, the append of new tokens with their
+ * position rotation, and decode attention over shared prefixes (the reco_paged_ calls).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -77,7 +77,8 @@ typedef enum {
     RECO_OP_PAGED_DECODE = 5, /* the paged calls: sized by reco_paged_workspace_bytes */
     RECO_OP_PAGED_WEIGHTS = 6,
     RECO_OP_PAGED_EVICT = 7,
-    RECO_OP_PAGED_APPEND = 8
+    RECO_OP_PAGED_APPEND = 8,
+    RECO_OP_PAGED_PREFIX = 9
 } reco_op;
 
 /* A paged cache: the rows of a sequence lie in pages of one pool that all sequences
@@ -140,8 +141,9 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
 
 /* Workspace bytes a paged call needs for this cache: RECO_OP_PAGED_DECODE,
  * RECO_OP_PAGED_WEIGHTS (it holds the logits of a token, 4 bytes per query head and row
- * of max_pages * page), RECO_OP_PAGED_EVICT or RECO_OP_PAGED_APPEND.  Only the sizes in kv are read.  The size
- * does not depend on the device or on lens.  Alignment: 256 bytes.  The decode's two
+ * of max_pages * page), RECO_OP_PAGED_EVICT, RECO_OP_PAGED_APPEND or
+ * RECO_OP_PAGED_PREFIX.  Only the sizes in kv are read.  The size
+ * does not depend on the device or on lens.  Alignment: 256 bytes.  The decodes'
  * are refused for more than 16 query heads per KV head, as the calls are.            */
 reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size_t *bytes_out);
 
@@ -379,6 +381,37 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
                                            const void *v_new, int32_t *lens, float scale, int window, int sinks,
                                            void *out, reco_dtype out_dtype, float *lse, float *weights, void *ws,
                                            size_t ws_bytes, cudaStream_t stream);
+
+/* reco_paged_decode_attn for a batch whose sequences share the rows of a prefix: several answers
+ * to one question (the paper samples several reasoning paths per question), whose rows lie
+ * once in the pool and are read once per group instead of once per sequence.
+ * Sequences next to each other with equal group[b] are a group; they share their first
+ * P = shared[b] rows, in every layer and head.  Row j of a sequence lies
+ *   for j < P   in the page that the table of the group's FIRST sequence names,
+ *   for j >= P  in the page that its own table names (entry j / page, row j % page, as ever;
+ *               the page that P falls into is each sequence's own, its rows below P unused),
+ * so that the entries of whole pages of the prefix are looked at in the first sequence's table
+ * only.  A sequence alone in its group reads all its rows through its own table.  lens counts
+ * all rows of a unit, those of the prefix among them: shared[b] <= lens[layer, b, h].  With
+ * these rows, out, lse, the append of k_new and v_new and the advance of lens are those of
+ * reco_paged_decode_attn without a window (the append goes through the sequence's own table).
+ *   group    : [B] int32 (device), any values; equal values that are not next to each other
+ *              are different groups
+ *   shared   : [B] int32 (device), the same for all sequences of a group; 0: nothing shared
+ *   ws       : reco_paged_workspace_bytes(RECO_OP_PAGED_PREFIX, kv) bytes, otherwise as
+ *              reco_paged_decode_attn's
+ * The pages of the prefix must not receive rows behind it that another sequence reads, but may
+ * hold the first sequence's own rows.  Cutting a unit below its prefix (reco_paged_evict) ends
+ * the sharing: its rows must be its own then.
+ * Errors are those of reco_paged_decode_attn, unit by unit (zeros, lse = -inf, the length kept).
+ * Also in error: a sequence whose shared[b] is negative or above the length of one of its units
+ * (that unit), or differs from that of the group's first sequence (all units of the
+ * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Precision as
+ * reco_decode_attn's, but for bf16 output from bf16 caches, where the probabilities of
+ * prefix rows enter their product with V as bf16 (2^-8 of each).                      */
+reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
+                                   int32_t *lens, const int32_t *group, const int32_t *shared, float scale, void *out,
+                                   reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes, cudaStream_t stream);
 
 /* Appends the keys and values of new tokens to a paged cache, the keys (and queries) rotated by
  * the tokens' positions on the way: prompts, pieces of prompts, or one token per sequence.  The

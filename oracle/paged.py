@@ -107,3 +107,49 @@ def append(K, V, table, lens, k, v, starts, pos=None, inv_freq=(), interleaved=F
                     K[ly, table[b, r // page], h, r % page] = rotate(k[ly, t, h], s, inv_freq, interleaved)
                     V[ly, table[b, r // page], h, r % page] = v[ly, t, h]
         lens[:, b] += starts[b + 1] - starts[b]
+
+
+def prefix_lead(group):
+    """The first sequence of each sequence's group (equal values next to each other)."""
+    lead = list(range(len(group)))
+    for b in range(1, len(group)):
+        if group[b] == group[b - 1]:
+            lead[b] = lead[b - 1]
+    return lead
+
+
+def prefix_decode(K, V, table, lens, q, kn, vn, scale, group, shared, skip=()):
+    """One token of sequences that share prefixes: decode(), the rows below shared[b] looked up in the table of
+    the group's first sequence.  Units in `skip` (layer, b, h) are left alone (zeros, -inf)."""
+    Ly, B, Hq, d = q.shape
+    H, page = K.shape[2], K.shape[3]
+    G = Hq // H
+    lead = prefix_lead(group)
+    out, lse = np.zeros((Ly, B, Hq, d)), np.full((Ly, B, Hq), -np.inf)
+    big, seen, absv = np.zeros((Ly, B, Hq)), np.zeros((Ly, B, Hq), int), np.zeros((Ly, B, Hq, d))
+    for ly, b, h in np.ndindex(Ly, B, H):
+        if (ly, b, h) in skip:
+            continue
+        n = int(lens[ly, b, h])
+        if kn is not None:
+            K[ly, table[b, n // page], h, n % page] = kn[ly, b, h]
+            V[ly, table[b, n // page], h, n % page] = vn[ly, b, h]
+            n += 1
+            lens[ly, b, h] = n
+        if n == 0:
+            continue
+        j = np.arange(n)
+        ids = np.where(j < shared[b], table[lead[b], j // page], table[b, j // page])
+        k, v = K[ly, ids, h, j % page].astype(np.float64), V[ly, ids, h, j % page].astype(np.float64)
+        for g in range(G):
+            i = (ly, b, h * G + g)
+            z = scale * (k @ q[i].astype(np.float64))
+            m = z.max()
+            with np.errstate(invalid="ignore"):  # logits that are all -inf
+                e = np.exp(z - m) if m > -np.inf or np.isnan(m) else np.zeros(n)
+            if e.sum() == 0:
+                continue
+            p = e / e.sum()
+            out[i], lse[i] = p @ v, m + np.log(e.sum())
+            big[i], seen[i], absv[i] = abs(scale) * (np.abs(k) @ np.abs(q[i])).max(), n, p @ np.abs(v)
+    return out, lse, big, seen, absv

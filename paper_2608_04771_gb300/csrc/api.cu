@@ -259,6 +259,7 @@ reco_status reco_workspace_bytes(reco_op op, const reco_kv *kv, int w, size_t *b
     case RECO_OP_PAGED_WEIGHTS:
     case RECO_OP_PAGED_EVICT:
     case RECO_OP_PAGED_APPEND:
+    case RECO_OP_PAGED_PREFIX:
         return fail(RECO_EINVAL, "op %d is sized by reco_paged_workspace_bytes", (int)op);
     }
     return fail(RECO_EINVAL, "unknown op %d", (int)op);
@@ -269,10 +270,11 @@ reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size
     if (!bytes_out) return fail(RECO_EINVAL, "NULL pointer");
     reco_status st = check_paged(kv, false);
     if (st != RECO_OK) return st;
-    if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS) {
+    if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS || op == RECO_OP_PAGED_PREFIX) {
         const int G = kv->H_q / kv->H_kv;
         if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
-        *bytes_out = reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
+        *bytes_out = op == RECO_OP_PAGED_PREFIX ? reco::prefix_ws_layout(*kv, nullptr).bytes
+                                                : reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
     } else if (op == RECO_OP_PAGED_EVICT)
         *bytes_out = reco::evict_ws_layout(*kv, nullptr).bytes;
     else if (op == RECO_OP_PAGED_APPEND)
@@ -465,7 +467,7 @@ namespace {
 reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
                                  int32_t *lens, float scale, int window, int sinks, void *out, reco_dtype out_dtype,
                                  float *lse, float *weights, void *ws, size_t ws_bytes, cudaStream_t stream,
-                                 const char *name)
+                                 const char *name, const int32_t *group = nullptr, const int32_t *shared = nullptr)
 {
     reco_status st = check_paged(kv);
     if (st != RECO_OK) return st;
@@ -481,11 +483,18 @@ reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const v
     const int G = kv->H_q / kv->H_kv;
     if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
     if (!(scale == scale)) return fail(RECO_EINVAL, "scale is NaN");
+    unsigned *err;
+    cudaError_t e;
+    if (group || shared) {
+        reco::PrefixWs lay = reco::prefix_ws_layout(*kv, ws);
+        if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK || (st = error_word(&err)) != RECO_OK) return st;
+        e = reco::launch_paged_prefix(*kv, q, k_new, v_new, lens, group, shared, scale, out, out_dtype, lse, lay, err, stream);
+        return e == cudaSuccess ? RECO_OK : cuda_fail(e, name);
+    }
     reco::PagedDecodeWs lay = reco::paged_decode_ws_layout(*kv, weights != nullptr, ws);
     if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK) return st;
-    unsigned *err;
     if ((st = error_word(&err)) != RECO_OK) return st;
-    cudaError_t e = reco::launch_paged_decode(*kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse,
+    e = reco::launch_paged_decode(*kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse,
                                               weights, lay, err, stream);
     return e == cudaSuccess ? RECO_OK : cuda_fail(e, name);
 }
@@ -509,6 +518,16 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
     if (!weights) return fail(RECO_EINVAL, "weights is NULL");
     return paged_decode_checked(kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse, weights, ws,
                                 ws_bytes, stream, "reco_paged_decode_attn_weights launch");
+}
+
+reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
+                                   int32_t *lens, const int32_t *group, const int32_t *shared, float scale, void *out,
+                                   reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes, cudaStream_t stream)
+{
+    if (!group || !shared) return fail(RECO_EINVAL, "NULL group or shared");
+    if (((uintptr_t)group | (uintptr_t)shared) & 3u) return fail(RECO_EINVAL, "group and shared must be 4-byte aligned");
+    return paged_decode_checked(kv, q, k_new, v_new, lens, scale, 0, 0, out, out_dtype, lse, nullptr, ws, ws_bytes, stream,
+                                "reco_paged_prefix_attn launch", group, shared);
 }
 
 reco_status reco_paged_evict(const reco_paged_kv *kv, float *weights, int32_t *lens, const int32_t *budget, int w,

@@ -26,6 +26,8 @@ constexpr size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 // 256, 1024 or 8192 bytes here, 39 to 40.4 with 2048, 4352, 12288 or 16384; other evictions stay within 3%.)
 constexpr size_t kPagedZeroBytes = 8192;
 
+// CTAs of a paged decode at most (two partial slots each in its workspace).
+constexpr int kPagedMaxGrid = 256;
 // The append's counters, one per group of layers, in that place behind those of the other calls.
 constexpr size_t kAppendCounters = 4096;
 constexpr int kAppendGroups = 512;
@@ -95,11 +97,38 @@ struct EvictWs {
     size_t bytes;
 };
 
+// Decode attention over shared prefixes.  A group of at least two sequences with a prefix: its first sequence, their
+// number, the prefix's rows, and the work of the groups before it (of a layer and KV head).
+struct PrefixRun {
+    int b0, n, p, pad;
+    long long work;
+};
+struct PrefixTotal {
+    long long work;  // of all groups, per layer and KV head
+    int n;           // groups listed
+};
+constexpr int kPrefixTile = 128;     // rows of the prefix in a tile
+constexpr int kPrefixMaxRows = 256;  // query rows of a row tile, at most
+
+struct PrefixWs {
+    PagedDecodeWs own;
+    int32_t *run_of;     // [B] the sequence's group in runs, -1: it has no shared rows, -2: in error
+    PrefixRun *runs;     // [B / 2 + 1]
+    PrefixTotal *total;
+    float *own_out, *own_l2;  // the own part, [heads][d] and [heads] (log2; +inf: in error)
+    float *part_o;            // [heads][d]
+    float2 *part_ml;          // [heads]
+    float *cont_o;            // [CTAs][row tile][d]
+    float2 *cont_ml;
+    size_t bytes;
+};
+
 ScoreWs score_ws_layout(const reco_kv &kv, int w, void *base);
 SelectWs select_ws_layout(const reco_kv &kv, void *base);
 DecodeWs decode_ws_layout(const reco_kv &kv, void *base);
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base);
 EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base);
+PrefixWs prefix_ws_layout(const reco_paged_kv &kv, void *base);
 
 // Rows a unit of the paged cache may hold.
 inline int paged_cap(const reco_paged_kv &kv) { return kv.max_pages * kv.page; }
@@ -143,6 +172,13 @@ cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t 
 // The eviction's selection: kept rows into idx, weights compacted, lens cut, the compaction's list.
 cudaError_t launch_select_budget(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
                                  int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s);
+// The part of decode attention over shared prefixes that is each sequence's own (l2: log2 of the sums), and all of it.
+cudaError_t launch_paged_own(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new, int32_t *lens,
+                             const int32_t *group, const int32_t *shared, float scale, float *out, float *l2,
+                             const PagedDecodeWs &ws, unsigned *err, cudaStream_t s);
+cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new, int32_t *lens,
+                                const int32_t *group, const int32_t *shared, float scale, void *out, reco_dtype out_dtype,
+                                float *lse, const PrefixWs &ws, unsigned *err, cudaStream_t s);
 // q, q_out: nullptr or both.
 cudaError_t launch_paged_append(const reco_paged_kv &kv, const reco_rows &k, const reco_rows &v, const reco_rows *q,
                                 const reco_rows *q_out, int T, const int32_t *starts, const int32_t *pos,

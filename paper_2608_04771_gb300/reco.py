@@ -17,14 +17,14 @@ _lib = None
 RECO_OK, RECO_EINVAL, RECO_EUNSUPPORTED, RECO_ECUDA, RECO_EDEVICE = range(5)
 RECO_F32, RECO_BF16 = 0, 1
 RECO_OP_SCORE, RECO_OP_SELECT, RECO_OP_DECODE, RECO_OP_PPL, RECO_OP_SAMPLE = range(5)
-RECO_OP_PAGED_DECODE, RECO_OP_PAGED_WEIGHTS, RECO_OP_PAGED_EVICT, RECO_OP_PAGED_APPEND = range(5, 9)
+RECO_OP_PAGED_DECODE, RECO_OP_PAGED_WEIGHTS, RECO_OP_PAGED_EVICT, RECO_OP_PAGED_APPEND, RECO_OP_PAGED_PREFIX = range(5, 10)
 
 EXPORTS = ("reco_retention_ratio", "reco_keep_count", "reco_penalty_band", "reco_probe_trigger",
            "reco_workspace_bytes", "reco_last_error", "reco_check", "reco_score_cache",
            "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact", "reco_select_topm", "reco_compact",
            "reco_decode_attn", "reco_decode_attn_ring", "reco_reflect_penalty", "reco_penalty_sample", "reco_answer_ppl",
            "reco_answer_ppl_static", "reco_paged_workspace_bytes", "reco_paged_decode_attn",
-           "reco_paged_decode_attn_weights", "reco_paged_evict", "reco_paged_append")
+           "reco_paged_decode_attn_weights", "reco_paged_evict", "reco_paged_append", "reco_paged_prefix_attn")
 RECO_PPL_STATIC_MAX_ROWS = 65536
 
 
@@ -96,7 +96,8 @@ def lib():
     L.reco_paged_evict.argtypes = [pkvp, vp, vp, vp, i32, i32, vp, vp, sz, vp]
     rows = ctypes.POINTER(reco_rows)
     L.reco_paged_append.argtypes = [pkvp, rows, rows, rows, rows, i32, vp, vp, vp, i32, i32, vp, vp, sz, vp]
-    for name in ("reco_paged_append", "reco_paged_workspace_bytes", "reco_paged_decode_attn", "reco_paged_decode_attn_weights",
+    L.reco_paged_prefix_attn.argtypes = [pkvp, vp, vp, vp, vp, vp, vp, f32, vp, i32, vp, vp, sz, vp]
+    for name in ("reco_paged_append", "reco_paged_prefix_attn", "reco_paged_workspace_bytes", "reco_paged_decode_attn", "reco_paged_decode_attn_weights",
                  "reco_paged_evict", "reco_retention_ratio", "reco_keep_count", "reco_workspace_bytes", "reco_check",
                  "reco_score_cache", "reco_score_cache_lse", "reco_lse_push", "reco_copy_row", "reco_select_compact",
                  "reco_select_topm", "reco_compact",
@@ -356,6 +357,17 @@ def reco_paged_decode_attn_weights(kv: reco_paged_kv, q, k_new, v_new, lens, sca
     _ok(lib().reco_paged_decode_attn_weights(ctypes.byref(kv), q.data_ptr(), _ptr(k_new), _ptr(v_new), lens.data_ptr(),
                                              scale, window, sinks, out.data_ptr(), _dtype_code(out.dtype), _ptr(lse),
                                              weights.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def reco_paged_prefix_attn(kv: reco_paged_kv, q, k_new, v_new, lens, group, shared, scale: float, out, lse, ws, stream=None):
+    """reco_paged_decode_attn for sequences that share a prefix: those next to each other with equal group[b] read
+    their first shared[b] rows, once for all of them, through the first one's table.  group and shared are int32 [B]."""
+    _check_paged_decode(kv, q, k_new, v_new, lens, out, lse, ws)
+    _check_tensor("group", group, (kv.B,), torch.int32, kv.expect[0])
+    _check_tensor("shared", shared, (kv.B,), torch.int32, kv.expect[0])
+    _ok(lib().reco_paged_prefix_attn(ctypes.byref(kv), q.data_ptr(), _ptr(k_new), _ptr(v_new), lens.data_ptr(), group.data_ptr(),
+                                     shared.data_ptr(), scale, out.data_ptr(), _dtype_code(out.dtype), _ptr(lse), ws.data_ptr(),
+                                     ws.numel(), _stream(stream)))
 
 
 def reco_paged_evict(kv: reco_paged_kv, weights, lens, budget, w: int, sinks: int, kept_idx, ws, stream=None):
