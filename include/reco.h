@@ -403,6 +403,7 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  * The pages of the prefix must not receive rows behind it that another sequence reads, but may
  * hold the first sequence's own rows.  Cutting a unit below its prefix (reco_paged_evict) ends
  * the sharing: its rows must be its own then.
+ * An infinity in a V row that is seen makes its element of out infinite or NaN.
  * Errors are those of reco_paged_decode_attn, unit by unit (zeros, lse = -inf, the length kept).
  * Also in error: a sequence whose shared[b] is negative or above the length of one of its units
  * (that unit), or differs from that of the group's first sequence (all units of the

@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan(const int32_t *__res
     if (off) raise_error(err, ERR_LEN);
 }
 
-// ---------------------------------------------------------------- prefix part, plain FMAs
+// ---------------------------------------------------------------- prefix part, float32
 // Eight warps.  A warp takes 8 of the tile's query rows and, where the tile has fewer than 64, a share of the keys of
 // each tile (WR row groups, 8 / WR key groups).  QK^T: a half-warp has four rows, a lane of it WR keys; PV: a lane has D / 32
 // columns of all eight rows and takes the probabilities from shared memory.  Every sum is float32.
@@ -97,40 +97,20 @@ template <int D> __device__ __forceinline__ int chunk_at(int r, int c) { return 
 
 __device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 
-template <typename T, int D> __device__ __forceinline__ void load_row_chunk(float *dst, int r, int c, const char *src)
-{
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4 *>(dst + chunk_at<D>(r, c)) =
-            src ? __ldg(reinterpret_cast<const float4 *>(src) + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    } else {
-        const uint2 w = src ? __ldg(reinterpret_cast<const uint2 *>(src) + c) : make_uint2(0, 0);
-        *reinterpret_cast<float4 *>(dst + chunk_at<D>(r, c)) =
-            make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                        __uint_as_float(w.y & 0xffff0000u));
-    }
-}
-
-template <typename T, int D, int WR>
+template <int D, int WR>
 __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPiece &pc, float *sm, int *sm_bad)
 {
     constexpr int WK = 8 / WR, E = D / 32, KEYS = kPrefixTile / WK;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, half = lane >> 4, l16 = lane & 15;
     float *Q = sm, *K = Q + kPlainRows * D, *V = K + kPrefixTile * D, *ps = V + kPrefixTile * D + wid * 8 * kPrefixTile;
     float2 *ml = reinterpret_cast<float2 *>(V + kPrefixTile * D + 8 * 8 * kPrefixTile);
-    const int nrows = min(kPlainRows, pc.n * a.G - pc.rt * kPlainRows);
+    const int nrows = pc.nrows;
     __syncthreads();
     if (tid == 0) *sm_bad = 0;
     for (int i = tid; i < 8 * WR * (D / 4); i += 256) {
         const int r = i / (D / 4), c = i % (D / 4);
-        const char *src = r < nrows ? (const char *)a.q + a.q_row(pc, pc.rt * kPlainRows + r) * D * sizeof(T) : nullptr;
-        float *dst = Q + r * D + 4 * c;
-        if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(dst) = src ? __ldg(reinterpret_cast<const float4 *>(src) + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-            const uint2 w = src ? __ldg(reinterpret_cast<const uint2 *>(src) + c) : make_uint2(0, 0);
-            *reinterpret_cast<float4 *>(dst) = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
-                                                           __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-        }
+        *reinterpret_cast<float4 *>(Q + r * D + 4 * c) =
+            r < nrows ? ld4((const float *)a.q + a.q_row(pc, pc.rt * kPlainRows + r) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     float o[8][E], m[4], l[4];
 #pragma unroll
@@ -147,18 +127,18 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         __syncthreads();  // the last tile has been read
         for (int i = tid; i < kPrefixTile * (D / 4); i += 256) {
             const int r = i / (D / 4), c = i % (D / 4);
-            const char *kr = nullptr, *vr = nullptr;
+            float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
             if (r < live) {
                 const long long row = a.pool_row(pc, k0 + r);
                 if (row >= 0) {
-                    kr = (const char *)a.K + row * D * (long long)sizeof(T);
-                    vr = (const char *)a.V + row * D * (long long)sizeof(T);
+                    k = ld4((const float *)a.K + row * D + 4 * c);
+                    v = ld4((const float *)a.V + row * D + 4 * c);
                 } else {
                     *sm_bad = 1;
                 }
             }
-            load_row_chunk<T, D>(K, r, c, kr);
-            load_row_chunk<T, D>(V, r, c, vr);
+            *reinterpret_cast<float4 *>(K + chunk_at<D>(r, c)) = k;
+            *reinterpret_cast<float4 *>(V + chunk_at<D>(r, c)) = v;
         }
         __syncthreads();
         float s[4][WR];
@@ -286,14 +266,14 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         }
         float *po;
         float2 *pm;
-        a.partial<D>(pc, r, kPlainRows, po, pm);
+        a.partial<D>(pc, r, po, pm);
         *reinterpret_cast<float4 *>(po + 4 * c) = acc;
         if (c == 0) *pm = make_float2(M, bad ? -1.f : L);
     }
     if (bad && tid == 0) raise_error(a.err, ERR_PAGE);
 }
 
-template <typename T, int D> __global__ void __launch_bounds__(256, 1) prefix_plain(const __grid_constant__ PrefixArgs a)
+template <int D> __global__ void __launch_bounds__(256, 1) prefix_plain(const __grid_constant__ PrefixArgs a)
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ int sm_bad;
@@ -301,16 +281,15 @@ template <typename T, int D> __global__ void __launch_bounds__(256, 1) prefix_pl
     wait_prior_grid();
     PrefixWalk w = a.range();
     PrefixPiece pc;
-    while (a.next(w, kPlainRows, pc)) {
-        const int nrows = min(kPlainRows, pc.n * a.G - pc.rt * kPlainRows);
-        if (nrows <= 8)
-            plain_piece<T, D, 1>(a, pc, sm, &sm_bad);
-        else if (nrows <= 16)
-            plain_piece<T, D, 2>(a, pc, sm, &sm_bad);
-        else if (nrows <= 32)
-            plain_piece<T, D, 4>(a, pc, sm, &sm_bad);
+    while (a.next(w, pc)) {
+        if (pc.nrows <= 8)
+            plain_piece<D, 1>(a, pc, sm, &sm_bad);
+        else if (pc.nrows <= 16)
+            plain_piece<D, 2>(a, pc, sm, &sm_bad);
+        else if (pc.nrows <= 32)
+            plain_piece<D, 4>(a, pc, sm, &sm_bad);
         else
-            plain_piece<T, D, 8>(a, pc, sm, &sm_bad);
+            plain_piece<D, 8>(a, pc, sm, &sm_bad);
     }
 }
 
@@ -326,7 +305,7 @@ template <int D> __global__ void __launch_bounds__(128) prefix_join(const __grid
     if (run >= 0) {
         rn = a.p.runs[run];
         total = a.p.total->work * a.p.layers * a.p.Hkv;
-        ctas = prefix_ctas(total, a.grid);
+        ctas = prefix_ctas(total, a.grid, a.p.rows);
         lh0 = ((long long)layer * a.p.Hkv + h) * a.p.total->work;
     }
     const size_t q0 = (size_t)lb * a.p.Hq + (size_t)h * G;
@@ -347,12 +326,16 @@ template <int D> __global__ void __launch_bounds__(128) prefix_join(const __grid
             M = Mn;
         };
         if (run >= 0 && !err) {
-            const int r = (b - rn.b0) * G + g, rt = r / a.rows, kt = (rn.p + kPrefixTile - 1) / kPrefixTile;
-            const long long w0 = lh0 + rn.work + (long long)rt * kt;
-            const int c0 = prefix_cta(w0, total, ctas), c1 = prefix_cta(w0 + kt - 1, total, ctas);
+            const int rows = a.p.rows, r = (b - rn.b0) * G + g, rt = r / rows, kt = (rn.p + kPrefixTile - 1) / kPrefixTile;
+            const int unit = prefix_unit(rn.n * G, rt, rows);
+            const long long w0 = lh0 + rn.work + (long long)rt * kt * ((rows + 127) / 128);
+            const int c0 = prefix_cta(w0, total, ctas);
+            int c1 = prefix_cta(w0 + (long long)kt * unit - 1, total, ctas);
+            // (the last one may have no more than the end of a key tile, which is the one's before)
+            if (c1 > c0 && prefix_begin(c1, total, ctas) - w0 > (long long)(kt - 1) * unit) --c1;
             add(a.p.part_ml[q0 + g], ld4(a.p.part_o + (q0 + g) * D + 4 * c));
             for (int s = c0 + 1; s <= c1; ++s) {
-                const size_t at = (size_t)s * a.p.cont_rows + r % a.rows;
+                const size_t at = (size_t)s * a.p.cont_rows + r % rows;
                 add(a.p.cont_ml[at], ld4(a.p.cont_o + at * D + 4 * c));
             }
         }
@@ -410,7 +393,7 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
 {
     const bool f32 = kv.dtype == RECO_F32;
     const int cap = paged_cap(kv), units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv;
-    const int rows = kPlainRows;
+    const int rows = f32 ? kPlainRows : kPrefixMaxRows;
     cudaError_t e = launch_pdl(prefix_plan, dim3(1), dim3(kPlanThreads), 0, s, group, shared, kv.B, G, cap, rows, ws.runs,
                                ws.run_of, ws.total, err);
     if (e != cudaSuccess) return e;
@@ -437,14 +420,18 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     a.n_pages = kv.n_pages;
     a.max_pages = kv.max_pages;
     a.shift = __builtin_ctz((unsigned)kv.page);
+    a.rows = rows;
     a.cont_rows = prefix_cont_rows(kv);
     a.c2 = scale * kLog2e;
     a.err = err;
-    void (*fn)(PrefixArgs) = kv.d == 64 ? (f32 ? prefix_plain<float, 64> : prefix_plain<__nv_bfloat16, 64>)
-                                        : (f32 ? prefix_plain<float, 128> : prefix_plain<__nv_bfloat16, 128>);
-    const int smem = kv.d == 64 ? plain_smem<64>() : plain_smem<128>();
-    if ((e = allow_smem((const void *)fn, smem)) != cudaSuccess) return e;
-    if ((e = launch_pdl(fn, dim3(grid), dim3(256), smem, s, a)) != cudaSuccess) return e;
+    if (f32) {
+        void (*fn)(PrefixArgs) = kv.d == 64 ? prefix_plain<64> : prefix_plain<128>;
+        const int smem = kv.d == 64 ? plain_smem<64>() : plain_smem<128>();
+        if ((e = allow_smem((const void *)fn, smem)) != cudaSuccess) return e;
+        if ((e = launch_pdl(fn, dim3(grid), dim3(256), smem, s, a)) != cudaSuccess) return e;
+    } else {
+        if ((e = launch_prefix_tc(kv, a, grid, out_dtype, s)) != cudaSuccess) return e;
+    }
     PrefixJoin j = {};
     j.p = a;
     j.own_out = ws.own_out;
@@ -453,7 +440,6 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     j.out = out;
     j.lse = lse;
     j.grid = grid;
-    j.rows = rows;
     j.cap = cap;
     j.append = k_new ? 1 : 0;
     j.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;

@@ -236,7 +236,10 @@ def test_nan_and_infinities_among_the_rows(dtype):
     c.run()
     reco.reco_check()
     assert torch.isfinite(c.lse).all() and torch.isfinite(c.out[0, :2]).all()
-    assert torch.isinf(c.out[0, 2:, :2, 9]).all() and torch.isfinite(c.out[0, 2:, :2, :9]).all()
+    # an infinite value: infinity, or NaN where a probability enters in two bf16 parts (the second is of either sign or
+    # zero: hi * inf + lo * inf), in its element alone
+    bad = c.out[0, 2:, :2, 9]
+    assert (torch.isinf(bad) if dtype == F32 else ~torch.isfinite(bad)).all() and torch.isfinite(c.out[0, 2:, :2, :9]).all()
     c = batch()
     c.q[:] = c.q.abs()
     c.K[0, int(c.table[0, 1]), 0, 2, 9] = float("inf")
