@@ -36,10 +36,12 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 // Programmatic dependent launch.  Kernels launched with launch_pdl() may be scheduled
 // while the previous kernel in the stream drains; each one calls wait_prior_grid()
 // before it reads anything a previous kernel wrote (it returns at once when the launch
-// was an ordinary one).  No kernel signals its dependents early, so a dependent grid
+// was an ordinary one).  The last kernel of a call does not signal its dependents early, so a dependent grid
 // starts only as the previous one's blocks exit: what overlaps is launch processing and
-// the part of a kernel before its wait.
+// the part of a kernel before its wait.  (Inside a call of several kernels one may: release_next_grid.)
 __device__ __forceinline__ void wait_prior_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Lets the dependent grid's CTAs start wherever there is room for them (once every CTA of this grid has said so).
+__device__ __forceinline__ void release_next_grid() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,

@@ -107,18 +107,24 @@ struct PrefixTotal {
     long long work;  // of all groups, per layer and KV head
     int n;           // groups listed
 };
-constexpr int kPrefixTile = 128;     // rows of the prefix in a tile
+// A unit's own rows: the work of those before it in its block of units, the row its first tile begins at, its rows (with an
+// appended one), the first that is its own (-1: the unit is in error).
+struct PrefixUnit {
+    int work, k0, n, lo;
+};
+constexpr int kPrefixTile = 128;     // cached rows in a tile
 constexpr int kPrefixMaxRows = 256;  // query rows of a row tile, at most
+constexpr int kPrefixBlock = 1024;   // units of a block of the plan
 
 struct PrefixWs {
-    PagedDecodeWs own;
     int32_t *run_of;     // [B] the sequence's group in runs, -1: it has no shared rows, -2: in error
     PrefixRun *runs;     // [B / 2 + 1]
     PrefixTotal *total;
-    float *own_out, *own_l2;  // the own part, [heads][d] and [heads] (log2; +inf: in error)
-    float *part_o;            // [heads][d]
-    float2 *part_ml;          // [heads]
-    float *cont_o;            // [CTAs][row tile][d]
+    PrefixUnit *units;    // [units]
+    int32_t *block_work;  // [blocks of units] work of their own rows
+    float *own_o, *part_o;     // [heads][d]: first partials of own rows and of prefixes
+    float2 *own_ml, *part_ml;  // [heads]
+    float *cont_o;             // [CTAs][row tile][d]: the other partial of a CTA
     float2 *cont_ml;
     size_t bytes;
 };
@@ -172,10 +178,6 @@ cudaError_t launch_paged_evict(const reco_paged_kv &kv, float *weights, int32_t 
 // The eviction's selection: kept rows into idx, weights compacted, lens cut, the compaction's list.
 cudaError_t launch_select_budget(const reco_paged_kv &kv, float *weights, int32_t *lens, const int32_t *budget, int w,
                                  int sinks, int32_t *idx, const EvictWs &ws, unsigned *err, cudaStream_t s);
-// The part of decode attention over shared prefixes that is each sequence's own (l2: log2 of the sums), and all of it.
-cudaError_t launch_paged_own(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new, int32_t *lens,
-                             const int32_t *group, const int32_t *shared, float scale, float *out, float *l2,
-                             const PagedDecodeWs &ws, unsigned *err, cudaStream_t s);
 cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const void *k_new, const void *v_new, int32_t *lens,
                                 const int32_t *group, const int32_t *shared, float scale, void *out, reco_dtype out_dtype,
                                 float *lse, const PrefixWs &ws, unsigned *err, cudaStream_t s);
@@ -202,5 +204,8 @@ int device_sm_count();
 // Returns false if the driver entry point is unavailable or the encode fails.
 bool encode_bf16_2d(void *map /* CUtensorMap */, const void *base, unsigned long long rows, int cols,
                     int box_cols, int box_rows);
+
+// The same over [rows][heads][d] with boxes of box_rows x box_heads x 64 elements.
+bool encode_bf16_heads(void *map, const void *base, unsigned long long rows, int heads, int d, int box_heads, int box_rows);
 
 }  // namespace reco

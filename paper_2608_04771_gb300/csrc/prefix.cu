@@ -3,16 +3,16 @@
 // first sequence names.
 //
 // For a query head with logits x_j over the prefix (j < P) and over its sequence's own rows (j >= P), the softmax over
-// both is that of the two parts joined: with M = max(m_p, m_o) to base 2,
-//   l = 2^(m_p - M) l_p + 2^(m_o - M) l_o,   out = (2^(m_p - M) o_p + 2^(m_o - M) o_o) / l.
-// Four launches: prefix_plan lists the groups; the own part is paged_kernel.cuh's decode kernel, with the prefix out of
-// sight; the prefix part reads the prefix's rows once for all query heads of a group; prefix_join joins the parts and
-// advances the lengths.
+// both is that of the parts joined: with M the largest of the parts' maxima m_i (to base 2),
+//   l = sum_i 2^(m_i - M) l_i,   out = sum_i 2^(m_i - M) o_i / l.
+// Three launches: prefix_plan appends the new rows, lists the groups and counts the work; the attention (float32 here, bf16
+// in prefix_tc.cu) reads a prefix's rows once for all query heads of its group, and each unit's own rows;
+// prefix_join joins the parts and advances the lengths.
 //
-// The prefix part: of a layer, KV head and group of n sequences, R = n G query rows are cut into tiles, the P rows of
-// the prefix into tiles of 128; the (row tile, key tile) pairs of all layers, heads and groups laid end to end
-// (key tiles innermost) are shared out evenly to one CTA per SM.  An item (a row tile against its prefix) that is cut
-// between CTAs leaves several partials (max, sum, output); its first one lies by query head, the others by CTA.
+// The work: the n sequences of a group are cut into row tiles, rows into tiles of 128; the (row tile, key tile) pairs of
+// all layers, heads and groups, then the key tiles of the units' own rows, laid end to end, are shared out evenly to
+// one CTA per SM.  An item (a row tile against its prefix, a unit against its own rows) that is cut between CTAs leaves
+// several partials (max, sum, output), joined in the order of the CTAs: the same inputs give the same bits.
 #include <algorithm>
 
 #include "decode_block.cuh"
@@ -21,8 +21,6 @@
 namespace reco {
 
 // ---------------------------------------------------------------- plan
-constexpr int kPlanThreads = 1024;
-
 // Inclusive scan over the CTA's threads: of maxima or sums.
 template <bool MAX, typename V> __device__ __forceinline__ V scan_block(V x, V *sm)
 {
@@ -39,52 +37,133 @@ template <bool MAX, typename V> __device__ __forceinline__ V scan_block(V x, V *
     return x;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) prefix_plan(const int32_t *__restrict__ group, const int32_t *__restrict__ shared,
-                                                            int B, int G, int cap, int rows, PrefixRun *runs,
-                                                            int32_t *run_of, PrefixTotal *total, unsigned *err)
+struct PlanArgs {
+    void *K, *V;
+    const void *k_new, *v_new;  // or nullptr
+    const int32_t *table, *lens, *group, *shared;
+    int units, B, Hkv, cap, n_pages, max_pages, shift, row_bytes;
+    PrefixRows rows;
+    PrefixWs ws;
+    unsigned *err;
+};
+
+__device__ __forceinline__ bool has_company(const int32_t *group, int B, int b)
 {
-    __shared__ long long sm[kPlanThreads / 32], sm_work;
+    const int g = __ldg(group + b);
+    const int prev = b > 0 ? __ldg(group + b - 1) : ~g, next = b + 1 < B ? __ldg(group + b + 1) : ~g;
+    return prev == g || next == g;
+}
+
+// The groups of at least two sequences that share rows, in order, and each sequence's.
+__device__ void plan_groups(const PlanArgs &a)
+{
+    __shared__ long long sm[kPrefixBlock / 32], sm_work;
     __shared__ int sm_start, sm_runs;
     if (threadIdx.x == 0) {
         sm_work = 0;
         sm_start = -1;
         sm_runs = 0;
     }
-    wait_prior_grid();
     bool off = false;
-    for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    for (int b0 = 0; b0 < a.B; b0 += kPrefixBlock) {
         const int b = b0 + threadIdx.x;
-        const bool in = b < B;
-        const int g = in ? __ldg(group + b) : 0;
-        const bool first = in && (b == 0 || __ldg(group + b - 1) != g), last = in && (b == B - 1 || __ldg(group + b + 1) != g);
+        const bool in = b < a.B;
+        const int g = in ? __ldg(a.group + b) : 0;
+        const bool first = in && (b == 0 || __ldg(a.group + b - 1) != g), last = in && (b == a.B - 1 || __ldg(a.group + b + 1) != g);
         __syncthreads();
         const int c_start = sm_start, c_runs = sm_runs;
         const long long c_work = sm_work;
         const int start = max(c_start, scan_block<true>(first ? b : -1, reinterpret_cast<int *>(sm)));
-        const int p = in ? __ldg(shared + start) : 0;
-        const bool valid = p >= 0 && p <= cap, kept = in && valid && p > 0 && !(first && last);
+        const int p = in ? __ldg(a.shared + start) : 0;
+        const bool valid = p >= 0 && p <= a.cap, kept = in && valid && p > 0 && !(first && last);
         const int run = c_runs + scan_block<false>(first && kept ? 1 : 0, reinterpret_cast<int *>(sm)) - 1;
-        const long long mine = last && kept ? prefix_work(b - start + 1, G, p, rows) : 0;
+        const long long mine = last && kept ? a.rows.work(b - start + 1, p) : 0;
         const long long work = c_work + scan_block<false>(mine, sm);
-        if (last && kept) runs[run] = PrefixRun{start, b - start + 1, p, 0, work - mine};
+        if (last && kept) a.ws.runs[run] = PrefixRun{start, b - start + 1, p, 0, work - mine};
         if (in) {
-            const bool wrong = !valid || __ldg(shared + b) != p;
+            const bool wrong = !valid || __ldg(a.shared + b) != p;
             off |= wrong;
-            run_of[b] = wrong ? -2 : (kept ? run : -1);
+            a.ws.run_of[b] = wrong ? -2 : (kept ? run : -1);
         }
         __syncthreads();
-        if (threadIdx.x == kPlanThreads - 1) {
+        if (threadIdx.x == kPrefixBlock - 1) {
             sm_start = start;
             sm_runs = run + 1;
             sm_work = work;
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) *total = PrefixTotal{sm_work, sm_runs};
-    if (off) raise_error(err, ERR_LEN);
+    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs};
+    if (off) raise_error(a.err, ERR_LEN);
 }
 
-// ---------------------------------------------------------------- prefix part, float32
+// Whether a unit's length and prefix are in order, and the pool row of its new row (-1: its table names no page for it).
+__device__ __forceinline__ bool unit_fine(const PlanArgs &a, int L, int p) { return unit_ok(L, a.cap, a.k_new != nullptr) && p >= 0 && p <= L; }
+__device__ __forceinline__ long long new_row(const PlanArgs &a, int u, int L)
+{
+    const int lb = u / a.Hkv, layer = lb / a.B, b = lb - layer * a.B;
+    const int e = __ldg(a.table + (long long)b * a.max_pages + (L >> a.shift));
+    if ((unsigned)e >= (unsigned)a.n_pages) return -1;
+    return ((((long long)layer * a.n_pages + e) * a.Hkv + (u - lb * a.Hkv)) << a.shift) + (L & ((1 << a.shift) - 1));
+}
+
+// A block of units: their own rows and the work of those.
+__device__ void plan_units(const PlanArgs &a, int block)
+{
+    __shared__ int sm[kPrefixBlock / 32];
+    const int u = block * kPrefixBlock + threadIdx.x, append = a.k_new ? 1 : 0;
+    PrefixUnit x = {0, 0, 0, -1};
+    int work = 0;
+    if (u < a.units) {
+        const int L = __ldcg(a.lens + u), b = u / a.Hkv % a.B, p = __ldg(a.shared + b);
+        const bool company = has_company(a.group, a.B, b);
+        if (!unit_fine(a, L, p)) {
+            raise_error(a.err, append && L == a.cap ? ERR_ROOM : ERR_LEN);
+        } else if (append && new_row(a, u, L) < 0) {
+            raise_error(a.err, ERR_PAGE);
+        } else {
+            x.n = L + append;
+            x.lo = company ? p : 0;
+            x.k0 = x.lo & -min(kPrefixTile, 1 << a.shift);  // the tensor cores' kernel copies whole boxes
+            work = x.n > x.lo ? 2 * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
+        }
+    }
+    const int before = scan_block<false>(work, sm) - work;
+    if (u < a.units) {
+        x.work = before;
+        a.ws.units[u] = x;
+    }
+    if (threadIdx.x == kPrefixBlock - 1) a.ws.block_work[block] = before + work;
+}
+
+// New rows into the pool, 16 bytes a thread.
+__device__ void plan_rows(const PlanArgs &a, int block)
+{
+    const int chunks = a.row_bytes / 16;
+    const long long i = (long long)block * kPrefixBlock + threadIdx.x;
+    const int u = (int)(i / (2 * chunks)), c = (int)(i - (long long)u * 2 * chunks), at = c < chunks ? c : c - chunks;
+    if (u >= a.units) return;
+    const uint4 x = __ldg(reinterpret_cast<const uint4 *>(c < chunks ? a.k_new : a.v_new) + (long long)u * chunks + at);
+    const int L = __ldcg(a.lens + u);
+    if (!unit_fine(a, L, __ldg(a.shared + u / a.Hkv % a.B))) return;
+    const long long r = new_row(a, u, L);
+    if (r >= 0) reinterpret_cast<uint4 *>(c < chunks ? a.K : a.V)[r * chunks + at] = x;
+}
+
+__global__ void __launch_bounds__(kPrefixBlock) prefix_plan(const __grid_constant__ PlanArgs a)
+{
+    release_next_grid();  // (the attention's CTAs set themselves up meanwhile)
+    wait_prior_grid();
+    const int blocks = (a.units + kPrefixBlock - 1) / kPrefixBlock;
+    if (blockIdx.x == 0)
+        plan_groups(a);
+    else if ((int)blockIdx.x <= blocks)
+        plan_units(a, blockIdx.x - 1);
+    else
+        plan_rows(a, blockIdx.x - 1 - blocks);
+}
+
+// ---------------------------------------------------------------- attention, float32
 // Eight warps.  A warp takes 8 of the tile's query rows and, where the tile has fewer than 64, a share of the keys of
 // each tile (WR row groups, 8 / WR key groups).  QK^T: a half-warp has four rows, a lane of it WR keys; PV: a lane has D / 32
 // columns of all eight rows and takes the probabilities from shared memory.  Every sum is float32.
@@ -104,13 +183,13 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, half = lane >> 4, l16 = lane & 15;
     float *Q = sm, *K = Q + kPlainRows * D, *V = K + kPrefixTile * D, *ps = V + kPrefixTile * D + wid * 8 * kPrefixTile;
     float2 *ml = reinterpret_cast<float2 *>(V + kPrefixTile * D + 8 * 8 * kPrefixTile);
-    const int nrows = pc.nrows;
+    const int nrows = pc.nseq * a.G;
     __syncthreads();
     if (tid == 0) *sm_bad = 0;
     for (int i = tid; i < 8 * WR * (D / 4); i += 256) {
         const int r = i / (D / 4), c = i % (D / 4);
         *reinterpret_cast<float4 *>(Q + r * D + 4 * c) =
-            r < nrows ? ld4((const float *)a.q + a.q_row(pc, pc.rt * kPlainRows + r) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            r < nrows ? ld4((const float *)a.q + a.q_row(pc, r / a.G, r % a.G) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     float o[8][E], m[4], l[4];
 #pragma unroll
@@ -123,12 +202,12 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         l[r] = 0.f;
     }
     for (int t = pc.t0; t < pc.t1; ++t) {
-        const int k0 = t * kPrefixTile, live = min(kPrefixTile, pc.p - k0);
+        const int k0 = pc.k0 + t * kPrefixTile, live = min(kPrefixTile, pc.end - k0), low = pc.lo - k0;
         __syncthreads();  // the last tile has been read
         for (int i = tid; i < kPrefixTile * (D / 4); i += 256) {
             const int r = i / (D / 4), c = i % (D / 4);
             float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-            if (r < live) {
+            if (r < live && r >= low) {
                 const long long row = a.pool_row(pc, k0 + r);
                 if (row >= 0) {
                     k = ld4((const float *)a.K + row * D + 4 * c);
@@ -167,7 +246,7 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
             float mb = -INFINITY;
 #pragma unroll
             for (int j = 0; j < WR; ++j) {
-                s[r][j] = kb + 16 * j < live ? s[r][j] * a.c2 : -INFINITY;
+                s[r][j] = kb + 16 * j < live && kb + 16 * j >= low ? s[r][j] * a.c2 : -INFINITY;
                 mb = fmaxf(mb, s[r][j]);
             }
 #pragma unroll
@@ -266,7 +345,7 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         }
         float *po;
         float2 *pm;
-        a.partial<D>(pc, r, po, pm);
+        a.partial<D>(pc, r / a.G, r % a.G, po, pm);
         *reinterpret_cast<float4 *>(po + 4 * c) = acc;
         if (c == 0) *pm = make_float2(M, bad ? -1.f : L);
     }
@@ -279,14 +358,16 @@ template <int D> __global__ void __launch_bounds__(256, 1) prefix_plain(const __
     __shared__ int sm_bad;
     float *sm = reinterpret_cast<float *>(smem_raw);
     wait_prior_grid();
+    release_next_grid();
     PrefixWalk w = a.range();
     PrefixPiece pc;
     while (a.next(w, pc)) {
-        if (pc.nrows <= 8)
+        const int nrows = pc.nseq * a.G;
+        if (nrows <= 8)
             plain_piece<D, 1>(a, pc, sm, &sm_bad);
-        else if (pc.nrows <= 16)
+        else if (nrows <= 16)
             plain_piece<D, 2>(a, pc, sm, &sm_bad);
-        else if (pc.nrows <= 32)
+        else if (nrows <= 32)
             plain_piece<D, 4>(a, pc, sm, &sm_bad);
         else
             plain_piece<D, 8>(a, pc, sm, &sm_bad);
@@ -294,66 +375,123 @@ template <int D> __global__ void __launch_bounds__(256, 1) prefix_plain(const __
 }
 
 // ---------------------------------------------------------------- join
-// One CTA per unit: a query head's own part and the partials of its prefix, in the order of the CTAs.
-template <int D> __global__ void __launch_bounds__(128) prefix_join(const __grid_constant__ PrefixJoin a)
+// One CTA per unit.  The partials of a query head: the own rows' first one, their others by CTA, and the same of the
+// prefix.  A warp finds a head's factors; then a thread adds up four columns of a head over an equal part of the partials.
+struct JoinArgs {
+    PrefixArgs p;
+    int32_t *lens;
+    void *out;
+    float *lse;  // or nullptr
+    int grid, append, out_bf16;
+};
+constexpr int kJoinThreads = 256;
+
+template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(const __grid_constant__ JoinArgs a)
 {
-    wait_prior_grid();
-    const int u = blockIdx.x, h = u % a.p.Hkv, lb = u / a.p.Hkv, b = lb % a.p.B, layer = lb / a.p.B, G = a.p.G;
-    const int run = a.p.run_of[b], L = a.lens[u];
-    PrefixRun rn = {};
-    long long total = 0, lh0 = 0, ctas = 1;
-    if (run >= 0) {
-        rn = a.p.runs[run];
-        total = a.p.total->work * a.p.layers * a.p.Hkv;
-        ctas = prefix_ctas(total, a.grid, a.p.rows);
-        lh0 = ((long long)layer * a.p.Hkv + h) * a.p.total->work;
-    }
+    constexpr int Q = D / 4;
+    extern __shared__ float sm_f[];  // [G][np] factors
+    __shared__ float2 sm_ML[16];
+    __shared__ __align__(16) float4 sm_o[kJoinThreads];
+    // (the attention has released this grid once the plan was complete: it may be read at once)
+    const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const int h = u % a.p.Hkv, lb = u / a.p.Hkv, layer = lb / a.p.B, b = lb - layer * a.p.B, G = a.p.G;
+    const int run = a.p.run_of[b];
+    const PrefixUnit x = a.p.units[u];
+    const PrefixTotal total = *a.p.total;
     const size_t q0 = (size_t)lb * a.p.Hq + (size_t)h * G;
-    bool ok = unit_ok(L, a.cap, a.append) && run != -2;
-    for (int x = threadIdx.x; x < G * (D / 4); x += blockDim.x) {
-        const int g = x / (D / 4), c = x % (D / 4);
-        float M = a.own_l2[q0 + g], Ls = M == -INFINITY ? 0.f : 1.f;
-        bool err = M == INFINITY || !ok;
-        float4 o = ld4(a.own_out + (q0 + g) * D + 4 * c);
-        auto add = [&](float2 ml, float4 v) {
-            const float Mn = fmaxf(M, ml.x), f = part_factor(M, Mn), k = part_factor(ml.x, Mn);
-            err |= ml.y < 0.f;
-            Ls = Ls * f + ml.y * k;
-            o.x = o.x * f + v.x * k;
-            o.y = o.y * f + v.y * k;
-            o.z = o.z * f + v.z * k;
-            o.w = o.w * f + v.w * k;
-            M = Mn;
+    const bool ok = x.lo >= 0 && run != -2;
+    // partials: [0, n_own) of the own rows, then n_pre of the prefix; CTAs of the first ones
+    int n_own = 0, n_pre = 0, own_c = 0, pre_c = 0, pre_row = 0;
+    if (ok) {
+        const long long pre = total.work * a.p.layers * a.p.Hkv, all = pre + a.p.own_total();
+        const int n = prefix_ctas(all, a.grid);
+        auto ctas = [&](long long w0, int tiles, int unit, int &c) {
+            c = prefix_cta(w0, all, n);
+            return 1 + prefix_cta(w0 + (long long)(tiles - 1) * unit, all, n) - c;
         };
-        if (run >= 0 && !err) {
-            const int rows = a.p.rows, r = (b - rn.b0) * G + g, rt = r / rows, kt = (rn.p + kPrefixTile - 1) / kPrefixTile;
-            const int unit = prefix_unit(rn.n * G, rt, rows);
-            const long long w0 = lh0 + rn.work + (long long)rt * kt * ((rows + 127) / 128);
-            const int c0 = prefix_cta(w0, total, ctas);
-            int c1 = prefix_cta(w0 + (long long)kt * unit - 1, total, ctas);
-            // (the last one may have no more than the end of a key tile, which is the one's before)
-            if (c1 > c0 && prefix_begin(c1, total, ctas) - w0 > (long long)(kt - 1) * unit) --c1;
-            add(a.p.part_ml[q0 + g], ld4(a.p.part_o + (q0 + g) * D + 4 * c));
-            for (int s = c0 + 1; s <= c1; ++s) {
-                const size_t at = (size_t)s * a.p.cont_rows + r % rows;
-                add(a.p.cont_ml[at], ld4(a.p.cont_o + at * D + 4 * c));
+        if (x.n > x.lo) {
+            long long w0 = pre + x.work + kOwnExtra;
+            for (int i = 0; i < u / kPrefixBlock; ++i) w0 += __ldg(a.p.block_work + i);
+            n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, 2, own_c);
+        }
+        if (run >= 0) {
+            const PrefixRun rn = a.p.runs[run];
+            const PrefixRows rows = a.p.rows;
+            const int i = b - rn.b0, rt = i / rows.per, kt = (rn.p + kPrefixTile - 1) / kPrefixTile;
+            n_pre = ctas(((long long)layer * a.p.Hkv + h) * total.work + rn.work + 2ll * rt * kt, kt, rows.unit(rn.n, rt), pre_c);
+            pre_row = (i - rt * rows.per) * G;
+        }
+    }
+    wait_prior_grid();
+    const int np = n_own + n_pre;
+    auto place = [&](int i, int g, const float *&o, const float2 *&ml) {
+        const bool own = i < n_own;
+        const int k = own ? i : i - n_own;
+        const size_t at = k == 0 ? q0 + g : (size_t)((own ? own_c : pre_c) + k) * a.p.cont_rows + (own ? 0 : pre_row) + g;
+        o = (k > 0 ? a.p.cont_o : (own ? a.p.own_o : a.p.part_o)) + at * D;
+        ml = (k > 0 ? a.p.cont_ml : (own ? a.p.own_ml : a.p.part_ml)) + at;
+    };
+    const float *po;
+    const float2 *pm;
+    bool err = !ok;
+    for (int g = wid; g < G; g += kJoinThreads / 32) {
+        float M = -INFINITY, L = 0.f;
+        for (int i = lane; i < np; i += 32) {
+            place(i, g, po, pm);
+            M = fmaxf(M, pm->x);
+        }
+        M = warp_max(M);
+        for (int i = lane; i < np; i += 32) {
+            place(i, g, po, pm);
+            const float2 y = *pm;
+            const float f = part_factor(y.x, M);
+            err |= y.y < 0.f;
+            L += y.y * f;
+            sm_f[g * np + i] = f;
+        }
+        L = warp_sum(L);
+        if (lane == 0) sm_ML[g] = make_float2(M, L);
+    }
+    err = __syncthreads_or(err);
+    // threads: (part, head, four columns)
+    const int slots = G * Q, parts = max(1, kJoinThreads / slots), part = tid / slots;
+    for (int s = tid - part * slots; s < slots && part < parts; s += kJoinThreads) {  // (one turn where parts > 1)
+        const int g = s / Q, c = s - g * Q;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int i = part; i < np; i += parts) {
+            place(i, g, po, pm);
+            const float4 v = *reinterpret_cast<const float4 *>(po + 4 * c);
+            const float f = sm_f[g * np + i];
+            o.x += v.x * f;
+            o.y += v.y * f;
+            o.z += v.z * f;
+            o.w += v.w * f;
+        }
+        if (parts > 1) {
+            sm_o[tid] = o;
+            asm volatile("bar.sync 1, %0;" ::"r"((parts * slots + 31) / 32 * 32) : "memory");
+            if (part > 0) break;
+            for (int k = 1; k < parts; ++k) {
+                const float4 v = sm_o[k * slots + s];
+                o.x += v.x;
+                o.y += v.y;
+                o.z += v.z;
+                o.w += v.w;
             }
         }
-        if (err) {
-            Ls = 0.f;
-            o = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        const float inv = sum_inverse(Ls);
+        const float2 ML = sm_ML[g];
+        const float L = err ? 0.f : ML.y, inv = sum_inverse(L);
+        if (err) o = make_float4(0.f, 0.f, 0.f, 0.f);
         const float4 v = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
         if (a.out_bf16)
             *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.out) + (q0 + g) * D + 4 * c) =
                 make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
         else
             *reinterpret_cast<float4 *>(reinterpret_cast<float *>(a.out) + (q0 + g) * D + 4 * c) = v;
-        if (c == 0 && a.lse) a.lse[q0 + g] = sum_log2(M, Ls) * kLn2;
-        ok &= !err;
+        if (c == 0 && a.lse) a.lse[q0 + g] = sum_log2(ML.x, L) * kLn2;
     }
-    if (__syncthreads_and(ok) && a.append && threadIdx.x == 0) a.lens[u] = L + 1;
+    if (tid == 0 && a.append && !err) a.lens[u] = x.n;
 }
 
 // ---------------------------------------------------------------- host side
@@ -364,21 +502,22 @@ static int prefix_cont_rows(const reco_paged_kv &kv)
 
 PrefixWs prefix_ws_layout(const reco_paged_kv &kv, void *base)
 {
-    PrefixWs ws;
-    ws.own = paged_decode_ws_layout(kv, false, base);
-    size_t off = align256(ws.own.bytes);
+    size_t off = kPagedZeroBytes;
     auto take = [&](size_t bytes) {
         char *r = base ? (char *)base + off : nullptr;
         off += align256(bytes);
         return r;
     };
-    const size_t heads = (size_t)kv.n_layers * kv.B * kv.H_q;
+    const size_t heads = (size_t)kv.n_layers * kv.B * kv.H_q, units = (size_t)kv.n_layers * kv.B * kv.H_kv;
     const size_t rows = (size_t)prefix_cont_rows(kv) * kPagedMaxGrid;
+    PrefixWs ws;
     ws.run_of = (int32_t *)take((size_t)kv.B * 4);
     ws.runs = (PrefixRun *)take(((size_t)kv.B / 2 + 1) * sizeof(PrefixRun));
     ws.total = (PrefixTotal *)take(sizeof(PrefixTotal));
-    ws.own_out = (float *)take(heads * kv.d * 4);
-    ws.own_l2 = (float *)take(heads * 4);
+    ws.units = (PrefixUnit *)take(units * sizeof(PrefixUnit));
+    ws.block_work = (int32_t *)take((units + kPrefixBlock - 1) / kPrefixBlock * 4);
+    ws.own_o = (float *)take(heads * kv.d * 4);
+    ws.own_ml = (float2 *)take(heads * 8);
     ws.part_o = (float *)take(heads * kv.d * 4);
     ws.part_ml = (float2 *)take(heads * 8);
     ws.cont_o = (float *)take(rows * kv.d * 4);
@@ -392,14 +531,31 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
                                 float *lse, const PrefixWs &ws, unsigned *err, cudaStream_t s)
 {
     const bool f32 = kv.dtype == RECO_F32;
-    const int cap = paged_cap(kv), units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv;
-    const int rows = f32 ? kPlainRows : kPrefixMaxRows;
-    cudaError_t e = launch_pdl(prefix_plan, dim3(1), dim3(kPlanThreads), 0, s, group, shared, kv.B, G, cap, rows, ws.runs,
-                               ws.run_of, ws.total, err);
+    const int units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv, blocks = (units + kPrefixBlock - 1) / kPrefixBlock;
+    const PrefixRows rows = f32 ? PrefixRows{kPlainRows / G, kPlainRows / G} : PrefixRows{2 * (128 / G), 128 / G};
+    PlanArgs p = {};
+    p.K = kv.k;
+    p.V = kv.v;
+    p.k_new = k_new;
+    p.v_new = v_new;
+    p.table = kv.table;
+    p.lens = lens;
+    p.group = group;
+    p.shared = shared;
+    p.units = units;
+    p.B = kv.B;
+    p.Hkv = kv.H_kv;
+    p.cap = paged_cap(kv);
+    p.n_pages = kv.n_pages;
+    p.max_pages = kv.max_pages;
+    p.shift = __builtin_ctz((unsigned)kv.page);
+    p.row_bytes = kv.d * (f32 ? 4 : 2);
+    p.rows = rows;
+    p.ws = ws;
+    p.err = err;
+    const long long copies = k_new ? ((long long)units * 2 * (p.row_bytes / 16) + kPrefixBlock - 1) / kPrefixBlock : 0;
+    cudaError_t e = launch_pdl(prefix_plan, dim3((unsigned)(1 + blocks + copies)), dim3(kPrefixBlock), 0, s, p);
     if (e != cudaSuccess) return e;
-    e = launch_paged_own(kv, q, k_new, v_new, lens, group, shared, scale, ws.own_out, ws.own_l2, ws.own, err, s);
-    if (e != cudaSuccess) return e;
-    const int grid = std::min(device_sm_count(), kPagedMaxGrid);
     PrefixArgs a = {};
     a.K = kv.k;
     a.V = kv.v;
@@ -408,8 +564,12 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     a.runs = ws.runs;
     a.run_of = ws.run_of;
     a.total = ws.total;
+    a.units = ws.units;
+    a.block_work = ws.block_work;
     a.part_o = ws.part_o;
     a.part_ml = ws.part_ml;
+    a.own_o = ws.own_o;
+    a.own_ml = ws.own_ml;
     a.cont_o = ws.cont_o;
     a.cont_ml = ws.cont_ml;
     a.layers = kv.n_layers;
@@ -419,11 +579,14 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     a.G = G;
     a.n_pages = kv.n_pages;
     a.max_pages = kv.max_pages;
-    a.shift = __builtin_ctz((unsigned)kv.page);
+    a.shift = p.shift;
+    a.n_units = units;
+    a.n_blocks = blocks;
     a.rows = rows;
     a.cont_rows = prefix_cont_rows(kv);
     a.c2 = scale * kLog2e;
     a.err = err;
+    const int grid = std::min(device_sm_count(), kPagedMaxGrid);
     if (f32) {
         void (*fn)(PrefixArgs) = kv.d == 64 ? prefix_plain<64> : prefix_plain<128>;
         const int smem = kv.d == 64 ? plain_smem<64>() : plain_smem<128>();
@@ -432,18 +595,15 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     } else {
         if ((e = launch_prefix_tc(kv, a, grid, out_dtype, s)) != cudaSuccess) return e;
     }
-    PrefixJoin j = {};
+    JoinArgs j = {};
     j.p = a;
-    j.own_out = ws.own_out;
-    j.own_l2 = ws.own_l2;
     j.lens = lens;
     j.out = out;
     j.lse = lse;
     j.grid = grid;
-    j.cap = cap;
     j.append = k_new ? 1 : 0;
     j.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;
-    e = launch_pdl(kv.d == 64 ? prefix_join<64> : prefix_join<128>, dim3(units), dim3(128), 0, s, j);
+    e = launch_pdl(kv.d == 64 ? prefix_join<64> : prefix_join<128>, dim3(units), dim3(kJoinThreads), (size_t)G * (2 * grid + 2) * 4, s, j);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

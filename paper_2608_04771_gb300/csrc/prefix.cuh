@@ -1,41 +1,69 @@
-// prefix.cuh -- what the kernels of decode attention over shared prefixes (prefix.cu) have in common: the list of groups,
-// a CTA's walk over its share of the work, and where partials go.
+// prefix.cuh -- what the kernels of decode attention over shared prefixes (prefix.cu) have in common: the work, a
+// CTA's walk over its share of it, and where partials go.
 #pragma once
 #include "common.cuh"
 #include "internal.h"
 
 namespace reco {
 
-// The work of a row tile (rt of a group of R query rows, `rows` to a tile) against one key tile: 1 for every 128 query
-// rows begun, what the tensor cores take at once.
-__host__ __device__ inline int prefix_unit(int R, int rt, int rows)
-{
-    const int left = R - rt * rows;
-    return ((left < rows ? left : rows) + 127) / 128;
-}
-// Work of a group per layer and KV head.
-__host__ __device__ inline long long prefix_work(int n, int G, int p, int rows)
-{
-    const int R = n * G, last = (R - 1) / rows, kt = (p + kPrefixTile - 1) / kPrefixTile;
-    return (long long)kt * ((long long)last * ((rows + 127) / 128) + prefix_unit(R, last, rows));
-}
-// The work is shared out to n CTAs, each with some key tile of every row tile that it gets (so that the joining kernel
-// finds a partial from every CTA between an item's first and last).  CTA c's begins at total * c / n; the CTA that unit w
-// of the work falls to.  A key tile whose work is cut goes to the CTA that its first unit falls to.
-__device__ __forceinline__ long long prefix_ctas(long long total, int grid, int rows)
-{
-    const long long most = total / ((rows + 127) / 128);
-    return most < 1 ? 1 : (most < grid ? most : grid);
-}
-__device__ __forceinline__ long long prefix_begin(long long c, long long total, long long n) { return total * c / n; }
-__device__ __forceinline__ int prefix_cta(long long w, long long total, long long n) { return (int)(((w + 1) * n - 1) / total); }
-
-// A CTA's part of an item: key tiles [t0, t1) of the prefix (p rows, first sequence b0) against row tile rt of nrows rows.
-struct PrefixPiece {
-    int layer, h, b0, p, rt, nrows, t0, t1;
+// A row tile takes the query heads of up to `per` sequences of a group, of which `half` make what the tensor cores take
+// at once (128 rows).  Work is counted in units: 2 for a key tile, what its bytes cost, but 1 for the last row tile of a
+// group of several, if it has no more than `half` sequences: its rows come from L2, and it takes half the products.
+// A unit's own rows cost kOwnExtra more, for the start and the end of an item.
+constexpr int kOwnExtra = 2;
+struct PrefixRows {
+    int per, half;
+    __host__ __device__ int unit(int n, int rt) const { return rt > 0 && n - rt * per <= half && per > half ? 1 : 2; }
+    // work of a group of n sequences with p rows, per layer and KV head
+    __host__ __device__ long long work(int n, int p) const
+    {
+        const int last = (n - 1) / per, kt = (p + kPrefixTile - 1) / kPrefixTile;
+        return (long long)kt * (2ll * last + unit(n, last));
+    }
 };
+
+#ifdef __CUDACC__
+// The work is shared out to n CTAs, no less than a key tile's to each.  CTA c's begins at total * c / n; prefix_cta is the
+// CTA that unit w of the work falls to.  A key tile whose work is cut goes to the CTA that its first unit falls to: tile t
+// of an item whose tiles begin at w0, `unit` to each, to that of w0 + t * unit.
+// (64-bit divisions take some hundred instructions: most are of 32-bit numbers)
+__device__ __forceinline__ long long quotient(long long a, long long b)
+{
+    return ((unsigned long long)a | (unsigned long long)b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
+__device__ __forceinline__ int prefix_ctas(long long total, int grid)
+{
+    const long long most = total >> 1;
+    return most < 1 ? 1 : (most < grid ? (int)most : grid);
+}
+__device__ __forceinline__ long long prefix_begin_at(int c, long long total, int n) { return quotient(total * c, n); }
+__device__ __forceinline__ int prefix_cta(long long w, long long total, int n) { return (int)quotient((w + 1) * n - 1, total); }
+
+// The last i of [0, n) with key(i) <= x, by a warp (key does not decrease, key(0) <= x).
+template <typename F> __device__ __forceinline__ int warp_last(int n, long long x, F key)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0;
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lane * step;
+        const bool le = at < n && (lane == 0 || key(lo + at) <= x);
+        const int k = 31 - __clz(__ballot_sync(0xffffffffu, le));
+        lo += k * step;
+        n = min(step, n - k * step);
+    }
+    return lo;
+}
+
+// A CTA's part of an item: a row tile (nseq sequences from s0 on of the group that begins at sequence b0) against key
+// tiles [t0, t1) of the rows [lo, end), looked up in b0's table; tile t begins at row k0 + 128 t.
+struct PrefixPiece {
+    int layer, h, b0, s0, nseq, k0, lo, end, t0, t1;
+    bool own;
+};
+// The work of the prefixes of all layers and heads lies before that of the units' own rows.
 struct PrefixWalk {
-    long long w, end;
+    long long w, end, prefix;  // next unit of the work, the last, and where the own rows' begins
+    int u, base;               // next unit (-1: not looked for), and the work before its block
 };
 
 struct PrefixArgs {
@@ -44,92 +72,116 @@ struct PrefixArgs {
     const PrefixRun *runs;
     const int32_t *run_of;
     const PrefixTotal *total;
-    float *part_o, *cont_o;      // by query head; by CTA and row of the tile
-    float2 *part_ml, *cont_ml;   // (max to base 2, sum; -1: in error)
-    int layers, B, Hq, Hkv, G, n_pages, max_pages, shift;
-    int rows;       // query rows of a row tile
+    const PrefixUnit *units;
+    const int32_t *block_work;
+    float *part_o, *own_o, *cont_o;
+    float2 *part_ml, *own_ml, *cont_ml;  // (max to base 2, sum; -1: in error)
+    int layers, B, Hq, Hkv, G, n_pages, max_pages, shift, n_units, n_blocks;
+    PrefixRows rows;
     int cont_rows;  // rows a CTA has in cont_o: those of the largest row tile
-    float c2;  // scale * log2(e)
+    float c2;       // scale * log2(e)
     unsigned *err;
 
-#ifdef __CUDACC__
+    __device__ __forceinline__ long long prefix_total() const { return total->work * layers * Hkv; }
+    __device__ __forceinline__ int own_total() const
+    {
+        int sum = 0;
+#pragma unroll 8
+        for (int i = 0; i < n_blocks; ++i) sum += __ldg(block_work + i);
+        return sum;
+    }
     __device__ __forceinline__ PrefixWalk range() const
     {
-        const long long all = total->work * layers * Hkv;
-        const long long n = prefix_ctas(all, (int)gridDim.x, rows);
-        if (all == 0 || blockIdx.x >= n) return PrefixWalk{0, 0};
-        return PrefixWalk{prefix_begin(blockIdx.x, all, n), prefix_begin(blockIdx.x + 1, all, n)};
+        PrefixWalk w;
+        w.prefix = prefix_total();
+        w.u = -1;
+        w.base = 0;
+        const long long all = w.prefix + own_total();
+        const int n = prefix_ctas(all, (int)gridDim.x), c = blockIdx.x;
+        w.w = c < n ? prefix_begin_at(c, all, n) : 0;
+        w.end = c < n ? prefix_begin_at(c + 1, all, n) : 0;
+        return w;
     }
+    // (whole warps)
     __device__ __forceinline__ bool next(PrefixWalk &w, PrefixPiece &pc) const
     {
         while (w.w < w.end) {
-            const long long per = total->work, lh = w.w / per, rem = w.w - lh * per;
-            int lo = 0, n = total->n;
-            while (n > 1) {  // the last group that begins at or before rem
-                const int half = n >> 1;
-                if (runs[lo + half].work <= rem) {
-                    lo += half;
-                    n -= half;
-                } else {
-                    n = half;
-                }
+            if (w.w < w.prefix) {
+                const long long per = total->work, lh = quotient(w.w, per), rem = w.w - lh * per;
+                const PrefixRun r = runs[warp_last(total->n, rem, [&](int i) { return runs[i].work; })];
+                const int kt = (r.p + kPrefixTile - 1) / kPrefixTile;
+                const long long in = rem - r.work, full = 2ll * kt;
+                const int rt = (int)quotient(in, full), unit = rows.unit(r.n, rt), u = (int)(in - rt * full);
+                const int e = (int)min((long long)kt * unit, u + (w.end - w.w));
+                pc.layer = (int)lh / Hkv;
+                pc.h = (int)lh - pc.layer * Hkv;
+                pc.b0 = r.b0;
+                pc.s0 = rt * rows.per;
+                pc.nseq = min(rows.per, r.n - pc.s0);
+                pc.k0 = pc.lo = 0;
+                pc.end = r.p;
+                pc.t0 = (u + unit - 1) / unit;
+                pc.t1 = (e + unit - 1) / unit;
+                pc.own = false;
+                w.w += e - u;
+                if (pc.t0 < pc.t1) return true;
+                continue;
             }
-            const PrefixRun r = runs[lo];
-            const int kt = (r.p + kPrefixTile - 1) / kPrefixTile;
-            const long long in = rem - r.work, full = (long long)kt * ((rows + 127) / 128);
-            pc.layer = (int)(lh / Hkv);
-            pc.h = (int)(lh - (long long)pc.layer * Hkv);
-            pc.b0 = r.b0;
-            pc.p = r.p;
-            pc.rt = (int)(in / full);
-            pc.nrows = min(rows, r.n * G - pc.rt * rows);
-            const int unit = prefix_unit(r.n * G, pc.rt, rows), u = (int)(in - pc.rt * full);
-            const int e = (int)min((long long)kt * unit, u + (w.end - w.w));
-            pc.t0 = (u + unit - 1) / unit;
-            pc.t1 = (e + unit - 1) / unit;
-            w.w += e - u;
+            const int at = (int)(w.w - w.prefix);
+            if (w.u < 0) {  // the unit that this falls to
+                int blk = 0;
+                while (blk + 1 < n_blocks && w.base + __ldg(block_work + blk) <= at) w.base += __ldg(block_work + blk++);
+                const int u0 = blk * kPrefixBlock;
+                w.u = u0 + warp_last(min(kPrefixBlock, n_units - u0), at - w.base, [&](int i) { return units[u0 + i].work; });
+            }
+            const PrefixUnit x = units[w.u];
+            const int kt = x.n > x.lo && x.lo >= 0 ? (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile : 0;
+            const int lb = w.u / Hkv;
+            pc.layer = lb / B;
+            pc.h = w.u - lb * Hkv;
+            pc.b0 = lb - pc.layer * B;
+            pc.s0 = 0;
+            pc.nseq = 1;
+            pc.k0 = x.k0;
+            pc.lo = x.lo;
+            pc.end = x.n;
+            const int in = at - w.base - x.work, size = kt > 0 ? 2 * kt + kOwnExtra : 0;
+            const int e = (int)min((long long)size, in + (w.end - w.w));
+            pc.t0 = max(0, in - kOwnExtra + 1) >> 1;
+            pc.t1 = max(0, e - kOwnExtra + 1) >> 1;
+            pc.own = true;
+            if (e == size) {  // the next unit, maybe of the next block
+                ++w.u;
+                if (w.u % kPrefixBlock == 0 && w.u < n_units) w.base += __ldg(block_work + w.u / kPrefixBlock - 1);
+            }
+            w.w += e - in;
             if (pc.t0 < pc.t1) return true;
         }
         return false;
     }
-    // Query head of row r of the group's rows (sequence by sequence), as a row of q.
-    __device__ __forceinline__ long long q_row(const PrefixPiece &pc, int r) const
+    // Query head g of a tile's sequence s, as a row of q.
+    __device__ __forceinline__ long long q_row(const PrefixPiece &pc, int s, int g) const
     {
-        const int s = r / G;
-        return ((long long)pc.layer * B + pc.b0 + s) * Hq + pc.h * G + (r - s * G);
+        return ((long long)pc.layer * B + pc.b0 + pc.s0 + s) * Hq + pc.h * G + g;
     }
-    // Pool row of row j of the prefix, -1 where its table entry names no page.
+    // Pool row of row j, -1 where its table entry names no page.
     __device__ __forceinline__ long long pool_row(const PrefixPiece &pc, int j) const
     {
         const int e = __ldg(table + (long long)pc.b0 * max_pages + (j >> shift));
         if ((unsigned)e >= (unsigned)n_pages) return -1;
         return ((((long long)pc.layer * n_pages + e) * Hkv + pc.h) << shift) + (j & ((1 << shift) - 1));
     }
-    template <int D> __device__ __forceinline__ void partial(const PrefixPiece &pc, int r, float *&o, float2 *&ml) const
+    // Where the partial of head g of the tile's sequence s goes: an item's first by query head, the others by CTA.
+    template <int D> __device__ __forceinline__ void partial(const PrefixPiece &pc, int s, int g, float *&o, float2 *&ml) const
     {
-        if (pc.t0 == 0) {
-            const long long at = q_row(pc, pc.rt * rows + r);
-            o = part_o + at * D;
-            ml = part_ml + at;
-        } else {
-            const long long at = (long long)blockIdx.x * cont_rows + r;
-            o = cont_o + at * D;
-            ml = cont_ml + at;
-        }
+        const long long at = pc.t0 == 0 ? q_row(pc, s, g) : (long long)blockIdx.x * cont_rows + s * G + g;
+        o = (pc.t0 != 0 ? cont_o : (pc.own ? own_o : part_o)) + at * D;
+        ml = (pc.t0 != 0 ? cont_ml : (pc.own ? own_ml : part_ml)) + at;
     }
-#endif
 };
 
-// The prefix part over bf16 caches (prefix_tc.cu).
+// The attention of all pieces over bf16 caches (prefix_tc.cu).
 cudaError_t launch_prefix_tc(const reco_paged_kv &kv, const PrefixArgs &a, int grid, reco_dtype out_dtype, cudaStream_t s);
-
-struct PrefixJoin {
-    PrefixArgs p;
-    const float *own_out, *own_l2;
-    int32_t *lens;
-    void *out;
-    float *lse;  // or nullptr
-    int grid, cap, append, out_bf16;
-};
+#endif
 
 }  // namespace reco
