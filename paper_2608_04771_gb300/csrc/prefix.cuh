@@ -27,7 +27,7 @@ struct PrefixRows {
 // CTA that unit w of the work falls to.  A key tile whose work is cut goes to the CTA that its first unit falls to: tile t
 // of an item whose tiles begin at w0, `unit` to each, to that of w0 + t * unit.
 // (64-bit divisions take some hundred instructions: most are of 32-bit numbers)
-__device__ __forceinline__ long long quotient(long long a, long long b)
+__device__ __noinline__ static long long quotient(long long a, long long b)
 {
     return ((unsigned long long)a | (unsigned long long)b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }

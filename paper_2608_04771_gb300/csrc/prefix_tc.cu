@@ -7,21 +7,27 @@
 // nothing more while the bytes are.
 //
 // One CTA per SM, persistent over its share of the key tiles (PrefixArgs::next), of warps
-//   0      copies, all by TMA: queries (a box of a group's sequences, or one sequence's, into one of two tiles), K and V
-//          (a box per page and 64 columns, one lane each, into a ring of tiles);
-//   1      issues the products;
-//   4..11  two softmax groups of four warps, a query row per thread.
-// Two streams of products alternate, so that one's softmax runs beside the other's products: a row tile of more than
-// 128 rows has a half in each stream, which share every K and V tile; otherwise the streams are the even and the
-// odd key tiles, and join at the end of the piece.  A stream's S (128 columns of TMEM) is overwritten by its P in bf16, which
-// the second product takes from there; O stays in TMEM, and is rescaled only when a row's maximum has grown by
-// more than 2^8 (kLazyLog2: probabilities against the older maximum stay exact in float32).
-// The copies and the score products run ahead into the next piece while the groups finish one.
+//   0      finds the pieces, a few ahead of the others, and copies, all by TMA: queries (a box of a group's sequences, or
+//          one sequence's, into one of two tiles), K and V (a box per page and 64 columns, a lane each, into a ring of tiles);
+//   1, 3   one thread each, which issue the products of a stream;
+//   2      clears V rows that no query sees in tiles that a border crosses (their probabilities are zero, but NaN
+//          times zero is not);
+//   4..11  two softmax groups of four warps, one per stream, a query row per thread.
+// The two streams: a row tile of more than 128 rows has a half in each, otherwise each takes half of the keys of every tile
+// and they join at the end of the piece.  A stream goes by blocks of 64 keys, two of which have a place for their S in
+// TMEM, so that the group works on one while the other's product runs.  S is overwritten by P in bf16, which the second
+// product takes from there; O stays in TMEM, and is rescaled only when a row's probabilities against
+// the maximum so far sum to more than 2^12 in a block.
+//
+// What the steps cost (cycles a block of 64 keys, 64 sequences of 5 heads over 100001 rows): see launch_prefix_tc.
 //
 // P enters its product in bf16: with float32 output in two parts (2^-17 of each probability is lost), with bf16
 // output in one (2^-8 of each, on average over the rows the size of the output's own rounding).  Sums take the
 // probabilities as they were before.
 //
+// A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
+// to come when phase k + 1 is.  So every slot is waited for by both threads, every time; what a group waits for
+// only now and then (pv_done) has a barrier for even and for odd blocks, which it cannot fall behind.
 // Every wait is bounded; one that runs out raises the error word and the CTA's abort flag, which ends the others.
 #include <algorithm>
 
@@ -58,16 +64,38 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
+constexpr long long kPolls = 1LL << 19;  // of a wait, each suspended for up to two microseconds
+
+// The blocks of 64 keys of a piece that fall to stream s: block j begins `first` + `step` j columns from the start of the
+// piece, of whose columns [lo, hi) count.
+struct PrefixBlocks {
+    int n, first, step, lo, hi;
+    __device__ __forceinline__ PrefixBlocks(const PrefixPiece &x, bool pair, int s)
+    {
+        const int k0 = x.k0 + x.t0 * kPrefixTile, nt = x.t1 - x.t0;
+        lo = max(0, x.lo - k0);
+        hi = min(x.end - k0, nt * kPrefixTile);
+        n = pair ? 2 * nt : nt;
+        first = pair ? 0 : 64 * s;
+        step = pair ? 64 : 128;
+    }
+};
+
 template <int D> struct PrefixTc {
     static constexpr int HALVES = D / 64;
     static constexpr int BOX = 128 * 128;  // 128 rows of 64 bf16
     static constexpr int TILE = HALVES * BOX;
     static constexpr int Q_BYTES = 2 * TILE;
     static constexpr int NS = D == 128 ? 5 : 10;  // K and V tiles in the ring
+    static constexpr int NP = 4;                  // pieces found ahead
     static constexpr int THREADS = 32 * 12;
     struct Small {  // behind the tiles
-        uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], o_free, met;
+        uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2], landed[2], cleared[2];
+        uint64_t o_free, met;
+        uint64_t piece_full[NP], piece_empty[NP];
         float2 ml[2][128];
+        PrefixPiece piece[NP];
+        int bad[NP];  // a page that is none was met
         uint32_t tmem;
         int abort;
     };
@@ -82,7 +110,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
               const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQ1, const __grid_constant__ PrefixArgs a)
 {
     using C = PrefixTc<D>;
-    constexpr int NS = C::NS, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
+    constexpr int NS = C::NS, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
     constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -99,17 +127,25 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         prefetch_tensormap(&tmQ1);
         for (int i = 0; i < NS; ++i) {
             mbar_init(smem_addr(&sm.full[i]), 1);
-            mbar_init(smem_addr(&sm.empty[i]), 1);
+            mbar_init(smem_addr(&sm.empty[i]), 2);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&sm.q_full[s]), 1);
-            mbar_init(smem_addr(&sm.q_empty[s]), 1);
-            mbar_init(smem_addr(&sm.s_full[s]), 1);
-            mbar_init(smem_addr(&sm.p_full[s]), 4);
-            mbar_init(smem_addr(&sm.pv_done[s]), 1);
+            mbar_init(smem_addr(&sm.q_empty[s]), 2);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(smem_addr(&sm.s_full[s][b]), 1);
+                mbar_init(smem_addr(&sm.p_full[s][b]), 4);
+                mbar_init(smem_addr(&sm.pv_done[s][b]), 1);
+            }
+            mbar_init(smem_addr(&sm.landed[s]), 1);
+            mbar_init(smem_addr(&sm.cleared[s]), 1);
         }
         mbar_init(smem_addr(&sm.o_free), 8);
         mbar_init(smem_addr(&sm.met), 8);
+        for (int i = 0; i < C::NP; ++i) {
+            mbar_init(smem_addr(&sm.piece_full[i]), 1);
+            mbar_init(smem_addr(&sm.piece_empty[i]), 11);  // the threads of warps 1 and 3, warp 2, the softmax's eight
+        }
         sm.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
@@ -121,27 +157,36 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
-    volatile int *abort_flag = &sm.abort;
     wait_prior_grid();
     release_next_grid();  // the join looks up its places meanwhile
-    // registers of the launch, 168 a thread: 88 for warps 0 to 3, 208 for the softmax, which holds a row of S
-    static_assert(128 * 88 + 256 * 208 <= C::THREADS * 168, "no more than the launch has");
-    auto wait = [&](uint64_t &bar, int k) { return warp_wait(smem_addr(&bar), k & 1, abort_flag, a.err); };  // its phase k
+    // a whole warp's wait for phase k of a barrier
+    auto wait = [&](uint64_t &bar, int k) { return warp_wait(smem_addr(&bar), k & 1, &sm.abort, a.err, kPolls); };
 
+    // registers of the launch, 168 a thread: 88 for warps 0 to 3, 208 for the softmax, which holds a row of a block
+    static_assert(128 * 88 + 256 * 208 <= C::THREADS * 168, "no more than the launch has");
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         PrefixWalk w = a.range();
         PrefixPiece pc;
-        // ---- copies.  Lane (box, half) of a tile copies 64 columns of the box's rows: a page, or half a page of 256
+        // ---- pieces and copies.  Lane (box, half) of a tile copies 64 columns of the box's rows: a page, or half a page
+        // of 256
         const int rows = min(128, 1 << a.shift), boxes = 128 / rows;
         const int box = lane / HALVES, half = lane % HALVES;
         int slot = 0, nq = 0;
         bool ok = true;
-        while (ok && a.next(w, pc)) {
-            auto row_of = [&](int t) {
-                const int k = pc.k0 + t * kPrefixTile + box * rows;
-                return box < boxes && k < pc.end ? a.pool_row(pc, k) : -1ll;
-            };
+        for (int np = 0; ok; ++np) {
+            const bool more = a.next(w, pc);
+            if (!(ok = wait(sm.piece_empty[np % NP], np / NP + 1))) break;
+            if (lane == 0) {
+                if (!more) pc.t1 = pc.t0 = 0;
+                sm.piece[np % NP] = pc;
+                sm.bad[np % NP] = 0;
+                mbar_arrive(smem_addr(&sm.piece_full[np % NP]));
+            }
+            __syncwarp();
+            if (!more) break;
+            auto needed = [&](int t) { return box < boxes && pc.k0 + t * kPrefixTile + box * rows < pc.end; };
+            auto row_of = [&](int t) { return needed(t) ? a.pool_row(pc, pc.k0 + t * kPrefixTile + box * rows) : -1ll; };
             long long row = row_of(pc.t0);
             for (int s = 0; s < (pc.nseq > a.rows.half ? 2 : 1); ++s, ++nq) {
                 const int i = nq & 1;
@@ -157,6 +202,10 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             }
             for (int t = pc.t0; ok && t < pc.t1; ++t) {
                 const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+                if (__any_sync(0xffffffffu, needed(t) && row < 0) && lane == 0) {
+                    *(volatile int *)&sm.bad[np % NP] = 1;
+                    raise_error(a.err, ERR_PAGE);
+                }
                 const long long next = t + 1 < pc.t1 ? row_of(t + 1) : -1ll;
                 for (int kv = 0; kv < 2; ++kv, ++slot) {
                     const int i = slot % NS;
@@ -172,143 +221,201 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             }
         }
         // no copy is left in flight when the CTA ends
-        for (int j = max(0, slot - NS); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % NS]), (j / NS) & 1, kTcSpin);
-        for (int j = max(0, nq - 2); j < nq; ++j) mbar_wait_bounded(smem_addr(&sm.q_full[j & 1]), (j >> 1) & 1, kTcSpin);
-    } else if (warp == 1) {
+        for (int j = max(0, slot - NS); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % NS]), (j / NS) & 1, kPolls);
+        for (int j = max(0, nq - 2); j < nq; ++j) mbar_wait_bounded(smem_addr(&sm.q_full[j & 1]), (j >> 1) & 1, kPolls);
+    } else if (warp == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        PrefixWalk w = a.range();
-        PrefixPiece pc;
-        // ---- products
-        constexpr uint32_t ID_S = idesc_bf16(128, 128), ID_O = idesc_bf16(128, D) | kIdescMnB;
-        int slot0 = 0, nq = 0, ns[2] = {0, 0}, pieces = 0;  // ring slots, query tiles, products of each stream so far
+        // ---- V rows outside the rows that count, within the product's steps of 16
+        int slot = 1, nc = 0;
         bool ok = true;
-        while (ok && a.next(w, pc)) {
-            const int nt = pc.t1 - pc.t0;
-            const bool pair = pc.nseq > a.rows.half;
-            const int jobs = pair ? 2 * nt : nt;
-            auto scores = [&](int j) {
-                const int s = j & 1, t = pair ? j >> 1 : j, slot = slot0 + 2 * t, i = slot % NS;
-                const int q = nq + (pair ? s : 0);  // the tile of queries
-                if ((pair ? j < 2 : j == 0) && !wait(sm.q_full[q & 1], q >> 1)) return false;
-                if ((!pair || s == 0) && !wait(sm.full[i], slot / NS)) return false;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t ad = sw128_desc(Qs + (q & 1) * TILE), bd = sw128_desc(ring + i * TILE);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t off = (uint64_t)(((k >> 2) * BOX + (k & 3) * 32) >> 4);
-                        tc_mma(tmem + S_COL + 128 * s, ad + off, bd + off, ID_S, k > 0);
-                    }
-                    tc_commit(smem_addr(&sm.s_full[s]));
-                    if (!pair || s == 1) tc_commit(smem_addr(&sm.empty[i]));
-                    if (pair ? t == nt - 1 : j == jobs - 1) tc_commit(smem_addr(&sm.q_empty[q & 1]));
-                }
+        for (int np = 0; ok; ++np) {
+            if (!(ok = wait(sm.piece_full[np % NP], np / NP))) break;
+            const PrefixPiece x = sm.piece[np % NP];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
+            if (x.t1 == x.t0) break;
+            for (int t = x.t0; t < x.t1; ++t, slot += 2) {
+                const int k0 = x.k0 + t * kPrefixTile, low = max(0, x.lo - k0), live = min(kPrefixTile, x.end - k0);
+                if (((low | live) & 15) == 0) continue;
+                if (!(ok = wait(sm.landed[0], nc) && wait(sm.landed[1], nc))) break;
+                ++nc;
+                const uint32_t tile = ring + (slot % NS) * TILE;
+                auto clear = [&](int r0, int n) {
+                    for (int i = lane; i < n * 8 * HALVES; i += 32)
+                        sts_u4(tile + (i / (8 * n)) * BOX + (r0 + (i >> 3) % n) * 128 + (i & 7) * 16, make_uint4(0, 0, 0, 0));
+                };
+                if (low & 15) clear(low & ~15, low & 15);
+                if (live & 15) clear(live, 16 - (live & 15));
+                fence_async_shared();
                 __syncwarp();
-                return true;
-            };
-            auto values = [&](int j) {
-                const int s = j & 1, t = pair ? j >> 1 : j, slot = slot0 + 2 * t + 1, i = slot % NS;
-                // rows of the tile that count: [low, live); the product takes them in steps of 16
-                const int k0 = pc.k0 + (pc.t0 + t) * kPrefixTile, low = max(0, pc.lo - k0), live = min(kPrefixTile, pc.end - k0);
-                const int step0 = low >> 4, step1 = (live + 15) / 16;
-                if (!pair || s == 0) {
-                    if (!wait(sm.full[i], slot / NS)) return false;
-                    // other rows of those steps: zero, as their probabilities are (NaN times zero is not)
-                    auto clear = [&](int r0, int n) {
-                        for (int x = lane; x < n * 8 * HALVES; x += 32)
-                            sts_u4(ring + i * TILE + (x / (8 * n)) * BOX + (r0 + (x >> 3) % n) * 128 + (x & 7) * 16, make_uint4(0, 0, 0, 0));
-                    };
-                    if ((low | live) & 15) {
-                        if (low & 15) clear(low & ~15, low & 15);
-                        if (live & 15) clear(live, 16 * step1 - live);
-                        fence_async_shared();
-                        __syncwarp();
-                    }
-                }
-                if (!wait(sm.p_full[s], ns[s]++)) return false;
-                if (j == 0 && pieces > 0 && !wait(sm.o_free, pieces - 1)) return false;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t bd = sw128_desc_mn(ring + i * TILE, BOX);
-                    const uint32_t p = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
-                    for (int k = step0; k < step1; ++k) {
-                        tc_mma_ts(o, p + 8 * k, bd + (uint64_t)(k * 2048 >> 4), ID_O, k > step0 || j > 1);
-                        if (PARTS == 2) tc_mma_ts(o, p + 64 + 8 * k, bd + (uint64_t)(k * 2048 >> 4), ID_O, 1);
-                    }
-                    tc_commit(smem_addr(&sm.pv_done[s]));
-                    if (!pair || s == 1) tc_commit(smem_addr(&sm.empty[i]));
-                }
-                __syncwarp();
-                return true;
-            };
-            for (int j = 0; ok && j < jobs + 2; ++j) {
-                if (j >= 2 && j - 2 < jobs) ok = values(j - 2);
-                if (ok && j < jobs) ok = scores(j);
+                if (lane < 2) mbar_arrive(smem_addr(&sm.cleared[lane]));
             }
-            slot0 += 2 * nt;
-            nq += pair ? 2 : 1;
-            ++pieces;
         }
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        // ---- products of stream s
+        constexpr uint32_t ID_S = idesc_bf16(128, 64), ID_O = idesc_bf16(128, D) | kIdescMnB;
+        const int s = warp >> 1;
+        if (elect_one()) {
+            auto wait1 = [&](uint32_t bar, uint32_t parity) { return thread_wait(bar, parity, &sm.abort, a.err, kPolls); };
+            const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX);
+            const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
+            const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
+                           p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
+            // ring places of the next K and V tile, and the parity of their phase; query tiles, score and value products,
+            // cleared tiles so far
+            int ki = 0, vi = 1, nq = 0, n = 0, nv = 0, nc = 0;
+            uint32_t kp = 0, vp = 0;
+            auto step = [&](int &i, uint32_t &p) {
+                i += 2;
+                p ^= i >= NS ? 1u : 0u;
+                i -= i >= NS ? NS : 0;
+            };
+            bool ok = true;
+            for (int np = 0; ok; ++np) {
+                if (!(ok = wait1(smem_addr(&sm.piece_full[np % NP]), np / NP & 1))) break;
+                const PrefixPiece &x = sm.piece[np % NP];
+                const bool pair = x.nseq > a.rows.half;
+                const PrefixBlocks bl(x, pair, s);
+                mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
+                if (bl.n == 0) break;
+                const int q = nq + (pair ? s : 0);
+                for (int i = 0; ok && i < (pair ? 2 : 1); ++i, ++nq) ok = wait1(smem_addr(&sm.q_full[nq & 1]), nq >> 1 & 1);
+                const uint64_t ad = qd + (uint64_t)((q & 1) * TILE >> 4);
+                uint32_t more = 0;
+#pragma unroll 1
+                for (int j = 0; ok && j < bl.n + 2; ++j) {
+                    if (j >= 2) {  // O += P V of block j - 2
+                        const int c = bl.first + bl.step * (j - 2);
+                        if (!pair || (j & 1) == 0) {
+                            if (!(ok = wait1(full0 + 8 * vi, vp))) break;
+                            // a border that is not at a step of 16: V rows have to be cleared first
+                            const int t = c & ~127;
+                            if ((t == 0 && (bl.lo & 15)) || (t + 128 > bl.hi && (bl.hi & 15))) {
+                                mbar_arrive(smem_addr(&sm.landed[s]));
+                                if (!(ok = wait1(smem_addr(&sm.cleared[s]), nc++ & 1))) break;
+                            }
+                        }
+                        if (!(ok = wait1(p_full0 + 8 * (nv & 1), nv >> 1 & 1))) break;
+                        // (every piece waits for the outputs of the one before to have been read, for the barrier's phases)
+                        if (j == 2 && np > 0 && !(ok = wait1(smem_addr(&sm.o_free), (np - 1) & 1))) break;
+                        tc_fence_after();
+                        uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
+                        uint32_t p = st + 64 * (nv & 1);
+                        // rows of the block that count, in steps of 16
+                        const int k0 = max(0, bl.lo - c) >> 4, k1 = (min(64, bl.hi - c) + 15) >> 4;
+                        p += 8 * k0;
+                        bd += (uint32_t)(k0 * 2048 >> 4);
+#pragma unroll 1
+                        for (int k = k0; k < k1; ++k, p += 8, bd += 2048 >> 4) {
+                            tc_mma_ts(o, p, bd, ID_O, more);
+                            if (PARTS == 2) tc_mma_ts(o, p + 32, bd, ID_O, 1);
+                            more = 1;
+                        }
+                        tc_commit(pv_done0 + 8 * (nv & 1));
+                        ++nv;
+                        if (!pair || (j & 1)) {
+                            tc_commit(empty0 + 8 * vi);
+                            step(vi, vp);
+                        }
+                    }
+                    if (j < bl.n) {  // S = Q K^T of block j
+                        if ((!pair || (j & 1) == 0) && !(ok = wait1(full0 + 8 * ki, kp))) break;
+                        tc_fence_after();
+                        uint64_t qa = ad, bd = kd + (uint32_t)((ki * TILE + ((bl.first + bl.step * j) & 64) * 128) >> 4);
+                        const uint32_t d = st + 64 * (n & 1);
+#pragma unroll 1
+                        for (int k = 0; k < HALVES; ++k, qa += BOX >> 4, bd += BOX >> 4) {
+                            tc_mma(d, qa, bd, ID_S, k > 0);
+#pragma unroll
+                            for (int i = 1; i < 4; ++i) tc_mma(d, qa + 2 * i, bd + 2 * i, ID_S, 1);
+                        }
+                        tc_commit(s_full0 + 8 * (n & 1));
+                        ++n;
+                        if (!pair || (j & 1)) {
+                            tc_commit(empty0 + 8 * ki);
+                            step(ki, kp);
+                        }
+                        if (j == bl.n - 1) {
+                            tc_commit(smem_addr(&sm.q_empty[q & 1]));
+                            if (pair) mbar_arrive(smem_addr(&sm.q_empty[(q & 1) ^ 1]));
+                        }
+                    }
+                }
+            }
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        PrefixWalk w = a.range();
-        PrefixPiece pc;
         // ---- softmax: stream s, query row r of its tile
         const int s = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
-        const uint32_t sa = lane_base + S_COL + 128 * s;
-        // (a scale of zero: one that leaves every finite logit next to zero, and hides what is masked with -inf)
-        const float c2 = fmaxf(fabsf(a.c2), 1e-30f);
-        const bool minus = a.c2 < 0.f;
+        // (a scale of zero: one that leaves every finite logit next to zero, and hides what is masked)
+        const float c2 = fabsf(a.c2) < 1e-30f ? 1e-30f : a.c2, hide = c2 < 0.f ? INFINITY : -INFINITY;
         const int seq_r = r / a.G, g = r - seq_r * a.G;
-        int n = 0, met_n = 0, pieces = 0;  // products of this stream; meetings of the groups
+        int n = 0, met_n = 0;  // products of this stream; meetings of the groups
         bool ok = true;
-        while (ok && a.next(w, pc)) {
+        for (int np = 0; ok; ++np) {
+            if (!(ok = wait(sm.piece_full[np % NP], np / NP))) break;
+            const PrefixPiece pc = sm.piece[np % NP];
             const int nt = pc.t1 - pc.t0;
+            if (nt == 0) break;
             const bool pair = pc.nseq > a.rows.half;
             const int seq0 = pair && s ? a.rows.half : 0, nseq = pair ? (s ? pc.nseq - seq0 : a.rows.half) : pc.nseq;
             const bool any_row = quarter * 32 < nseq * a.G;
-            bool bad = false;  // a page that is none among the piece's
-            {
-                const int e0 = max(pc.lo, pc.k0 + pc.t0 * kPrefixTile) >> a.shift;
-                const int e1 = (min(pc.end, pc.k0 + pc.t1 * kPrefixTile) - 1) >> a.shift;
-                for (int e = e0 + lane; e <= e1; e += 32)
-                    bad |= (unsigned)__ldg(a.table + (long long)pc.b0 * a.max_pages + e) >= (unsigned)a.n_pages;
-                bad = __any_sync(0xffffffffu, bad);
-            }
+            const PrefixBlocks bl(pc, pair, s);
+            const bool there = seq_r < nseq;
             float m = -INFINITY, l = 0.f;
             const int first = n;
-            for (int t = pc.t0 + (pair ? 0 : s); ok && t < pc.t1; t += pair ? 1 : 2, ++n) {
-                if (!(ok = wait(sm.s_full[s], n))) break;
+#pragma unroll 1
+            for (int j = 0, c = bl.first; j < bl.n; ++j, c += bl.step) {
+                if (!(ok = wait(sm.s_full[s][n & 1], n >> 1))) break;
                 tc_fence_after();
-                const int k0 = pc.k0 + t * kPrefixTile, live = min(kPrefixTile, pc.end - k0), low = pc.lo - k0;
-                const bool whole = live == kPrefixTile && low <= 0;
                 if (any_row) {
-                    float v[128];
+                    const uint32_t sa = lane_base + S_COL + 128 * s + 64 * (n & 1);
+                    float v[64];
+                    tmem_ld32_nowait(sa, v);
+                    tmem_ld32_nowait(sa + 32, v + 32);
+                    tmem_ld_wait_regs<64>(v);
+                    if (c < bl.lo || c + 64 > bl.hi) {
+                        const int low = max(0, bl.lo - c), live = max(0, bl.hi - c - low);  // columns that count, from the first on
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) tmem_ld32_nowait(sa + 32 * x, v + 32 * x);
-                    tmem_ld_wait_regs<128>(v);
-                    if (minus || !whole) {
-#pragma unroll
-                        for (int x = 0; x < 128; ++x) v[x] = x < live && x >= low ? (minus ? -v[x] : v[x]) : -INFINITY;
+                        for (int x = 0; x < 64; ++x) v[x] = (unsigned)(x - low) < (unsigned)live ? v[x] : hide;
                     }
-                    float mx[4] = {v[0], v[1], v[2], v[3]};
+                    // Probabilities against the maximum so far.  No maximum of the block is looked for while their sum stays below
+                    // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).
+                    uint32_t hi[32], lo[PARTS == 2 ? 32 : 1];
+                    float sum;
+                    bool again = false;
+                    for (;;) {
+                        const float nb = again && m == -INFINITY ? 0.f : -m;
+                        const unsigned long long cc = pair_of(c2, c2), nn = pair_of(nb, nb);
+                        unsigned long long s4[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-                    for (int x = 4; x + 8 <= 128; x += 8)
+                        for (int y = 0; y < 32; ++y) {
+                            float p0, p1;
+                            unpair(fma_pair(pair_of(v[2 * y], v[2 * y + 1]), cc, nn), p0, p1);
+                            p0 = fast_exp2(p0);
+                            p1 = fast_exp2(p1);
+                            s4[y & 3] = add_pair(s4[y & 3], pair_of(p0, p1));
+                            if (PARTS == 2)
+                                split_bf16(p0, p1, hi[y], lo[y]);
+                            else
+                                hi[y] = pack_bf16(p0, p1);
+                        }
+                        float s0, s1;
+                        unpair(add_pair(add_pair(s4[0], s4[1]), add_pair(s4[2], s4[3])), s0, s1);
+                        sum = s0 + s1;
+                        const bool grow = there && !again && !(sum <= 0x1p12f);  // (at first the maximum is -inf: infinities and NaN)
+                        if (!__any_sync(0xffffffffu, grow)) break;
+                        again = true;
+                        float mx = -INFINITY;
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) mx[y] = max3(mx[y], v[x + y], v[x + 4 + y]);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) mx[y] = fmaxf(mx[y], v[124 + y]);
-                    const float mb = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * c2;
-                    const bool grow = mb > m + kLazyLog2;
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float mn = grow ? mb : m, al = grow ? fast_exp2(m - mn) : 1.f;
+                        for (int x = 0; x < 64; x += 2) mx = max3(mx, v[x] * c2, v[x + 1] * c2);
+                        const float mn = grow ? fmaxf(m, mx) : m, al = grow ? part_factor(m, mn) : 1.f;
                         l *= al;
                         m = mn;
                         if (n > first) {  // the output so far
-                            if (!(ok = wait(sm.pv_done[s], n - 1))) break;
+                            if (!(ok = wait(sm.pv_done[s][(n - 1) & 1], (n - 1) >> 1))) break;
                             tc_fence_after();
 #pragma unroll 1
                             for (int x = 0; x < D / 16; ++x) {
@@ -322,95 +429,90 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                             }
                         }
                     }
-                    const float nb = m == -INFINITY ? 0.f : -m;
-                    const unsigned long long cc = pair_of(c2, c2), nn = pair_of(nb, nb);
-                    unsigned long long sum[2] = {0ull, 0ull};
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t hi[16], lo[16];
-#pragma unroll
-                        for (int y = 0; y < 16; ++y) {
-                            const int i = 32 * x + 2 * y;
-                            float p0, p1;
-                            unpair(fma_pair(pair_of(v[i], v[i + 1]), cc, nn), p0, p1);
-                            p0 = fast_exp2(p0);
-                            p1 = fast_exp2(p1);
-                            sum[y & 1] = add_pair(sum[y & 1], pair_of(p0, p1));
-                            if (PARTS == 2)
-                                split_bf16(p0, p1, hi[y], lo[y]);
-                            else
-                                hi[y] = pack_bf16(p0, p1);
-                        }
-                        tmem_st16(sa + 16 * x, hi);
-                        if (PARTS == 2) tmem_st16(sa + 64 + 16 * x, lo);
+                    if (!ok) break;
+                    l += sum;
+                    tmem_st16(sa, hi);
+                    tmem_st16(sa + 16, hi + 16);
+                    if (PARTS == 2) {
+                        tmem_st16(sa + 32, lo);
+                        tmem_st16(sa + 48, lo + 16);
                     }
-                    float s0, s1;
-                    unpair(add_pair(sum[0], sum[1]), s0, s1);
-                    l += s0 + s1;
                     tmem_st_wait();
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sm.p_full[s]));
+                if (lane == 0) mbar_arrive(smem_addr(&sm.p_full[s][n & 1]));
+                ++n;
             }
             if (!ok) break;
             // ---- the piece's partial
-            if (n > first && !(ok = wait(sm.pv_done[s], n - 1))) break;
+            if (n > first && !(ok = wait(sm.pv_done[s][(n - 1) & 1], (n - 1) >> 1))) break;
             tc_fence_after();
-            int cols = D, col0 = 0;
             float f0 = 1.f, f1 = 0.f;
             if (!pair) {  // the streams join: each group takes half of the columns
-                // (a group without a product in this piece has not waited for the other to be done with the one before)
-                if (n == first && pieces > 0 && !(ok = wait(sm.o_free, pieces - 1))) break;
                 sm.ml[s][r] = make_float2(m, l);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sm.met));
                 if (!(ok = wait(sm.met, met_n++))) break;
+                tc_fence_after();
                 const float2 x = sm.ml[0][r], y = sm.ml[1][r];
                 m = fmaxf(x.x, y.x);
                 f0 = part_factor(x.x, m);
                 f1 = part_factor(y.x, m);
-                l = x.y * f0 + (nt > 1 ? y.y * f1 : 0.f);
-                cols = D / 2;
-                col0 = s * cols;
+                l = x.y * f0 + y.y * f1;
             }
             if (any_row) {
                 float *po = nullptr;
                 float2 *pm = nullptr;
-                if (seq_r < nseq) {
+                if (there) {
                     a.partial<D>(pc, seq0 + seq_r, g, po, pm);
-                    if (pair || s == 0) *pm = make_float2(m, bad ? -1.f : l);
+                    if (pair || s == 0) *pm = make_float2(m, *(volatile int *)&sm.bad[np % NP] ? -1.f : l);
                 }
-#pragma unroll 1
-                for (int x = 0; x < cols; x += 16) {
-                    float o[16];
-                    const uint32_t oa = lane_base + O_COL + col0 + x;
-                    tmem_ld16_nowait(oa + (pair ? D * s : 0), o);
-                    tmem_ld_wait_regs<16>(o);
-                    if (!pair) {
-                        float o1[16];
-                        if (nt > 1) {
-                            tmem_ld16_nowait(oa + D, o1);
-                            tmem_ld_wait_regs<16>(o1);
-                        }
-#pragma unroll
-                        for (int y = 0; y < 16; ++y) o[y] = o[y] * f0 + (nt > 1 ? o1[y] * f1 : 0.f);
-                    }
+                auto store = [&](int c, const float (&o)[32]) {
                     if (po != nullptr)
 #pragma unroll
-                        for (int y = 0; y < 16; y += 4)
-                            *reinterpret_cast<float4 *>(po + col0 + x + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                        for (int y = 0; y < 32; y += 4)
+                            *reinterpret_cast<float4 *>(po + c + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                };
+                if (pair) {
+#pragma unroll 1
+                    for (int x = 0; x < D; x += 64) {
+                        float o[2][32];
+                        tmem_ld32_nowait(lane_base + O_COL + D * s + x, o[0]);
+                        tmem_ld32_nowait(lane_base + O_COL + D * s + x + 32, o[1]);
+                        tmem_ld_wait_regs<32>(o[0]);
+                        tmem_ld_wait_regs<32>(o[1]);
+                        store(x, o[0]);
+                        store(x + 32, o[1]);
+                    }
+                } else {
+                    // (a stream that saw nothing has a factor of zero, and maybe no output)
+                    constexpr int H = D / 2;
+                    const uint32_t oa = lane_base + O_COL + H * s;
+#pragma unroll 1
+                    for (int x = 0; x < H; x += 32) {
+                        float o[2][32];
+                        tmem_ld32_nowait(oa + x, o[0]);
+                        tmem_ld32_nowait(oa + D + x, o[1]);
+                        tmem_ld_wait_regs<32>(o[0]);
+                        tmem_ld_wait_regs<32>(o[1]);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[0][i] = (f0 != 0.f ? o[0][i] * f0 : 0.f) + (f1 != 0.f ? o[1][i] * f1 : 0.f);
+                        store(H * s + x, o[0]);
+                    }
                 }
             }
-            if (bad && tid == 128) raise_error(a.err, ERR_PAGE);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sm.o_free));
-            ++pieces;
+            if (lane == 0) {
+                mbar_arrive(smem_addr(&sm.o_free));
+                mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
+            }
         }
     }
     __syncthreads();
     if (warp == 1) {
+        __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }

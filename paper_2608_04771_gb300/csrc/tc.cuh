@@ -140,11 +140,25 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N)
 constexpr long long kTcSpin = 1LL << 22;  // polls, each suspended for up to a few microseconds
 // Bounded wait of a converged warp on an mbarrier phase; the same answer in every lane.  A wait
 // that runs out raises the CTA's abort flag, which ends the other roles' waits too.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned *err)
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned *err,
+                                          long long polls = kTcSpin)
 {
-    for (long long i = 0; i < kTcSpin; ++i) {
+    for (long long i = 0; i < polls; ++i) {
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
         if ((i & 1023) == 1023 && __any_sync(0xffffffffu, *abort_flag != 0)) return false;
+    }
+    *abort_flag = 1;
+    raise_error(err, ERR_INTERNAL);
+    return false;
+}
+
+// The same by one thread.
+__device__ __forceinline__ bool thread_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned *err,
+                                            long long polls)
+{
+    for (long long i = 0; i < polls; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 1023) == 1023 && *abort_flag != 0) return false;
     }
     *abort_flag = 1;
     raise_error(err, ERR_INTERNAL);

@@ -191,6 +191,19 @@ def test_many_short_groups():
     Batch(8, 3, 4, 2, 64, F32, 16, group, shared, rng.integers(0, 30, (3, n, 2))).go()
 
 
+@pytest.mark.parametrize("n,P,mine,Ly,page", [(24, 140, 20, 6, 64), (39, 0, 130, 3, 16), (12, 1000, 60, 4, 128), (3, 300, 1, 28, 16)])
+def test_the_same_bits_again_and_again(n, P, mine, Ly, page):
+    """Many short items one after the other in every CTA, whose roles then run far apart: nothing depends on when."""
+    own = np.random.default_rng(n).integers(0, mine, (Ly, n, 2))
+    c = Batch(n, Ly, 14, 2, 128, BF, page, np.repeat(np.arange(n // 3), 3).tolist(), [P] * n, own, out_dtype=F32, garbage=False).go()
+    out, lse = c.out.clone(), c.lse.clone()
+    for _ in range(150):
+        c.lens -= 1
+        c.run()
+        assert torch.equal(bits(out), bits(c.out)) and torch.equal(lse, c.lse)
+    reco.reco_check()
+
+
 @pytest.mark.parametrize("n", [255, 256, 257, 1023, 1024, 1025, 2500])
 def test_plans_of_many_sequences(n):
     rng = np.random.default_rng(n)
