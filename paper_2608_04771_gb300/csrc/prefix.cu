@@ -59,6 +59,7 @@ __device__ void plan_groups(const PlanArgs &a)
 {
     __shared__ long long sm[kPrefixBlock / 32], sm_work;
     __shared__ int sm_start, sm_runs;
+    bool several = false;  // row tiles
     if (threadIdx.x == 0) {
         sm_work = 0;
         sm_start = -1;
@@ -79,6 +80,7 @@ __device__ void plan_groups(const PlanArgs &a)
         const int run = c_runs + scan_block<false>(first && kept ? 1 : 0, reinterpret_cast<int *>(sm)) - 1;
         const long long mine = last && kept ? a.rows.work(b - start + 1, p) : 0;
         const long long work = c_work + scan_block<false>(mine, sm);
+        several |= last && kept && b - start + 1 > a.rows.per;
         if (last && kept) a.ws.runs[run] = PrefixRun{start, b - start + 1, p, 0, work - mine};
         if (in) {
             const bool wrong = !valid || __ldg(a.shared + b) != p;
@@ -92,8 +94,8 @@ __device__ void plan_groups(const PlanArgs &a)
             sm_work = work;
         }
     }
-    __syncthreads();
-    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs};
+    several = __syncthreads_or(several);
+    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs, several ? a.rows.unit(a.rows.per + 1, 0) : kOwnUnit};
     if (off) raise_error(a.err, ERR_LEN);
 }
 
@@ -125,7 +127,7 @@ __device__ void plan_units(const PlanArgs &a, int block)
             x.n = L + append;
             x.lo = company ? p : 0;
             x.k0 = x.lo & -min(kPrefixTile, 1 << a.shift);  // the tensor cores' kernel copies whole boxes
-            work = x.n > x.lo ? 2 * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
+            work = x.n > x.lo ? kOwnUnit * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
         }
     }
     const int before = scan_block<false>(work, sm) - work;
@@ -403,22 +405,24 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
     // partials: [0, n_own) of the own rows, then n_pre of the prefix; CTAs of the first ones
     int n_own = 0, n_pre = 0, own_c = 0, pre_c = 0, pre_row = 0;
     if (ok) {
-        const long long pre = total.work * a.p.layers * a.p.Hkv, all = pre + a.p.own_total();
-        const int n = prefix_ctas(all, a.grid);
+        const long long pre = total.work * a.p.layers * a.p.Hkv;
+        const long long all = pre + a.p.own_total();
+        const PrefixShare share(all, a.grid, total.most);
         auto ctas = [&](long long w0, int tiles, int unit, int &c) {
-            c = prefix_cta(w0, all, n);
-            return 1 + prefix_cta(w0 + (long long)(tiles - 1) * unit, all, n) - c;
+            c = share.cta(w0);
+            return 1 + share.cta(w0 + (long long)(tiles - 1) * unit) - c;
         };
         if (x.n > x.lo) {
             long long w0 = pre + x.work + kOwnExtra;
             for (int i = 0; i < u / kPrefixBlock; ++i) w0 += __ldg(a.p.block_work + i);
-            n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, 2, own_c);
+            n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, kOwnUnit, own_c);
         }
         if (run >= 0) {
             const PrefixRun rn = a.p.runs[run];
             const PrefixRows rows = a.p.rows;
             const int i = b - rn.b0, rt = i / rows.per, kt = (rn.p + kPrefixTile - 1) / kPrefixTile;
-            n_pre = ctas(((long long)layer * a.p.Hkv + h) * total.work + rn.work + 2ll * rt * kt, kt, rows.unit(rn.n, rt), pre_c);
+            n_pre = ctas(((long long)layer * a.p.Hkv + h) * total.work + rn.work + (long long)rt * kt * rows.unit(rn.n, 0), kt,
+                         rows.unit(rn.n, rt), pre_c);
             pre_row = (i - rt * rows.per) * G;
         }
     }

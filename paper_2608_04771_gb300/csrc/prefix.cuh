@@ -7,37 +7,44 @@
 namespace reco {
 
 // A row tile takes the query heads of up to `per` sequences of a group, of which `half` make what the tensor cores take
-// at once (128 rows).  Work is counted in units: 2 for a key tile, what its bytes cost, but 1 for the last row tile of a
-// group of several, if it has no more than `half` sequences: its rows come from L2, and it takes half the products.
-// A unit's own rows cost kOwnExtra more, for the start and the end of an item.
-constexpr int kOwnExtra = 2;
+// at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy: a key tile takes
+// 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has several
+// row tiles, which find the keys in L2, 9 for a whole one (1.9 us) and 6 for the last one if it has no more than `half`
+// sequences (1.2 us).  The start and the end of a unit's own rows take kOwnExtra more.
+constexpr int kOwnUnit = 8, kOwnExtra = 11;
 struct PrefixRows {
     int per, half;
-    __host__ __device__ int unit(int n, int rt) const { return rt > 0 && n - rt * per <= half && per > half ? 1 : 2; }
-    // work of a group of n sequences with p rows, per layer and KV head
+    // a key tile's of row tile rt of n sequences (all but the last row tile have the first one's)
+    __host__ __device__ int unit(int n, int rt) const { return n <= per ? 8 : (n - rt * per <= half && per > half ? 6 : 9); }
+    // a group's of n sequences with p rows, per layer and KV head
     __host__ __device__ long long work(int n, int p) const
     {
         const int last = (n - 1) / per, kt = (p + kPrefixTile - 1) / kPrefixTile;
-        return (long long)kt * (2ll * last + unit(n, last));
+        return (long long)kt * ((long long)last * unit(n, 0) + unit(n, last));
     }
 };
 
 #ifdef __CUDACC__
-// The work is shared out to n CTAs, no less than a key tile's to each.  CTA c's begins at total * c / n; prefix_cta is the
-// CTA that unit w of the work falls to.  A key tile whose work is cut goes to the CTA that its first unit falls to: tile t
-// of an item whose tiles begin at w0, `unit` to each, to that of w0 + t * unit.
 // (64-bit divisions take some hundred instructions: most are of 32-bit numbers)
 __device__ __noinline__ static long long quotient(long long a, long long b)
 {
     return ((unsigned long long)a | (unsigned long long)b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
-__device__ __forceinline__ int prefix_ctas(long long total, int grid)
-{
-    const long long most = total >> 1;
-    return most < 1 ? 1 : (most < grid ? (int)most : grid);
-}
-__device__ __forceinline__ long long prefix_begin_at(int c, long long total, int n) { return quotient(total * c, n); }
-__device__ __forceinline__ int prefix_cta(long long w, long long total, int n) { return (int)quotient((w + 1) * n - 1, total); }
+// How the work is shared out to the CTAs: evenly, or, where that left less than a key tile's to each, a tile's (`most`).
+// A key tile whose work is cut goes to the CTA that its first unit falls to: tile t of an item whose tiles begin at w0,
+// `unit` to each, to that of w0 + t * unit.  (Every CTA between an item's first and last then has one of its tiles.)
+struct PrefixShare {
+    long long total;
+    int n, most;  // CTAs with work; 0: evenly
+    __device__ __forceinline__ PrefixShare(long long all, int grid, int most_unit) : total(all)
+    {
+        const bool few = all <= (long long)grid * most_unit;
+        most = few ? most_unit : 0;
+        n = few ? ((int)all + most_unit - 1) / most_unit : grid;
+    }
+    __device__ __forceinline__ long long begin(int c) const { return most ? min(total, (long long)c * most) : quotient(total * c, n); }
+    __device__ __forceinline__ int cta(long long w) const { return most ? (int)w / most : (int)quotient((w + 1) * n - 1, total); }
+};
 
 // The last i of [0, n) with key(i) <= x, by a warp (key does not decrease, key(0) <= x).
 template <typename F> __device__ __forceinline__ int warp_last(int n, long long x, F key)
@@ -96,10 +103,10 @@ struct PrefixArgs {
         w.prefix = prefix_total();
         w.u = -1;
         w.base = 0;
-        const long long all = w.prefix + own_total();
-        const int n = prefix_ctas(all, (int)gridDim.x), c = blockIdx.x;
-        w.w = c < n ? prefix_begin_at(c, all, n) : 0;
-        w.end = c < n ? prefix_begin_at(c + 1, all, n) : 0;
+        const PrefixShare share(w.prefix + own_total(), (int)gridDim.x, total->most);
+        const int c = blockIdx.x;
+        w.w = c < share.n ? share.begin(c) : 0;
+        w.end = c < share.n ? share.begin(c + 1) : 0;
         return w;
     }
     // (whole warps)
@@ -110,7 +117,7 @@ struct PrefixArgs {
                 const long long per = total->work, lh = quotient(w.w, per), rem = w.w - lh * per;
                 const PrefixRun r = runs[warp_last(total->n, rem, [&](int i) { return runs[i].work; })];
                 const int kt = (r.p + kPrefixTile - 1) / kPrefixTile;
-                const long long in = rem - r.work, full = 2ll * kt;
+                const long long in = rem - r.work, full = (long long)kt * rows.unit(r.n, 0);
                 const int rt = (int)quotient(in, full), unit = rows.unit(r.n, rt), u = (int)(in - rt * full);
                 const int e = (int)min((long long)kt * unit, u + (w.end - w.w));
                 pc.layer = (int)lh / Hkv;
@@ -145,10 +152,10 @@ struct PrefixArgs {
             pc.k0 = x.k0;
             pc.lo = x.lo;
             pc.end = x.n;
-            const int in = at - w.base - x.work, size = kt > 0 ? 2 * kt + kOwnExtra : 0;
+            const int in = at - w.base - x.work, size = kt > 0 ? kOwnUnit * kt + kOwnExtra : 0;
             const int e = (int)min((long long)size, in + (w.end - w.w));
-            pc.t0 = max(0, in - kOwnExtra + 1) >> 1;
-            pc.t1 = max(0, e - kOwnExtra + 1) >> 1;
+            pc.t0 = max(0, in - kOwnExtra + kOwnUnit - 1) / kOwnUnit;
+            pc.t1 = max(0, e - kOwnExtra + kOwnUnit - 1) / kOwnUnit;
             pc.own = true;
             if (e == size) {  // the next unit, maybe of the next block
                 ++w.u;

@@ -9,7 +9,7 @@
 // One CTA per SM, persistent over its share of the key tiles (PrefixArgs::next), of warps
 //   0      finds the pieces, a few ahead of the others, and copies, all by TMA: queries (a box of a group's sequences, or
 //          one sequence's, into one of two tiles), K and V (a box per page and 64 columns, a lane each, into a ring of tiles);
-//   1, 3   one thread each, which issue the products of a stream;
+//   1, 3   issue the products of a stream each;
 //   2      clears V rows that no query sees in tiles that a border crosses (their probabilities are zero, but NaN
 //          times zero is not);
 //   4..11  two softmax groups of four warps, one per stream, a query row per thread.
@@ -159,8 +159,13 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
     const uint32_t tmem = sm.tmem;
     wait_prior_grid();
     release_next_grid();  // the join looks up its places meanwhile
-    // a whole warp's wait for phase k of a barrier
-    auto wait = [&](uint64_t &bar, int k) { return warp_wait(smem_addr(&bar), k & 1, &sm.abort, a.err, kPolls); };
+    // A wait for phase k of a barrier, by every lane for itself; `ok` says whether it came (the same in all lanes but
+    // where a wait runs out: the roles look at all lanes' once per step).
+    bool ok = true;
+    auto await = [&](uint32_t bar, int k) {
+        if (!mbar_try_wait(bar, k & 1)) ok &= thread_wait(bar, k & 1, &sm.abort, a.err, kPolls);
+    };
+    auto fine = [&]() { return __all_sync(0xffffffffu, ok) != 0; };
 
     // registers of the launch, 168 a thread: 88 for warps 0 to 3, 208 for the softmax, which holds a row of a block
     static_assert(128 * 88 + 256 * 208 <= C::THREADS * 168, "no more than the launch has");
@@ -173,10 +178,9 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         const int rows = min(128, 1 << a.shift), boxes = 128 / rows;
         const int box = lane / HALVES, half = lane % HALVES;
         int slot = 0, nq = 0;
-        bool ok = true;
-        for (int np = 0; ok; ++np) {
+        for (int np = 0; fine(); ++np) {
             const bool more = a.next(w, pc);
-            if (!(ok = wait(sm.piece_empty[np % NP], np / NP + 1))) break;
+            await(smem_addr(&sm.piece_empty[np % NP]), np / NP + 1);
             if (lane == 0) {
                 if (!more) pc.t1 = pc.t0 = 0;
                 sm.piece[np % NP] = pc;
@@ -190,7 +194,8 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             long long row = row_of(pc.t0);
             for (int s = 0; s < (pc.nseq > a.rows.half ? 2 : 1); ++s, ++nq) {
                 const int i = nq & 1;
-                if (!(ok = wait(sm.q_empty[i], (nq >> 1) + 1))) break;
+                await(smem_addr(&sm.q_empty[i]), (nq >> 1) + 1);
+                if (!fine()) break;
                 if (lane == 0) {
                     const uint32_t bar = smem_addr(&sm.q_full[i]);
                     mbar_expect_tx(bar, (uint32_t)((pc.own ? 1 : a.rows.half) * a.G * HALVES * 128));
@@ -200,16 +205,18 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                 }
                 __syncwarp();
             }
-            for (int t = pc.t0; ok && t < pc.t1; ++t) {
+            for (int t = pc.t0; fine() && t < pc.t1; ++t) {
                 const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
                 if (__any_sync(0xffffffffu, needed(t) && row < 0) && lane == 0) {
                     *(volatile int *)&sm.bad[np % NP] = 1;
                     raise_error(a.err, ERR_PAGE);
                 }
                 const long long next = t + 1 < pc.t1 ? row_of(t + 1) : -1ll;
+#pragma unroll 1
                 for (int kv = 0; kv < 2; ++kv, ++slot) {
                     const int i = slot % NS;
-                    if (!(ok = wait(sm.empty[i], slot / NS + 1))) break;
+                    await(smem_addr(&sm.empty[i]), slot / NS + 1);
+                    if (!fine()) break;
                     const uint32_t bar = smem_addr(&sm.full[i]);
                     if (lane == 0) mbar_expect_tx(bar, (uint32_t)(n * rows * 128));
                     __syncwarp();
@@ -227,9 +234,9 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // ---- V rows outside the rows that count, within the product's steps of 16
         int slot = 1, nc = 0;
-        bool ok = true;
-        for (int np = 0; ok; ++np) {
-            if (!(ok = wait(sm.piece_full[np % NP], np / NP))) break;
+        for (int np = 0; fine(); ++np) {
+            await(smem_addr(&sm.piece_full[np % NP]), np / NP);
+            if (!fine()) break;
             const PrefixPiece x = sm.piece[np % NP];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
@@ -237,8 +244,9 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             for (int t = x.t0; t < x.t1; ++t, slot += 2) {
                 const int k0 = x.k0 + t * kPrefixTile, low = max(0, x.lo - k0), live = min(kPrefixTile, x.end - k0);
                 if (((low | live) & 15) == 0) continue;
-                if (!(ok = wait(sm.landed[0], nc) && wait(sm.landed[1], nc))) break;
-                ++nc;
+                await(smem_addr(&sm.landed[0]), nc);
+                await(smem_addr(&sm.landed[1]), nc++);
+                if (!fine()) break;
                 const uint32_t tile = ring + (slot % NS) * TILE;
                 auto clear = [&](int r0, int n) {
                     for (int i = lane; i < n * 8 * HALVES; i += 32)
@@ -256,93 +264,98 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         // ---- products of stream s
         constexpr uint32_t ID_S = idesc_bf16(128, 64), ID_O = idesc_bf16(128, D) | kIdescMnB;
         const int s = warp >> 1;
-        if (elect_one()) {
-            auto wait1 = [&](uint32_t bar, uint32_t parity) { return thread_wait(bar, parity, &sm.abort, a.err, kPolls); };
-            const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX);
-            const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
-            const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
-                           p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
-            // ring places of the next K and V tile, and the parity of their phase; query tiles, score and value products,
-            // cleared tiles so far
-            int ki = 0, vi = 1, nq = 0, n = 0, nv = 0, nc = 0;
-            uint32_t kp = 0, vp = 0;
-            auto step = [&](int &i, uint32_t &p) {
-                i += 2;
-                p ^= i >= NS ? 1u : 0u;
-                i -= i >= NS ? NS : 0;
-            };
-            bool ok = true;
-            for (int np = 0; ok; ++np) {
-                if (!(ok = wait1(smem_addr(&sm.piece_full[np % NP]), np / NP & 1))) break;
-                const PrefixPiece &x = sm.piece[np % NP];
-                const bool pair = x.nseq > a.rows.half;
-                const PrefixBlocks bl(x, pair, s);
-                mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
-                if (bl.n == 0) break;
-                const int q = nq + (pair ? s : 0);
-                for (int i = 0; ok && i < (pair ? 2 : 1); ++i, ++nq) ok = wait1(smem_addr(&sm.q_full[nq & 1]), nq >> 1 & 1);
-                const uint64_t ad = qd + (uint64_t)((q & 1) * TILE >> 4);
-                uint32_t more = 0;
+        // (the whole warp goes through the loops, so that what it computes is known to be uniform: operands of the products
+        // come from uniform registers, and one thread alone issued a product every 70 to 125 cycles)
+        const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX);
+        const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
+        const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
+                       p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
+        // ring places of the next K and V tile, and the parity of their phase; query tiles, blocks, cleared tiles so far
+        int ki = 0, vi = 1, kp = 0, vp = 0, nq = 0, n = 0, nc = 0;
+        auto step = [&](int &i, int &p) {
+            i += 2;
+            p ^= i >= NS ? 1 : 0;
+            i -= i >= NS ? NS : 0;
+        };
+        for (int np = 0; fine(); ++np) {
+            await(smem_addr(&sm.piece_full[np % NP]), np / NP);
+            if (!fine()) break;
+            const PrefixPiece x = sm.piece[np % NP];
+            const bool pair = x.nseq > a.rows.half;
+            const PrefixBlocks bl(x, pair, s);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
+            if (bl.n == 0) break;
+            const int q = nq + (pair ? s : 0);
+            for (int i = 0; i < (pair ? 2 : 1); ++i, ++nq) await(smem_addr(&sm.q_full[nq & 1]), nq >> 1);
+            const uint64_t ad = qd + (uint64_t)((q & 1) * TILE >> 4);
+            uint32_t more = 0;
+            // a border that is not at a step of 16 crosses the first or the last tile: V rows have to be cleared first
+            const int crossed0 = bl.lo & 15 ? 0 : -1, crossed1 = bl.hi & 15 ? (bl.hi - 1) >> 7 : -1;
 #pragma unroll 1
-                for (int j = 0; ok && j < bl.n + 2; ++j) {
-                    if (j >= 2) {  // O += P V of block j - 2
-                        const int c = bl.first + bl.step * (j - 2);
-                        if (!pair || (j & 1) == 0) {
-                            if (!(ok = wait1(full0 + 8 * vi, vp))) break;
-                            // a border that is not at a step of 16: V rows have to be cleared first
-                            const int t = c & ~127;
-                            if ((t == 0 && (bl.lo & 15)) || (t + 128 > bl.hi && (bl.hi & 15))) {
-                                mbar_arrive(smem_addr(&sm.landed[s]));
-                                if (!(ok = wait1(smem_addr(&sm.cleared[s]), nc++ & 1))) break;
-                            }
-                        }
-                        if (!(ok = wait1(p_full0 + 8 * (nv & 1), nv >> 1 & 1))) break;
-                        // (every piece waits for the outputs of the one before to have been read, for the barrier's phases)
-                        if (j == 2 && np > 0 && !(ok = wait1(smem_addr(&sm.o_free), (np - 1) & 1))) break;
-                        tc_fence_after();
-                        uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
-                        uint32_t p = st + 64 * (nv & 1);
-                        // rows of the block that count, in steps of 16
-                        const int k0 = max(0, bl.lo - c) >> 4, k1 = (min(64, bl.hi - c) + 15) >> 4;
-                        p += 8 * k0;
-                        bd += (uint32_t)(k0 * 2048 >> 4);
-#pragma unroll 1
-                        for (int k = k0; k < k1; ++k, p += 8, bd += 2048 >> 4) {
-                            tc_mma_ts(o, p, bd, ID_O, more);
-                            if (PARTS == 2) tc_mma_ts(o, p + 32, bd, ID_O, 1);
-                            more = 1;
-                        }
-                        tc_commit(pv_done0 + 8 * (nv & 1));
-                        ++nv;
-                        if (!pair || (j & 1)) {
-                            tc_commit(empty0 + 8 * vi);
-                            step(vi, vp);
+            for (int j = 0; j < bl.n + 2 && fine(); ++j) {
+                const int odd = j & 1;
+                if (j >= 2) {  // O += P V of block j - 2
+                    const int c = bl.first + bl.step * (j - 2), nv = n + j - 2;
+                    if (!pair || !odd) {
+                        await(full0 + 8 * vi, vp);
+                        const int t = c >> 7;
+                        if (t == crossed0 || t == crossed1) {
+                            if (lane == 0) mbar_arrive(smem_addr(&sm.landed[s]));
+                            await(smem_addr(&sm.cleared[s]), nc++);
                         }
                     }
-                    if (j < bl.n) {  // S = Q K^T of block j
-                        if ((!pair || (j & 1) == 0) && !(ok = wait1(full0 + 8 * ki, kp))) break;
-                        tc_fence_after();
-                        uint64_t qa = ad, bd = kd + (uint32_t)((ki * TILE + ((bl.first + bl.step * j) & 64) * 128) >> 4);
-                        const uint32_t d = st + 64 * (n & 1);
-#pragma unroll 1
-                        for (int k = 0; k < HALVES; ++k, qa += BOX >> 4, bd += BOX >> 4) {
-                            tc_mma(d, qa, bd, ID_S, k > 0);
+                    await(p_full0 + 8 * (nv & 1), nv >> 1);
+                    // (every piece waits for the outputs of the one before to have been read, for the barrier's phases)
+                    if (j == 2 && np > 0) await(smem_addr(&sm.o_free), np - 1);
+                    tc_fence_after();
+                    const uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
+                    const uint32_t p = st + 64 * (nv & 1);
+                    const int k0 = max(0, bl.lo - c) >> 4, k1 = min(4, (bl.hi - c + 15) >> 4);  // rows that count, in steps of 16
+                    if (elect_one()) {
+                        if (k0 == 0 && k1 == 4) {
 #pragma unroll
-                            for (int i = 1; i < 4; ++i) tc_mma(d, qa + 2 * i, bd + 2 * i, ID_S, 1);
+                            for (int k = 0; k < 4; ++k) {
+                                tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > 0 ? 1u : more);
+                                if (PARTS == 2) tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                            }
+                        } else {
+#pragma unroll 1
+                            for (int k = k0; k < k1; ++k) {
+                                tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > k0 ? 1u : more);
+                                if (PARTS == 2) tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                            }
                         }
-                        tc_commit(s_full0 + 8 * (n & 1));
-                        ++n;
-                        if (!pair || (j & 1)) {
-                            tc_commit(empty0 + 8 * ki);
-                            step(ki, kp);
+                        tc_commit(pv_done0 + 8 * (nv & 1));
+                        if (!pair || odd) tc_commit(empty0 + 8 * vi);
+                    }
+                    __syncwarp();
+                    more |= k0 < k1 ? 1u : 0u;
+                    if (!pair || odd) step(vi, vp);
+                }
+                if (j < bl.n) {  // S = Q K^T of block j
+                    if (!pair || !odd) await(full0 + 8 * ki, kp);
+                    tc_fence_after();
+                    const uint64_t bd = kd + (uint32_t)((ki * TILE + ((bl.first + bl.step * j) & 64) * 128) >> 4);
+                    const uint32_t d = st + 64 * ((n + j) & 1);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((k >> 2) * BOX + (k & 3) * 32) >> 4;
+                            tc_mma(d, ad + off, bd + off, ID_S, k > 0);
                         }
+                        tc_commit(s_full0 + 8 * ((n + j) & 1));
+                        if (!pair || odd) tc_commit(empty0 + 8 * ki);
                         if (j == bl.n - 1) {
                             tc_commit(smem_addr(&sm.q_empty[q & 1]));
                             if (pair) mbar_arrive(smem_addr(&sm.q_empty[(q & 1) ^ 1]));
                         }
                     }
+                    __syncwarp();
+                    if (!pair || odd) step(ki, kp);
                 }
             }
+            n += bl.n;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -352,10 +365,11 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         // (a scale of zero: one that leaves every finite logit next to zero, and hides what is masked)
         const float c2 = fabsf(a.c2) < 1e-30f ? 1e-30f : a.c2, hide = c2 < 0.f ? INFINITY : -INFINITY;
         const int seq_r = r / a.G, g = r - seq_r * a.G;
-        int n = 0, met_n = 0;  // products of this stream; meetings of the groups
-        bool ok = true;
-        for (int np = 0; ok; ++np) {
-            if (!(ok = wait(sm.piece_full[np % NP], np / NP))) break;
+        const uint32_t s_full0 = smem_addr(&sm.s_full[s][0]), p_full0 = smem_addr(&sm.p_full[s][0]);
+        int n = 0, met_n = 0;  // blocks of this stream; meetings of the groups
+        for (int np = 0; fine(); ++np) {
+            await(smem_addr(&sm.piece_full[np % NP]), np / NP);
+            if (!fine()) break;
             const PrefixPiece pc = sm.piece[np % NP];
             const int nt = pc.t1 - pc.t0;
             if (nt == 0) break;
@@ -367,8 +381,9 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             float m = -INFINITY, l = 0.f;
             const int first = n;
 #pragma unroll 1
-            for (int j = 0, c = bl.first; j < bl.n; ++j, c += bl.step) {
-                if (!(ok = wait(sm.s_full[s][n & 1], n >> 1))) break;
+            for (int j = 0, c = bl.first; j < bl.n && fine(); ++j, c += bl.step) {
+                await(s_full0 + 8 * (n & 1), n >> 1);
+                __syncwarp();
                 tc_fence_after();
                 if (any_row) {
                     const uint32_t sa = lane_base + S_COL + 128 * s + 64 * (n & 1);
@@ -415,7 +430,8 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                         l *= al;
                         m = mn;
                         if (n > first) {  // the output so far
-                            if (!(ok = wait(sm.pv_done[s][(n - 1) & 1], (n - 1) >> 1))) break;
+                            await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
+                            __syncwarp();
                             tc_fence_after();
 #pragma unroll 1
                             for (int x = 0; x < D / 16; ++x) {
@@ -429,7 +445,6 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                             }
                         }
                     }
-                    if (!ok) break;
                     l += sum;
                     tmem_st16(sa, hi);
                     tmem_st16(sa + 16, hi + 16);
@@ -441,19 +456,21 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sm.p_full[s][n & 1]));
+                if (lane == 0) mbar_arrive(p_full0 + 8 * (n & 1));
                 ++n;
             }
-            if (!ok) break;
+            if (!fine()) break;
             // ---- the piece's partial
-            if (n > first && !(ok = wait(sm.pv_done[s][(n - 1) & 1], (n - 1) >> 1))) break;
+            await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
+            __syncwarp();
             tc_fence_after();
             float f0 = 1.f, f1 = 0.f;
             if (!pair) {  // the streams join: each group takes half of the columns
                 sm.ml[s][r] = make_float2(m, l);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sm.met));
-                if (!(ok = wait(sm.met, met_n++))) break;
+                await(smem_addr(&sm.met), met_n++);
+                __syncwarp();
                 tc_fence_after();
                 const float2 x = sm.ml[0][r], y = sm.ml[1][r];
                 m = fmaxf(x.x, y.x);
