@@ -174,17 +174,26 @@ static EncodeTiledFn encode_fn()
     return fn;
 }
 
-bool encode_bf16_2d(void *map, const void *base, unsigned long long rows, int cols, int box_cols, int box_rows)
+static bool encode_2d(void *map, const void *base, unsigned long long rows, int cols, int box_cols, int box_rows, bool f32)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
+    const cuuint64_t strides[1] = {(cuuint64_t)cols * (f32 ? 4 : 2)};
     const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
-    return fn(reinterpret_cast<CUtensorMap *>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base),
+    return fn(reinterpret_cast<CUtensorMap *>(map), f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base),
               dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_bf16_2d(void *map, const void *base, unsigned long long rows, int cols, int box_cols, int box_rows)
+{
+    return encode_2d(map, base, rows, cols, box_cols, box_rows, false);
+}
+bool encode_f32_2d(void *map, const void *base, unsigned long long rows, int cols, int box_cols, int box_rows)
+{
+    return encode_2d(map, base, rows, cols, box_cols, box_rows, true);
 }
 
 bool encode_bf16_heads(void *map, const void *base, unsigned long long rows, int heads, int d, int box_heads, int box_rows)

@@ -206,7 +206,9 @@ int device_sm_count();
 bool encode_bf16_2d(void *map /* CUtensorMap */, const void *base, unsigned long long rows, int cols,
                     int box_cols, int box_rows);
 
-// The same over [rows][heads][d] with boxes of box_rows x box_heads x 64 elements.
+// The same over a float32 matrix (box_cols * 4 <= 128).
+bool encode_f32_2d(void *map, const void *base, unsigned long long rows, int cols, int box_cols, int box_rows);
+// A bf16 map over [rows][heads][d] with boxes of box_rows x box_heads x 64 elements.
 bool encode_bf16_heads(void *map, const void *base, unsigned long long rows, int heads, int d, int box_heads, int box_rows);
 
 }  // namespace reco

@@ -17,6 +17,7 @@
 
 #include "decode_block.cuh"
 #include "prefix.cuh"
+#include "tc.cuh"
 
 namespace reco {
 
@@ -166,88 +167,104 @@ __global__ void __launch_bounds__(kPrefixBlock) prefix_plan(const __grid_constan
 }
 
 // ---------------------------------------------------------------- attention, float32
-// Eight warps.  A warp takes 8 of the tile's query rows and, where the tile has fewer than 64, a share of the keys of
-// each tile (WR row groups, 8 / WR key groups).  QK^T: a half-warp has four rows, a lane of it WR keys; PV: a lane has D / 32
-// columns of all eight rows and takes the probabilities from shared memory.  Every sum is float32.
-constexpr int kPlainRows = 64;
+// Plain FMAs, every sum float32.  A copying warp and eight that compute; one of these takes RW of the tile's query rows (32 at
+// most) and, where the tile has fewer, a share of its 128 keys (WR row groups, 8 / WR key groups).  K and V tiles come by
+// TMA, a box per page and 32 columns, into a ring of three; swizzled, so that lanes that read the same columns of different
+// rows meet different banks.  A warp waits for a tile, and lets it go, for itself.
+// QK^T: a half-warp has RW / 2 rows, a lane of it KPL keys, so that six to ten 16-byte reads feed up to 64 FMAs; PV: a lane
+// has D / 32 columns of all rows, and takes the probabilities from shared memory.
+constexpr int kPlainRows = 32;
+constexpr long long kPlainPolls = 1LL << 19;  // of a wait, each suspended for up to two microseconds
+constexpr int kPlainWarps = 8, kPlainThreads = 32 * (kPlainWarps + 1);
 
-template <int D> constexpr int plain_smem() { return (kPlainRows * D + 2 * kPrefixTile * D + 8 * 8 * kPrefixTile) * 4 + 8 * 8 * 8; }
-
-// Float offset of 16-byte chunk c of row r: rows that lie a multiple of 8 chunks apart spread over the banks.
-template <int D> __device__ __forceinline__ int chunk_at(int r, int c) { return r * D + ((c ^ (r & 7)) << 2); }
+template <int D> struct PlainSmem {
+    float ring[3][kPrefixTile * D];       // [D / 32][128][32], swizzled
+    float q[kPlainRows * D];              // queries, then probabilities by warp; at a piece's end the warps' outputs as they
+    float p[D == 128 ? 32 * D : 64 * D];  // join: 8 warps of 8 rows
+    float2 ml[64];
+    uint64_t full[3], empty[3];
+    int bad[4];                           // a page that is none was met, by piece
+    int abort;
+};
+static_assert(sizeof(PlainSmem<128>) <= 227 * 1024, "shared memory of a CTA");
 
 __device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+// Float offset of 16-byte chunk c of row r of a tile, of the queries.
+__device__ __forceinline__ int tile_at(int r, int c) { return (c >> 3) * (kPrefixTile * 32) + r * 32 + (((c ^ r) & 7) << 2); }
+template <int D> __device__ __forceinline__ int query_at(int r, int c) { return r * D + ((c ^ (r & 7)) << 2); }
+__device__ __forceinline__ void bar_plain() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kPlainWarps) : "memory"); }
 
-template <int D, int WR>
-__device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPiece &pc, float *sm, int *sm_bad)
+template <int D, int WR, int RW>
+__device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPiece &pc, int piece, PlainSmem<D> &sm, int &slot, bool &ok)
 {
-    constexpr int WK = 8 / WR, E = D / 32, KEYS = kPrefixTile / WK;
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, half = lane >> 4, l16 = lane & 15;
-    float *Q = sm, *K = Q + kPlainRows * D, *V = K + kPrefixTile * D, *ps = V + kPrefixTile * D + wid * 8 * kPrefixTile;
-    float2 *ml = reinterpret_cast<float2 *>(V + kPrefixTile * D + 8 * 8 * kPrefixTile);
+    constexpr int WK = 8 / WR, E = D / 32, KEYS = kPrefixTile / WK;  // keys of a tile that a warp takes
+    constexpr int RPL = RW / 2, KPL = KEYS / 16;                     // rows and keys of a lane
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, kl = lane & 15, rl = lane >> 4;
     const int nrows = pc.nseq * a.G;
-    __syncthreads();
-    if (tid == 0) *sm_bad = 0;
-    for (int i = tid; i < 8 * WR * (D / 4); i += 256) {
+    float *ps = sm.p + wid * 8 * KEYS;  // [KEYS][8]
+    for (int i = tid; i < RW * WR * (D / 4); i += 32 * kPlainWarps) {
         const int r = i / (D / 4), c = i % (D / 4);
-        *reinterpret_cast<float4 *>(Q + r * D + 4 * c) =
+        *reinterpret_cast<float4 *>(sm.q + query_at<D>(r, c)) =
             r < nrows ? ld4((const float *)a.q + a.q_row(pc, r / a.G, r % a.G) * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    float o[8][E], m[4], l[4];
+    bar_plain();
+    float o[RW][E], m[RPL], l[RPL];
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
+    for (int r = 0; r < RW; ++r)
 #pragma unroll
         for (int e = 0; e < E; ++e) o[r][e] = 0.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RPL; ++r) {
         m[r] = -INFINITY;
         l[r] = 0.f;
     }
-    for (int t = pc.t0; t < pc.t1; ++t) {
-        const int k0 = pc.k0 + t * kPrefixTile, live = min(kPrefixTile, pc.end - k0), low = pc.lo - k0;
-        __syncthreads();  // the last tile has been read
-        for (int i = tid; i < kPrefixTile * (D / 4); i += 256) {
-            const int r = i / (D / 4), c = i % (D / 4);
-            float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-            if (r < live && r >= low) {
-                const long long row = a.pool_row(pc, k0 + r);
-                if (row >= 0) {
-                    k = ld4((const float *)a.K + row * D + 4 * c);
-                    v = ld4((const float *)a.V + row * D + 4 * c);
-                } else {
-                    *sm_bad = 1;
+    auto landed = [&]() {
+        const uint32_t bar = smem_addr(&sm.full[slot % 3]);
+        if (!mbar_try_wait(bar, slot / 3 & 1)) ok &= thread_wait(bar, slot / 3 & 1, &sm.abort, a.err, kPlainPolls);
+        __syncwarp();
+    };
+    auto done = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sm.empty[slot % 3]));
+        ++slot;
+    };
+#pragma unroll 1
+    for (int t = pc.t0; t < pc.t1 && __all_sync(0xffffffffu, ok); ++t) {
+        const int k0 = pc.k0 + t * kPrefixTile, live = pc.end - k0, low = pc.lo - k0;  // rows of the tile that count: [low, live)
+        landed();
+        float s[RPL][KPL];
+#pragma unroll
+        for (int r = 0; r < RPL; ++r)
+#pragma unroll
+            for (int j = 0; j < KPL; ++j) s[r][j] = 0.f;
+        const int kb = kg * KEYS + kl;
+        {
+            const float *K = sm.ring[slot % 3] + kb * 32, *Q = sm.q + (rw * RW + rl * RPL) * D;
+            const int kx = kb & 7, qx = rw * RW + rl * RPL;
+#pragma unroll 1
+            for (int cc = 0; cc < D / 4; cc += 8, K += kPrefixTile * 32)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    float4 qv[RPL];
+#pragma unroll
+                    for (int r = 0; r < RPL; ++r) qv[r] = ld4(Q + r * D + (((cc + c) ^ ((qx + r) & 7)) << 2));
+#pragma unroll
+                    for (int j = 0; j < KPL; ++j) {
+                        const float4 kv = ld4(K + 16 * j * 32 + ((c ^ kx) << 2));
+#pragma unroll
+                        for (int r = 0; r < RPL; ++r)
+                            s[r][j] = fmaf(qv[r].w, kv.w, fmaf(qv[r].z, kv.z, fmaf(qv[r].y, kv.y, fmaf(qv[r].x, kv.x, s[r][j]))));
+                    }
                 }
-            }
-            *reinterpret_cast<float4 *>(K + chunk_at<D>(r, c)) = k;
-            *reinterpret_cast<float4 *>(V + chunk_at<D>(r, c)) = v;
         }
-        __syncthreads();
-        float s[4][WR];
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < WR; ++j) s[r][j] = 0.f;
-        const int kb = kg * KEYS + l16;
-#pragma unroll 4
-        for (int c = 0; c < D / 4; ++c) {
-            float4 qv[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) qv[r] = ld4(Q + (rw * 8 + half * 4 + r) * D + 4 * c);
-#pragma unroll
-            for (int j = 0; j < WR; ++j) {
-                const float4 kv = ld4(K + chunk_at<D>(kb + 16 * j, c));
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    s[r][j] = fmaf(qv[r].w, kv.w, fmaf(qv[r].z, kv.z, fmaf(qv[r].y, kv.y, fmaf(qv[r].x, kv.x, s[r][j]))));
-            }
-        }
-        float al[4];
+        done();
+        float al[RPL];
         bool any = false;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < RPL; ++r) {
             float mb = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < WR; ++j) {
+            for (int j = 0; j < KPL; ++j) {
                 s[r][j] = kb + 16 * j < live && kb + 16 * j >= low ? s[r][j] * a.c2 : -INFINITY;
                 mb = fmaxf(mb, s[r][j]);
             }
@@ -261,33 +278,39 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
             any |= grow;
             const float base = mn == -INFINITY ? 0.f : mn;
 #pragma unroll
-            for (int j = 0; j < WR; ++j) {
+            for (int j = 0; j < KPL; ++j) {
                 s[r][j] = fast_exp2(s[r][j] - base);
                 l[r] += s[r][j];
             }
         }
 #pragma unroll
-        for (int j = 0; j < WR; ++j)
-            *reinterpret_cast<float4 *>(ps + (l16 + 16 * j) * 8 + 4 * half) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+        for (int j = 0; j < KPL; ++j)
+            *reinterpret_cast<float4 *>(ps + (kl + 16 * j) * 8 + rl * 4) =
+                make_float4(s[0][j], s[1][j], s[2][j], RPL == 4 ? s[RPL - 1][j] : 0.f);
         if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float f = __shfl_sync(0xffffffffu, al[r & 3], (r >> 2) * 16);
+            for (int r = 0; r < RW; ++r) {
+                const float f = __shfl_sync(0xffffffffu, al[r % RPL], (r / RPL) * 16);
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[r][e] *= f;
             }
         }
         __syncwarp();
-// a tile's products are summed before they join the output: the chain of additions into it is as long as the tiles
-        float acc[8][E];
+        landed();
+        // a tile's products are summed before they join the output: the chain of additions into it is as long as the tiles
+        float acc[RW][E];
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int r = 0; r < RW; ++r)
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[r][e] = 0.f;
+        const float *V = sm.ring[slot % 3] + (D == 128 ? (lane >> 3) * (kPrefixTile * 32) : (lane >> 4) * (kPrefixTile * 32));
+        const int vc = D == 128 ? lane & 7 : (lane & 15) >> 1, vo = D == 128 ? 0 : 2 * (lane & 1);
+        // (rows that do not count are not touched: whatever they hold, NaN times a probability of zero is not zero)
+        const int ka = max(0, low - kg * KEYS), ke = min(KEYS, live - kg * KEYS);
 #pragma unroll 4
-        for (int k = 0; k < KEYS; ++k) {
+        for (int k = ka; k < ke; ++k) {
             float v[E];
-            const float *vr = V + chunk_at<D>(kg * KEYS + k, lane * E / 4) + (lane * E & 3);
+            const float *vr = V + (kg * KEYS + k) * 32 + (((vc ^ k) & 7) << 2) + vo;
             if constexpr (E == 4) {
                 const float4 f = ld4(vr);
                 v[0] = f.x;
@@ -302,43 +325,44 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
             const float4 p0 = ld4(ps + 8 * k), p1 = ld4(ps + 8 * k + 4);
             const float p[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(p[r], v[e], acc[r][e]);
+                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(p[r / RPL * 4 + r % RPL], v[e], acc[r][e]);
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int r = 0; r < RW; ++r)
 #pragma unroll
             for (int e = 0; e < E; ++e) o[r][e] += acc[r][e];
+        done();
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RPL; ++r)
 #pragma unroll
         for (int x = 1; x < 16; x <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], x);
-    // the key groups join through shared memory (the tile's place)
-    __syncthreads();
-    float *os = K + wid * 8 * D;
+    // the key groups join through shared memory
+    bar_plain();  // queries and probabilities have been read
+    float *os = sm.q + wid * RW * D;
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
+    for (int r = 0; r < RW; ++r)
 #pragma unroll
         for (int e = 0; e < E; ++e) os[r * D + lane * E + e] = o[r][e];
-    if (l16 == 0)
+    if (kl == 0)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) ml[wid * 8 + half * 4 + r] = make_float2(m[r], l[r]);
-    __syncthreads();
-    const bool bad = *sm_bad != 0;
-    for (int i = tid; i < nrows * (D / 4); i += 256) {
-        const int r = i / (D / 4), c = i % (D / 4), w0 = r >> 3;
+        for (int r = 0; r < RPL; ++r) sm.ml[wid * RW + rl * RPL + r] = make_float2(m[r], l[r]);
+    bar_plain();
+    const bool bad = *(volatile int *)&sm.bad[piece & 3] != 0;
+    for (int i = tid; i < nrows * (D / 4); i += 32 * kPlainWarps) {
+        const int r = i / (D / 4), c = i % (D / 4), w0 = r / RW, rr = r - w0 * RW;
         float M = -INFINITY, L = 0.f;
 #pragma unroll
-        for (int x = 0; x < WK; ++x) M = fmaxf(M, ml[(w0 + x * WR) * 8 + (r & 7)].x);
+        for (int x = 0; x < WK; ++x) M = fmaxf(M, sm.ml[(w0 + x * WR) * RW + rr].x);
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int x = 0; x < WK; ++x) {
             const int w = w0 + x * WR;
-            const float2 y = ml[w * 8 + (r & 7)];
+            const float2 y = sm.ml[w * RW + rr];
             const float f = part_factor(y.x, M);
-            const float4 v = ld4(K + (w * 8 + (r & 7)) * D + 4 * c);
+            const float4 v = ld4(sm.q + (w * RW + rr) * D + 4 * c);
             L += y.y * f;
             acc.x += v.x * f;
             acc.y += v.y * f;
@@ -351,28 +375,86 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         *reinterpret_cast<float4 *>(po + 4 * c) = acc;
         if (c == 0) *pm = make_float2(M, bad ? -1.f : L);
     }
-    if (bad && tid == 0) raise_error(a.err, ERR_PAGE);
+    bar_plain();
 }
 
-template <int D> __global__ void __launch_bounds__(256, 1) prefix_plain(const __grid_constant__ PrefixArgs a)
+template <int D>
+__global__ void __launch_bounds__(kPlainThreads, 1)
+    prefix_plain(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PrefixArgs a)
 {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
-    __shared__ int sm_bad;
-    float *sm = reinterpret_cast<float *>(smem_raw);
+    PlainSmem<D> &sm = *reinterpret_cast<PlainSmem<D> *>(smem_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (smem_addr(smem_raw) & 1023u) {  // swizzled tiles need it
+        if (threadIdx.x == 0) raise_error(a.err, ERR_INTERNAL);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(smem_addr(&sm.full[i]), 1);
+            mbar_init(smem_addr(&sm.empty[i]), kPlainWarps);
+        }
+        for (int i = 0; i < 4; ++i) sm.bad[i] = 0;
+        sm.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_shared();
+    }
+    __syncthreads();
     wait_prior_grid();
-    release_next_grid();
+    release_next_grid();  // the join looks up its places meanwhile
     PrefixWalk w = a.range();
     PrefixPiece pc;
-    while (a.next(w, pc)) {
+    bool ok = true;
+    int slot = 0;
+    if (warp == kPlainWarps) {
+        // ---- copies.  Lane (box, part) of a tile copies 32 columns of the box's rows: a page, or half a page of 256
+        constexpr int PARTS = D / 32;
+        const int rows = min(kPrefixTile, 1 << a.shift), boxes = kPrefixTile / rows;
+        const int box = lane / PARTS, part = lane % PARTS;
+        for (int piece = 0; prefix_next(&a, &w, &pc); ++piece) {
+            // (at most three tiles ahead: a piece's place is that of the fourth before, which is done)
+            if (lane == 0) *(volatile int *)&sm.bad[piece & 3] = 0;
+            __syncwarp();
+            for (int t = pc.t0; t < pc.t1; ++t) {
+                const int k = pc.k0 + t * kPrefixTile + box * rows;
+                const bool needed = box < boxes && k < pc.end;
+                const long long row = needed ? a.pool_row(pc, k) : -1;
+                const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+                if (__any_sync(0xffffffffu, needed && row < 0) && lane == 0) {
+                    *(volatile int *)&sm.bad[piece & 3] = 1;
+                    raise_error(a.err, ERR_PAGE);
+                }
+                for (int kv = 0; kv < 2; ++kv, ++slot) {
+                    const uint32_t empty = smem_addr(&sm.empty[slot % 3]), full = smem_addr(&sm.full[slot % 3]);
+                    if (!mbar_try_wait(empty, (slot / 3 + 1) & 1)) ok &= thread_wait(empty, (slot / 3 + 1) & 1, &sm.abort, a.err, kPlainPolls);
+                    if (!__all_sync(0xffffffffu, ok)) break;
+                    if (lane == 0) mbar_expect_tx(full, (uint32_t)(n * rows * 128));
+                    __syncwarp();
+                    if (row >= 0)
+                        tma_load_2d(smem_addr(sm.ring[slot % 3]) + part * (kPrefixTile * 128) + box * rows * 128, kv ? &tmV : &tmK, 32 * part,
+                                    (int)row, full);
+                    __syncwarp();
+                }
+                if (!__all_sync(0xffffffffu, ok)) break;
+            }
+            if (!__all_sync(0xffffffffu, ok)) break;
+        }
+        // no copy is left in flight when the CTA ends
+        for (int j = max(0, slot - 3); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % 3]), j / 3 & 1, kPlainPolls);
+        return;
+    }
+    for (int piece = 0; prefix_next(&a, &w, &pc); ++piece) {
         const int nrows = pc.nseq * a.G;
         if (nrows <= 8)
-            plain_piece<D, 1>(a, pc, sm, &sm_bad);
+            plain_piece<D, 1, 8>(a, pc, piece, sm, slot, ok);
         else if (nrows <= 16)
-            plain_piece<D, 2>(a, pc, sm, &sm_bad);
-        else if (nrows <= 32)
-            plain_piece<D, 4>(a, pc, sm, &sm_bad);
+            plain_piece<D, 2, 8>(a, pc, piece, sm, slot, ok);
+        else if (nrows <= 24)
+            plain_piece<D, 4, 6>(a, pc, piece, sm, slot, ok);
         else
-            plain_piece<D, 8>(a, pc, sm, &sm_bad);
+            plain_piece<D, 4, 8>(a, pc, piece, sm, slot, ok);
     }
 }
 
@@ -592,10 +674,14 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     a.err = err;
     const int grid = std::min(device_sm_count(), kPagedMaxGrid);
     if (f32) {
-        void (*fn)(PrefixArgs) = kv.d == 64 ? prefix_plain<64> : prefix_plain<128>;
-        const int smem = kv.d == 64 ? plain_smem<64>() : plain_smem<128>();
+        CUtensorMap mk = {}, mv = {};
+        const unsigned long long pool = (unsigned long long)kv.n_layers * kv.n_pages * kv.H_kv * kv.page;
+        const int box = std::min(kPrefixTile, kv.page);
+        if (!encode_f32_2d(&mk, kv.k, pool, kv.d, 32, box) || !encode_f32_2d(&mv, kv.v, pool, kv.d, 32, box)) return cudaErrorInvalidValue;
+        void (*fn)(CUtensorMap, CUtensorMap, PrefixArgs) = kv.d == 64 ? prefix_plain<64> : prefix_plain<128>;
+        const int smem = kv.d == 64 ? (int)sizeof(PlainSmem<64>) : (int)sizeof(PlainSmem<128>);
         if ((e = allow_smem((const void *)fn, smem)) != cudaSuccess) return e;
-        if ((e = launch_pdl(fn, dim3(grid), dim3(256), smem, s, a)) != cudaSuccess) return e;
+        if ((e = launch_pdl(fn, dim3(grid), dim3(kPlainThreads), smem, s, mk, mv, a)) != cudaSuccess) return e;
     } else {
         if ((e = launch_prefix_tc(kv, a, grid, out_dtype, s)) != cudaSuccess) return e;
     }

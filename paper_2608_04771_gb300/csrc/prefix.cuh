@@ -187,6 +187,9 @@ struct PrefixArgs {
     }
 };
 
+// PrefixArgs::next as a function of its own: the kernels look for a piece in several places.
+__device__ __noinline__ static bool prefix_next(const PrefixArgs *a, PrefixWalk *w, PrefixPiece *pc) { return a->next(*w, *pc); }
+
 // The attention of all pieces over bf16 caches (prefix_tc.cu).
 cudaError_t launch_prefix_tc(const reco_paged_kv &kv, const PrefixArgs &a, int grid, reco_dtype out_dtype, cudaStream_t s);
 #endif
