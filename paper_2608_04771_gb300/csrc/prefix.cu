@@ -60,7 +60,8 @@ __device__ void plan_groups(const PlanArgs &a)
 {
     __shared__ long long sm[kPrefixBlock / 32], sm_work;
     __shared__ int sm_start, sm_runs;
-    bool several = false;  // row tiles
+    __shared__ int sm_most;
+    if (threadIdx.x == 0) sm_most = a.rows.own();
     if (threadIdx.x == 0) {
         sm_work = 0;
         sm_start = -1;
@@ -81,7 +82,7 @@ __device__ void plan_groups(const PlanArgs &a)
         const int run = c_runs + scan_block<false>(first && kept ? 1 : 0, reinterpret_cast<int *>(sm)) - 1;
         const long long mine = last && kept ? a.rows.work(b - start + 1, p) : 0;
         const long long work = c_work + scan_block<false>(mine, sm);
-        several |= last && kept && b - start + 1 > a.rows.per;
+        if (last && kept) atomicMax(&sm_most, a.rows.unit(b - start + 1, 0));
         if (last && kept) a.ws.runs[run] = PrefixRun{start, b - start + 1, p, 0, work - mine};
         if (in) {
             const bool wrong = !valid || __ldg(a.shared + b) != p;
@@ -95,8 +96,8 @@ __device__ void plan_groups(const PlanArgs &a)
             sm_work = work;
         }
     }
-    several = __syncthreads_or(several);
-    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs, several ? a.rows.unit(a.rows.per + 1, 0) : kOwnUnit};
+    __syncthreads();
+    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs, sm_most};
     if (off) raise_error(a.err, ERR_LEN);
 }
 
@@ -128,7 +129,7 @@ __device__ void plan_units(const PlanArgs &a, int block)
             x.n = L + append;
             x.lo = company ? p : 0;
             x.k0 = x.lo & -min(kPrefixTile, 1 << a.shift);  // the tensor cores' kernel copies whole boxes
-            work = x.n > x.lo ? kOwnUnit * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
+            work = x.n > x.lo ? a.rows.own() * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
         }
     }
     const int before = scan_block<false>(work, sm) - work;
@@ -497,7 +498,7 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
         if (x.n > x.lo) {
             long long w0 = pre + x.work + kOwnExtra;
             for (int i = 0; i < u / kPrefixBlock; ++i) w0 += __ldg(a.p.block_work + i);
-            n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, kOwnUnit, own_c);
+            n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, a.p.rows.own(), own_c);
         }
         if (run >= 0) {
             const PrefixRun rn = a.p.runs[run];
@@ -618,7 +619,7 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
 {
     const bool f32 = kv.dtype == RECO_F32;
     const int units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv, blocks = (units + kPrefixBlock - 1) / kPrefixBlock;
-    const PrefixRows rows = f32 ? PrefixRows{kPlainRows / G, kPlainRows / G} : PrefixRows{2 * (128 / G), 128 / G};
+    const PrefixRows rows = f32 ? PrefixRows{kPlainRows / G, kPlainRows / G, G, 1} : PrefixRows{2 * (128 / G), 128 / G, G, 0};
     PlanArgs p = {};
     p.K = kv.k;
     p.V = kv.v;

@@ -7,15 +7,22 @@
 namespace reco {
 
 // A row tile takes the query heads of up to `per` sequences of a group, of which `half` make what the tensor cores take
-// at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy: a key tile takes
-// 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has several
-// row tiles, which find the keys in L2, 9 for a whole one (1.9 us) and 6 for the last one if it has no more than `half`
-// sequences (1.2 us).  The start and the end of a unit's own rows take kOwnExtra more.
-constexpr int kOwnUnit = 8, kOwnExtra = 11;
+// at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy.  bf16: a key tile
+// takes 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has
+// several row tiles, which find the keys in L2, 9 for a whole one (1.9 us) and 6 for the last one if it has no more than
+// `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows, 24 with 16, 33 with 24, 40 with 32.
+// The start and the end of a unit's own rows take kOwnExtra more.
+constexpr int kOwnExtra = 11;
 struct PrefixRows {
-    int per, half;
-    // a key tile's of row tile rt of n sequences (all but the last row tile have the first one's)
-    __host__ __device__ int unit(int n, int rt) const { return n <= per ? 8 : (n - rt * per <= half && per > half ? 6 : 9); }
+    int per, half, G, f32;
+    __host__ __device__ int plain(int n) const { return n * G <= 8 ? 15 : (n * G <= 16 ? 24 : (n * G <= 24 ? 33 : 40)); }
+    // a key tile's of row tile rt of n sequences (all but the last row tile have the first one's), of a unit's own rows
+    __host__ __device__ int unit(int n, int rt) const
+    {
+        if (f32) return plain(n - rt * per < per ? n - rt * per : per);
+        return n <= per ? 8 : (n - rt * per <= half && per > half ? 6 : 9);
+    }
+    __host__ __device__ int own() const { return f32 ? plain(1) : 8; }
     // a group's of n sequences with p rows, per layer and KV head
     __host__ __device__ long long work(int n, int p) const
     {
@@ -152,10 +159,10 @@ struct PrefixArgs {
             pc.k0 = x.k0;
             pc.lo = x.lo;
             pc.end = x.n;
-            const int in = at - w.base - x.work, size = kt > 0 ? kOwnUnit * kt + kOwnExtra : 0;
+            const int in = at - w.base - x.work, unit = rows.own(), size = kt > 0 ? unit * kt + kOwnExtra : 0;
             const int e = (int)min((long long)size, in + (w.end - w.w));
-            pc.t0 = max(0, in - kOwnExtra + kOwnUnit - 1) / kOwnUnit;
-            pc.t1 = max(0, e - kOwnExtra + kOwnUnit - 1) / kOwnUnit;
+            pc.t0 = max(0, in - kOwnExtra + unit - 1) / unit;
+            pc.t1 = max(0, e - kOwnExtra + unit - 1) / unit;
             pc.own = true;
             if (e == size) {  // the next unit, maybe of the next block
                 ++w.u;
