@@ -34,7 +34,9 @@ struct AppendArgs {
     unsigned *err;
 };
 
-constexpr int kAppendWarps = 8;
+// Small CTAs, 40 warps of them on an SM (28 layers of 4096 tokens, 7B-class heads: 335 us; with eight warps a CTA 361; two or
+// three rows of a lane in flight take registers that cost warps: 368 and 371).
+constexpr int kAppendWarps = 4;
 
 // Upper 32 bits of pos * f / (2 pi) in turns, modulo one, as a signed fraction of 2^31 half turns.
 __device__ __forceinline__ unsigned long long turn_step(float f)
@@ -92,7 +94,7 @@ __device__ __forceinline__ int sequence_of(const int32_t *starts, int B, int t, 
 }
 
 template <typename T, int D, bool PAIRS>
-__global__ void __launch_bounds__(32 * kAppendWarps) paged_append(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(32 * kAppendWarps, 10) paged_append(const __grid_constant__ AppendArgs a)
 {
     constexpr int E = Chunk<T>::E, PL = D / (2 * E), HP = 32 / PL, A = E / HP;  // chunks of E elements; PL lanes a row
     constexpr int ROW = D * (int)sizeof(T);
