@@ -488,8 +488,10 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                 auto store = [&](int c, const float (&o)[32]) {
                     if (po != nullptr)
 #pragma unroll
-                        for (int y = 0; y < 32; y += 4)
-                            *reinterpret_cast<float4 *>(po + c + y) = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+                        for (int y = 0; y < 32; y += 8)  // whole sectors
+                            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(po + c + y), "f"(o[y]), "f"(o[y + 1]),
+                                         "f"(o[y + 2]), "f"(o[y + 3]), "f"(o[y + 4]), "f"(o[y + 5]), "f"(o[y + 6]), "f"(o[y + 7])
+                                         : "memory");
                 };
                 if (pair) {
 #pragma unroll 1
