@@ -8,10 +8,10 @@
 //
 // One CTA per SM, persistent over its share of the key tiles (PrefixArgs::next), of warps
 //   0      finds the pieces, a few ahead of the others, and copies, all by TMA: queries (a box of a group's sequences, or
-//          one sequence's, into one of two tiles), K and V (a box per page and 64 columns, a lane each, into a ring of tiles);
+//          one sequence's, into one of two places) and K tiles (a box per page and 64 columns, a lane each, into a ring);
+//   2      copies V tiles the same way, into a ring of their own (a copy takes some 75 cycles to issue: pages of 16 rows are
+//          32 copies a tile, as long as a tile's bytes take);
 //   1, 3   issue the products of a stream each;
-//   2      clears V rows that no query sees in tiles that a border crosses (their probabilities are zero, but NaN
-//          times zero is not);
 //   4..11  two softmax groups of four warps, one per stream, a query row per thread.
 // The two streams: a row tile of more than 128 rows has a half in each, otherwise each takes half of the keys of every tile
 // and they join at the end of the piece.  A stream goes by blocks of 64 keys, two of which have a place for their S in
@@ -19,14 +19,19 @@
 // product takes from there; O stays in TMEM, and is rescaled only when a row's probabilities against
 // the maximum so far sum to more than 2^12 in a block.
 //
-// What the steps cost (cycles a block of 64 keys, 64 sequences of 5 heads over 100001 rows): see launch_prefix_tc.
+// Measured, GB300, the whole call with its plan and its join.  28 layers, 8 sequences of 28 query and 4 key heads of 128 over
+// 16001 shared rows and 1000 to 4000 of their own (1.9 GB of K and V): 293 us, 0.96 of the copy rate.  64 sequences of 40 and
+// 8 heads over 100001 shared rows: 171 us, where the bytes once and the products are 67 us each; two row tiles read every K
+// and V tile, one of 250 rows in 1.9 us of a CTA (its products alone would take 1.3) and one of 70 in 1.2.  One layer, 16
+// sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 27 us, a chain of launches and
+// look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V rows: 301, 169 and 28.4 us.
 //
 // P enters its product in bf16: with float32 output in two parts (2^-17 of each probability is lost), with bf16
 // output in one (2^-8 of each, on average over the rows the size of the output's own rounding).  Sums take the
 // probabilities as they were before.
 //
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
-// to come when phase k + 1 is.  So every slot is waited for by both threads, every time; what a group waits for
+// to come when phase k + 1 is.  So every place is waited for by both issuing warps, every time; what a group waits for
 // only now and then (pv_done) has a barrier for even and for odd blocks, which it cannot fall behind.
 // Every wait is bounded; one that runs out raises the error word and the CTA's abort flag, which ends the others.
 #include <algorithm>
@@ -86,11 +91,11 @@ template <int D> struct PrefixTc {
     static constexpr int BOX = 128 * 128;  // 128 rows of 64 bf16
     static constexpr int TILE = HALVES * BOX;
     static constexpr int Q_BYTES = 2 * TILE;
-    static constexpr int NS = D == 128 ? 5 : 10;  // K and V tiles in the ring
+    static constexpr int NK = D == 128 ? 3 : 5, NV = D == 128 ? 2 : 5, NS = NK + NV;  // places for K tiles, then V tiles
     static constexpr int NP = 4;                  // pieces found ahead
     static constexpr int THREADS = 32 * 12;
     struct Small {  // behind the tiles
-        uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2], landed[2], cleared[2];
+        uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2];
         uint64_t o_free, met;
         uint64_t piece_full[NP], piece_empty[NP];
         float2 ml[2][128];
@@ -110,7 +115,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
               const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQ1, const __grid_constant__ PrefixArgs a)
 {
     using C = PrefixTc<D>;
-    constexpr int NS = C::NS, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
+    constexpr int NS = C::NS, NK = C::NK, NV = C::NV, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
     constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -137,8 +142,6 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                 mbar_init(smem_addr(&sm.p_full[s][b]), 4);
                 mbar_init(smem_addr(&sm.pv_done[s][b]), 1);
             }
-            mbar_init(smem_addr(&sm.landed[s]), 1);
-            mbar_init(smem_addr(&sm.cleared[s]), 1);
         }
         mbar_init(smem_addr(&sm.o_free), 8);
         mbar_init(smem_addr(&sm.met), 8);
@@ -167,16 +170,31 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
     };
     auto fine = [&]() { return __all_sync(0xffffffffu, ok) != 0; };
 
+    // A box takes 64 columns of a page, or of half a page of 256: lane (box, half) of a tile looks its row up and copies it.
+    const int box_rows = min(128, 1 << a.shift), box = lane / HALVES, half = lane % HALVES;
+    auto box_needed = [&](const PrefixPiece &x, int t) {
+        return box < 128 / box_rows && x.k0 + t * kPrefixTile + box * box_rows < x.end;
+    };
+    auto box_row = [&](const PrefixPiece &x, int t) {
+        return box_needed(x, t) ? (int)a.pool_row(x, x.k0 + t * kPrefixTile + box * box_rows) : -1;
+    };
+    auto copy_tile = [&](int i, int phase, int row, const CUtensorMap *map) {  // into place i, for its phase
+        const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        await(smem_addr(&sm.empty[i]), phase + 1);
+        if (!fine()) return;
+        const uint32_t bar = smem_addr(&sm.full[i]);
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)(n * box_rows * 128));
+        __syncwarp();
+        if (row >= 0) tma_load_2d(ring + i * TILE + half * BOX + box * box_rows * 128, map, 64 * half, row, bar);
+        __syncwarp();
+    };
     // registers of the launch, 168 a thread: 88 for warps 0 to 3, 208 for the softmax, which holds a row of a block
     static_assert(128 * 88 + 256 * 208 <= C::THREADS * 168, "no more than the launch has");
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         PrefixWalk w = a.range();
         PrefixPiece pc;
-        // ---- pieces and copies.  Lane (box, half) of a tile copies 64 columns of the box's rows: a page, or half a page
-        // of 256
-        const int rows = min(128, 1 << a.shift), boxes = 128 / rows;
-        const int box = lane / HALVES, half = lane % HALVES;
+        // ---- pieces, queries, K tiles
         int slot = 0, nq = 0;
         for (int np = 0; fine(); ++np) {
             const bool more = a.next(w, pc);
@@ -189,9 +207,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             }
             __syncwarp();
             if (!more) break;
-            auto needed = [&](int t) { return box < boxes && pc.k0 + t * kPrefixTile + box * rows < pc.end; };
-            auto row_of = [&](int t) { return needed(t) ? a.pool_row(pc, pc.k0 + t * kPrefixTile + box * rows) : -1ll; };
-            long long row = row_of(pc.t0);
+            int row = box_row(pc, pc.t0);
             for (int s = 0; s < (pc.nseq > a.rows.half ? 2 : 1); ++s, ++nq) {
                 const int i = nq & 1;
                 await(smem_addr(&sm.q_empty[i]), (nq >> 1) + 1);
@@ -205,35 +221,23 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                 }
                 __syncwarp();
             }
-            for (int t = pc.t0; fine() && t < pc.t1; ++t) {
-                const int n = __popc(__ballot_sync(0xffffffffu, row >= 0));
-                if (__any_sync(0xffffffffu, needed(t) && row < 0) && lane == 0) {
+            for (int t = pc.t0; fine() && t < pc.t1; ++t, ++slot) {
+                if (__any_sync(0xffffffffu, box_needed(pc, t) && row < 0) && lane == 0) {
                     *(volatile int *)&sm.bad[np % NP] = 1;
                     raise_error(a.err, ERR_PAGE);
                 }
-                const long long next = t + 1 < pc.t1 ? row_of(t + 1) : -1ll;
-#pragma unroll 1
-                for (int kv = 0; kv < 2; ++kv, ++slot) {
-                    const int i = slot % NS;
-                    await(smem_addr(&sm.empty[i]), slot / NS + 1);
-                    if (!fine()) break;
-                    const uint32_t bar = smem_addr(&sm.full[i]);
-                    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(n * rows * 128));
-                    __syncwarp();
-                    if (row >= 0)
-                        tma_load_2d(ring + i * TILE + half * BOX + box * rows * 128, kv ? &tmV : &tmK, 64 * half, (int)row, bar);
-                    __syncwarp();
-                }
+                const int next = t + 1 < pc.t1 ? box_row(pc, t + 1) : -1;
+                copy_tile(slot % NK, slot / NK, row, &tmK);
                 row = next;
             }
         }
         // no copy is left in flight when the CTA ends
-        for (int j = max(0, slot - NS); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % NS]), (j / NS) & 1, kPolls);
+        for (int j = max(0, slot - NK); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % NK]), (j / NK) & 1, kPolls);
         for (int j = max(0, nq - 2); j < nq; ++j) mbar_wait_bounded(smem_addr(&sm.q_full[j & 1]), (j >> 1) & 1, kPolls);
     } else if (warp == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        // ---- V rows outside the rows that count, within the product's steps of 16
-        int slot = 1, nc = 0;
+        // ---- V tiles
+        int slot = 0;
         for (int np = 0; fine(); ++np) {
             await(smem_addr(&sm.piece_full[np % NP]), np / NP);
             if (!fine()) break;
@@ -241,24 +245,14 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
             if (x.t1 == x.t0) break;
-            for (int t = x.t0; t < x.t1; ++t, slot += 2) {
-                const int k0 = x.k0 + t * kPrefixTile, low = max(0, x.lo - k0), live = min(kPrefixTile, x.end - k0);
-                if (((low | live) & 15) == 0) continue;
-                await(smem_addr(&sm.landed[0]), nc);
-                await(smem_addr(&sm.landed[1]), nc++);
-                if (!fine()) break;
-                const uint32_t tile = ring + (slot % NS) * TILE;
-                auto clear = [&](int r0, int n) {
-                    for (int i = lane; i < n * 8 * HALVES; i += 32)
-                        sts_u4(tile + (i / (8 * n)) * BOX + (r0 + (i >> 3) % n) * 128 + (i & 7) * 16, make_uint4(0, 0, 0, 0));
-                };
-                if (low & 15) clear(low & ~15, low & 15);
-                if (live & 15) clear(live, 16 - (live & 15));
-                fence_async_shared();
-                __syncwarp();
-                if (lane < 2) mbar_arrive(smem_addr(&sm.cleared[lane]));
+            int row = box_row(x, x.t0);
+            for (int t = x.t0; fine() && t < x.t1; ++t, ++slot) {
+                const int next = t + 1 < x.t1 ? box_row(x, t + 1) : -1;
+                copy_tile(NK + slot % NV, slot / NV, row, &tmV);
+                row = next;
             }
         }
+        for (int j = max(0, slot - NV); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[NK + j % NV]), (j / NV) & 1, kPolls);
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // ---- products of stream s
@@ -270,12 +264,19 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
         const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
                        p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
-        // ring places of the next K and V tile, and the parity of their phase; query tiles, blocks, cleared tiles so far
-        int ki = 0, vi = 1, kp = 0, vp = 0, nq = 0, n = 0, nc = 0;
-        auto step = [&](int &i, int &p) {
-            i += 2;
-            p ^= i >= NS ? 1 : 0;
-            i -= i >= NS ? NS : 0;
+        // places of the next K and V tile, and the parity of their phase; query tiles, blocks so far
+        int ki = 0, vi = NK, kp = 0, vp = 0, nq = 0, n = 0;
+        auto step_k = [&]() {
+            if (++ki == NK) {
+                ki = 0;
+                kp ^= 1;
+            }
+        };
+        auto step_v = [&]() {
+            if (++vi == NS) {
+                vi = NK;
+                vp ^= 1;
+            }
         };
         for (int np = 0; fine(); ++np) {
             await(smem_addr(&sm.piece_full[np % NP]), np / NP);
@@ -290,20 +291,25 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
             for (int i = 0; i < (pair ? 2 : 1); ++i, ++nq) await(smem_addr(&sm.q_full[nq & 1]), nq >> 1);
             const uint64_t ad = qd + (uint64_t)((q & 1) * TILE >> 4);
             uint32_t more = 0;
-            // a border that is not at a step of 16 crosses the first or the last tile: V rows have to be cleared first
-            const int crossed0 = bl.lo & 15 ? 0 : -1, crossed1 = bl.hi & 15 ? (bl.hi - 1) >> 7 : -1;
 #pragma unroll 1
             for (int j = 0; j < bl.n + 2 && fine(); ++j) {
                 const int odd = j & 1;
                 if (j >= 2) {  // O += P V of block j - 2
                     const int c = bl.first + bl.step * (j - 2), nv = n + j - 2;
-                    if (!pair || !odd) {
-                        await(full0 + 8 * vi, vp);
-                        const int t = c >> 7;
-                        if (t == crossed0 || t == crossed1) {
-                            if (lane == 0) mbar_arrive(smem_addr(&sm.landed[s]));
-                            await(smem_addr(&sm.cleared[s]), nc++);
-                        }
+                    if (!pair || !odd) await(full0 + 8 * vi, vp);
+                    // rows that no query sees, within the product's steps of 16: zero, as their probabilities are (NaN times zero is
+                    // not).  (With a pair, both warps may do it: zeros over zeros.)
+                    const int r0 = c < bl.lo ? min(64, bl.lo - c) : 0, r1 = max(0, min(64, bl.hi - c));  // rows that count: [r0, r1)
+                    if (((r0 | r1) & 15) != 0) {
+                        const uint32_t rows = ring + vi * TILE + (c & 64) * 128;
+                        auto clear = [&](int r, int k) {
+                            for (int i = lane; i < k * 8 * HALVES; i += 32)
+                                sts_u4(rows + (i / (8 * k)) * BOX + (r + (i >> 3) % k) * 128 + (i & 7) * 16, make_uint4(0, 0, 0, 0));
+                        };
+                        if (r0 & 15) clear(r0 & ~15, r0 & 15);
+                        if (r1 & 15) clear(r1, 16 - (r1 & 15));
+                        fence_async_shared();
+                        __syncwarp();
                     }
                     await(p_full0 + 8 * (nv & 1), nv >> 1);
                     // (every piece waits for the outputs of the one before to have been read, for the barrier's phases)
@@ -311,7 +317,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                     tc_fence_after();
                     const uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
                     const uint32_t p = st + 64 * (nv & 1);
-                    const int k0 = max(0, bl.lo - c) >> 4, k1 = min(4, (bl.hi - c + 15) >> 4);  // rows that count, in steps of 16
+                    const int k0 = r0 >> 4, k1 = (r1 + 15) >> 4;
                     if (elect_one()) {
                         if (k0 == 0 && k1 == 4) {
 #pragma unroll
@@ -331,7 +337,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                     }
                     __syncwarp();
                     more |= k0 < k1 ? 1u : 0u;
-                    if (!pair || odd) step(vi, vp);
+                    if (!pair || odd) step_v();
                 }
                 if (j < bl.n) {  // S = Q K^T of block j
                     if (!pair || !odd) await(full0 + 8 * ki, kp);
@@ -352,7 +358,7 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                         }
                     }
                     __syncwarp();
-                    if (!pair || odd) step(ki, kp);
+                    if (!pair || odd) step_k();
                 }
             }
             n += bl.n;
