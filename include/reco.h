@@ -408,8 +408,11 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  * Also in error: a sequence whose shared[b] is negative or above the length of one of its units
  * (that unit), or differs from that of the group's first sequence (all units of the
  * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Precision as
- * reco_decode_attn's, but for bf16 output from bf16 caches, where the probabilities of
- * prefix rows enter their product with V as bf16 (2^-8 of each).                      */
+ * reco_decode_attn's, but from bf16 caches the probabilities enter their product with V as
+ * bf16: rounded once with bf16 output (each is off by 2^-8 of itself at most), in two parts with
+ * float32 output (2^-17).
+ * Refused also: float32 caches with more than 8 query heads per KV head and more than some
+ * 1.1e10 rows (n_layers * B * H_kv * max_pages * page).                               */
 reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,
                                    int32_t *lens, const int32_t *group, const int32_t *shared, float scale, void *out,
                                    reco_dtype out_dtype, float *lse, void *ws, size_t ws_bytes, cudaStream_t stream);
@@ -429,8 +432,9 @@ reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const
  *   positions lose nothing); the rest is float32, rounded once to the cache's type.
  *   k, v     : [n_layers][T][H_kv] rows, cache dtype
  *   q, q_out : [n_layers][T][H_q] rows, cache dtype, or both NULL.  q_out may be q itself (the
- *              same view); otherwise it overlaps no input
- *   T        : tokens that k, v, q and pos have room for, 0 <= T <= 2^30 (0: nothing to do)
+ *              same view); otherwise it overlaps no input, nor do its rows overlap
+ *   T        : tokens that k, v, q and pos have room for, 0 <= T <= 2^30 (0: nothing to do),
+ *              n_layers * T <= 2^36
  *   starts   : [B + 1] int32 (device), 0 <= starts[b] <= starts[b+1] <= T; tokens of no
  *              sequence (behind starts[B], say) are not read, nor their rows of q_out written
  *   pos      : [T] int32 (device), any values; may be NULL if rot == 0

@@ -106,6 +106,17 @@ reco_status check_paged(const reco_paged_kv *kv, bool need_ptrs = true)
     return RECO_OK;
 }
 
+// What the decodes refuse beyond check_paged; the one over shared prefixes counts the work of the units' own rows in 32 bits.
+reco_status check_paged_decode(const reco_paged_kv *kv, bool prefix)
+{
+    const int G = kv->H_q / kv->H_kv;
+    if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
+    if (prefix && reco::prefix_own_most(*kv) >= (1LL << 31))
+        return fail(RECO_EUNSUPPORTED, "%lld units of up to %lld rows are more than one call counts",
+                    (long long)kv->n_layers * kv->B * kv->H_kv, (long long)kv->max_pages * kv->page);
+    return RECO_OK;
+}
+
 reco_status check_ws(void *ws, size_t have, size_t need)
 {
     if (need == 0) return RECO_OK;
@@ -293,8 +304,7 @@ reco_status reco_paged_workspace_bytes(reco_op op, const reco_paged_kv *kv, size
     reco_status st = check_paged(kv, false);
     if (st != RECO_OK) return st;
     if (op == RECO_OP_PAGED_DECODE || op == RECO_OP_PAGED_WEIGHTS || op == RECO_OP_PAGED_PREFIX) {
-        const int G = kv->H_q / kv->H_kv;
-        if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
+        if ((st = check_paged_decode(kv, op == RECO_OP_PAGED_PREFIX)) != RECO_OK) return st;
         *bytes_out = op == RECO_OP_PAGED_PREFIX ? reco::prefix_ws_layout(*kv, nullptr).bytes
                                                 : reco::paged_decode_ws_layout(*kv, op == RECO_OP_PAGED_WEIGHTS, nullptr).bytes;
     } else if (op == RECO_OP_PAGED_EVICT)
@@ -502,8 +512,7 @@ reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const v
     if (out_dtype != RECO_F32 && out_dtype != RECO_BF16) return fail(RECO_EINVAL, "unknown out_dtype %d", (int)out_dtype);
     if (window < 0 || sinks < 0) return fail(RECO_EINVAL, "window %d and sinks %d must be >= 0", window, sinks);
     if (window == 0 && sinks > 0) return fail(RECO_EINVAL, "sinks without a window (window 0 sees every row)");
-    const int G = kv->H_q / kv->H_kv;
-    if (G > 16) return fail(RECO_EUNSUPPORTED, "G = %d query heads per KV head (at most 16)", G);
+    if ((st = check_paged_decode(kv, group || shared)) != RECO_OK) return st;
     if (!(scale == scale)) return fail(RECO_EINVAL, "scale is NaN");
     unsigned *err;
     cudaError_t e;
@@ -516,8 +525,7 @@ reco_status paged_decode_checked(const reco_paged_kv *kv, const void *q, const v
     reco::PagedDecodeWs lay = reco::paged_decode_ws_layout(*kv, weights != nullptr, ws);
     if ((st = check_ws(ws, ws_bytes, lay.bytes)) != RECO_OK) return st;
     if ((st = error_word(&err)) != RECO_OK) return st;
-    e = reco::launch_paged_decode(*kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse,
-                                              weights, lay, err, stream);
+    e = reco::launch_paged_decode(*kv, q, k_new, v_new, lens, scale, window, sinks, out, out_dtype, lse, weights, lay, err, stream);
     return e == cudaSuccess ? RECO_OK : cuda_fail(e, name);
 }
 }  // namespace
@@ -609,6 +617,8 @@ reco_status reco_paged_append(const reco_paged_kv *kv, const reco_rows *k, const
     reco_status st = check_paged(kv);
     if (st != RECO_OK) return st;
     if (T < 0 || T > (1 << 30)) return fail(RECO_EINVAL, "T = %d tokens outside [0, 2^30]", T);
+    // (the CTAs of a group of layers are counted in 32 bits)
+    if ((long long)T * kv->n_layers > (1LL << 36)) return fail(RECO_EUNSUPPORTED, "%d tokens in %d layers (at most 2^36)", T, kv->n_layers);
     if (!starts || !lens) return fail(RECO_EINVAL, "NULL starts or lens");
     if (((uintptr_t)starts | (uintptr_t)lens | (uintptr_t)pos | (uintptr_t)inv_freq) & 3u)
         return fail(RECO_EINVAL, "starts, pos, inv_freq and lens must be 4-byte aligned");

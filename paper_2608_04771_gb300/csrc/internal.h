@@ -135,6 +135,8 @@ SelectWs select_ws_layout(const reco_kv &kv, void *base);
 DecodeWs decode_ws_layout(const reco_kv &kv, void *base);
 PagedDecodeWs paged_decode_ws_layout(const reco_paged_kv &kv, bool weights, void *base);
 EvictWs evict_ws_layout(const reco_paged_kv &kv, void *base);
+// Units of work in the own rows of a cache that is full, at most.
+long long prefix_own_most(const reco_paged_kv &kv);
 PrefixWs prefix_ws_layout(const reco_paged_kv &kv, void *base);
 
 // Rows a unit of the paged cache may hold.

@@ -587,6 +587,18 @@ static int prefix_cont_rows(const reco_paged_kv &kv)
     return (int)std::min<long long>(kPrefixMaxRows, (long long)kv.B * (kv.H_q / kv.H_kv));
 }
 
+static PrefixRows prefix_rows(const reco_paged_kv &kv)
+{
+    const int G = kv.H_q / kv.H_kv;
+    return kv.dtype == RECO_F32 ? PrefixRows{kPlainRows / G, kPlainRows / G, G, 1} : PrefixRows{2 * (128 / G), 128 / G, G, 0};
+}
+
+long long prefix_own_most(const reco_paged_kv &kv)
+{
+    const long long tiles = ((long long)paged_cap(kv) + kPrefixTile - 1) / kPrefixTile + 1;  // (the first may begin before the own rows)
+    return (long long)kv.n_layers * kv.B * kv.H_kv * (tiles * prefix_rows(kv).own() + kOwnExtra);
+}
+
 PrefixWs prefix_ws_layout(const reco_paged_kv &kv, void *base)
 {
     size_t off = kPagedZeroBytes;
@@ -619,7 +631,7 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
 {
     const bool f32 = kv.dtype == RECO_F32;
     const int units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv, blocks = (units + kPrefixBlock - 1) / kPrefixBlock;
-    const PrefixRows rows = f32 ? PrefixRows{kPlainRows / G, kPlainRows / G, G, 1} : PrefixRows{2 * (128 / G), 128 / G, G, 0};
+    const PrefixRows rows = prefix_rows(kv);
     PlanArgs p = {};
     p.K = kv.k;
     p.V = kv.v;

@@ -87,6 +87,11 @@ def test_descriptors_that_are_refused(L, bad, status):
     assert _call(L, kv=_kv(**bad)) == status
 
 
+def test_more_tokens_than_a_call_counts_are_refused(L):
+    kv = _kv(n_layers=1000, B=3, H_q=2, H_kv=1)
+    assert _call(L, kv=kv, T=2 ** 30, k=(64, 0, 0, 0), v=(64, 0, 0, 0)) == reco.RECO_EUNSUPPORTED and b"2^36" in L.reco_last_error()
+
+
 def test_nothing_to_append_is_no_launch(L):
     """T = 0 returns before anything is launched (there is no GPU here), with views that point nowhere."""
     assert _call(L, T=0, k=(0, 0, 0, 0), v=(0, 0, 0, 0), pos=None, inv_freq=None) == reco.RECO_OK

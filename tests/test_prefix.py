@@ -85,6 +85,22 @@ def test_workspace_size(L):
         reco.reco_workspace_bytes(reco.RECO_OP_PAGED_PREFIX, reco.reco_kv(16, 32, 1, 1, 2, 1, 64, 64, 0))
 
 
+def test_more_rows_than_a_call_counts_are_refused(L):
+    """The work of the own rows is counted in 32 bits: 24 a tile of 128 float32 rows with more than eight heads, 15 with
+    fewer, 8 in bf16; the descriptor's own limit of 2^34 rows leaves room for all but the first."""
+    big = dict(n_layers=1, B=2 ** 10, H_kv=1, n_pages=1000, max_pages=2 ** 15, page=256)
+    for H_q, dtype, fine in ((9, reco.RECO_F32, False), (8, reco.RECO_F32, True), (16, reco.RECO_BF16, True)):
+        for shrink in (0, 1):
+            kv = _kv(H_q=H_q, dtype=dtype, **{**big, "B": big["B"] * 2 - 1 if not shrink else big["B"]})
+            size = ctypes.c_size_t()
+            st = L.reco_paged_workspace_bytes(reco.RECO_OP_PAGED_PREFIX, ctypes.byref(kv), ctypes.byref(size))
+            assert st == (reco.RECO_OK if fine or shrink else reco.RECO_EUNSUPPORTED), (H_q, dtype, shrink)
+    kv = _kv(H_q=9, dtype=reco.RECO_F32, **{**big, "B": 2047})
+    p = ctypes.c_void_p(256)
+    st = L.reco_paged_prefix_attn(ctypes.byref(kv), p, None, None, p, p, p, 0.1, p, reco.RECO_F32, None, p, 1 << 40, None)
+    assert st == reco.RECO_EUNSUPPORTED and b"more than one call counts" in L.reco_last_error()
+
+
 def test_binding_refuses_tensors_the_library_would_misread():
     K, table = torch.zeros(2, 5, 2, 16, 64), torch.zeros(3, 4, dtype=torch.int32)
     kv = reco.make_paged_kv(K, K.clone(), table, 4)
