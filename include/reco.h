@@ -409,8 +409,8 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  * (that unit), or differs from that of the group's first sequence (all units of the
  * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Precision as
  * reco_decode_attn's, but from bf16 caches the probabilities enter their product with V as
- * bf16: rounded once with bf16 output (each is off by 2^-8 of itself at most), in two parts with
- * float32 output (2^-17).
+ * bf16: rounded once with bf16 output (each is off by 2^-8 of itself at most), in three parts with
+ * float32 output (2^-26).
  * Refused also: float32 caches with more than 8 query heads per KV head and more than some
  * 1.1e10 rows (n_layers * B * H_kv * max_pages * page).                               */
 reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const void *k_new, const void *v_new,

@@ -26,9 +26,10 @@
 // sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 27 us, a chain of launches and
 // look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V rows: 301, 169 and 28.4 us.
 //
-// P enters its product in bf16: with float32 output in two parts (2^-17 of each probability is lost), with bf16
-// output in one (2^-8 of each, on average over the rows the size of the output's own rounding).  Sums take the
-// probabilities as they were before.
+// P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
+// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Of these the second lies
+// beside the first, TMEM has no room for the third: it comes from shared memory, where the ring is a tile or two shorter.
+// Sums take the probabilities as they were before.
 //
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
 // to come when phase k + 1 is.  So every place is waited for by both issuing warps, every time; what a group waits for
@@ -69,6 +70,17 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
+// (a, b) in three parts of bf16: two and what is left of both, which the third holds but for 2^-26.
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint32_t &lo, float &ra, float &rb)
+{
+    hi = pack_bf16(a, b);
+    ra = a - __uint_as_float(hi << 16);
+    rb = b - __uint_as_float(hi & 0xffff0000u);
+    lo = pack_bf16(ra, rb);
+    ra -= __uint_as_float(lo << 16);
+    rb -= __uint_as_float(lo & 0xffff0000u);
+}
+
 constexpr long long kPolls = 1LL << 19;  // of a wait, each suspended for up to two microseconds
 
 // The blocks of 64 keys of a piece that fall to stream s: block j begins `first` + `step` j columns from the start of the
@@ -86,12 +98,13 @@ struct PrefixBlocks {
     }
 };
 
-template <int D> struct PrefixTc {
+template <int D, int PARTS> struct PrefixTc {
     static constexpr int HALVES = D / 64;
     static constexpr int BOX = 128 * 128;  // 128 rows of 64 bf16
     static constexpr int TILE = HALVES * BOX;
     static constexpr int Q_BYTES = 2 * TILE;
-    static constexpr int NK = D == 128 ? 3 : 5, NV = D == 128 ? 2 : 5, NS = NK + NV;  // places for K tiles, then V tiles
+    static constexpr int REST = PARTS == 3 ? 2 * BOX : 0;  // the probabilities' third parts, by stream
+    static constexpr int TILES = 5 * 128 / D - REST / TILE, NK = (TILES + 1) / 2, NV = TILES - NK, NS = TILES;  // places for K tiles, then V tiles
     static constexpr int NP = 4;                  // pieces found ahead
     static constexpr int THREADS = 32 * 12;
     struct Small {  // behind the tiles
@@ -105,22 +118,22 @@ template <int D> struct PrefixTc {
         int abort;
     };
     // (all of it dynamic: the tiles begin where the CTA's shared memory does, at a multiple of 1024)
-    static constexpr int SMEM = Q_BYTES + NS * TILE + (int)sizeof(Small);
+    static constexpr int SMEM = Q_BYTES + REST + NS * TILE + (int)sizeof(Small);
     static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
 };
 
 template <int D, int PARTS>
-__global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
+__global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
     prefix_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQ1, const __grid_constant__ PrefixArgs a)
 {
-    using C = PrefixTc<D>;
+    using C = PrefixTc<D, PARTS>;
     constexpr int NS = C::NS, NK = C::NK, NV = C::NV, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
     constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = smem_addr(smem_raw), Qs = base, ring = base + C::Q_BYTES;
-    typename C::Small &sm = *reinterpret_cast<typename C::Small *>(smem_raw + C::Q_BYTES + NS * TILE);
+    const uint32_t base = smem_addr(smem_raw), Qs = base, rest = base + C::Q_BYTES, ring = rest + C::REST;
+    typename C::Small &sm = *reinterpret_cast<typename C::Small *>(smem_raw + C::Q_BYTES + C::REST + NS * TILE);
     if (base & 1023u) {  // swizzled tiles need it
         if (tid == 0) raise_error(a.err, ERR_INTERNAL);
         return;
@@ -260,7 +273,8 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
         const int s = warp >> 1;
         // (the whole warp goes through the loops, so that what it computes is known to be uniform: operands of the products
         // come from uniform registers, and one thread alone issued a product every 70 to 125 cycles)
-        const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX);
+        const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX),
+                       rd = sw128_desc(rest + s * BOX);
         const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
         const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
                        p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
@@ -323,13 +337,19 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > 0 ? 1u : more);
-                                if (PARTS == 2) tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                if (PARTS == 3) {
+                                    tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma(o, rd + (uint32_t)(k * 32 >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                }
                             }
                         } else {
 #pragma unroll 1
                             for (int k = k0; k < k1; ++k) {
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > k0 ? 1u : more);
-                                if (PARTS == 2) tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                if (PARTS == 3) {
+                                    tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma(o, rd + (uint32_t)(k * 32 >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                }
                             }
                         }
                         tc_commit(pv_done0 + 8 * (nv & 1));
@@ -404,7 +424,13 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                     }
                     // Probabilities against the maximum so far.  No maximum of the block is looked for while their sum stays below
                     // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).
-                    uint32_t hi[32], lo[PARTS == 2 ? 32 : 1];
+                    uint32_t hi[32], lo[PARTS == 3 ? 32 : 1];
+                    uint32_t third[4];
+                    const uint32_t row = rest + s * BOX + r * 128;
+                    if (PARTS == 3 && n > 0) {  // the product before has read its third parts
+                        await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
+                        __syncwarp();
+                    }
                     float sum;
                     bool again = false;
                     for (;;) {
@@ -418,10 +444,14 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                             p0 = fast_exp2(p0);
                             p1 = fast_exp2(p1);
                             s4[y & 3] = add_pair(s4[y & 3], pair_of(p0, p1));
-                            if (PARTS == 2)
-                                split_bf16(p0, p1, hi[y], lo[y]);
-                            else
+                            if (PARTS == 3) {
+                                float r0, r1;
+                                split_bf16(p0, p1, hi[y], lo[y], r0, r1);
+                                third[y & 3] = pack_bf16(r0, r1);
+                                if ((y & 3) == 3) sts_u4(row + ((y >> 2 ^ (r & 7)) << 4), make_uint4(third[0], third[1], third[2], third[3]));
+                            } else {
                                 hi[y] = pack_bf16(p0, p1);
+                            }
                         }
                         float s0, s1;
                         unpair(add_pair(add_pair(s4[0], s4[1]), add_pair(s4[2], s4[3])), s0, s1);
@@ -454,9 +484,10 @@ __global__ void __launch_bounds__(PrefixTc<D>::THREADS, 1)
                     l += sum;
                     tmem_st16(sa, hi);
                     tmem_st16(sa + 16, hi + 16);
-                    if (PARTS == 2) {
+                    if (PARTS == 3) {
                         tmem_st16(sa + 32, lo);
                         tmem_st16(sa + 48, lo + 16);
+                        fence_async_shared();
                     }
                     tmem_st_wait();
                 }
@@ -555,11 +586,11 @@ cudaError_t launch_prefix_tc(const reco_paged_kv &kv, const PrefixArgs &a, int g
         return cudaErrorInvalidValue;
     typedef void (*Kernel)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, PrefixArgs);
     const bool one = out_dtype == RECO_BF16;
-    const Kernel fn = kv.d == 64 ? (one ? prefix_tc<64, 1> : prefix_tc<64, 2>) : (one ? prefix_tc<128, 1> : prefix_tc<128, 2>);
-    const int smem = kv.d == 64 ? PrefixTc<64>::SMEM : PrefixTc<128>::SMEM;
+    const Kernel fn = kv.d == 64 ? (one ? prefix_tc<64, 1> : prefix_tc<64, 3>) : (one ? prefix_tc<128, 1> : prefix_tc<128, 3>);
+    const int smem = kv.d == 64 ? (one ? PrefixTc<64, 1>::SMEM : PrefixTc<64, 3>::SMEM) : (one ? PrefixTc<128, 1>::SMEM : PrefixTc<128, 3>::SMEM);
     cudaError_t e = allow_smem((const void *)fn, smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(fn, dim3(grid), dim3(PrefixTc<64>::THREADS), smem, s, mk, mv, mq, mq1, a);
+    e = launch_pdl(fn, dim3(grid), dim3(PrefixTc<64, 1>::THREADS), smem, s, mk, mv, mq, mq1, a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

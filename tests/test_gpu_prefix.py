@@ -4,7 +4,7 @@ of append, attention and eviction together.
 Bounds as test_gpu_paged.py's (u = 2^-24): a logit (d + 4) u big and the exponential's 2 u big and 2^-22; a
 probability twice that and 2^-21; an output that times sum_j p_j |v_j|, its chain of additions (blocks of up to 128
 rows, then blocks, then pieces: 192 + n / 8 of them) and the parts' joining (32 more), u each; over bf16 caches the
-probabilities enter in two bf16 parts, 2^-17, or, with bf16 output, those of the prefix in one, 2^-8; a bf16
+probabilities enter in three bf16 parts, 2^-26, or, with bf16 output, in one, 2^-8; a bf16
 output half a bf16 step.  A part's log2 is rounded where the parts join: 2 u of the lse's size more per probability.
 """
 import numpy as np
@@ -106,7 +106,7 @@ class Batch:
         prob = 2 * ((d + 6) * U * big) + 2.0 ** -21 + 4 * U * size
         chain = (192 + 32 + seen / 8) * U
         bf16 = self.dtype == BF
-        part = 0.0 if not bf16 else (2.0 ** -17 if self.out_dtype == F32 else 2.0 ** -8)
+        part = 0.0 if not bf16 else (2.0 ** -26 if self.out_dtype == F32 else 2.0 ** -8)
         t_out = (prob + chain + part)[..., None] * absv
         t_out = t_out * (1 + 2.0 ** -8) + np.abs(ro) * 2.0 ** -8 if self.out_dtype == BF else t_out + np.abs(ro) * U
         t_lse = (d + 6) * U * big + 2.0 ** -21 + chain + 4 * U * size
@@ -454,7 +454,7 @@ def test_a_prompt_once_then_its_answers(dtype):
         reco.reco_paged_decode_attn(priv, q_rot, None, None, lens_c, d ** -0.5, outs[1][0], None, ws)
         reco.reco_check()
         assert torch.equal(lens, lens_c)
-        # rows: |q k| of some tens at most; two parts of 2^-17 or float32 sums on each side
+        # rows: |q k| of some tens at most; parts of 2^-17 (the decode's) or float32 sums
         assert (outs[0][0] - outs[1][0]).abs().max() < (2 ** -14 if dtype == BF else 2 ** -17)
         if t == 30:  # the same cut of both: the prefix's rows stay (sinks), answers lose all but their latest 12 rows and 8 more
             wts = torch.rand((Ly, n, H, per * page), generator=g, device=DEV)
