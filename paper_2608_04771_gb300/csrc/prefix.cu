@@ -129,7 +129,7 @@ __device__ void plan_units(const PlanArgs &a, int block)
             x.n = L + append;
             x.lo = company ? p : 0;
             x.k0 = x.lo & -min(kPrefixTile, 1 << a.shift);  // the tensor cores' kernel copies whole boxes
-            work = x.n > x.lo ? a.rows.own() * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + kOwnExtra : 0;
+            work = x.n > x.lo ? a.rows.own() * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + a.rows.extra() : 0;
         }
     }
     const int before = scan_block<false>(work, sm) - work;
@@ -168,41 +168,60 @@ __global__ void __launch_bounds__(kPrefixBlock) prefix_plan(const __grid_constan
 }
 
 // ---------------------------------------------------------------- attention, float32
-// Plain FMAs, every sum float32.  A copying warp and eight that compute; one of these takes RW of the tile's query rows (32 at
-// most) and, where the tile has fewer, a share of its 128 keys (WR row groups, 8 / WR key groups).  K and V tiles come by
-// TMA, a box per page and 32 columns, into a ring of three; swizzled, so that lanes that read the same columns of different
-// rows meet different banks.  A warp waits for a tile, and lets it go, for itself.
-// QK^T: a half-warp has RW / 2 rows, a lane of it KPL keys, so that six to ten 16-byte reads feed up to 64 FMAs; PV: a lane
-// has D / 32 columns of all rows, and takes the probabilities from shared memory.
+// Plain FMAs (two to an instruction), every sum float32.  A warp finds the pieces and copies; eight compute: one takes RW of
+// the tile's query rows (32 at most) and a share of its 128 keys (WR row groups, 8 / WR key groups).  K and V tiles come
+// by TMA, a box per page and 32 columns, into a ring of three; swizzled, so that lanes that read the same columns of
+// different rows meet different banks.  A warp waits for a tile, and lets it go, for itself.
+// QK^T: eight lanes share a row group's keys, four the rows: RW / 4 rows and KEYS / 8 keys to a lane, so that six to eight
+// 16-byte reads feed up to 64 FMAs.  PV: a lane has D / 32 columns of all RW rows, and takes the probabilities from shared
+// memory.  28 layers of 8 sequences in two groups (12 and 2 heads of 128, 1500 to 2000 shared rows, 315 MB): 121 us, where
+// the bytes are 46 and the FMAs 40.  A tile of 32 rows takes 14300 cycles, of which the FMAs could issue in 8200: no tile
+// is waited for, two warps a scheduler hide too little of what shared memory takes.  Halving its reads (8 keys and 8
+// rows to a lane, d split four ways and joined by shuffles) gained nothing; one FMA to an instruction: 131 us; row
+// groups of 8 with 16 lanes a row, at 168 registers: 146 us.
 constexpr int kPlainRows = 32;
 constexpr long long kPlainPolls = 1LL << 19;  // of a wait, each suspended for up to two microseconds
-constexpr int kPlainWarps = 8, kPlainThreads = 32 * (kPlainWarps + 1);
+constexpr int kPlainWarps = 8, kPlainThreads = 32 * (kPlainWarps + 4);  // (registers are split by groups of four warps)
 
 template <int D> struct PlainSmem {
     float ring[3][kPrefixTile * D];       // [D / 32][128][32], swizzled
     float q[kPlainRows * D];              // queries, then probabilities by warp; at a piece's end the warps' outputs as they
     float p[D == 128 ? 32 * D : 64 * D];  // join: 8 warps of 8 rows
-    float2 ml[64];
-    uint64_t full[3], empty[3];
+    float2 ml[128];
+    uint64_t full[3], empty[3], piece_full[4], piece_empty[4];
+    PrefixPiece piece[4];                 // found ahead by the copying warp
     int bad[4];                           // a page that is none was met, by piece
     int abort;
 };
 static_assert(sizeof(PlainSmem<128>) <= 227 * 1024, "shared memory of a CTA");
 
+__device__ __forceinline__ ulonglong2 ld2x2(const float *p) { return *reinterpret_cast<const ulonglong2 *>(p); }
 __device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 // Float offset of 16-byte chunk c of row r of a tile, of the queries.
 __device__ __forceinline__ int tile_at(int r, int c) { return (c >> 3) * (kPrefixTile * 32) + r * 32 + (((c ^ r) & 7) << 2); }
 template <int D> __device__ __forceinline__ int query_at(int r, int c) { return r * D + ((c ^ (r & 7)) << 2); }
 __device__ __forceinline__ void bar_plain() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kPlainWarps) : "memory"); }
 
+// Whether x holds in all threads that compute; also their barrier.
+__device__ __forceinline__ bool all_plain(bool x)
+{
+    int r;
+    asm volatile("{.reg .pred p, q; setp.ne.b32 p, %1, 0; barrier.cta.red.and.pred q, 1, %2, p; selp.b32 %0, 1, 0, q;}"
+                 : "=r"(r)
+                 : "r"((int)x), "n"(32 * kPlainWarps)
+                 : "memory");
+    return r != 0;
+}
+
 template <int D, int WR, int RW>
 __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPiece &pc, int piece, PlainSmem<D> &sm, int &slot, bool &ok)
 {
     constexpr int WK = 8 / WR, E = D / 32, KEYS = kPrefixTile / WK;  // keys of a tile that a warp takes
-    constexpr int RPL = RW / 2, KPL = KEYS / 16;                     // rows and keys of a lane
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, kl = lane & 15, rl = lane >> 4;
+    constexpr int RPL = RW / 4, KPL = KEYS / 8;                      // rows and keys of a lane
+    constexpr int PASSES = RW > 8 ? 2 : 1, RH = RW / PASSES;         // the warps' outputs meet in 64 rows of shared memory
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, rw = wid % WR, kg = wid / WR, kl = (lane >> 1 & 3) | (lane >> 4 & 1) << 2, rl = (lane & 1) | (lane >> 3 & 1) << 1;
     const int nrows = pc.nseq * a.G;
-    float *ps = sm.p + wid * 8 * KEYS;  // [KEYS][8]
+    float *ps = sm.p + wid * RW * KEYS;  // [KEYS][RW]
     for (int i = tid; i < RW * WR * (D / 4); i += 32 * kPlainWarps) {
         const int r = i / (D / 4), c = i % (D / 4);
         *reinterpret_cast<float4 *>(sm.q + query_at<D>(r, c)) =
@@ -233,32 +252,41 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
     for (int t = pc.t0; t < pc.t1 && __all_sync(0xffffffffu, ok); ++t) {
         const int k0 = pc.k0 + t * kPrefixTile, live = pc.end - k0, low = pc.lo - k0;  // rows of the tile that count: [low, live)
         landed();
-        float s[RPL][KPL];
+        unsigned long long s2[RPL][KPL];  // (sums over even and over odd columns)
 #pragma unroll
         for (int r = 0; r < RPL; ++r)
 #pragma unroll
-            for (int j = 0; j < KPL; ++j) s[r][j] = 0.f;
+            for (int j = 0; j < KPL; ++j) s2[r][j] = 0ull;
         const int kb = kg * KEYS + kl;
         {
-            const float *K = sm.ring[slot % 3] + kb * 32, *Q = sm.q + (rw * RW + rl * RPL) * D;
-            const int kx = kb & 7, qx = rw * RW + rl * RPL;
+            const float *K = sm.ring[slot % 3] + kb * 32, *Q = sm.q + (rw * RW + rl) * D;
+            const int kx = kb & 7, qx = rw * RW + rl;
 #pragma unroll 1
             for (int cc = 0; cc < D / 4; cc += 8, K += kPrefixTile * 32)
-#pragma unroll
+#pragma unroll 4
                 for (int c = 0; c < 8; ++c) {
-                    float4 qv[RPL];
+                    ulonglong2 qv[RPL];
 #pragma unroll
-                    for (int r = 0; r < RPL; ++r) qv[r] = ld4(Q + r * D + (((cc + c) ^ ((qx + r) & 7)) << 2));
+                    for (int r = 0; r < RPL; ++r) qv[r] = ld2x2(Q + 4 * r * D + (((cc + c) ^ ((qx + 4 * r) & 7)) << 2));
 #pragma unroll
                     for (int j = 0; j < KPL; ++j) {
-                        const float4 kv = ld4(K + 16 * j * 32 + ((c ^ kx) << 2));
+                        const ulonglong2 kv = ld2x2(K + 8 * j * 32 + ((c ^ kx) << 2));
 #pragma unroll
                         for (int r = 0; r < RPL; ++r)
-                            s[r][j] = fmaf(qv[r].w, kv.w, fmaf(qv[r].z, kv.z, fmaf(qv[r].y, kv.y, fmaf(qv[r].x, kv.x, s[r][j]))));
+                            s2[r][j] = fma_pair(qv[r].y, kv.y, fma_pair(qv[r].x, kv.x, s2[r][j]));
                     }
                 }
         }
         done();
+        float s[RPL][KPL];
+#pragma unroll
+        for (int r = 0; r < RPL; ++r)
+#pragma unroll
+            for (int j = 0; j < KPL; ++j) {
+                float x, y;
+                unpair(s2[r][j], x, y);
+                s[r][j] = x + y;
+            }
         float al[RPL];
         bool any = false;
 #pragma unroll
@@ -266,11 +294,11 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
             float mb = -INFINITY;
 #pragma unroll
             for (int j = 0; j < KPL; ++j) {
-                s[r][j] = kb + 16 * j < live && kb + 16 * j >= low ? s[r][j] * a.c2 : -INFINITY;
+                s[r][j] = kb + 8 * j < live && kb + 8 * j >= low ? s[r][j] * a.c2 : -INFINITY;
                 mb = fmaxf(mb, s[r][j]);
             }
 #pragma unroll
-            for (int x = 1; x < 16; x <<= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x));
+            for (int x = 0; x < 3; ++x) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, x < 2 ? 2 << x : 16));
             const bool grow = mb > m[r] + kLazyLog2;  // lazy rescale, as in the decode's consumers
             const float mn = grow ? mb : m[r];
             al[r] = grow ? fast_exp2(m[r] - mn) : 1.f;
@@ -286,12 +314,12 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         }
 #pragma unroll
         for (int j = 0; j < KPL; ++j)
-            *reinterpret_cast<float4 *>(ps + (kl + 16 * j) * 8 + rl * 4) =
-                make_float4(s[0][j], s[1][j], s[2][j], RPL == 4 ? s[RPL - 1][j] : 0.f);
+#pragma unroll
+            for (int r = 0; r < RPL; ++r) ps[(kl + 8 * j) * RW + 4 * r + rl] = s[r][j];
         if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
-                const float f = __shfl_sync(0xffffffffu, al[r % RPL], (r / RPL) * 16);
+                const float f = __shfl_sync(0xffffffffu, al[r / 4], (r & 1) | (r & 2) << 2);
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[r][e] *= f;
             }
@@ -299,11 +327,11 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         __syncwarp();
         landed();
         // a tile's products are summed before they join the output: the chain of additions into it is as long as the tiles
-        float acc[RW][E];
+        unsigned long long acc[RW / 2][E];  // (of two rows)
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
+        for (int r = 0; r < RW / 2; ++r)
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[r][e] = 0.f;
+            for (int e = 0; e < E; ++e) acc[r][e] = 0ull;
         const float *V = sm.ring[slot % 3] + (D == 128 ? (lane >> 3) * (kPrefixTile * 32) : (lane >> 4) * (kPrefixTile * 32));
         const int vc = D == 128 ? lane & 7 : (lane & 15) >> 1, vo = D == 128 ? 0 : 2 * (lane & 1);
         // (rows that do not count are not touched: whatever they hold, NaN times a probability of zero is not zero)
@@ -323,58 +351,71 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
                 v[0] = f.x;
                 v[1] = f.y;
             }
-            const float4 p0 = ld4(ps + 8 * k), p1 = ld4(ps + 8 * k + 4);
-            const float p[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
 #pragma unroll
-            for (int r = 0; r < RW; ++r)
+            for (int r = 0; r < RW; r += 4) {
+                const ulonglong2 p = ld2x2(ps + RW * k + r);
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[r][e] = fmaf(p[r / RPL * 4 + r % RPL], v[e], acc[r][e]);
+                for (int e = 0; e < E; ++e) {
+                    const unsigned long long vv = pair_of(v[e], v[e]);
+                    acc[r / 2][e] = fma_pair(p.x, vv, acc[r / 2][e]);
+                    acc[r / 2 + 1][e] = fma_pair(p.y, vv, acc[r / 2 + 1][e]);
+                }
+            }
         }
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
+        for (int r = 0; r < RW / 2; ++r)
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[r][e] += acc[r][e];
+            for (int e = 0; e < E; ++e) {
+                float x, y;
+                unpair(acc[r][e], x, y);
+                o[2 * r][e] += x;
+                o[2 * r + 1][e] += y;
+            }
         done();
     }
 #pragma unroll
     for (int r = 0; r < RPL; ++r)
 #pragma unroll
-        for (int x = 1; x < 16; x <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], x);
+        for (int x = 0; x < 3; ++x) l[r] += __shfl_xor_sync(0xffffffffu, l[r], x < 2 ? 2 << x : 16);
     // the key groups join through shared memory
-    bar_plain();  // queries and probabilities have been read
-    float *os = sm.q + wid * RW * D;
-#pragma unroll
-    for (int r = 0; r < RW; ++r)
-#pragma unroll
-        for (int e = 0; e < E; ++e) os[r * D + lane * E + e] = o[r][e];
+    const bool bad = *(volatile int *)&sm.bad[piece & 3] != 0;
     if (kl == 0)
 #pragma unroll
-        for (int r = 0; r < RPL; ++r) sm.ml[wid * RW + rl * RPL + r] = make_float2(m[r], l[r]);
-    bar_plain();
-    const bool bad = *(volatile int *)&sm.bad[piece & 3] != 0;
-    for (int i = tid; i < nrows * (D / 4); i += 32 * kPlainWarps) {
-        const int r = i / (D / 4), c = i % (D / 4), w0 = r / RW, rr = r - w0 * RW;
-        float M = -INFINITY, L = 0.f;
+        for (int r = 0; r < RPL; ++r) sm.ml[wid * RW + 4 * r + rl] = make_float2(m[r], l[r]);
+    float *os = sm.q + wid * RH * D;
 #pragma unroll
-        for (int x = 0; x < WK; ++x) M = fmaxf(M, sm.ml[(w0 + x * WR) * RW + rr].x);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int pass = 0; pass < PASSES; ++pass) {
+        bar_plain();  // queries and probabilities, or the outputs of the pass before, have been read
 #pragma unroll
-        for (int x = 0; x < WK; ++x) {
-            const int w = w0 + x * WR;
-            const float2 y = sm.ml[w * RW + rr];
-            const float f = part_factor(y.x, M);
-            const float4 v = ld4(sm.q + (w * RW + rr) * D + 4 * c);
-            L += y.y * f;
-            acc.x += v.x * f;
-            acc.y += v.y * f;
-            acc.z += v.z * f;
-            acc.w += v.w * f;
+        for (int r = 0; r < RH; ++r)
+#pragma unroll
+            for (int e = 0; e < E; ++e) os[r * D + lane * E + e] = o[pass * RH + r][e];
+        bar_plain();
+        for (int i = tid; i < RH * WR * (D / 4); i += 32 * kPlainWarps) {
+            const int at = i / (D / 4), c = i % (D / 4), w0 = at / RH, rh = at - w0 * RH, rr = pass * RH + rh, r = w0 * RW + rr;
+            if (r >= nrows) continue;
+            float M = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int x = 0; x < WK; ++x) M = fmaxf(M, sm.ml[(w0 + x * WR) * RW + rr].x);
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int x = 0; x < WK; ++x) {
+                const int w = w0 + x * WR;
+                const float2 y = sm.ml[w * RW + rr];
+                const float f = part_factor(y.x, M);
+                const float4 v = ld4(sm.q + (w * RH + rh) * D + 4 * c);
+                L += y.y * f;
+                acc.x += v.x * f;
+                acc.y += v.y * f;
+                acc.z += v.z * f;
+                acc.w += v.w * f;
+            }
+            float *po;
+            float2 *pm;
+            a.partial<D>(pc, r / a.G, r % a.G, po, pm);
+            *reinterpret_cast<float4 *>(po + 4 * c) = acc;
+            if (c == 0) *pm = make_float2(M, bad ? -1.f : L);
         }
-        float *po;
-        float2 *pm;
-        a.partial<D>(pc, r / a.G, r % a.G, po, pm);
-        *reinterpret_cast<float4 *>(po + 4 * c) = acc;
-        if (c == 0) *pm = make_float2(M, bad ? -1.f : L);
     }
     bar_plain();
 }
@@ -397,7 +438,10 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
             mbar_init(smem_addr(&sm.full[i]), 1);
             mbar_init(smem_addr(&sm.empty[i]), kPlainWarps);
         }
-        for (int i = 0; i < 4; ++i) sm.bad[i] = 0;
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(smem_addr(&sm.piece_full[i]), 1);
+            mbar_init(smem_addr(&sm.piece_empty[i]), kPlainWarps);
+        }
         sm.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_shared();
@@ -405,20 +449,33 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
     __syncthreads();
     wait_prior_grid();
     release_next_grid();  // the join looks up its places meanwhile
-    PrefixWalk w = a.range();
-    PrefixPiece pc;
     bool ok = true;
     int slot = 0;
-    if (warp == kPlainWarps) {
-        // ---- copies.  Lane (box, part) of a tile copies 32 columns of the box's rows: a page, or half a page of 256
+    auto await = [&](uint64_t *bar, int k) {
+        if (!mbar_try_wait(smem_addr(bar), k & 1)) ok &= thread_wait(smem_addr(bar), k & 1, &sm.abort, a.err, kPlainPolls);
+    };
+    auto fine = [&]() { return __all_sync(0xffffffffu, ok) != 0; };
+    // registers of the launch, 168 a thread, as the roles need them: 128 (56) + 256 (224)
+    if (warp >= kPlainWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // ---- pieces and copies.  Lane (box, part) of a tile copies 32 columns of the box's rows: a page, or half a page of 256
         constexpr int PARTS = D / 32;
         const int rows = min(kPrefixTile, 1 << a.shift), boxes = kPrefixTile / rows;
         const int box = lane / PARTS, part = lane % PARTS;
-        for (int piece = 0; prefix_next(&a, &w, &pc); ++piece) {
-            // (at most three tiles ahead: a piece's place is that of the fourth before, which is done)
-            if (lane == 0) *(volatile int *)&sm.bad[piece & 3] = 0;
+        PrefixWalk w = a.range();
+        PrefixPiece pc;
+        for (int piece = 0; warp == kPlainWarps && fine(); ++piece) {
+            const bool more = a.next(w, pc);
+            await(&sm.piece_empty[piece & 3], piece / 4 + 1);
+            if (lane == 0) {
+                if (!more) pc.t1 = pc.t0 = 0;
+                sm.piece[piece & 3] = pc;
+                sm.bad[piece & 3] = 0;
+                mbar_arrive(smem_addr(&sm.piece_full[piece & 3]));
+            }
             __syncwarp();
-            for (int t = pc.t0; t < pc.t1; ++t) {
+            if (!more) break;
+            for (int t = pc.t0; t < pc.t1 && fine(); ++t) {
                 const int k = pc.k0 + t * kPrefixTile + box * rows;
                 const bool needed = box < boxes && k < pc.end;
                 const long long row = needed ? a.pool_row(pc, k) : -1;
@@ -428,9 +485,9 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
                     raise_error(a.err, ERR_PAGE);
                 }
                 for (int kv = 0; kv < 2; ++kv, ++slot) {
-                    const uint32_t empty = smem_addr(&sm.empty[slot % 3]), full = smem_addr(&sm.full[slot % 3]);
-                    if (!mbar_try_wait(empty, (slot / 3 + 1) & 1)) ok &= thread_wait(empty, (slot / 3 + 1) & 1, &sm.abort, a.err, kPlainPolls);
-                    if (!__all_sync(0xffffffffu, ok)) break;
+                    await(&sm.empty[slot % 3], slot / 3 + 1);
+                    if (!fine()) break;
+                    const uint32_t full = smem_addr(&sm.full[slot % 3]);
                     if (lane == 0) mbar_expect_tx(full, (uint32_t)(n * rows * 128));
                     __syncwarp();
                     if (row >= 0)
@@ -438,24 +495,29 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
                                     (int)row, full);
                     __syncwarp();
                 }
-                if (!__all_sync(0xffffffffu, ok)) break;
             }
-            if (!__all_sync(0xffffffffu, ok)) break;
         }
         // no copy is left in flight when the CTA ends
         for (int j = max(0, slot - 3); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[j % 3]), j / 3 & 1, kPlainPolls);
-        return;
-    }
-    for (int piece = 0; prefix_next(&a, &w, &pc); ++piece) {
-        const int nrows = pc.nseq * a.G;
-        if (nrows <= 8)
-            plain_piece<D, 1, 8>(a, pc, piece, sm, slot, ok);
-        else if (nrows <= 16)
-            plain_piece<D, 2, 8>(a, pc, piece, sm, slot, ok);
-        else if (nrows <= 24)
-            plain_piece<D, 4, 6>(a, pc, piece, sm, slot, ok);
-        else
-            plain_piece<D, 4, 8>(a, pc, piece, sm, slot, ok);
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        // ---- attention
+        for (int piece = 0;; ++piece) {
+            await(&sm.piece_full[piece & 3], piece / 4);
+            __syncwarp();
+            const PrefixPiece pc = sm.piece[piece & 3];
+            if (!all_plain(ok) || pc.t0 == pc.t1) break;
+            const int nrows = pc.nseq * a.G;
+            if (nrows <= 8)
+                plain_piece<D, 1, 8>(a, pc, piece, sm, slot, ok);
+            else if (nrows <= 16)
+                plain_piece<D, 2, 8>(a, pc, piece, sm, slot, ok);
+            else if (nrows <= 24)
+                plain_piece<D, 2, 12>(a, pc, piece, sm, slot, ok);
+            else
+                plain_piece<D, 2, 16>(a, pc, piece, sm, slot, ok);
+            if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[piece & 3]));
+        }
     }
 }
 
@@ -496,7 +558,7 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
             return 1 + share.cta(w0 + (long long)(tiles - 1) * unit) - c;
         };
         if (x.n > x.lo) {
-            long long w0 = pre + x.work + kOwnExtra;
+            long long w0 = pre + x.work + a.p.rows.extra();
             for (int i = 0; i < u / kPrefixBlock; ++i) w0 += __ldg(a.p.block_work + i);
             n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, a.p.rows.own(), own_c);
         }
@@ -596,7 +658,7 @@ static PrefixRows prefix_rows(const reco_paged_kv &kv)
 long long prefix_own_most(const reco_paged_kv &kv)
 {
     const long long tiles = ((long long)paged_cap(kv) + kPrefixTile - 1) / kPrefixTile + 1;  // (the first may begin before the own rows)
-    return (long long)kv.n_layers * kv.B * kv.H_kv * (tiles * prefix_rows(kv).own() + kOwnExtra);
+    return (long long)kv.n_layers * kv.B * kv.H_kv * (tiles * prefix_rows(kv).own() + prefix_rows(kv).extra());
 }
 
 PrefixWs prefix_ws_layout(const reco_paged_kv &kv, void *base)

@@ -10,9 +10,8 @@ namespace reco {
 // at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy.  bf16: a key tile
 // takes 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has
 // several row tiles, which find the keys in L2, 9 for a whole one (1.9 us) and 6 for the last one if it has no more than
-// `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows, 24 with 16, 33 with 24, 40 with 32.
-// The start and the end of a unit's own rows take kOwnExtra more.
-constexpr int kOwnExtra = 11;
+// `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows (5300 cycles), 24 with 16 (8300), 33 with
+// 24, 40 with 32 (14300).  The start and the end of a unit's own rows take extra() more.
 struct PrefixRows {
     int per, half, G, f32;
     __host__ __device__ int plain(int n) const { return n * G <= 8 ? 15 : (n * G <= 16 ? 24 : (n * G <= 24 ? 33 : 40)); }
@@ -22,6 +21,7 @@ struct PrefixRows {
         if (f32) return plain(n - rt * per < per ? n - rt * per : per);
         return n <= per ? 8 : (n - rt * per <= half && per > half ? 6 : 9);
     }
+    __host__ __device__ int extra() const { return f32 ? 5 : 11; }
     __host__ __device__ int own() const { return f32 ? plain(1) : 8; }
     // a group's of n sequences with p rows, per layer and KV head
     __host__ __device__ long long work(int n, int p) const
@@ -66,6 +66,27 @@ template <typename F> __device__ __forceinline__ int warp_last(int n, long long 
         n = min(step, n - k * step);
     }
     return lo;
+}
+
+// Two float32 in a register pair, and arithmetic on both at once.
+__device__ __forceinline__ unsigned long long pair_of(float a, float b)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ unsigned long long fma_pair(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add_pair(unsigned long long a, unsigned long long b)
+{
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 // A CTA's part of an item: a row tile (nseq sequences from s0 on of the group that begins at sequence b0) against key
@@ -159,10 +180,10 @@ struct PrefixArgs {
             pc.k0 = x.k0;
             pc.lo = x.lo;
             pc.end = x.n;
-            const int in = at - w.base - x.work, unit = rows.own(), size = kt > 0 ? unit * kt + kOwnExtra : 0;
+            const int in = at - w.base - x.work, unit = rows.own(), size = kt > 0 ? unit * kt + rows.extra() : 0;
             const int e = (int)min((long long)size, in + (w.end - w.w));
-            pc.t0 = max(0, in - kOwnExtra + unit - 1) / unit;
-            pc.t1 = max(0, e - kOwnExtra + unit - 1) / unit;
+            pc.t0 = max(0, in - rows.extra() + unit - 1) / unit;
+            pc.t1 = max(0, e - rows.extra() + unit - 1) / unit;
             pc.own = true;
             if (e == size) {  // the next unit, maybe of the next block
                 ++w.u;
@@ -193,9 +214,6 @@ struct PrefixArgs {
         ml = (pc.t0 != 0 ? cont_ml : (pc.own ? own_ml : part_ml)) + at;
     }
 };
-
-// PrefixArgs::next as a function of its own: the kernels look for a piece in several places.
-__device__ __noinline__ static bool prefix_next(const PrefixArgs *a, PrefixWalk *w, PrefixPiece *pc) { return a->next(*w, *pc); }
 
 // The attention of all pieces over bf16 caches (prefix_tc.cu).
 cudaError_t launch_prefix_tc(const reco_paged_kv &kv, const PrefixArgs &a, int grid, reco_dtype out_dtype, cudaStream_t s);
