@@ -410,6 +410,58 @@ def test_two_calls_at_once():
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_pools_beyond_32_bits(dtype):
+    """The same rows at the far end of a pool of more than 2^32 bytes: the same bits."""
+    b = Batch(31, 2, 8, 2, 64, dtype, 64, [0, 0, 0, 1], [300, 300, 300, 0], [[[5], [130], [0], [77]]])
+    n_pages, far = b.K.shape[1], 2 ** 33 // (b.K[0, 0].numel() * b.K.element_size()) // 2
+    K, V = (torch.full((2, far, *b.K.shape[2:]), float("nan"), device=DEV, dtype=dtype) for _ in range(2))
+    K[:, far - n_pages:], V[:, far - n_pages:] = b.K, b.V
+    table = torch.where((b.table >= 0) & (b.table < n_pages), b.table + (far - n_pages), -1)
+    lens = b.lens.clone()
+    b.go()
+    out, lse = torch.empty_like(b.out), torch.empty_like(b.lse)
+    kv = reco.make_paged_kv(K, V, table, 8)
+    ws = reco.paged_workspace(reco.RECO_OP_PAGED_PREFIX, kv, DEV)
+    reco.reco_paged_prefix_attn(kv, b.q, b.kn, b.vn, lens, b.groups, b.shared, b.scale, out, lse, ws)
+    reco.reco_check()
+    assert K.numel() * K.element_size() >= 2 ** 33 and torch.equal(bits(out), bits(b.out)) and torch.equal(bits(lse), bits(b.lse))
+    assert torch.equal(lens, b.lens)
+    for pool, small in ((K, b.K), (V, b.V)):
+        assert torch.equal(bits(pool[:, far - n_pages:]), bits(small))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_pages_named_twice(dtype):
+    """Rows may be read through one page in several places: in one prefix, in two groups, as a sequence's own."""
+    b = Batch(32, 1, 12, 2, 128, dtype, 32, [0, 0, 1, 1, 2], [192, 192, 192, 192, 0], [[[40], [40], [40], [40], [230]]])
+    b.table[0, 3] = b.table[0, 1]
+    b.table[2, :6] = b.table[0, :6]
+    b.table[4, 2] = b.table[0, 1]
+    b.go()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_call_for_another_stream_waits_for_nothing_else(dtype):
+    """Calls that follow each other on two streams, ordered by events alone, with a workspace each."""
+    b = Batch(33, 2, 14, 2, 128, dtype, 16, [0] * 6, [700] * 6, 40)
+    ref, before = b.reference(), (b.K.clone(), b.V.clone())
+    lens, ws = b.lens.clone(), reco.paged_workspace(reco.RECO_OP_PAGED_PREFIX, b.kv, DEV)
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b.run(stream=s)
+    first = b.out, b.lse
+    t.wait_stream(s)
+    with torch.cuda.stream(t):
+        b.lens.copy_(lens)
+        b.out, b.lse = torch.empty_like(b.out), torch.empty_like(b.lse)
+        b.run(ws=ws)
+    torch.cuda.synchronize()
+    reco.reco_check()
+    assert torch.equal(bits(first[0]), bits(b.out)) and torch.equal(bits(first[1]), bits(b.lse))
+    b.check(ref, before)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_a_prompt_once_then_its_answers(dtype):
     """Append of a prompt, answers over it, token by token with rotation, eviction of the answers' own rows: against
     the same calls on private copies of the prompt (reco_paged_decode_attn), bit for bit where rows are moved and
