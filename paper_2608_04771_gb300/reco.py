@@ -384,10 +384,10 @@ def reco_paged_evict(kv: reco_paged_kv, weights, lens, budget, w: int, sinks: in
                                _ptr(kept_idx), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
-def _rows(name, t, shape, kv):
+def _rows(name, t, shape, dtype, dev):
     """A [layers, T, heads, d] tensor of the cache's type as a view with its strides."""
-    if t.shape != shape or t.dtype != kv.expect[1] or t.get_device() != kv.expect[0]:
-        raise ValueError(f"{name} must be {list(shape)} of {kv.expect[1]} on the cache's device, not {list(t.shape)} of {t.dtype}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be {list(shape)} of {dtype} on the cache's device, not {list(t.shape)} of {t.dtype}")
     layer, token, head, one = t.stride()
     if one != 1:
         raise ValueError(f"the elements of a row of {name} must lie next to each other")
@@ -400,16 +400,18 @@ def reco_paged_append(kv: reco_paged_kv, k, v, starts, lens, ws, pos=None, inv_f
     [layers, T, H_kv, d], q and q_out [layers, T, H_q, d], of any strides but the last; tokens starts[b] to
     starts[b + 1] - 1 are sequence b's.  inv_freq [rot / 2] float32 gives the angles per position (None: no
     rotation), pos [T] int32 the positions; pairs are (i, i + rot / 2), or neighbours if interleaved."""
-    dev, _, (Ly, B, H_q, d), _, _, units, _ = kv.expect
+    dev, dtype, (Ly, B, H_q, d), _, _, units, _ = kv.expect
     if k.dim() != 4:
         raise ValueError("k must be [layers, T, H_kv, d]")
     T = k.shape[1]
-    kr, vr = _rows("k", k, (Ly, T, kv.H_kv, d), kv), _rows("v", v, (Ly, T, kv.H_kv, d), kv)
+    shape = (Ly, T, units[2], d)
+    kr, vr = _rows("k", k, shape, dtype, dev), _rows("v", v, shape, dtype, dev)
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out must both be given or both be None")
     qr = qor = None
     if q is not None:
-        qr, qor = ctypes.byref(_rows("q", q, (Ly, T, H_q, d), kv)), ctypes.byref(_rows("q_out", q_out, (Ly, T, H_q, d), kv))
+        shape = (Ly, T, H_q, d)
+        qr, qor = _rows("q", q, shape, dtype, dev), _rows("q_out", q_out, shape, dtype, dev)
     _check_tensor("starts", starts, (B + 1,), torch.int32, dev)
     _check_tensor("lens", lens, units, torch.int32, dev)
     rot = 0
@@ -421,9 +423,8 @@ def reco_paged_append(kv: reco_paged_kv, k, v, starts, lens, ws, pos=None, inv_f
     if pos is not None:
         _check_tensor("pos", pos, (T,), torch.int32, dev)
     _check_place(ws, dev)
-    _ok(lib().reco_paged_append(ctypes.byref(kv), ctypes.byref(kr), ctypes.byref(vr), qr, qor, T, starts.data_ptr(),
-                                _ptr(pos), _ptr(inv_freq) if rot else None, rot, 1 if interleaved else 0, lens.data_ptr(),
-                                ws.data_ptr(), ws.numel(), _stream(stream)))
+    _ok(lib().reco_paged_append(kv, kr, vr, qr, qor, T, starts.data_ptr(), _ptr(pos), _ptr(inv_freq) if rot else None, rot,
+                                1 if interleaved else 0, lens.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def reco_reflect_penalty(logits, ids, rewards, tau_l=0.4, tau_h=0.8, beta=4.0, beta_out=None,

@@ -412,7 +412,8 @@ def test_two_calls_at_once():
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_pools_beyond_32_bits(dtype):
     """The same rows at the far end of a pool of more than 2^32 bytes: the same bits."""
-    b = Batch(31, 2, 8, 2, 64, dtype, 64, [0, 0, 0, 1], [300, 300, 300, 0], [[[5], [130], [0], [77]]])
+    b = Batch(31, 2, 8, 2, 64, dtype, 64, [0, 0, 0, 1], [300, 300, 300, 0],
+              np.ones((2, 4, 2), int) * [[[5], [130], [0], [77]]])
     n_pages, far = b.K.shape[1], 2 ** 33 // (b.K[0, 0].numel() * b.K.element_size()) // 2
     K, V = (torch.full((2, far, *b.K.shape[2:]), float("nan"), device=DEV, dtype=dtype) for _ in range(2))
     K[:, far - n_pages:], V[:, far - n_pages:] = b.K, b.V
@@ -433,7 +434,8 @@ def test_pools_beyond_32_bits(dtype):
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_pages_named_twice(dtype):
     """Rows may be read through one page in several places: in one prefix, in two groups, as a sequence's own."""
-    b = Batch(32, 1, 12, 2, 128, dtype, 32, [0, 0, 1, 1, 2], [192, 192, 192, 192, 0], [[[40], [40], [40], [40], [230]]])
+    b = Batch(32, 1, 12, 2, 128, dtype, 32, [0, 0, 1, 1, 2], [192, 192, 192, 192, 0],
+              np.ones((1, 5, 2), int) * [[[40], [40], [40], [40], [230]]])
     b.table[0, 3] = b.table[0, 1]
     b.table[2, :6] = b.table[0, :6]
     b.table[4, 2] = b.table[0, 1]
