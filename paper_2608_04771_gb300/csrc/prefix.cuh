@@ -9,8 +9,8 @@ namespace reco {
 // A row tile takes the query heads of up to `per` sequences of a group, of which `half` make what the tensor cores take
 // at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy.  bf16: a key tile
 // takes 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has
-// several row tiles, which find the keys in L2, 9 for a whole one (1.9 us) and 6 for the last one if it has no more than
-// `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows (5300 cycles), 24 with 16 (8300), 33 with
+// several row tiles, which are bound by their products, 9 for a whole one (1.9 us) and 6 for the last one if it has no more
+// than `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows (5300 cycles), 24 with 16 (8300), 33 with
 // 24, 40 with 32 (14300).  The start and the end of a unit's own rows take extra() more.
 struct PrefixRows {
     int per, half, G, f32;

@@ -21,10 +21,13 @@
 //
 // Measured, GB300, the whole call with its plan and its join.  28 layers, 8 sequences of 28 query and 4 key heads of 128 over
 // 16001 shared rows and 1000 to 4000 of their own (1.9 GB of K and V): 293 us, 0.96 of the copy rate.  64 sequences of 40 and
-// 8 heads over 100001 shared rows: 171 us, where the bytes once and the products are 67 us each; two row tiles read every K
-// and V tile, one of 250 rows in 1.9 us of a CTA (its products alone would take 1.3) and one of 70 in 1.2.  One layer, 16
-// sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 27 us, a chain of launches and
-// look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V rows: 301, 169 and 28.4 us.
+// 8 heads over 100001 shared rows: 169 us, where the bytes once and the products are 67 us each; two row tiles read every K
+// and V tile, one of 250 rows in 1.9 us of a CTA (its products alone would take 1.3) and one of 70 in 1.2.  Memory is not
+// what bounds them (165 us with all rows in 26 MB of pages): a product with 64 keys reads 6 KB of shared memory, 48 cycles, for
+// 32 cycles of the tensor cores (42% active), and a block's softmax and two hand-overs are as long as the other stream's
+// products.  One layer, 16 sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 27 us, a
+// chain of launches and look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V
+// rows: 301, 169 and 28.4 us.
 //
 // P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
 // of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Of these the second lies
