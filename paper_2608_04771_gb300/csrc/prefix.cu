@@ -693,7 +693,8 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
 {
     const bool f32 = kv.dtype == RECO_F32;
     const int units = kv.n_layers * kv.B * kv.H_kv, G = kv.H_q / kv.H_kv, blocks = (units + kPrefixBlock - 1) / kPrefixBlock;
-    const PrefixRows rows = prefix_rows(kv);
+    PrefixRows rows = prefix_rows(kv);
+    if (!f32 && out_dtype == RECO_F32) rows.per = rows.half;  // (one stream of products)
     PlanArgs p = {};
     p.K = kv.k;
     p.V = kv.v;

@@ -31,8 +31,13 @@
 //
 // P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
 // of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Of these the second lies
-// beside the first, TMEM has no room for the third: it comes from shared memory, where the ring is a tile or two shorter.
+// beside the first, TMEM has no room for the third: it comes from shared memory, where the ring is a tile shorter.
 // Sums take the probabilities as they were before.
+// The tensor cores cut sums off rather than round them: some 2^-26 of the output is lost with every addition to it, always
+// towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing;
+// with float32 output every block's product starts from zero, and four warps add the blocks up in registers: there is one
+// stream then, with two places for its products, the other stream's softmax warps are those that add, and a row tile has
+// 128 rows.
 //
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
 // to come when phase k + 1 is.  So every place is waited for by both issuing warps, every time; what a group waits for
@@ -64,6 +69,13 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint3
     rb -= __uint_as_float(lo & 0xffff0000u);
 }
 
+__device__ __forceinline__ void st_global_v8(float *p, const float *x)  // a whole sector
+{
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]),
+                 "f"(x[5]), "f"(x[6]), "f"(x[7])
+                 : "memory");
+}
+
 constexpr long long kPolls = 1LL << 19;  // of a wait, each suspended for up to two microseconds
 
 // The blocks of 64 keys of a piece that fall to stream s: block j begins `first` + `step` j columns from the start of the
@@ -86,15 +98,17 @@ template <int D, int PARTS> struct PrefixTc {
     static constexpr int BOX = 128 * 128;  // 128 rows of 64 bf16
     static constexpr int TILE = HALVES * BOX;
     static constexpr int Q_BYTES = 2 * TILE;
-    static constexpr int REST = PARTS == 3 ? 2 * BOX : 0;  // the probabilities' third parts, by stream
+    static constexpr int STREAMS = PARTS == 3 ? 1 : 2;
+    static constexpr int REST = PARTS == 3 ? 2 * BOX : 0;  // the probabilities' third parts, of two blocks
     static constexpr int TILES = 5 * 128 / D - REST / TILE, NK = (TILES + 1) / 2, NV = TILES - NK, NS = TILES;  // places for K tiles, then V tiles
     static constexpr int NP = 4;                  // pieces found ahead
     static constexpr int THREADS = 32 * 12;
     struct Small {  // behind the tiles
         uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2];
-        uint64_t o_free, met;
+        uint64_t o_free, met[2], o_read[2];
         uint64_t piece_full[NP], piece_empty[NP];
-        float2 ml[2][128];
+        float2 ml[2][STREAMS == 1 ? 1 : 128];
+        float al[2][STREAMS == 1 ? 128 : 1];
         PrefixPiece piece[NP];
         int bad[NP];  // a page that is none was met
         uint32_t tmem;
@@ -112,7 +126,9 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
 {
     using C = PrefixTc<D, PARTS>;
     constexpr int NS = C::NS, NK = C::NK, NV = C::NV, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
-    constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O
+    constexpr bool ALONE = C::STREAMS == 1;
+    constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O;
+    constexpr uint32_t ML_COL = 128;            // one stream: maxima and sums of two pieces
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t base = smem_addr(smem_raw), Qs = base, rest = base + C::Q_BYTES, ring = rest + C::REST;
@@ -128,11 +144,13 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
         prefetch_tensormap(&tmQ1);
         for (int i = 0; i < NS; ++i) {
             mbar_init(smem_addr(&sm.full[i]), 1);
-            mbar_init(smem_addr(&sm.empty[i]), 2);
+            mbar_init(smem_addr(&sm.empty[i]), ALONE ? 1 : 2);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_addr(&sm.q_full[s]), 1);
-            mbar_init(smem_addr(&sm.q_empty[s]), 2);
+            mbar_init(smem_addr(&sm.q_empty[s]), ALONE ? 1 : 2);
+            mbar_init(smem_addr(&sm.met[s]), ALONE ? 4 : 8);
+            mbar_init(smem_addr(&sm.o_read[s]), 4);
             for (int b = 0; b < 2; ++b) {
                 mbar_init(smem_addr(&sm.s_full[s][b]), 1);
                 mbar_init(smem_addr(&sm.p_full[s][b]), 4);
@@ -140,10 +158,9 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             }
         }
         mbar_init(smem_addr(&sm.o_free), 8);
-        mbar_init(smem_addr(&sm.met), 8);
         for (int i = 0; i < C::NP; ++i) {
             mbar_init(smem_addr(&sm.piece_full[i]), 1);
-            mbar_init(smem_addr(&sm.piece_empty[i]), 11);  // the threads of warps 1 and 3, warp 2, the softmax's eight
+            mbar_init(smem_addr(&sm.piece_empty[i]), ALONE ? 10 : 11);  // warps 1, 2 and 3, and from 4 on eight
         }
         sm.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -249,6 +266,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             }
         }
         for (int j = max(0, slot - NV); j < slot; ++j) mbar_wait_bounded(smem_addr(&sm.full[NK + j % NV]), (j / NV) & 1, kPolls);
+    } else if (ALONE && warp == 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     } else if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         // ---- products of stream s
@@ -257,8 +276,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
         // (the whole warp goes through the loops, so that what it computes is known to be uniform: operands of the products
         // come from uniform registers, and one thread alone issued a product every 70 to 125 cycles)
         const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX),
-                       rd = sw128_desc(rest + s * BOX);
-        const uint32_t st = tmem + S_COL + 128 * s, o = tmem + O_COL + D * s;
+                       rd = sw128_desc(rest);
+        const uint32_t st = tmem + S_COL + 128 * s, o0 = tmem + O_COL + D * s;
         const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
                        p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
         // places of the next K and V tile, and the parity of their phase; query tiles, blocks so far
@@ -280,7 +299,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             if (!fine()) break;
             const PrefixPiece x = sm.piece[np % NP];
             const bool pair = x.nseq > a.rows.half;
-            const PrefixBlocks bl(x, pair, s);
+            const bool both = pair || ALONE;  // the stream takes all keys
+            const PrefixBlocks bl(x, both, s);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
             if (bl.n == 0) break;
@@ -293,7 +313,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                 const int odd = j & 1;
                 if (j >= 2) {  // O += P V of block j - 2
                     const int c = bl.first + bl.step * (j - 2), nv = n + j - 2;
-                    if (!pair || !odd) await(full0 + 8 * vi, vp);
+                    if (!both || !odd) await(full0 + 8 * vi, vp);
                     // rows that no query sees, within the product's steps of 16: zero, as their probabilities are (NaN times zero is
                     // not).  (With a pair, both warps may do it: zeros over zeros.)
                     const int r0 = c < bl.lo ? min(64, bl.lo - c) : 0, r1 = max(0, min(64, bl.hi - c));  // rows that count: [r0, r1)
@@ -310,10 +330,13 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                     }
                     await(p_full0 + 8 * (nv & 1), nv >> 1);
                     // (every piece waits for the outputs of the one before to have been read, for the barrier's phases)
-                    if (j == 2 && np > 0) await(smem_addr(&sm.o_free), np - 1);
+                    if (ALONE)
+                        await(smem_addr(&sm.o_read[nv & 1]), (nv >> 1) + 1);
+                    else if (j == 2 && np > 0)
+                        await(smem_addr(&sm.o_free), np - 1);
                     tc_fence_after();
                     const uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
-                    const uint32_t p = st + 64 * (nv & 1);
+                    const uint32_t p = st + 64 * (nv & 1), o = o0 + (ALONE ? D * (nv & 1) : 0);
                     const int k0 = r0 >> 4, k1 = (r1 + 15) >> 4;
                     if (elect_one()) {
                         if (k0 == 0 && k1 == 4) {
@@ -322,7 +345,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > 0 ? 1u : more);
                                 if (PARTS == 3) {
                                     tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma(o, rd + (uint32_t)(k * 32 >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma(o, rd + (uint32_t)(((nv & 1) * BOX + k * 32) >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                                 }
                             }
                         } else {
@@ -331,19 +354,19 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > k0 ? 1u : more);
                                 if (PARTS == 3) {
                                     tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma(o, rd + (uint32_t)(k * 32 >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma(o, rd + (uint32_t)(((nv & 1) * BOX + k * 32) >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                                 }
                             }
                         }
                         tc_commit(pv_done0 + 8 * (nv & 1));
-                        if (!pair || odd) tc_commit(empty0 + 8 * vi);
+                        if (!both || odd) tc_commit(empty0 + 8 * vi);
                     }
                     __syncwarp();
-                    more |= k0 < k1 ? 1u : 0u;
-                    if (!pair || odd) step_v();
+                    if (!ALONE) more |= k0 < k1 ? 1u : 0u;
+                    if (!both || odd) step_v();
                 }
                 if (j < bl.n) {  // S = Q K^T of block j
-                    if (!pair || !odd) await(full0 + 8 * ki, kp);
+                    if (!both || !odd) await(full0 + 8 * ki, kp);
                     tc_fence_after();
                     const uint64_t bd = kd + (uint32_t)((ki * TILE + ((bl.first + bl.step * j) & 64) * 128) >> 4);
                     const uint32_t d = st + 64 * ((n + j) & 1);
@@ -354,17 +377,80 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                             tc_mma(d, ad + off, bd + off, ID_S, k > 0);
                         }
                         tc_commit(s_full0 + 8 * ((n + j) & 1));
-                        if (!pair || odd) tc_commit(empty0 + 8 * ki);
+                        if (!both || odd) tc_commit(empty0 + 8 * ki);
                         if (j == bl.n - 1) {
                             tc_commit(smem_addr(&sm.q_empty[q & 1]));
                             if (pair) mbar_arrive(smem_addr(&sm.q_empty[(q & 1) ^ 1]));
                         }
                     }
                     __syncwarp();
-                    if (!pair || odd) step_k();
+                    if (!both || odd) step_k();
                 }
             }
             n += bl.n;
+        }
+    } else if (ALONE && warp >= 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        // ---- outputs: the blocks' products add up in registers, query row r
+        const int quarter = warp & 3, r = quarter * 32 + lane, seq_r = r / a.G, g = r - seq_r * a.G;
+        const uint32_t oa = tmem + ((uint32_t)(quarter * 32) << 16) + O_COL;
+        int n = 0;
+        for (int np = 0; fine(); ++np) {
+            await(smem_addr(&sm.piece_full[np % NP]), np / NP);
+            if (!fine()) break;
+            const PrefixPiece pc = sm.piece[np % NP];
+            if (pc.t1 == pc.t0) break;
+            const PrefixBlocks bl(pc, true, 0);
+            const bool any_row = quarter * 32 < pc.nseq * a.G;
+            float o[D];
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] = 0.f;
+#pragma unroll 1
+            for (int j = 0; j < bl.n && fine(); ++j, ++n) {
+                await(smem_addr(&sm.pv_done[0][n & 1]), n >> 1);
+                __syncwarp();
+                tc_fence_after();
+                if (any_row) {
+                    await(smem_addr(&sm.p_full[0][n & 1]), n >> 1);  // (long over: what the softmax wrote is seen)
+                    const float al = sm.al[n & 1][ALONE ? r : 0];
+                    if (__any_sync(0xffffffffu, al != 1.f)) {
+#pragma unroll
+                        for (int i = 0; i < D; ++i) o[i] *= al;
+                    }
+                    const int c = bl.step * j;
+                    if (c < bl.hi && c + 64 > bl.lo) {  // (otherwise nothing was multiplied)
+#pragma unroll
+                        for (int x = 0; x < D; x += 32) {
+                            float y[32];
+                            tmem_ld32_nowait(oa + D * (n & 1) + x, y);
+                            tmem_ld_wait_regs<32>(y);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[x + i] += y[i];
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sm.o_read[n & 1]));
+            }
+            if (!fine()) break;
+            await(smem_addr(&sm.met[np & 1]), np >> 1);
+            __syncwarp();
+            tc_fence_after();
+            float ml[16];
+            tmem_ld16_nowait(oa - O_COL + ML_COL + 16 * (np & 1), ml);
+            tmem_ld_wait_regs<16>(ml);
+            tc_fence_before();
+            if (seq_r < pc.nseq) {
+                float *po;
+                float2 *pm;
+                a.partial<D>(pc, seq_r, g, po, pm);
+                *pm = make_float2(ml[0], *(volatile int *)&sm.bad[np % NP] ? -1.f : ml[1]);
+#pragma unroll
+                for (int y = 0; y < D; y += 8) st_global_v8(po + y, o + y);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -385,7 +471,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             const bool pair = pc.nseq > a.rows.half;
             const int seq0 = pair && s ? a.rows.half : 0, nseq = pair ? (s ? pc.nseq - seq0 : a.rows.half) : pc.nseq;
             const bool any_row = quarter * 32 < nseq * a.G;
-            const PrefixBlocks bl(pc, pair, s);
+            const PrefixBlocks bl(pc, pair || ALONE, s);
             const bool there = seq_r < nseq;
             float m = -INFINITY, l = 0.f;
             const int first = n;
@@ -409,12 +495,9 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                     // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).
                     uint32_t hi[32], lo[PARTS == 3 ? 32 : 1];
                     uint32_t third[4];
-                    const uint32_t row = rest + s * BOX + r * 128;
-                    if (PARTS == 3 && n > 0) {  // the product before has read its third parts
-                        await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
-                        __syncwarp();
-                    }
-                    float sum;
+                    // (S of this block came behind the product of two before, which has read its third parts)
+                    const uint32_t row = rest + (n & 1) * BOX + r * 128;
+                    float sum, factor = 1.f;
                     bool again = false;
                     for (;;) {
                         const float nb = again && m == -INFINITY ? 0.f : -m;
@@ -448,7 +531,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         const float mn = grow ? fmaxf(m, mx) : m, al = grow ? part_factor(m, mn) : 1.f;
                         l *= al;
                         m = mn;
-                        if (n > first) {  // the output so far
+                        factor = al;
+                        if (!ALONE && n > first) {  // the output so far
                             await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
                             __syncwarp();
                             tc_fence_after();
@@ -471,6 +555,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         tmem_st16(sa + 32, lo);
                         tmem_st16(sa + 48, lo + 16);
                         fence_async_shared();
+                        await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (the factor of two blocks before, too)
+                        sm.al[n & 1][ALONE ? r : 0] = factor;
                     }
                     tmem_st_wait();
                 }
@@ -480,19 +566,31 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                 ++n;
             }
             if (!fine()) break;
+            if (ALONE) {
+                uint32_t ml[16] = {__float_as_uint(m), __float_as_uint(l)};  // (in TMEM: shared memory is full)
+                tmem_st16(lane_base + ML_COL + 16 * (np & 1), ml);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_addr(&sm.met[np & 1]));
+                    mbar_arrive(smem_addr(&sm.piece_empty[np % NP]));
+                }
+                continue;
+            }
             // ---- the piece's partial
             await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
             __syncwarp();
             tc_fence_after();
             float f0 = 1.f, f1 = 0.f;
             if (!pair) {  // the streams join: each group takes half of the columns
-                sm.ml[s][r] = make_float2(m, l);
+                sm.ml[s][ALONE ? 0 : r] = make_float2(m, l);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sm.met));
-                await(smem_addr(&sm.met), met_n++);
+                if (lane == 0) mbar_arrive(smem_addr(&sm.met[0]));
+                await(smem_addr(&sm.met[0]), met_n++);
                 __syncwarp();
                 tc_fence_after();
-                const float2 x = sm.ml[0][r], y = sm.ml[1][r];
+                const float2 x = sm.ml[0][ALONE ? 0 : r], y = sm.ml[1][ALONE ? 0 : r];
                 m = fmaxf(x.x, y.x);
                 f0 = part_factor(x.x, m);
                 f1 = part_factor(y.x, m);
@@ -508,10 +606,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                 auto store = [&](int c, const float (&o)[32]) {
                     if (po != nullptr)
 #pragma unroll
-                        for (int y = 0; y < 32; y += 8)  // whole sectors
-                            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(po + c + y), "f"(o[y]), "f"(o[y + 1]),
-                                         "f"(o[y + 2]), "f"(o[y + 3]), "f"(o[y + 4]), "f"(o[y + 5]), "f"(o[y + 6]), "f"(o[y + 7])
-                                         : "memory");
+                        for (int y = 0; y < 32; y += 8) st_global_v8(po + c + y, o + y);
                 };
                 if (pair) {
 #pragma unroll 1
