@@ -559,6 +559,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         sm.al[n & 1][ALONE ? r : 0] = factor;
                     }
                     tmem_st_wait();
+                } else if (ALONE) {
+                    await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (warps without rows go no further ahead than the others)
                 }
                 tc_fence_before();
                 __syncwarp();
