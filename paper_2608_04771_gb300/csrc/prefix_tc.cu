@@ -30,9 +30,8 @@
 // rows: 301, 169 and 28.4 us.
 //
 // P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
-// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Of these the second lies
-// beside the first, TMEM has no room for the third: it comes from shared memory, where the ring is a tile shorter.
-// Sums take the probabilities as they were before.
+// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Sums
+// take the probabilities as they were before.
 // The tensor cores cut sums off rather than round them: some 2^-26 of the output is lost with every addition to it, always
 // towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing;
 // with float32 output every block's product starts from zero, and four warps add the blocks up in registers: there is one
@@ -99,8 +98,7 @@ template <int D, int PARTS> struct PrefixTc {
     static constexpr int TILE = HALVES * BOX;
     static constexpr int Q_BYTES = 2 * TILE;
     static constexpr int STREAMS = PARTS == 3 ? 1 : 2;
-    static constexpr int REST = PARTS == 3 ? 2 * BOX : 0;  // the probabilities' third parts, of two blocks
-    static constexpr int TILES = 5 * 128 / D - REST / TILE, NK = (TILES + 1) / 2, NV = TILES - NK, NS = TILES;  // places for K tiles, then V tiles
+    static constexpr int TILES = 5 * 128 / D, NK = (TILES + 1) / 2, NV = TILES - NK, NS = TILES;  // places for K tiles, then V tiles
     static constexpr int NP = 4;                  // pieces found ahead
     static constexpr int THREADS = 32 * 12;
     struct Small {  // behind the tiles
@@ -115,7 +113,7 @@ template <int D, int PARTS> struct PrefixTc {
         int abort;
     };
     // (all of it dynamic: the tiles begin where the CTA's shared memory does, at a multiple of 1024)
-    static constexpr int SMEM = Q_BYTES + REST + NS * TILE + (int)sizeof(Small);
+    static constexpr int SMEM = Q_BYTES + NS * TILE + (int)sizeof(Small);
     static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
 };
 
@@ -128,11 +126,11 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
     constexpr int NS = C::NS, NK = C::NK, NV = C::NV, NP = C::NP, BOX = C::BOX, TILE = C::TILE, HALVES = C::HALVES;
     constexpr bool ALONE = C::STREAMS == 1;
     constexpr uint32_t S_COL = 0, O_COL = 256;  // TMEM: S (then P) of the streams, 128 columns each, then their O;
-    constexpr uint32_t ML_COL = 128;            // one stream: maxima and sums of two pieces
+    constexpr uint32_t P3_COL = 128, ML_COL = 192;  // one stream: third parts of P, 32 columns a place; maxima and sums of two pieces
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t base = smem_addr(smem_raw), Qs = base, rest = base + C::Q_BYTES, ring = rest + C::REST;
-    typename C::Small &sm = *reinterpret_cast<typename C::Small *>(smem_raw + C::Q_BYTES + C::REST + NS * TILE);
+    const uint32_t base = smem_addr(smem_raw), Qs = base, ring = base + C::Q_BYTES;
+    typename C::Small &sm = *reinterpret_cast<typename C::Small *>(smem_raw + C::Q_BYTES + NS * TILE);
     if (base & 1023u) {  // swizzled tiles need it
         if (tid == 0) raise_error(a.err, ERR_INTERNAL);
         return;
@@ -275,8 +273,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
         const int s = warp >> 1;
         // (the whole warp goes through the loops, so that what it computes is known to be uniform: operands of the products
         // come from uniform registers, and one thread alone issued a product every 70 to 125 cycles)
-        const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX),
-                       rd = sw128_desc(rest);
+        const uint64_t qd = sw128_desc(Qs), kd = sw128_desc(ring), vd = sw128_desc_mn(ring, BOX);
         const uint32_t st = tmem + S_COL + 128 * s, o0 = tmem + O_COL + D * s;
         const uint32_t full0 = smem_addr(&sm.full[0]), empty0 = smem_addr(&sm.empty[0]), s_full0 = smem_addr(&sm.s_full[s][0]),
                        p_full0 = smem_addr(&sm.p_full[s][0]), pv_done0 = smem_addr(&sm.pv_done[s][0]);
@@ -345,7 +342,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > 0 ? 1u : more);
                                 if (PARTS == 3) {
                                     tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma(o, rd + (uint32_t)(((nv & 1) * BOX + k * 32) >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                                 }
                             }
                         } else {
@@ -354,7 +351,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > k0 ? 1u : more);
                                 if (PARTS == 3) {
                                     tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma(o, rd + (uint32_t)(((nv & 1) * BOX + k * 32) >> 4), bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                    tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                                 }
                             }
                         }
@@ -493,10 +490,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                     }
                     // Probabilities against the maximum so far.  No maximum of the block is looked for while their sum stays below
                     // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).
-                    uint32_t hi[32], lo[PARTS == 3 ? 32 : 1];
-                    uint32_t third[4];
-                    // (S of this block came behind the product of two before, which has read its third parts)
-                    const uint32_t row = rest + (n & 1) * BOX + r * 128;
+                    uint32_t hi[32], lo[PARTS == 3 ? 32 : 1], rest[PARTS == 3 ? 32 : 1];
                     float sum, factor = 1.f;
                     bool again = false;
                     for (;;) {
@@ -513,8 +507,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                             if (PARTS == 3) {
                                 float r0, r1;
                                 split_bf16(p0, p1, hi[y], lo[y], r0, r1);
-                                third[y & 3] = pack_bf16(r0, r1);
-                                if ((y & 3) == 3) sts_u4(row + ((y >> 2 ^ (r & 7)) << 4), make_uint4(third[0], third[1], third[2], third[3]));
+                                rest[y] = pack_bf16(r0, r1);
                             } else {
                                 hi[y] = pack_bf16(p0, p1);
                             }
@@ -554,7 +547,8 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                     if (PARTS == 3) {
                         tmem_st16(sa + 32, lo);
                         tmem_st16(sa + 48, lo + 16);
-                        fence_async_shared();
+                        tmem_st16(lane_base + P3_COL + 32 * (n & 1), rest);
+                        tmem_st16(lane_base + P3_COL + 32 * (n & 1) + 16, rest + 16);
                         await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (the factor of two blocks before, too)
                         sm.al[n & 1][ALONE ? r : 0] = factor;
                     }
