@@ -30,13 +30,14 @@
 // rows: 301, 169 and 28.4 us.
 //
 // P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
-// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Sums
-// take the probabilities as they were before.
+// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Sums take the probabilities
+// as they were before.
 // The tensor cores cut sums off rather than round them: some 2^-26 of the output is lost with every addition to it, always
-// towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing;
-// with float32 output every block's product starts from zero, and four warps add the blocks up in registers: there is one
-// stream then, with two places for its products, the other stream's softmax warps are those that add, and a row tile has
-// 128 rows.
+// towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing.
+// With float32 output every block's product starts from zero, and four warps add the blocks up in registers: one stream
+// with two places for its products, the other stream's softmax warps are those that add, and a row tile has 128 rows.  The
+// 28 layers above take 526 us so, 2500 cycles a block: 1600 for the softmax of the one warp that a scheduler has, the rest
+// waits and hand-overs (a third place for S: no gain; parts by cutting bits off instead of conversions: spills, 706 us).
 //
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
 // to come when phase k + 1 is.  So every place is waited for by both issuing warps, every time; what a group waits for
@@ -57,7 +58,7 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
-// (a, b) in three parts of bf16: two and what is left of both, which the third holds but for 2^-26.
+// (a, b) as two parts of bf16 and what is left, which a third holds but for 2^-26.
 __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &hi, uint32_t &lo, float &ra, float &rb)
 {
     hi = pack_bf16(a, b);
@@ -563,7 +564,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             }
             if (!fine()) break;
             if (ALONE) {
-                uint32_t ml[16] = {__float_as_uint(m), __float_as_uint(l)};  // (in TMEM: shared memory is full)
+                uint32_t ml[16] = {__float_as_uint(m), __float_as_uint(l)};  // (in TMEM, as S was: 16 columns are the least that a store takes here)
                 tmem_st16(lane_base + ML_COL + 16 * (np & 1), ml);
                 tmem_st_wait();
                 tc_fence_before();
