@@ -409,6 +409,24 @@ def test_two_calls_at_once():
         c.check(r, x)
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64), (128, 256)])
+def test_float32_output_of_groups_of_many_sizes(d, page):
+    """Short pieces of few and of many query rows in turn, whose warps have rows in one and none in the next."""
+    sizes, prefix = [1, 2, 33, 1, 40, 3, 26, 64], [0, 140, 129, 300, 260, 515, 31, 700]
+    group = [g for g, n in enumerate(sizes) for _ in range(n)]
+    shared = [p for n, p in zip(sizes, prefix) for _ in range(n)]
+    mine = np.random.default_rng(5).integers(0, 200, (3, len(group), 2))
+    b = Batch(34, 3, 8, 2, d, BF, page, group, shared, mine, out_dtype=F32)
+    lens = b.lens.clone()
+    b.go()
+    out, lse = b.out.clone(), b.lse.clone()
+    for _ in range(20):
+        b.lens.copy_(lens)
+        b.run()
+        reco.reco_check()
+        assert torch.equal(bits(b.out), bits(out)) and torch.equal(bits(b.lse), bits(lse))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_pools_beyond_32_bits(dtype):
     """The same rows at the far end of a pool of more than 2^32 bytes: the same bits."""
