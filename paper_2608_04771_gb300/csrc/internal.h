@@ -114,6 +114,7 @@ struct PrefixUnit {
     int work, k0, n, lo;
 };
 constexpr int kPrefixTile = 128;     // cached rows in a tile
+constexpr int kPrefixJoinRows = 32;  // own rows that are taken where the parts join, at most
 constexpr int kPrefixMaxRows = 256;  // query rows of a row tile, at most
 constexpr int kPrefixBlock = 1024;   // units of a block of the plan
 

@@ -129,7 +129,7 @@ __device__ void plan_units(const PlanArgs &a, int block)
             x.n = L + append;
             x.lo = company ? p : 0;
             x.k0 = x.lo & -min(kPrefixTile, 1 << a.shift);  // the tensor cores' kernel copies whole boxes
-            work = x.n > x.lo ? a.rows.own() * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + a.rows.extra() : 0;
+            work = x.n - x.lo > a.rows.few ? a.rows.own() * ((x.n - x.k0 + kPrefixTile - 1) / kPrefixTile) + a.rows.extra() : 0;
         }
     }
     const int before = scan_block<false>(work, sm) - work;
@@ -524,6 +524,10 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 // ---------------------------------------------------------------- join
 // One CTA per unit.  The partials of a query head: the own rows' first one, their others by CTA, and the same of the
 // prefix.  A warp finds a head's factors; then a thread adds up four columns of a head over an equal part of the partials.
+// Where units are many, own rows that are few (at the start of an answer) are one more part, taken here with plain FMAs: as
+// an item of the attention they cost 2 us and more of a CTA that holds an SM, here several units share one.  (24 layers, 26
+// sequences of 8 key heads with at most 18 rows of their own, 4992 units: 210 -> 107 us.  128 units, half of them with
+// up to 32: 27.7 -> 29.9, the join waits for them; so only above 600 units.)
 struct JoinArgs {
     PrefixArgs p;
     int32_t *lens;
@@ -533,11 +537,13 @@ struct JoinArgs {
 };
 constexpr int kJoinThreads = 256;
 
-template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(const __grid_constant__ JoinArgs a)
+template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefix_join(const __grid_constant__ JoinArgs a)
 {
     constexpr int Q = D / 4;
     extern __shared__ float sm_f[];  // [G][np] factors
     __shared__ float2 sm_ML[16];
+    __shared__ float sm_p[16][kPrefixJoinRows], sm_fo[16];
+    __shared__ int sm_row[kPrefixJoinRows];
     __shared__ __align__(16) float4 sm_o[kJoinThreads];
     // (the attention has released this grid once the plan was complete: it may be read at once)
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -557,7 +563,7 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
             c = share.cta(w0);
             return 1 + share.cta(w0 + (long long)(tiles - 1) * unit) - c;
         };
-        if (x.n > x.lo) {
+        if (x.n - x.lo > a.p.rows.few) {
             long long w0 = pre + x.work + a.p.rows.extra();
             for (int i = 0; i < u / kPrefixBlock; ++i) w0 += __ldg(a.p.block_work + i);
             n_own = ctas(w0, (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile, a.p.rows.own(), own_c);
@@ -571,6 +577,72 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
             pre_row = (i - rt * rows.per) * G;
         }
     }
+    // ---- few own rows: logits, then probabilities in sm_p (a warp's heads are those that it joins below)
+    const int few = FEW && ok && x.n > x.lo && x.n - x.lo <= a.p.rows.few ? x.n - x.lo : 0;
+    bool err = !ok;
+    auto four = [&](const void *base, size_t at, int n, float (&v)[4]) {  // n = 2 or 4 elements
+        if (a.p.rows.f32) {
+            const float *f = (const float *)base + at;
+            if (n == 4) {
+                const float4 y = *reinterpret_cast<const float4 *>(f);
+                v[0] = y.x, v[1] = y.y, v[2] = y.z, v[3] = y.w;
+            } else {
+                const float2 y = *reinterpret_cast<const float2 *>(f);
+                v[0] = y.x, v[1] = y.y;
+            }
+        } else {
+            const uint32_t *f = reinterpret_cast<const uint32_t *>((const __nv_bfloat16 *)base + at);
+#pragma unroll
+            for (int i = 0; i < 4; i += 2)
+                if (i < n) {
+                    const uint32_t y = f[i / 2];
+                    v[i] = __uint_as_float(y << 16);
+                    v[i + 1] = __uint_as_float(y & 0xffff0000u);
+                }
+        }
+    };
+    float2 own_ml[2];  // of heads wid and wid + 8
+    if (few > 0) {
+        constexpr int E = D / 32, R = kPrefixJoinRows * 32 / kJoinThreads;  // elements of a lane, rows of a warp
+        PrefixPiece pc = {};
+        pc.layer = layer;
+        pc.h = h;
+        pc.b0 = b;
+        float k[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int j = wid + kJoinThreads / 32 * i;
+            const long long row = j < few ? a.p.pool_row(pc, x.lo + j) : 0;
+            if (row < 0 && lane == 0) raise_error(a.p.err, ERR_PAGE);
+            err |= row < 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[i][e] = 0.f;
+            if (j < few && row >= 0) four(a.p.K, (size_t)row * D + lane * E, E, k[i]);
+            if (j < few && lane == 0) sm_row[j] = row < 0 ? 0 : (int)row;
+        }
+        for (int g = 0; g < G; ++g) {
+            float q[4];
+            four(a.p.q, (q0 + g) * D + lane * E, E, q);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float dot = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) dot = fmaf(q[e], k[i][e], dot);
+                dot = warp_sum(dot);
+                if (lane == 0) sm_p[g][wid + kJoinThreads / 32 * i] = dot * a.p.c2;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int g = wid + t * (kJoinThreads / 32);
+            if (g >= G) break;
+            const float s = lane < few ? sm_p[g][lane] : -INFINITY, M = warp_max(s);
+            const float p = fast_exp2(s - (M == -INFINITY ? 0.f : M));
+            sm_p[g][lane] = p;
+            own_ml[t] = make_float2(M, warp_sum(p));
+        }
+    }
     wait_prior_grid();
     const int np = n_own + n_pre;
     auto place = [&](int i, int g, const float *&o, const float2 *&ml) {
@@ -582,9 +654,9 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
     };
     const float *po;
     const float2 *pm;
-    bool err = !ok;
     for (int g = wid; g < G; g += kJoinThreads / 32) {
-        float M = -INFINITY, L = 0.f;
+        const float2 own = g < kJoinThreads / 32 ? own_ml[0] : own_ml[1];
+        float M = few > 0 ? own.x : -INFINITY, L = 0.f;
         for (int i = lane; i < np; i += 32) {
             place(i, g, po, pm);
             M = fmaxf(M, pm->x);
@@ -599,7 +671,12 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
             sm_f[g * np + i] = f;
         }
         L = warp_sum(L);
-        if (lane == 0) sm_ML[g] = make_float2(M, L);
+        const float fo = few > 0 ? part_factor(own.x, M) : 0.f;
+        if (few > 0) L += own.y * fo;
+        if (lane == 0) {
+            sm_ML[g] = make_float2(M, L);
+            sm_fo[g] = fo;
+        }
     }
     err = __syncthreads_or(err);
     // threads: (part, head, four columns)
@@ -607,6 +684,20 @@ template <int D> __global__ void __launch_bounds__(kJoinThreads) prefix_join(con
     for (int s = tid - part * slots; s < slots && part < parts; s += kJoinThreads) {  // (one turn where parts > 1)
         const int g = s / Q, c = s - g * Q;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int j = part; j < few; j += parts) {
+            float v[4];
+            four(a.p.V, (size_t)sm_row[j] * D + 4 * c, 4, v);
+            const float p = sm_p[g][j];
+            o.x = fmaf(p, v[0], o.x);
+            o.y = fmaf(p, v[1], o.y);
+            o.z = fmaf(p, v[2], o.z);
+            o.w = fmaf(p, v[3], o.w);
+        }
+        if (few > 0) {
+            const float f = sm_fo[g];
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        }
 #pragma unroll 4
         for (int i = part; i < np; i += parts) {
             place(i, g, po, pm);
@@ -651,8 +742,8 @@ static int prefix_cont_rows(const reco_paged_kv &kv)
 
 static PrefixRows prefix_rows(const reco_paged_kv &kv)
 {
-    const int G = kv.H_q / kv.H_kv;
-    return kv.dtype == RECO_F32 ? PrefixRows{kPlainRows / G, kPlainRows / G, G, 1} : PrefixRows{2 * (128 / G), 128 / G, G, 0};
+    const int G = kv.H_q / kv.H_kv, few = (long long)kv.n_layers * kv.B * kv.H_kv > 600 ? kPrefixJoinRows : 0;
+    return kv.dtype == RECO_F32 ? PrefixRows{kPlainRows / G, kPlainRows / G, G, 1, few} : PrefixRows{2 * (128 / G), 128 / G, G, 0, few};
 }
 
 long long prefix_own_most(const reco_paged_kv &kv)
@@ -769,7 +860,9 @@ cudaError_t launch_paged_prefix(const reco_paged_kv &kv, const void *q, const vo
     j.grid = grid;
     j.append = k_new ? 1 : 0;
     j.out_bf16 = out_dtype == RECO_BF16 ? 1 : 0;
-    e = launch_pdl(kv.d == 64 ? prefix_join<64> : prefix_join<128>, dim3(units), dim3(kJoinThreads), (size_t)G * (2 * grid + 2) * 4, s, j);
+    void (*join)(JoinArgs) = rows.few ? (kv.d == 64 ? prefix_join<64, true> : prefix_join<128, true>)
+                                      : (kv.d == 64 ? prefix_join<64, false> : prefix_join<128, false>);
+    e = launch_pdl(join, dim3(units), dim3(kJoinThreads), (size_t)G * (2 * grid + 2) * 4, s, j);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -14,6 +14,7 @@ namespace reco {
 // 24, 40 with 32 (14300).  The start and the end of a unit's own rows take extra() more.
 struct PrefixRows {
     int per, half, G, f32;
+    int few;  // so many own rows at most are left to the join
     __host__ __device__ int plain(int n) const { return n * G <= 8 ? 15 : (n * G <= 16 ? 24 : (n * G <= 24 ? 33 : 40)); }
     // a key tile's of row tile rt of n sequences (all but the last row tile have the first one's), of a unit's own rows
     __host__ __device__ int unit(int n, int rt) const
@@ -169,8 +170,9 @@ struct PrefixArgs {
                 const int u0 = blk * kPrefixBlock;
                 w.u = u0 + warp_last(min(kPrefixBlock, n_units - u0), at - w.base, [&](int i) { return units[u0 + i].work; });
             }
+            if (w.u >= n_units) return false;
             const PrefixUnit x = units[w.u];
-            const int kt = x.n > x.lo && x.lo >= 0 ? (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile : 0;
+            const int kt = x.lo >= 0 && x.n - x.lo > rows.few ? (x.n - x.k0 + kPrefixTile - 1) / kPrefixTile : 0;
             const int lb = w.u / Hkv;
             pc.layer = lb / B;
             pc.h = w.u - lb * Hkv;
@@ -181,6 +183,11 @@ struct PrefixArgs {
             pc.lo = x.lo;
             pc.end = x.n;
             const int in = at - w.base - x.work, unit = rows.own(), size = kt > 0 ? unit * kt + rows.extra() : 0;
+            if (size == 0) {  // (and maybe many like it: the next one with work is looked for)
+                w.u = -1;
+                w.base = 0;
+                continue;
+            }
             const int e = (int)min((long long)size, in + (w.end - w.w));
             pc.t0 = max(0, in - rows.extra() + unit - 1) / unit;
             pc.t1 = max(0, e - rows.extra() + unit - 1) / unit;

@@ -427,6 +427,31 @@ def test_float32_output_of_groups_of_many_sizes(d, page):
         assert torch.equal(bits(b.out), bits(out)) and torch.equal(bits(b.lse), bits(lse))
 
 
+@pytest.mark.parametrize("dtype,d,G,out_dtype", [(BF, 128, 5, BF), (BF, 64, 16, F32), (F32, 128, 7, F32), (F32, 64, 2, F32), (BF, 128, 1, F32)])
+@pytest.mark.parametrize("append", [True, False])
+def test_many_units_with_few_rows_of_their_own(dtype, d, G, out_dtype, append):
+    """Units with none, one, 31 to 33 and 200 rows behind prefixes and without any, among units in error."""
+    sizes, prefix = [1, 9, 1, 14, 2, 8], [0, 65, 0, 130, 33, 0]
+    group = [g for g, n in enumerate(sizes) for _ in range(n)]
+    shared = [p for n, p in zip(sizes, prefix) for _ in range(n)]
+    mine = np.random.default_rng(6).choice([0, 1, 2, 17, 30, 31, 32, 33, 200], (10, len(group), 2))
+    b = Batch(35, 10, 2 * G, 2, d, dtype, 16, group, shared, mine, append=append, out_dtype=out_dtype)
+    b.go()
+    if append:  # a page of own rows that is none: that sequence's units alone
+        mine[:, 3] = 20
+        b = Batch(36, 10, 2 * G, 2, d, dtype, 16, group, shared, mine, append=True, out_dtype=out_dtype)
+        whole = Batch(36, 10, 2 * G, 2, d, dtype, 16, group, shared, mine, append=True, out_dtype=out_dtype)
+        whole.go()
+        b.table[3, 4] = -1  # rows 64 to 79 of the sequence, whose prefix ends at 65
+        lens = b.lens.clone()
+        b.run()
+        with pytest.raises(reco.RecoError):
+            reco.reco_check()
+        keep = [i for i in range(len(group)) if i != 3]
+        assert (b.out[:, 3] == 0).all() and torch.isneginf(b.lse[:, 3]).all() and torch.equal(b.lens[:, 3], lens[:, 3])
+        assert torch.equal(bits(b.out[:, keep]), bits(whole.out[:, keep])) and torch.equal(b.lens[:, keep], whole.lens[:, keep])
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_pools_beyond_32_bits(dtype):
     """The same rows at the far end of a pool of more than 2^32 bytes: the same bits."""
