@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
     }
     __syncthreads();
     wait_prior_grid();
-    release_next_grid();  // the join looks up its places meanwhile
+    release_next_grid();  // (the join's CTAs start as this grid's end, and wait for all of it)
     bool ok = true;
     int slot = 0;
     auto await = [&](uint64_t *bar, int k) {
@@ -545,7 +545,7 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
     __shared__ float sm_p[16][kPrefixJoinRows], sm_fo[16];
     __shared__ int sm_row[kPrefixJoinRows];
     __shared__ __align__(16) float4 sm_o[kJoinThreads];
-    // (the attention has released this grid once the plan was complete: it may be read at once)
+    wait_prior_grid();  // (the plan's lists too: what earlier grids wrote is sure to be seen only behind this grid's own wait)
     const int u = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int h = u % a.p.Hkv, lb = u / a.p.Hkv, layer = lb / a.p.B, b = lb - layer * a.p.B, G = a.p.G;
     const int run = a.p.run_of[b];
@@ -643,7 +643,6 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
             own_ml[t] = make_float2(M, warp_sum(p));
         }
     }
-    wait_prior_grid();
     const int np = n_own + n_pre;
     auto place = [&](int i, int g, const float *&o, const float2 *&ml) {
         const bool own = i < n_own;

@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
     wait_prior_grid();
-    release_next_grid();  // the join looks up its places meanwhile
+    release_next_grid();  // (the join's CTAs start as this grid's end, and wait for all of it)
     // A wait for phase k of a barrier, by every lane for itself; `ok` says whether it came (the same in all lanes but
     // where a wait runs out: the roles look at all lanes' once per step).
     bool ok = true;
