@@ -680,7 +680,7 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
     err = __syncthreads_or(err);
     // threads: (part, head, four columns)
     const int slots = G * Q, parts = max(1, kJoinThreads / slots), part = tid / slots;
-    for (int s = tid - part * slots; s < slots && part < parts; s += kJoinThreads) {  // (one turn where parts > 1)
+    auto sum = [&](int s) {  // of head and columns s, over the rows and partials of this thread's part
         const int g = s / Q, c = s - g * Q;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
@@ -707,18 +707,10 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
             o.z += v.z * f;
             o.w += v.w * f;
         }
-        if (parts > 1) {
-            sm_o[tid] = o;
-            asm volatile("bar.sync 1, %0;" ::"r"((parts * slots + 31) / 32 * 32) : "memory");
-            if (part > 0) break;
-            for (int k = 1; k < parts; ++k) {
-                const float4 v = sm_o[k * slots + s];
-                o.x += v.x;
-                o.y += v.y;
-                o.z += v.z;
-                o.w += v.w;
-            }
-        }
+        return o;
+    };
+    auto store = [&](int s, float4 o) {
+        const int g = s / Q, c = s - g * Q;
         const float2 ML = sm_ML[g];
         const float L = err ? 0.f : ML.y, inv = sum_inverse(L);
         if (err) o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -729,6 +721,23 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
         else
             *reinterpret_cast<float4 *>(reinterpret_cast<float *>(a.out) + (q0 + g) * D + 4 * c) = v;
         if (c == 0 && a.lse) a.lse[q0 + g] = sum_log2(ML.x, L) * kLn2;
+    };
+    if (parts > 1) {  // one turn; threads behind the last part (16, with d 64 and 3 or 5 heads) meet the barrier with the others
+        if (part < parts) sm_o[tid] = sum(tid - part * slots);
+        __syncthreads();
+        if (part == 0) {
+            float4 o = sm_o[tid];
+            for (int k = 1; k < parts; ++k) {
+                const float4 v = sm_o[k * slots + tid];
+                o.x += v.x;
+                o.y += v.y;
+                o.z += v.z;
+                o.w += v.w;
+            }
+            store(tid, o);
+        }
+    } else {
+        for (int s = tid; s < slots; s += kJoinThreads) store(s, sum(s));
     }
     if (tid == 0 && a.append && !err) a.lens[u] = x.n;
 }
