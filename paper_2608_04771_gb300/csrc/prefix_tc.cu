@@ -552,6 +552,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         tmem_st16(lane_base + P3_COL + 32 * (n & 1) + 16, rest + 16);
                         await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (the factor of two blocks before, too)
                         sm.al[n & 1][ALONE ? r : 0] = factor;
+                        __syncwarp();
                     }
                     tmem_st_wait();
                 } else if (ALONE) {
@@ -609,6 +610,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
 #pragma unroll 1
                     for (int x = 0; x < D; x += 64) {
                         float o[2][32];
+                        __syncwarp();  // (lanes without a row stored nothing)
                         tmem_ld32_nowait(lane_base + O_COL + D * s + x, o[0]);
                         tmem_ld32_nowait(lane_base + O_COL + D * s + x + 32, o[1]);
                         tmem_ld_wait_regs<32>(o[0]);
@@ -623,6 +625,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
 #pragma unroll 1
                     for (int x = 0; x < H; x += 32) {
                         float o[2][32];
+                        __syncwarp();
                         tmem_ld32_nowait(oa + x, o[0]);
                         tmem_ld32_nowait(oa + D + x, o[1]);
                         tmem_ld_wait_regs<32>(o[0]);
