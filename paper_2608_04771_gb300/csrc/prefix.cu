@@ -238,10 +238,11 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         m[r] = -INFINITY;
         l[r] = 0.f;
     }
+    // (a tile that has not come is not let go either: its place would be filled again with a copy under way)
     auto landed = [&]() {
         const uint32_t bar = smem_addr(&sm.full[slot % 3]);
         if (!mbar_try_wait(bar, slot / 3 & 1)) ok &= thread_wait(bar, slot / 3 & 1, &sm.abort, a.err, kPlainPolls);
-        __syncwarp();
+        return __all_sync(0xffffffffu, ok) != 0;
     };
     auto done = [&]() {
         __syncwarp();
@@ -249,9 +250,9 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
         ++slot;
     };
 #pragma unroll 1
-    for (int t = pc.t0; t < pc.t1 && __all_sync(0xffffffffu, ok); ++t) {
+    for (int t = pc.t0; t < pc.t1; ++t) {
         const int k0 = pc.k0 + t * kPrefixTile, live = pc.end - k0, low = pc.lo - k0;  // rows of the tile that count: [low, live)
-        landed();
+        if (!landed()) break;
         unsigned long long s2[RPL][KPL];  // (sums over even and over odd columns)
 #pragma unroll
         for (int r = 0; r < RPL; ++r)
@@ -325,7 +326,7 @@ __device__ __forceinline__ void plain_piece(const PrefixArgs &a, const PrefixPie
             }
         }
         __syncwarp();
-        landed();
+        if (!landed()) break;
         // a tile's products are summed before they join the output: the chain of additions into it is as long as the tiles
         unsigned long long acc[RW / 2][E];  // (of two rows)
 #pragma unroll
@@ -467,6 +468,7 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
         for (int piece = 0; warp == kPlainWarps && fine(); ++piece) {
             const bool more = a.next(w, pc);
             await(&sm.piece_empty[piece & 3], piece / 4 + 1);
+            if (!fine()) break;
             if (lane == 0) {
                 if (!more) pc.t1 = pc.t0 = 0;
                 sm.piece[piece & 3] = pc;

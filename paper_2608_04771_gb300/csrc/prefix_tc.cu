@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
         for (int np = 0; fine(); ++np) {
             const bool more = a.next(w, pc);
             await(smem_addr(&sm.piece_empty[np % NP]), np / NP + 1);
+            if (!fine()) break;
             if (lane == 0) {
                 if (!more) pc.t1 = pc.t0 = 0;
                 sm.piece[np % NP] = pc;
@@ -304,10 +305,11 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
             if (bl.n == 0) break;
             const int q = nq + (pair ? s : 0);
             for (int i = 0; i < (pair ? 2 : 1); ++i, ++nq) await(smem_addr(&sm.q_full[nq & 1]), nq >> 1);
+            if (!fine()) break;
             const uint64_t ad = qd + (uint64_t)((q & 1) * TILE >> 4);
             uint32_t more = 0;
 #pragma unroll 1
-            for (int j = 0; j < bl.n + 2 && fine(); ++j) {
+            for (int j = 0; j < bl.n + 2; ++j) {
                 const int odd = j & 1;
                 if (j >= 2) {  // O += P V of block j - 2
                     const int c = bl.first + bl.step * (j - 2), nv = n + j - 2;
@@ -315,7 +317,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                     // rows that no query sees, within the product's steps of 16: zero, as their probabilities are (NaN times zero is
                     // not).  (With a pair, both warps may do it: zeros over zeros.)
                     const int r0 = c < bl.lo ? min(64, bl.lo - c) : 0, r1 = max(0, min(64, bl.hi - c));  // rows that count: [r0, r1)
-                    if (((r0 | r1) & 15) != 0) {
+                    if (((r0 | r1) & 15) != 0 && fine()) {
                         const uint32_t rows = ring + vi * TILE + (c & 64) * 128;
                         auto clear = [&](int r, int k) {
                             for (int i = lane; i < k * 8 * HALVES; i += 32)
@@ -332,6 +334,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         await(smem_addr(&sm.o_read[nv & 1]), (nv >> 1) + 1);
                     else if (j == 2 && np > 0)
                         await(smem_addr(&sm.o_free), np - 1);
+                    if (!fine()) break;  // (a place whose copy has not come is not let go: it would be filled again with one under way)
                     tc_fence_after();
                     const uint64_t bd = vd + (uint32_t)((vi * TILE + (c & 64) * 128) >> 4);
                     const uint32_t p = st + 64 * (nv & 1), o = o0 + (ALONE ? D * (nv & 1) : 0);
@@ -365,6 +368,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                 }
                 if (j < bl.n) {  // S = Q K^T of block j
                     if (!both || !odd) await(full0 + 8 * ki, kp);
+                    if (!fine()) break;
                     tc_fence_after();
                     const uint64_t bd = kd + (uint32_t)((ki * TILE + ((bl.first + bl.step * j) & 64) * 128) >> 4);
                     const uint32_t d = st + 64 * ((n + j) & 1);
