@@ -407,7 +407,8 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  * Errors are those of reco_paged_decode_attn, unit by unit (zeros, lse = -inf, the length kept).
  * Also in error: a sequence whose shared[b] is negative or above the length of one of its units
  * (that unit), or differs from that of the group's first sequence (all units of the
- * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Precision as
+ * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Should one of the
+ * call's own waits run out (each has a limit), every unit of the call is in error.  Precision as
  * reco_decode_attn's, but from bf16 caches the probabilities enter their product with V as
  * bf16: rounded once with bf16 output (each is off by 2^-8 of itself at most), in three parts with
  * float32 output (2^-26).

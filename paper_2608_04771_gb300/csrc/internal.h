@@ -107,6 +107,7 @@ struct PrefixTotal {
     long long work;  // of all groups, per layer and KV head
     int n;           // groups listed
     int most;        // of a key tile, at most
+    int stopped;     // a wait of the attention ran out: its partials say nothing
 };
 // A unit's own rows: the work of those before it in its block of units, the row its first tile begins at, its rows (with an
 // appended one), the first that is its own (-1: the unit is in error).

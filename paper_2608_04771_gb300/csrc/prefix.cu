@@ -97,7 +97,7 @@ __device__ void plan_groups(const PlanArgs &a)
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs, sm_most};
+    if (threadIdx.x == 0) *a.ws.total = PrefixTotal{sm_work, sm_runs, sm_most, 0};
     if (off) raise_error(a.err, ERR_LEN);
 }
 
@@ -429,7 +429,11 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
     PlainSmem<D> &sm = *reinterpret_cast<PlainSmem<D> *>(smem_raw);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (smem_addr(smem_raw) & 1023u) {  // swizzled tiles need it
-        if (threadIdx.x == 0) raise_error(a.err, ERR_INTERNAL);
+        wait_prior_grid();
+        if (threadIdx.x == 0) {
+            raise_error(a.err, ERR_INTERNAL);
+            a.total->stopped = 1;
+        }
         return;
     }
     if (threadIdx.x == 0) {
@@ -521,6 +525,8 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
             if (lane == 0) mbar_arrive(smem_addr(&sm.piece_empty[piece & 3]));
         }
     }
+    __syncthreads();
+    if (threadIdx.x == 0 && *(volatile int *)&sm.abort != 0) a.total->stopped = 1;
 }
 
 // ---------------------------------------------------------------- join
@@ -554,7 +560,7 @@ template <int D, bool FEW> __global__ void __launch_bounds__(kJoinThreads) prefi
     const PrefixUnit x = a.p.units[u];
     const PrefixTotal total = *a.p.total;
     const size_t q0 = (size_t)lb * a.p.Hq + (size_t)h * G;
-    const bool ok = x.lo >= 0 && run != -2;
+    const bool ok = x.lo >= 0 && run != -2 && total.stopped == 0;
     // partials: [0, n_own) of the own rows, then n_pre of the prefix; CTAs of the first ones
     int n_own = 0, n_pre = 0, own_c = 0, pre_c = 0, pre_row = 0;
     if (ok) {

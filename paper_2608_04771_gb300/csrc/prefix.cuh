@@ -107,7 +107,7 @@ struct PrefixArgs {
     const int32_t *table;
     const PrefixRun *runs;
     const int32_t *run_of;
-    const PrefixTotal *total;
+    PrefixTotal *total;  // (the attention sets `stopped`)
     const PrefixUnit *units;
     const int32_t *block_work;
     float *part_o, *own_o, *cont_o;

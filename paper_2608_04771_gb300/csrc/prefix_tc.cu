@@ -42,7 +42,8 @@
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
 // to come when phase k + 1 is.  So every place is waited for by both issuing warps, every time; what a group waits for
 // only now and then (pv_done) has a barrier for even and for odd blocks, which it cannot fall behind.
-// Every wait is bounded; one that runs out raises the error word and the CTA's abort flag, which ends the others.
+// Every wait is bounded; one that runs out raises the error word and the CTA's abort flag, which ends the others, and the
+// join then takes no partial of the call (PrefixTotal::stopped).
 #include <algorithm>
 
 #include "decode_block.cuh"
@@ -133,7 +134,11 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
     const uint32_t base = smem_addr(smem_raw), Qs = base, ring = base + C::Q_BYTES;
     typename C::Small &sm = *reinterpret_cast<typename C::Small *>(smem_raw + C::Q_BYTES + NS * TILE);
     if (base & 1023u) {  // swizzled tiles need it
-        if (tid == 0) raise_error(a.err, ERR_INTERNAL);
+        wait_prior_grid();
+        if (tid == 0) {
+            raise_error(a.err, ERR_INTERNAL);
+            a.total->stopped = 1;
+        }
         return;
     }
     if (tid == 0) {
@@ -649,6 +654,7 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
         }
     }
     __syncthreads();
+    if (tid == 0 && *(volatile int *)&sm.abort != 0) a.total->stopped = 1;
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();

@@ -1,5 +1,6 @@
-"""Decode attention over shared prefixes when one of its own waits runs out: the error word says so, and the next call is as
-ever.  No call's waits run out by themselves: here the library is linked once more, with tensor maps whose boxes are smaller than
+"""Decode attention over shared prefixes when one of its own waits runs out: the error word says so, every unit of the call is
+in error (zeros, lse = -inf, the length kept) whatever partials an earlier call has left in the workspace, and the next call
+is as ever.  No call's waits run out by themselves: here the library is linked once more, with tensor maps whose boxes are smaller than
 what the kernels wait for, and with a limit of 2^12 polls in place of 2^19."""
 import concurrent.futures as cf
 import ctypes
@@ -94,7 +95,7 @@ def test_a_wait_that_runs_out(cut_boxes, what, dtype, d, out_dtype, Ly):
         reco.reco_check()
     cut_boxes(ctypes.c_int(0))
     assert "internal-check" in str(e.value)
-    c.lens.copy_(lens)
+    assert (c.out == 0).all() and torch.isneginf(c.lse).all() and torch.equal(c.lens, lens)
     c.q.neg_()
     c.run()
     reco.reco_check()
