@@ -409,8 +409,8 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
  * (that unit), or differs from that of the group's first sequence (all units of the
  * sequence); a prefix page outside [0, n_pages) puts the units that need it in error.  Should one of the
  * call's own waits run out (each has a limit), every unit of the call is in error.  Precision as
- * reco_decode_attn's, but from bf16 caches the probabilities enter their product with V as
- * bf16: rounded once with bf16 output (each is off by 2^-8 of itself at most), in three parts with
+ * reco_decode_attn's; from bf16 caches the probabilities enter their product with V in parts of
+ * bf16, as there: in two with bf16 output (each is off by 2^-17 of itself at most), in three with
  * float32 output (2^-26).
  * Refused also: float32 caches with more than 8 query heads per KV head and more than some
  * 1.1e10 rows (n_layers * B * H_kv * max_pages * page).                               */

@@ -8,9 +8,10 @@ namespace reco {
 
 // A row tile takes the query heads of up to `per` sequences of a group, of which `half` make what the tensor cores take
 // at once (128 rows).  Work is counted in units of about 0.2 us of a CTA, measured with all of them busy.  bf16: a key tile
-// takes 8 where its bytes come from HBM (1.45 us) and, with up to 256 query rows, as much as its products; where a group has
-// several row tiles, which are bound by their products, 9 for a whole one (1.9 us) and 6 for the last one if it has no more
-// than `half` sequences (1.2 us).  float32 (twice the bytes, plain FMAs): 15 with 8 rows (5300 cycles), 24 with 16 (8300), 33 with
+// takes 8 where its bytes come from HBM (1.45 us) and a stream has half of its keys, 12 where the row tile has more than `half`
+// sequences (each stream all keys: products and softmax are the bound), 6 for a last row tile of no more, whose bytes the
+// others have brought (64 sequences of 5 heads over 100001 rows, two row tiles: 199 us with 12 and 6, 204 with 9 and 5, 209 with
+// 9 and 6, 221 with 9 and 7, 217 with 13 and 7).  With float32 output (one stream) row tiles of a group cost the same.  float32 (twice the bytes, plain FMAs): 15 with 8 rows (5300 cycles), 24 with 16 (8300), 33 with
 // 24, 40 with 32 (14300).  The start and the end of a unit's own rows take extra() more.
 struct PrefixRows {
     int per, half, G, f32;
@@ -20,7 +21,8 @@ struct PrefixRows {
     __host__ __device__ int unit(int n, int rt) const
     {
         if (f32) return plain(n - rt * per < per ? n - rt * per : per);
-        return n <= per ? 8 : (n - rt * per <= half && per > half ? 6 : 9);
+        if (per == half) return n <= per ? 8 : 9;
+        return n - rt * per > half ? 12 : (n <= per ? 8 : 6);
     }
     __host__ __device__ int extra() const { return f32 ? 5 : 11; }
     __host__ __device__ int own() const { return f32 ? plain(1) : 8; }

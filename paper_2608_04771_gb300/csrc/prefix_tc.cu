@@ -29,9 +29,11 @@
 // chain of launches and look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V
 // rows: 301, 169 and 28.4 us.
 //
-// P enters its product in bf16: with bf16 output in one part (2^-8 of each probability, on average over the rows the size
-// of the output's own rounding), with float32 output in three (2^-26; two would lose 2^-17).  Sums take the probabilities
-// as they were before.
+// P enters its product in parts of bf16: with bf16 output in two, as the decode's (2^-17 of each probability; one part, 2^-8, added
+// half as much again to the error of the output's own rounding: 2.3e-3 of the result against 1.7e-3), with float32 output
+// in three (2^-26; two would lose 2^-17).  Sums take the probabilities as they were before.  The parts are made once a block's
+// sum has been looked at: as every pair of probabilities came, they cost 100 bytes of spills, or stores to TMEM in between
+// (100001 rows below: 219 us either way, 209 so).
 // The tensor cores cut sums off rather than round them: some 2^-26 of the output is lost with every addition to it, always
 // towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing.
 // With float32 output every block's product starts from zero, and four warps add the blocks up in registers: one stream
@@ -349,19 +351,15 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > 0 ? 1u : more);
-                                if (PARTS == 3) {
-                                    tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                }
+                                tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                if (PARTS == 3) tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                             }
                         } else {
 #pragma unroll 1
                             for (int k = k0; k < k1; ++k) {
                                 tc_mma_ts(o, p + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, k > k0 ? 1u : more);
-                                if (PARTS == 3) {
-                                    tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                    tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
-                                }
+                                tc_mma_ts(o, p + 32 + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
+                                if (PARTS == 3) tc_mma_ts(o, tmem + P3_COL + 32 * (nv & 1) + 8 * k, bd + (uint32_t)(k * 2048 >> 4), ID_O, 1);
                             }
                         }
                         tc_commit(pv_done0 + 8 * (nv & 1));
@@ -490,20 +488,47 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                 if (any_row) {
                     const uint32_t sa = lane_base + S_COL + 128 * s + 64 * (n & 1);
                     float v[64];
-                    tmem_ld32_nowait(sa, v);
-                    tmem_ld32_nowait(sa + 32, v + 32);
-                    tmem_ld_wait_regs<64>(v);
-                    if (c < bl.lo || c + 64 > bl.hi) {
-                        const int low = max(0, bl.lo - c), live = max(0, bl.hi - c - low);  // columns that count, from the first on
+                    auto logits = [&]() {
+                        tmem_ld32_nowait(sa, v);
+                        tmem_ld32_nowait(sa + 32, v + 32);
+                        tmem_ld_wait_regs<64>(v);
+                        if (c < bl.lo || c + 64 > bl.hi) {
+                            const int low = max(0, bl.lo - c), live = max(0, bl.hi - c - low);  // columns that count, from the first on
 #pragma unroll
-                        for (int x = 0; x < 64; ++x) v[x] = (unsigned)(x - low) < (unsigned)live ? v[x] : hide;
-                    }
-                    // Probabilities against the maximum so far.  No maximum of the block is looked for while their sum stays below
-                    // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).
-                    uint32_t hi[32], lo[PARTS == 3 ? 32 : 1], rest[PARTS == 3 ? 32 : 1];
+                            for (int x = 0; x < 64; ++x) v[x] = (unsigned)(x - low) < (unsigned)live ? v[x] : hide;
+                        }
+                    };
+                    logits();
+                    // Probabilities against the maximum so far, in place of the logits.  But for a piece's first block, no maximum of
+                    // the block is looked for while their sum stays below 2^12 (each of them is below it, which float32 sums and
+                    // bf16's range do not mind).
                     float sum, factor = 1.f;
-                    bool again = false;
+                    bool again = n == first, grow = there && again;
                     for (;;) {
+                        if (again) {
+                            float mx = -INFINITY;
+#pragma unroll
+                            for (int x = 0; x < 64; x += 2) mx = max3(mx, v[x] * c2, v[x + 1] * c2);
+                            const float mn = grow ? fmaxf(m, mx) : m, al = grow ? part_factor(m, mn) : 1.f;
+                            l *= al;
+                            m = mn;
+                            factor = al;
+                            if (!ALONE && n > first) {  // the output so far
+                                await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
+                                __syncwarp();
+                                tc_fence_after();
+#pragma unroll 1
+                                for (int x = 0; x < D / 16; ++x) {
+                                    float o[16];
+                                    tmem_ld16_nowait(lane_base + O_COL + D * s + 16 * x, o);
+                                    tmem_ld_wait_regs<16>(o);
+                                    uint32_t ob[16];
+#pragma unroll
+                                    for (int y = 0; y < 16; ++y) ob[y] = __float_as_uint(o[y] * al);
+                                    tmem_st16(lane_base + O_COL + D * s + 16 * x, ob);
+                                }
+                            }
+                        }
                         const float nb = again && m == -INFINITY ? 0.f : -m;
                         const unsigned long long cc = pair_of(c2, c2), nn = pair_of(nb, nb);
                         unsigned long long s4[4] = {0ull, 0ull, 0ull, 0ull};
@@ -511,54 +536,33 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         for (int y = 0; y < 32; ++y) {
                             float p0, p1;
                             unpair(fma_pair(pair_of(v[2 * y], v[2 * y + 1]), cc, nn), p0, p1);
-                            p0 = fast_exp2(p0);
-                            p1 = fast_exp2(p1);
-                            s4[y & 3] = add_pair(s4[y & 3], pair_of(p0, p1));
-                            if (PARTS == 3) {
-                                float r0, r1;
-                                split_bf16(p0, p1, hi[y], lo[y], r0, r1);
-                                rest[y] = pack_bf16(r0, r1);
-                            } else {
-                                hi[y] = pack_bf16(p0, p1);
-                            }
+                            v[2 * y] = fast_exp2(p0);
+                            v[2 * y + 1] = fast_exp2(p1);
+                            s4[y & 3] = add_pair(s4[y & 3], pair_of(v[2 * y], v[2 * y + 1]));
                         }
                         float s0, s1;
                         unpair(add_pair(add_pair(s4[0], s4[1]), add_pair(s4[2], s4[3])), s0, s1);
                         sum = s0 + s1;
-                        const bool grow = there && !again && !(sum <= 0x1p12f);  // (at first the maximum is -inf: infinities and NaN)
+                        grow = there && !again && !(sum <= 0x1p12f);  // (while the maximum is -inf: infinities and NaN)
                         if (!__any_sync(0xffffffffu, grow)) break;
                         again = true;
-                        float mx = -INFINITY;
-#pragma unroll
-                        for (int x = 0; x < 64; x += 2) mx = max3(mx, v[x] * c2, v[x + 1] * c2);
-                        const float mn = grow ? fmaxf(m, mx) : m, al = grow ? part_factor(m, mn) : 1.f;
-                        l *= al;
-                        m = mn;
-                        factor = al;
-                        if (!ALONE && n > first) {  // the output so far
-                            await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
-                            __syncwarp();
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int x = 0; x < D / 16; ++x) {
-                                float o[16];
-                                tmem_ld16_nowait(lane_base + O_COL + D * s + 16 * x, o);
-                                tmem_ld_wait_regs<16>(o);
-                                uint32_t ob[16];
-#pragma unroll
-                                for (int y = 0; y < 16; ++y) ob[y] = __float_as_uint(o[y] * al);
-                                tmem_st16(lane_base + O_COL + D * s + 16 * x, ob);
-                            }
-                        }
+                        logits();
                     }
                     l += sum;
-                    tmem_st16(sa, hi);
-                    tmem_st16(sa + 16, hi + 16);
+#pragma unroll
+                    for (int x = 0; x < 32; x += 16) {
+                        uint32_t hi[16], lo[16], rest[16];
+#pragma unroll
+                        for (int y = 0; y < 16; ++y) {
+                            float r0, r1;
+                            split_bf16(v[2 * (x + y)], v[2 * (x + y) + 1], hi[y], lo[y], r0, r1);
+                            if (PARTS == 3) rest[y] = pack_bf16(r0, r1);
+                        }
+                        tmem_st16(sa + x, hi);
+                        tmem_st16(sa + 32 + x, lo);
+                        if (PARTS == 3) tmem_st16(lane_base + P3_COL + 32 * (n & 1) + x, rest);
+                    }
                     if (PARTS == 3) {
-                        tmem_st16(sa + 32, lo);
-                        tmem_st16(sa + 48, lo + 16);
-                        tmem_st16(lane_base + P3_COL + 32 * (n & 1), rest);
-                        tmem_st16(lane_base + P3_COL + 32 * (n & 1) + 16, rest + 16);
                         await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (the factor of two blocks before, too)
                         sm.al[n & 1][ALONE ? r : 0] = factor;
                         __syncwarp();
@@ -673,12 +677,12 @@ cudaError_t launch_prefix_tc(const reco_paged_kv &kv, const PrefixArgs &a, int g
         !encode_bf16_heads(&mq1, a.q, tokens, kv.H_q, kv.d, a.G, 1))
         return cudaErrorInvalidValue;
     typedef void (*Kernel)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, PrefixArgs);
-    const bool one = out_dtype == RECO_BF16;
-    const Kernel fn = kv.d == 64 ? (one ? prefix_tc<64, 1> : prefix_tc<64, 3>) : (one ? prefix_tc<128, 1> : prefix_tc<128, 3>);
-    const int smem = kv.d == 64 ? (one ? PrefixTc<64, 1>::SMEM : PrefixTc<64, 3>::SMEM) : (one ? PrefixTc<128, 1>::SMEM : PrefixTc<128, 3>::SMEM);
+    const bool two = out_dtype == RECO_BF16;
+    const Kernel fn = kv.d == 64 ? (two ? prefix_tc<64, 2> : prefix_tc<64, 3>) : (two ? prefix_tc<128, 2> : prefix_tc<128, 3>);
+    const int smem = kv.d == 64 ? (two ? PrefixTc<64, 2>::SMEM : PrefixTc<64, 3>::SMEM) : (two ? PrefixTc<128, 2>::SMEM : PrefixTc<128, 3>::SMEM);
     cudaError_t e = allow_smem((const void *)fn, smem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(fn, dim3(grid), dim3(PrefixTc<64, 1>::THREADS), smem, s, mk, mv, mq, mq1, a);
+    e = launch_pdl(fn, dim3(grid), dim3(PrefixTc<64, 2>::THREADS), smem, s, mk, mv, mq, mq1, a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
