@@ -429,8 +429,9 @@ reco_status reco_paged_prefix_attn(const reco_paged_kv *kv, const void *q, const
  *   rotate(x, s) turns the pairs (x_i, x_{i + rot/2}), or with `interleaved` the pairs
  *   (x_{2i}, x_{2i+1}), i < rot / 2, by the angle s * inv_freq[i]:
  *     (x, y) -> (x cos - y sin, y cos + x sin);   elements from rot on stay as they are.
- *   The angle is that of the exact product, reduced to a turn before it is rounded (far
- *   positions lose nothing); the rest is float32, rounded once to the cache's type.
+ *   The angle is that of the exact product to 2^-34 turns, at any position and frequency, and
+ *   reduced to an eighth of a turn before it is rounded to float32; the rest is float32,
+ *   rounded once to the cache's type.
  *   k, v     : [n_layers][T][H_kv] rows, cache dtype
  *   q, q_out : [n_layers][T][H_q] rows, cache dtype, or both NULL.  q_out may be q itself (the
  *              same view); otherwise it overlaps no input, nor do its rows overlap

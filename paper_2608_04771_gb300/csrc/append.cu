@@ -2,9 +2,12 @@
 // positions on the way.
 //
 // A pair (x, y) of a row turns by the angle pos * f:  x cos - y sin, y cos + x sin.  The angle is kept in turns, as a
-// 64-bit fraction: f / (2 pi) times 2^64 is rounded once (53 bits), times pos wraps around at whole turns by itself, and
-// what is left is exact, however far the position (a float32 product pos * f is off by 2^-24 of itself: 0.06 rad at a
-// position of a million).  Its upper 32 bits, times pi, go to sincospif.
+// 64-bit fraction: f / (2 pi), multiplied out in whole numbers with those digits of 1 / (2 pi) that make fractions of a turn (Payne
+// and Hanek's reduction, 1983), is rounded to a multiple of 2^-64, and times pos it wraps around at whole turns by itself.  What is
+// left is off by 2^-34 turns at most, however far the position (a float32 product pos * f is off by 2^-24 of itself: 0.06
+// rad at a position of a million).  Then the nearest quarter of a turn is taken off, exactly, and
+// the rest, an eighth of a turn at most either way, is rounded to float32 (2^-28 turns, 0.4 of float32's 2^-24 in rad; the whole
+// half turn would lose four times that) and goes to sincospif.
 //
 // Every row is read once and written once (bf16, d 128: 256 bytes each way), some ten operations an element: the copy
 // rate is the bound, and for a token per sequence the latency of a launch and of the chain starts -> lens -> table.
@@ -38,12 +41,37 @@ struct AppendArgs {
 // three rows of a lane in flight take registers that cost warps: 368 and 371).
 constexpr int kAppendWarps = 4;
 
-// Upper 32 bits of pos * f / (2 pi) in turns, modulo one, as a signed fraction of 2^31 half turns.
+// f / (2 pi) in 2^-64 turns, modulo whole turns, rounded (off by 0.51 of them).  f is m 2^e with a whole m below 2^24: the digits
+// of 1 / (2 pi) from the e-th behind the point on, 96 of them, times m.  (The same with doubles, in two parts, took 2.5 us of 640
+// tokens' 11: an SM has room for few of them at a time.)
+__constant__ uint32_t kPerRadian[12] = {0, 0, 0, 0, 0, 0x28be60dbu, 0x9391054au, 0x7f09d5f4u, 0x7d4d3770u, 0x36d8a566u, 0x4f10e410u, 0x7f9458eau};
 __device__ __forceinline__ unsigned long long turn_step(float f)
 {
-    double t = (double)f * 0.15915494309189533577;  // 1 / (2 pi)
-    t -= floor(t);
-    return __double2ull_rn(t * 18446744073709551616.0);  // 2^64; a fraction that rounds to 1 saturates
+    const uint32_t bits = __float_as_uint(f) & 0x7fffffffu, ex = min(bits >> 23, 254u);
+    const uint32_t m = ex ? (bits & 0x7fffffu) | 0x800000u : bits;
+    const int at = (int)max(ex, 1u) - 150 + 160, shift = at & 31;  // e + 160: 160 zeros stand before the point's digits
+    const uint32_t *w = kPerRadian + (at >> 5);
+    const uint32_t a = w[0], b = w[1], c = w[2], d = w[3];
+    unsigned long long t = (unsigned long long)m * __funnelshift_l(d, c, shift);
+    const uint32_t round = (uint32_t)t >> 31;
+    t = (unsigned long long)m * __funnelshift_l(c, b, shift) + (t >> 32);
+    const uint32_t lo = (uint32_t)t, hi = m * __funnelshift_l(b, a, shift) + (uint32_t)(t >> 32);
+    t = ((unsigned long long)hi << 32 | lo) + round;
+    return (int)__float_as_uint(f) < 0 ? 0ull - t : t;
+}
+
+// Sine and cosine of a phase in 2^-64 turns.
+__device__ __forceinline__ void turn_sincos(unsigned long long ph, float &s, float &c)
+{
+    const unsigned quarter = (unsigned)((ph + (1ull << 61)) >> 62);
+    float s0, c0;
+    sincospif(__ll2float_rn((long long)(ph - ((unsigned long long)quarter << 62))) * 0x1p-63f, &s0, &c0);
+    s = quarter & 1 ? c0 : s0;
+    c = quarter & 1 ? -s0 : c0;
+    if (quarter & 2) {
+        s = -s;
+        c = -c;
+    }
 }
 
 template <typename T> struct Chunk;  // 16 bytes as floats
@@ -125,7 +153,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 10) paged_append(const __gr
                     if (p < rp) {
                         const float f = __ldg(a.inv_freq + p * E + hg * A + i);
                         const unsigned long long ph = turn_step(f) * (unsigned long long)(long long)__ldg(a.pos + t);
-                        sincospif((float)(int)(ph >> 32) * 0x1p-31f, &ms[i], &mc[i]);
+                        turn_sincos(ph, ms[i], mc[i]);
                         if (!isfinite(f)) ms[i] = mc[i] = NAN;
                     }
                 }
