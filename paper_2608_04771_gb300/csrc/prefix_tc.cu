@@ -31,9 +31,9 @@
 //
 // P enters its product in parts of bf16: with bf16 output in two, as the decode's (2^-17 of each probability; one part, 2^-8, added
 // half as much again to the error of the output's own rounding: 2.3e-3 of the result against 1.7e-3), with float32 output
-// in three (2^-26; two would lose 2^-17).  Sums take the probabilities as they were before.  The parts are made once a block's
-// sum has been looked at: as every pair of probabilities came, they cost 100 bytes of spills, or stores to TMEM in between
-// (100001 rows below: 219 us either way, 209 so).
+// in three (2^-26; two would lose 2^-17).  Sums take the probabilities as they were before.  Two parts are made
+// once a block's sum has been looked at: as every pair of probabilities came, they cost 100 bytes of spills, or stores to
+// TMEM in between (100001 rows below: 219 us either way, 209 so).
 // The tensor cores cut sums off rather than round them: some 2^-26 of the output is lost with every addition to it, always
 // towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing.
 // With float32 output every block's product starts from zero, and four warps add the blocks up in registers: one stream
@@ -499,36 +499,29 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         }
                     };
                     logits();
-                    // Probabilities against the maximum so far, in place of the logits.  But for a piece's first block, no maximum of
-                    // the block is looked for while their sum stays below 2^12 (each of them is below it, which float32 sums and
-                    // bf16's range do not mind).
+                    // Probabilities against the maximum so far.  No maximum of the block is looked for while their sum stays below
+                    // 2^12 (each of them is below it, which float32 sums and bf16's range do not mind).  Two parts are made once that
+                    // is known, from the probabilities in place of the logits; three as the probabilities come, which leaves the one
+                    // group of warps that makes them least to wait for (28 layers below 524 us, made later 689).
                     float sum, factor = 1.f;
-                    bool again = n == first, grow = there && again;
+                    uint32_t hi[32], lo[32], rest[PARTS == 3 ? 32 : 1];
+                    auto parts = [&](int y, float p0, float p1) {
+                        float r0, r1;
+                        split_bf16(p0, p1, hi[y], lo[y], r0, r1);
+                        if (PARTS == 3) rest[y] = pack_bf16(r0, r1);
+                    };
+                    auto rise = [&](bool grow) {  // the maximum, for those whose probabilities it must lower
+                        float mx = -INFINITY;
+#pragma unroll
+                        for (int x = 0; x < 64; x += 2) mx = max3(mx, v[x] * c2, v[x + 1] * c2);
+                        const float mn = grow ? fmaxf(m, mx) : m;
+                        factor = grow ? part_factor(m, mn) : 1.f;
+                        l *= factor;
+                        m = mn;
+                    };
+                    bool again = PARTS == 2 && n == first;
+                    if (again) rise(there);
                     for (;;) {
-                        if (again) {
-                            float mx = -INFINITY;
-#pragma unroll
-                            for (int x = 0; x < 64; x += 2) mx = max3(mx, v[x] * c2, v[x + 1] * c2);
-                            const float mn = grow ? fmaxf(m, mx) : m, al = grow ? part_factor(m, mn) : 1.f;
-                            l *= al;
-                            m = mn;
-                            factor = al;
-                            if (!ALONE && n > first) {  // the output so far
-                                await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
-                                __syncwarp();
-                                tc_fence_after();
-#pragma unroll 1
-                                for (int x = 0; x < D / 16; ++x) {
-                                    float o[16];
-                                    tmem_ld16_nowait(lane_base + O_COL + D * s + 16 * x, o);
-                                    tmem_ld_wait_regs<16>(o);
-                                    uint32_t ob[16];
-#pragma unroll
-                                    for (int y = 0; y < 16; ++y) ob[y] = __float_as_uint(o[y] * al);
-                                    tmem_st16(lane_base + O_COL + D * s + 16 * x, ob);
-                                }
-                            }
-                        }
                         const float nb = again && m == -INFINITY ? 0.f : -m;
                         const unsigned long long cc = pair_of(c2, c2), nn = pair_of(nb, nb);
                         unsigned long long s4[4] = {0ull, 0ull, 0ull, 0ull};
@@ -536,33 +529,52 @@ __global__ void __launch_bounds__(PrefixTc<D, PARTS>::THREADS, 1)
                         for (int y = 0; y < 32; ++y) {
                             float p0, p1;
                             unpair(fma_pair(pair_of(v[2 * y], v[2 * y + 1]), cc, nn), p0, p1);
-                            v[2 * y] = fast_exp2(p0);
-                            v[2 * y + 1] = fast_exp2(p1);
-                            s4[y & 3] = add_pair(s4[y & 3], pair_of(v[2 * y], v[2 * y + 1]));
+                            p0 = fast_exp2(p0);
+                            p1 = fast_exp2(p1);
+                            s4[y & 3] = add_pair(s4[y & 3], pair_of(p0, p1));
+                            if (PARTS == 3) {
+                                parts(y, p0, p1);
+                            } else {
+                                v[2 * y] = p0;
+                                v[2 * y + 1] = p1;
+                            }
                         }
                         float s0, s1;
                         unpair(add_pair(add_pair(s4[0], s4[1]), add_pair(s4[2], s4[3])), s0, s1);
                         sum = s0 + s1;
-                        grow = there && !again && !(sum <= 0x1p12f);  // (while the maximum is -inf: infinities and NaN)
+                        const bool grow = there && !again && !(sum <= 0x1p12f);  // (while the maximum is -inf: infinities and NaN)
                         if (!__any_sync(0xffffffffu, grow)) break;
                         again = true;
-                        logits();
+                        if (PARTS == 2) logits();
+                        rise(grow);
+                        if (!ALONE && n > first) {  // the output so far
+                            await(smem_addr(&sm.pv_done[s][(n - 1) & 1]), (n - 1) >> 1);
+                            __syncwarp();
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int x = 0; x < D / 16; ++x) {
+                                float o[16];
+                                tmem_ld16_nowait(lane_base + O_COL + D * s + 16 * x, o);
+                                tmem_ld_wait_regs<16>(o);
+                                uint32_t ob[16];
+#pragma unroll
+                                for (int y = 0; y < 16; ++y) ob[y] = __float_as_uint(o[y] * factor);
+                                tmem_st16(lane_base + O_COL + D * s + 16 * x, ob);
+                            }
+                        }
                     }
                     l += sum;
+                    if (PARTS == 2) {
 #pragma unroll
-                    for (int x = 0; x < 32; x += 16) {
-                        uint32_t hi[16], lo[16], rest[16];
-#pragma unroll
-                        for (int y = 0; y < 16; ++y) {
-                            float r0, r1;
-                            split_bf16(v[2 * (x + y)], v[2 * (x + y) + 1], hi[y], lo[y], r0, r1);
-                            if (PARTS == 3) rest[y] = pack_bf16(r0, r1);
-                        }
-                        tmem_st16(sa + x, hi);
-                        tmem_st16(sa + 32 + x, lo);
-                        if (PARTS == 3) tmem_st16(lane_base + P3_COL + 32 * (n & 1) + x, rest);
+                        for (int y = 0; y < 32; ++y) parts(y, v[2 * y], v[2 * y + 1]);
                     }
+                    tmem_st16(sa, hi);
+                    tmem_st16(sa + 16, hi + 16);
+                    tmem_st16(sa + 32, lo);
+                    tmem_st16(sa + 48, lo + 16);
                     if (PARTS == 3) {
+                        tmem_st16(lane_base + P3_COL + 32 * (n & 1), rest);
+                        tmem_st16(lane_base + P3_COL + 32 * (n & 1) + 16, rest + 16);
                         await(smem_addr(&sm.o_read[n & 1]), (n >> 1) + 1);  // (the factor of two blocks before, too)
                         sm.al[n & 1][ALONE ? r : 0] = factor;
                         __syncwarp();
