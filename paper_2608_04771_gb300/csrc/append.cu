@@ -37,7 +37,7 @@ struct AppendArgs {
     unsigned *err;
 };
 
-// Small CTAs, 40 warps of them on an SM (28 layers of 4096 tokens, 7B-class heads: 335 us; with eight warps a CTA 361; two or
+// Small CTAs, 40 warps of them on an SM (28 layers of 4096 tokens, 7B-class heads: 330 us; with eight warps a CTA 357; two or
 // three rows of a lane in flight take registers that cost warps: 368 and 371).
 constexpr int kAppendWarps = 4;
 

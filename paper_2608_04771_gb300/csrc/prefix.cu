@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kPrefixBlock) prefix_plan(const __grid_constan
 // different rows meet different banks.  A warp waits for a tile, and lets it go, for itself.
 // QK^T: eight lanes share a row group's keys, four the rows: RW / 4 rows and KEYS / 8 keys to a lane, so that six to eight
 // 16-byte reads feed up to 64 FMAs.  PV: a lane has D / 32 columns of all RW rows, and takes the probabilities from shared
-// memory.  28 layers of 8 sequences in two groups (12 and 2 heads of 128, 1500 to 2000 shared rows, 315 MB): 121 us, where
+// memory.  28 layers of 8 sequences in two groups (12 and 2 heads of 128, 1500 to 2000 shared rows, 315 MB): 125 us, where
 // the bytes are 46 and the FMAs 40.  A tile of 32 rows takes 14300 cycles, of which the FMAs could issue in 8200: no tile
 // is waited for, two warps a scheduler hide too little of what shared memory takes.  Halving its reads (8 keys and 8
 // rows to a lane, d split four ways and joined by shuffles) gained nothing; one FMA to an instruction: 131 us; row
@@ -533,9 +533,10 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 // One CTA per unit.  The partials of a query head: the own rows' first one, their others by CTA, and the same of the
 // prefix.  A warp finds a head's factors; then a thread adds up four columns of a head over an equal part of the partials.
 // Where units are many, own rows that are few (at the start of an answer) are one more part, taken here with plain FMAs: as
-// an item of the attention they cost 2 us and more of a CTA that holds an SM, here several units share one.  (24 layers, 26
-// sequences of 8 key heads with at most 18 rows of their own, 4992 units: 210 -> 107 us.  128 units, half of them with
-// up to 32: 27.7 -> 29.9, the join waits for them; so only above 600 units.)
+// an item of the attention they cost 2 us and more of a CTA that holds an SM, here several units share one.  Few units would rather have the
+// attention take them beside the prefixes than the join behind it.  (28 query and 4 key heads, up to 32 own rows behind 1000: 128
+// units 28 us without, 34 with, 320 units 32 and 35, 640 units 47 and 40, 896 units 61 and 49, 2560 units 144 and 96, 4992 units 245
+// and 172; where half of the units have 300 own rows, 36 and 38 with 320 units, 55 either way with 640, 78 and 73 with 896.)
 struct JoinArgs {
     PrefixArgs p;
     int32_t *lens;

@@ -20,14 +20,14 @@
 // the maximum so far sum to more than 2^12 in a block.
 //
 // Measured, GB300, the whole call with its plan and its join.  28 layers, 8 sequences of 28 query and 4 key heads of 128 over
-// 16001 shared rows and 1000 to 4000 of their own (1.9 GB of K and V): 293 us, 0.96 of the copy rate.  64 sequences of 40 and
-// 8 heads over 100001 shared rows: 169 us, where the bytes once and the products are 67 us each; two row tiles read every K
-// and V tile, one of 250 rows in 1.9 us of a CTA (its products alone would take 1.3) and one of 70 in 1.2.  Memory is not
-// what bounds them (165 us with all rows in 26 MB of pages): a product with 64 keys reads 6 KB of shared memory, 48 cycles, for
-// 32 cycles of the tensor cores (42% active), and a block's softmax and two hand-overs are as long as the other stream's
-// products.  One layer, 16 sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 27 us, a
-// chain of launches and look-ups more than of bytes.  With one warp copying K and V in turn, and another clearing V
-// rows: 301, 169 and 28.4 us.
+// 16001 shared rows and 1000 to 4000 of their own (1.9 GB of K and V): 313 us, 0.90 of the copy rate.  64 sequences of 40 and
+// 8 heads over 100001 shared rows: 204 us, where the bytes once and the products (P in one part) are 67 us each; two row tiles
+// read every K and V tile, one of 250 rows in some 2.4 us of a CTA and one of 70 in 1.2.  Memory is not what bounds them (46%
+// of its rate): the tensor cores are active 49% of the time, a product of Q with 64 keys reads 6 KB of shared memory, 48
+// cycles, for 32 cycles of theirs, and a block's softmax and two hand-overs are as long as the other stream's products.  One
+// layer, 16 sequences of 28 and 4 heads, 4001 shared rows and 200 to 2000 of their own, 34 MB: 31.6 us, a chain of launches
+// and look-ups more than of bytes.  (With one warp copying K and V in turn and another clearing V rows, 301, 169 and 28.4 us
+// when they took 293, 170 and 27.4.)
 //
 // P enters its product in parts of bf16: with bf16 output in two, as the decode's (2^-17 of each probability; one part, 2^-8, added
 // half as much again to the error of the output's own rounding: 2.3e-3 of the result against 1.7e-3), with float32 output
@@ -38,7 +38,7 @@
 // towards zero (11 tiles cost 2.2e-6, 46 tiles 1.1e-5 of the result, against 64 bits).  With bf16 output that is nothing.
 // With float32 output every block's product starts from zero, and four warps add the blocks up in registers: one stream
 // with two places for its products, the other stream's softmax warps are those that add, and a row tile has 128 rows.  The
-// 28 layers above take 526 us so, 2500 cycles a block: 1600 for the softmax of the one warp that a scheduler has, the rest
+// 28 layers above take 525 us so, 2500 cycles a block: 1600 for the softmax of the one warp that a scheduler has, the rest
 // waits and hand-overs (a third place for S: no gain; parts by cutting bits off instead of conversions: spills, 706 us).
 //
 // A barrier's phases alternate in one bit: a wait for phase k must not begin before phase k - 1 is over, nor be still
