@@ -385,8 +385,9 @@ reco_status reco_paged_decode_attn_weights(const reco_paged_kv *kv, const void *
 /* reco_paged_decode_attn for a batch whose sequences share the rows of a prefix: several answers
  * to one question (the paper samples several reasoning paths per question), whose rows lie
  * once in the pool and are read once per group instead of once per sequence.  (The decode can
- * read the same pages through every sequence's own table, and is faster where they are few: up to
- * about 2000 shared rows with all layers in a call, 64 thousand of all sequences with one.)
+ * read the same pages through every sequence's own table, and is faster where they are few: up
+ * to about 2000 shared rows where all layers go in one call, and up to some 64 thousand, counted
+ * once per sequence, where a call has one layer.)
  * Sequences next to each other with equal group[b] are a group; they share their first
  * P = shared[b] rows, in every layer and head.  Row j of a sequence lies
  *   for j < P   in the page that the table of the group's FIRST sequence names,

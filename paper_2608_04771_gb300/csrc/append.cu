@@ -5,9 +5,9 @@
 // 64-bit fraction: f / (2 pi), multiplied out in whole numbers with those digits of 1 / (2 pi) that make fractions of a turn (Payne
 // and Hanek's reduction, 1983), is rounded to a multiple of 2^-64, and times pos it wraps around at whole turns by itself.  What is
 // left is off by 2^-34 turns at most, however far the position (a float32 product pos * f is off by 2^-24 of itself: 0.06
-// rad at a position of a million).  Then the nearest quarter of a turn is taken off, exactly, and
-// the rest, an eighth of a turn at most either way, is rounded to float32 (2^-28 turns, 0.4 of float32's 2^-24 in rad; the whole
-// half turn would lose four times that) and goes to sincospif.
+// rad at a position of a million).  Then the nearest quarter of a turn is taken off, exactly, and the rest, an eighth of a turn
+// at most either way, is rounded to float32 (2^-28 turns, 0.4 of 2^-24 in rad; half a turn would lose four times that) and goes
+// to sincospif.
 //
 // Every row is read once and written once (bf16, d 128: 256 bytes each way), some ten operations an element: the copy
 // rate is the bound, and for a token per sequence the latency of a launch and of the chain starts -> lens -> table.

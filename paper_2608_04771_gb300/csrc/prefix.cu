@@ -533,10 +533,11 @@ __global__ void __launch_bounds__(kPlainThreads, 1)
 // One CTA per unit.  The partials of a query head: the own rows' first one, their others by CTA, and the same of the
 // prefix.  A warp finds a head's factors; then a thread adds up four columns of a head over an equal part of the partials.
 // Where units are many, own rows that are few (at the start of an answer) are one more part, taken here with plain FMAs: as
-// an item of the attention they cost 2 us and more of a CTA that holds an SM, here several units share one.  Few units would rather have the
-// attention take them beside the prefixes than the join behind it.  (28 query and 4 key heads, up to 32 own rows behind 1000: 128
-// units 28 us without, 34 with, 320 units 32 and 35, 640 units 47 and 40, 896 units 61 and 49, 2560 units 144 and 96, 4992 units 245
-// and 172; where half of the units have 300 own rows, 36 and 38 with 320 units, 55 either way with 640, 78 and 73 with 896.)
+// an item of the attention they cost 2 us and more of a CTA that holds an SM, here several units share one.  Few units
+// would rather have the attention take them beside the prefixes than the join behind it.  (28 query and 4 key heads, up to
+// 32 own rows behind 1000: 128 units 28 us without, 34 with, 320 units 32 and 35, 640 units 47 and 40, 896 units 61 and 49,
+// 2560 units 144 and 96, 4992 units 245 and 172; where half of the units have 300 own rows, 36 and 38 with 320 units, 55
+// either way with 640, 78 and 73 with 896.)
 struct JoinArgs {
     PrefixArgs p;
     int32_t *lens;
